@@ -516,6 +516,121 @@ int32_t fold_loss_softmax_ce(const fold_sched* sched, const fold_packed* packed,
 int32_t fold_adam_step(int64_t n, float* param, uint16_t* param_bf16, const float* grad, float* m, float* v,
                        double lr, double beta1, double beta2, double eps, int32_t step, hipStream_t stream);
 
+/* ---- the vocabulary head ---------------------------------------------------
+ * Rows of node states scored against a vocabulary of tokens: the head of a
+ * model whose nodes predict words (LSTM chains over text, roots that name a
+ * token), where fold_loss_softmax_ce serves a few classes.  `rows` states are
+ * any matrix [rows, fold_row_ld(hidden)]: a whole pool (pool order) or
+ * roots_out (root order), and the gradient d_states of the same shape is
+ * fold_backward's dh_nodes or dh_roots.  The weights lie as a leaf table
+ * does, one row of `hidden` values a token, so the table of an embedding
+ * model can be the head's W and its d_leaf_table the head's dW (tied
+ * weights).  Logits are matrices [rows, fold_row_ld(vocab)] in memory: a
+ * program may mask them (-inf), between the head and what reads them.
+ *
+ * All of these calls enqueue on `stream`, never synchronise, never allocate
+ * and can be captured.  Matrices and workspaces are 16-byte aligned
+ * (FOLD_E_INVALID otherwise); rows is at most 2^31 - 1, vocab at most 2^30.
+ * rows = 0 is allowed (buffers that would be read may be NULL).  Workspaces
+ * hold nothing between calls; calls that overlap need one each.
+ *
+ * fold_vocab_logits: z = states W^T + bias.
+ *   dtype         FOLD_F32 or FOLD_BF16: states and W (products of bf16 values
+ *                 are summed in fp32)
+ *   states        device [rows, fold_row_ld(hidden)]; hidden 1 .. 4096
+ *   W             device [vocab, fold_row_ld(hidden)]; the pad columns of one
+ *                 of the two hold zeros, of the other any finite values
+ *   bias          device [vocab] fp32, or NULL; -inf takes a token out
+ *   logits_dtype  of `logits`: FOLD_F32, or FOLD_BF16 for a bf16 head
+ *   logits        device [rows, fold_row_ld(vocab)], written whole (pad
+ *                 columns zero)
+ * fold_vocab_backward: from dlogits, of `dtype` and finite in the pad columns
+ * (fold_loss_distill writes zeros there),
+ *     d_states = dlogits W                device [rows, fold_row_ld(hidden)]
+ *     dW      = dlogits^T states          device [vocab, fold_row_ld(hidden)]
+ *     dbias   = sum over the rows         device [vocab]
+ * all fp32; any of the three may be NULL (not computed).  They are written
+ * whole, pad columns zero; with FOLD_VOCAB_ACCUMULATE dW and dbias are added
+ * to what is there instead (dW's pad columns are then left alone).
+ *   ws  device workspace of >= fold_vocab_workspace_size bytes (may be NULL
+ *       where that is 0)
+ * FOLD_E_INVALID for sizes out of range, an unknown dtype or flag, NULL or
+ * misaligned buffers; FOLD_E_MISMATCH for a workspace that is too small. */
+#define FOLD_VOCAB_ACCUMULATE 1
+
+int32_t fold_vocab_logits(int32_t dtype, int64_t rows, int32_t hidden, int32_t vocab, const void* states,
+                          const void* W, const float* bias, int32_t logits_dtype, void* logits, hipStream_t stream);
+int32_t fold_vocab_workspace_size(int32_t dtype, int64_t rows, int32_t hidden, int32_t vocab, size_t* bytes);
+int32_t fold_vocab_backward(int32_t dtype, int64_t rows, int32_t hidden, int32_t vocab, const void* states,
+                            const void* W, const void* dlogits, float* d_states, float* dW, float* dbias,
+                            int32_t flags, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* fold_loss_distill: the loss of a student against the largest logits of a
+ * teacher, mixed with the cross entropy of a label, and its gradient.  For a
+ * row with teacher entries (i_j, t_j), j < num_teacher, and label y, with
+ * q = softmax(t / T) over the entries that count, p^T = softmax(z / T) and
+ * p = softmax(z) over the vocabulary:
+ *     loss = soft_weight T^2 sum_j q_j (log q_j - log p^T[i_j])
+ *          - hard_weight log p[y]
+ * and, of L = scale * (sum of the rows' losses),
+ *     dz_c = scale (soft_weight T (p^T_c - sum of q_j over i_j = c)
+ *                   + hard_weight (p_c - [c = y])).
+ * An entry counts if its token is in [0, vocab) and its logit is not -inf; a
+ * teacher with fewer than num_teacher pads with token -1.  The same token
+ * twice is two entries.  Without an entry that counts the first term is 0,
+ * without a label in [0, vocab) the second; a row with neither has loss 0 and
+ * gradient 0, whatever its logits hold.
+ *   sched       NULL: targets and losses are in row order.  Otherwise rows
+ *               are the pool rows of that schedule (rows = its num_nodes) and
+ *               the targets and losses are in NODE order
+ *   logits      device [rows, fold_row_ld(vocab)] of dtype (the pad columns
+ *               are not looked at)
+ *   teacher_token, teacher_logit  device [rows, num_teacher] int32, fp32;
+ *               num_teacher 0 .. 256
+ *   labels      device [rows] int32, or NULL (no labels)
+ *   temperature in [1e-3, 1e3]; the weights not negative
+ *   row_loss    device [rows] fp32, without the scale (written)
+ *   grad_dtype  of dlogits: dtype, or FOLD_BF16 for fp32 logits (a bf16 head)
+ *   dlogits     device [rows, fold_row_ld(vocab)], written whole (pad columns
+ *               zero); may be `logits` itself if the types are equal, must not
+ *               overlap it otherwise; NULL: the losses alone
+ *   ws          device workspace of >= fold_distill_workspace_size bytes
+ * Sums are fp32.  Logits of -inf (masked) have probability 0; a target there
+ * has loss +inf.  A row with a target whose logits are all -inf has loss +inf
+ * and gradient 0; one with NaN or +inf has loss and gradient NaN. */
+int32_t fold_distill_workspace_size(int32_t dtype, int64_t rows, int32_t vocab, int32_t num_teacher, size_t* bytes);
+int32_t fold_loss_distill(const fold_sched* sched, int32_t dtype, int64_t rows, int32_t vocab, const void* logits,
+                          int32_t num_teacher, const int32_t* teacher_token, const float* teacher_logit,
+                          const int32_t* labels, float temperature, float soft_weight, float hard_weight, float scale,
+                          float* row_loss, int32_t grad_dtype, void* dlogits, void* ws, size_t ws_bytes,
+                          hipStream_t stream);
+
+/* fold_token_logprobs: what a model says about given tokens.  For every row,
+ * with p = softmax(z) over the vocabulary:
+ *     logp[j]  = log p[tokens[j]]; 0 for a token outside [0, vocab), so that
+ *                sums over padded sequences need no mask
+ *     entropy  = - sum_c p_c log p_c
+ *     top_token, top_logp  the top_k largest log probabilities in order,
+ *                equal ones by the lowest token; entries for which no token
+ *                of probability above -inf is left hold -1 and -inf
+ *   sched       as in fold_loss_distill (tokens and results in NODE order)
+ *   logits      as in fold_loss_distill
+ *   tokens      device [rows, num_tokens] int32; num_tokens may be 0
+ *   logp        device [rows, num_tokens] fp32
+ *   entropy     device [rows] fp32, or NULL
+ *   top_token, top_logp  device [rows, top_k] int32, fp32; top_k 0 .. 32
+ *   ws          device workspace of >= fold_token_workspace_size bytes (may be
+ *               NULL where that is 0: many rows)
+ * Sums are fp32.  A row of -inf alone has log probabilities -inf and entropy
+ * 0; one with NaN or +inf has NaN for all of them and top tokens -1.
+ * Errors of both calls: FOLD_E_INVALID for sizes out of range, NULL or
+ * misaligned buffers, overlapping logits and dlogits; FOLD_E_MISMATCH for a
+ * workspace that is too small or a schedule of another size or device. */
+int32_t fold_token_workspace_size(int32_t dtype, int64_t rows, int32_t vocab, int32_t top_k, size_t* bytes);
+int32_t fold_token_logprobs(const fold_sched* sched, int32_t dtype, int64_t rows, int32_t vocab, const void* logits,
+                            int32_t num_tokens, const int32_t* tokens, float* logp, float* entropy, int32_t top_k,
+                            int32_t* top_token, float* top_logp, void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* ---- a whole step as one HIP graph ----------------------------------------
  * The level loop (Section 2: one batched iteration per depth, so a batch of
  * depth D costs O(D) launches instead of one per node) still issues a few

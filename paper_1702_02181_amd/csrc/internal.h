@@ -466,6 +466,27 @@ void launch_dropout_mask(const int* pos_node, int N, int H, int ld, unsigned thr
 void launch_adam(size_t n, float* p, uint16_t* p_bf16, const float* g, float* m, float* v, double b1, double b2,
                  double lr_t, double eps, hipStream_t st);
 
+// ---- vocabulary head (vocab.hip, token.hip) ----
+constexpr int kMaxTeacherTokens = 256;  // teacher's entries of a row: one a thread
+constexpr int kMaxTopTokens = 32;       // alternatives of a row
+int64_t vocab_tiles(int64_t rows, int H, int V);  // workgroups of the largest of the head's launches
+void launch_vocab_logits(int dtype, int64_t rows, int H, int V, const void* states, const void* W, const float* bias,
+                         int out_dtype, void* logits, hipStream_t st);
+size_t vocab_backward_bytes(int dtype, int64_t rows, int H, int V);
+void launch_vocab_backward(int dtype, int64_t rows, int H, int V, const void* states, const void* W,
+                           const void* dlogits, float* d_states, float* dW, float* dbias, int add, void* ws,
+                           hipStream_t st);
+size_t distill_workspace_bytes(int dtype, int64_t rows, int V, int num_teacher);
+// order: row p's targets and loss are at order[p] (NULL: p)
+void launch_distill(int dtype, const int* order, int64_t rows, int V, const void* logits, int num_teacher,
+                    const int* teacher_token, const float* teacher_logit, const int* labels, float temperature,
+                    float soft, float hard, float scale, float* row_loss, int grad_dtype, void* dlogits, void* ws,
+                    hipStream_t st);
+size_t token_workspace_bytes(int dtype, int64_t rows, int V, int top_k);
+void launch_token(int dtype, const int* order, int64_t rows, int V, const void* logits, int num_tokens,
+                  const int* tokens, float* logp, float* entropy, int top_k, int* top_token, float* top_logp, void* ws,
+                  hipStream_t st);
+
 // ---- achievable-peak probes (diag.hip) ----
 int32_t probe_mfma(int dtype, bool random_operands, hipStream_t st, double* tflops);
 int32_t probe_copy(void* dst, const void* src, size_t bytes, hipStream_t st, double* gbs);

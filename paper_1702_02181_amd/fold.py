@@ -9,14 +9,16 @@ The functions keep the ABI's names:
     fold_schedule, fold_sched_get_info, fold_sched_free, fold_trim,
     fold_pack_params, fold_packed_free, fold_workspace_size,
     fold_forward, fold_backward, fold_row_ld, fold_last_error,
-    fold_graph_create, fold_graph_launch, fold_graph_num_nodes, fold_graph_free
-``Schedule`` / ``Packed`` / ``StepGraph`` wrap them for tensors.
+    fold_graph_create, fold_graph_launch, fold_graph_num_nodes, fold_graph_free,
+    fold_vocab_logits, fold_vocab_backward, fold_loss_distill, fold_token_logprobs
+``Schedule`` / ``Packed`` / ``StepGraph`` / ``VocabHead``, ``distill_loss`` and ``token_logprobs`` wrap them for tensors.
 """
 from __future__ import annotations
 
 import ctypes
 import os
 from ctypes import POINTER, byref, c_int32, c_int64, c_size_t, c_void_p
+from typing import NamedTuple
 
 import numpy as np
 
@@ -114,6 +116,7 @@ class fold_step_buffers(ctypes.Structure):
 
 
 FOLD_STEP_BACKWARD, FOLD_STEP_ZERO_GRADS = 1, 2
+FOLD_VOCAB_ACCUMULATE = 1
 
 
 class fold_kernel_stat(ctypes.Structure):
@@ -139,7 +142,9 @@ EXPORTS = ["fold_schedule", "fold_sched_get_info", "fold_sched_free", "fold_pack
            "fold_graph_num_nodes", "fold_graph_free", "fold_pack_update", "fold_loss_softmax_ce",
            "fold_loss_workspace_size", "fold_adam_step", "fold_forward_dropout", "fold_backward_dropout",
            "fold_dropout_mask", "fold_forward_noalloc", "fold_schedule_typed", "fold_typed_sched_get_info",
-           "fold_typed_sched_free", "fold_level_launches", "fold_trim"]
+           "fold_typed_sched_free", "fold_level_launches", "fold_trim", "fold_vocab_logits", "fold_vocab_backward",
+           "fold_vocab_workspace_size", "fold_loss_distill", "fold_distill_workspace_size", "fold_token_logprobs",
+           "fold_token_workspace_size"]
 
 _lib = None
 
@@ -231,6 +236,25 @@ def lib():
     L.fold_adam_step.restype = c_int32
     L.fold_adam_step.argtypes = [c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, ctypes.c_double,
                                  ctypes.c_double, ctypes.c_double, ctypes.c_double, c_int32, c_void_p]
+    L.fold_vocab_logits.restype = c_int32
+    L.fold_vocab_logits.argtypes = [c_int32, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p,
+                                    c_void_p]
+    L.fold_vocab_workspace_size.restype = c_int32
+    L.fold_vocab_workspace_size.argtypes = [c_int32, c_int64, c_int32, c_int32, POINTER(c_size_t)]
+    L.fold_vocab_backward.restype = c_int32
+    L.fold_vocab_backward.argtypes = [c_int32, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
+                                      c_void_p, c_void_p, c_int32, c_void_p, c_size_t, c_void_p]
+    L.fold_distill_workspace_size.restype = c_int32
+    L.fold_distill_workspace_size.argtypes = [c_int32, c_int64, c_int32, c_int32, POINTER(c_size_t)]
+    L.fold_loss_distill.restype = c_int32
+    L.fold_loss_distill.argtypes = [c_void_p, c_int32, c_int64, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
+                                    ctypes.c_float, ctypes.c_float, ctypes.c_float, ctypes.c_float, c_void_p, c_int32,
+                                    c_void_p, c_void_p, c_size_t, c_void_p]
+    L.fold_token_workspace_size.restype = c_int32
+    L.fold_token_workspace_size.argtypes = [c_int32, c_int64, c_int32, c_int32, POINTER(c_size_t)]
+    L.fold_token_logprobs.restype = c_int32
+    L.fold_token_logprobs.argtypes = [c_void_p, c_int32, c_int64, c_int32, c_void_p, c_int32, c_void_p, c_void_p,
+                                      c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
     _lib = L
     return L
 
@@ -368,6 +392,51 @@ def fold_forward_noalloc(sched, packed, table, table_rows, h_pool, c_pool, roots
 def fold_dropout_mask(sched, hidden, p, seed, step, mask, stream=None):
     _check(lib().fold_dropout_mask(sched, int(hidden), float(p), int(seed) & (2 ** 64 - 1), int(step) & (2 ** 64 - 1),
                                    _ptr(mask), _stream(stream)))
+
+
+def fold_vocab_logits(dtype, rows, hidden, vocab, states, W, bias, logits_dtype, logits, stream=None):
+    _check(lib().fold_vocab_logits(int(dtype), int(rows), int(hidden), int(vocab), _ptr(states), _ptr(W), _ptr(bias),
+                                   int(logits_dtype), _ptr(logits), _stream(stream)))
+
+
+def fold_vocab_workspace_size(dtype, rows, hidden, vocab) -> int:
+    n = c_size_t()
+    _check(lib().fold_vocab_workspace_size(int(dtype), int(rows), int(hidden), int(vocab), byref(n)))
+    return int(n.value)
+
+
+def fold_vocab_backward(dtype, rows, hidden, vocab, states, W, dlogits, d_states, dW, dbias, flags, ws, ws_bytes,
+                        stream=None):
+    _check(lib().fold_vocab_backward(int(dtype), int(rows), int(hidden), int(vocab), _ptr(states), _ptr(W),
+                                     _ptr(dlogits), _ptr(d_states), _ptr(dW), _ptr(dbias), int(flags), _ptr(ws),
+                                     int(ws_bytes), _stream(stream)))
+
+
+def fold_distill_workspace_size(dtype, rows, vocab, num_teacher) -> int:
+    n = c_size_t()
+    _check(lib().fold_distill_workspace_size(int(dtype), int(rows), int(vocab), int(num_teacher), byref(n)))
+    return int(n.value)
+
+
+def fold_loss_distill(sched, dtype, rows, vocab, logits, num_teacher, teacher_token, teacher_logit, labels, temperature,
+                      soft_weight, hard_weight, scale, row_loss, grad_dtype, dlogits, ws, ws_bytes, stream=None):
+    _check(lib().fold_loss_distill(sched, int(dtype), int(rows), int(vocab), _ptr(logits), int(num_teacher),
+                                   _ptr(teacher_token), _ptr(teacher_logit), _ptr(labels), float(temperature),
+                                   float(soft_weight), float(hard_weight), float(scale), _ptr(row_loss),
+                                   int(grad_dtype), _ptr(dlogits), _ptr(ws), int(ws_bytes), _stream(stream)))
+
+
+def fold_token_workspace_size(dtype, rows, vocab, top_k) -> int:
+    n = c_size_t()
+    _check(lib().fold_token_workspace_size(int(dtype), int(rows), int(vocab), int(top_k), byref(n)))
+    return int(n.value)
+
+
+def fold_token_logprobs(sched, dtype, rows, vocab, logits, num_tokens, tokens, logp, entropy, top_k, top_token,
+                        top_logp, ws, ws_bytes, stream=None):
+    _check(lib().fold_token_logprobs(sched, int(dtype), int(rows), int(vocab), _ptr(logits), int(num_tokens),
+                                     _ptr(tokens), _ptr(logp), _ptr(entropy), int(top_k), _ptr(top_token),
+                                     _ptr(top_logp), _ptr(ws), int(ws_bytes), _stream(stream)))
 
 
 def fold_packed_free(handle):
@@ -636,3 +705,172 @@ class StepGraph:
             except Exception:
                 pass
             self.handle = None
+
+
+# ----------------------------------------------------------------------------- the vocabulary head
+
+def _row_ld(width: int) -> int:
+    return (width + 63) // 64 * 64
+
+
+def _code(dtype) -> int:
+    import torch
+    if dtype == torch.float32:
+        return FOLD_F32
+    if dtype == torch.bfloat16:
+        return FOLD_BF16
+    raise ValueError(f"expected float32 or bfloat16, got {dtype}")
+
+
+def _matrix(name, t, width, dtype=None, rows=None):
+    """A dense matrix [rows, fold_row_ld(width)] on the current device, as the library reads it."""
+    import torch
+    if not (t.is_cuda and t.dim() == 2 and t.is_contiguous()):
+        raise ValueError(f"{name}: a contiguous 2-D CUDA tensor is needed")
+    if t.shape[1] != _row_ld(width):
+        raise ValueError(f"{name}: rows of {_row_ld(width)} elements are needed (width {width}), got {t.shape[1]}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
+    if rows is not None and t.shape[0] != rows:
+        raise ValueError(f"{name}: expected {rows} rows, got {t.shape[0]}")
+    _here(name, t)
+    return t
+
+
+def _vector(name, t, dtype, *shape):
+    if not (t.is_cuda and t.is_contiguous()) or t.dtype != dtype or tuple(t.shape) != shape:
+        raise ValueError(f"{name}: a contiguous CUDA tensor {list(shape)} of {dtype} is needed, got "
+                         f"{list(t.shape)} of {t.dtype}")
+    _here(name, t)
+    return t
+
+
+def _here(name, t):
+    import torch
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _on(stream):
+    """New tensors belong to the stream that the call runs on."""
+    import contextlib
+
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+class VocabHead:
+    """The head z = s W^T + bias of a vocabulary (fold_vocab_logits, fold_vocab_backward).
+
+    weight: [vocab, fold_row_ld(hidden)], float32 or bfloat16, laid out as a leaf table (which may be it: tied
+    weights); bias: [vocab] float32 or None.  Results and workspaces are new tensors of the calls' stream."""
+
+    def __init__(self, weight, bias=None, hidden=None):
+        import torch
+        self.hidden = int(weight.shape[1] if hidden is None else hidden)
+        self.weight = _matrix("weight", weight, self.hidden)
+        self.vocab, self.dtype = int(weight.shape[0]), weight.dtype
+        self.code = _code(weight.dtype)
+        self.bias = None if bias is None else _vector("bias", bias, torch.float32, self.vocab)
+
+    def logits(self, states, dtype=None, out=None, stream=None):
+        """[rows, fold_row_ld(vocab)] logits of `states` [rows, fold_row_ld(hidden)], of dtype (the head's)."""
+        import torch
+        _matrix("states", states, self.hidden, self.dtype)
+        rows = states.shape[0]
+        with _on(stream):
+            if out is None:
+                out = torch.empty((rows, _row_ld(self.vocab)), dtype=dtype or self.dtype, device=states.device)
+            else:
+                _matrix("out", out, self.vocab, dtype, rows)
+            fold_vocab_logits(self.code, rows, self.hidden, self.vocab, states, self.weight, self.bias,
+                              _code(out.dtype), out, stream)
+        return out
+
+    def backward(self, states, dlogits, d_states=True, dW=True, dbias=True, accumulate=False, stream=None):
+        """(d_states, dW, dbias) of `dlogits` [rows, fold_row_ld(vocab)].  Each of the three: True for a new tensor, a
+        tensor to write, or None to leave it out.  accumulate: dW and dbias are added to the tensors given."""
+        import torch
+        _matrix("states", states, self.hidden, self.dtype)
+        rows = states.shape[0]
+        _matrix("dlogits", dlogits, self.vocab, self.dtype, rows)
+        if accumulate and (dW is True or dbias is True):
+            raise ValueError("accumulate needs the dW and dbias to add to (or None)")
+        f32 = dict(dtype=torch.float32, device=states.device)
+        with _on(stream):
+            if d_states is True:
+                d_states = torch.empty((rows, _row_ld(self.hidden)), **f32)
+            elif d_states is not None:
+                _matrix("d_states", d_states, self.hidden, torch.float32, rows)
+            if dW is True:
+                dW = torch.empty((self.vocab, _row_ld(self.hidden)), **f32)
+            elif dW is not None:
+                _matrix("dW", dW, self.hidden, torch.float32, self.vocab)
+            if dbias is True:
+                dbias = torch.empty(self.vocab, **f32)
+            elif dbias is not None:
+                _vector("dbias", dbias, torch.float32, self.vocab)
+            n = fold_vocab_workspace_size(self.code, rows, self.hidden, self.vocab)
+            ws = torch.empty(n, dtype=torch.uint8, device=states.device) if n else None
+            fold_vocab_backward(self.code, rows, self.hidden, self.vocab, states, self.weight, dlogits, d_states, dW,
+                                dbias, FOLD_VOCAB_ACCUMULATE if accumulate else 0, ws, n, stream)
+        return d_states, dW, dbias
+
+
+def distill_loss(logits, vocab, teacher_token=None, teacher_logit=None, labels=None, temperature=1.0, soft_weight=1.0,
+                 hard_weight=0.0, scale=1.0, dlogits=True, grad_dtype=None, sched=None, stream=None):
+    """(losses [rows], gradient [rows, fold_row_ld(vocab)]) of fold_loss_distill.
+
+    teacher_token, teacher_logit: [rows, num_teacher] int32, float32; labels: [rows] int32.  sched: a Schedule whose
+    pool rows the logits are; targets and losses are then in node order.  dlogits: True for a new tensor (of grad_dtype,
+    the logits' type by default), a tensor to write (the logits themselves, for one), or None for the losses alone."""
+    import torch
+    _matrix("logits", logits, vocab)
+    code, rows, k = _code(logits.dtype), logits.shape[0], 0
+    if (teacher_token is None) != (teacher_logit is None):
+        raise ValueError("teacher_token and teacher_logit come together")
+    if teacher_token is not None:
+        k = int(teacher_token.shape[-1])
+        _vector("teacher_token", teacher_token, torch.int32, rows, k)
+        _vector("teacher_logit", teacher_logit, torch.float32, rows, k)
+    if labels is not None:
+        _vector("labels", labels, torch.int32, rows)
+    with _on(stream):
+        if dlogits is True:
+            dlogits = torch.empty(logits.shape, dtype=grad_dtype or logits.dtype, device=logits.device)
+        elif dlogits is not None:
+            _matrix("dlogits", dlogits, vocab, grad_dtype, rows)
+        loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
+        n = fold_distill_workspace_size(code, rows, vocab, k)
+        ws = torch.empty(n, dtype=torch.uint8, device=logits.device) if n else None
+        fold_loss_distill(None if sched is None else sched.handle, code, rows, vocab, logits, k, teacher_token,
+                          teacher_logit, labels, temperature, soft_weight, hard_weight, scale, loss,
+                          code if dlogits is None else _code(dlogits.dtype), dlogits, ws, n, stream)
+    return loss, dlogits
+
+
+class TokenLogprobs(NamedTuple):
+    """logp [rows, num_tokens], entropy [rows], top_token and top_logp [rows, top_k]."""
+    logp: object
+    entropy: object
+    top_token: object
+    top_logp: object
+
+
+def token_logprobs(logits, vocab, tokens=None, top_k=0, sched=None, stream=None) -> TokenLogprobs:
+    """Log probabilities of `tokens` [rows, num_tokens] int32, the rows' entropy and their top_k alternatives
+    (fold_token_logprobs).  sched: as in distill_loss."""
+    import torch
+    _matrix("logits", logits, vocab)
+    code, rows, J, top_k = _code(logits.dtype), logits.shape[0], 0, int(top_k)
+    if tokens is not None:
+        J = int(tokens.shape[-1])
+        _vector("tokens", tokens, torch.int32, rows, J)
+    n = fold_token_workspace_size(code, rows, vocab, top_k)
+    with _on(stream):
+        new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
+        out = TokenLogprobs(new(rows, J), new(rows), new(rows, top_k, dtype=torch.int32), new(rows, top_k))
+        ws = new(n, dtype=torch.uint8) if n else None
+        fold_token_logprobs(None if sched is None else sched.handle, code, rows, vocab, logits, J, tokens, out.logp,
+                            out.entropy, top_k, out.top_token, out.top_logp, ws, n, stream)
+    return out

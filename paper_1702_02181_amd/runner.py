@@ -162,6 +162,22 @@ class DeviceRun:
         return out, dt
 
 
+def trained_tensors(dev: DeviceRun, train_table: bool):
+    """(fp32 master, bf16 copy or None, gradient) of every trained tensor of a workload's own parameters."""
+    out = []
+    for p, st, gt in zip(dev.w.params, dev.set_tensors, dev.grad_tensors):
+        if p.kind == gen.KIND_EMBED:
+            continue
+        for name, g in zip(("W_in", "W_rec", "bias"), gt):
+            if g is None:
+                continue
+            cur = st[name]
+            out.append((cur, None, g) if cur.dtype == torch.float32 else (cur.float(), cur, g))
+    if train_table:
+        out.append((dev.table.float(), dev.table, dev.d_table) if dev.bf16 else (dev.table, None, dev.d_table))
+    return out
+
+
 class TrainStep:
     """One training step of a workload through the C ABI (Section 3.5's setting: a class label on every node,
     softmax cross entropy on every node's state, Adam): zero the gradients, fold_forward,
@@ -201,23 +217,7 @@ class TrainStep:
         dev.alloc_grads(train_table)
         dev.set_upstream(np.zeros_like(w.dh_roots))
         dev.dh_nodes = self.dh_nodes
-        # (fp32 master, bf16 copy or None, gradient) of every trained tensor
-        self.tensors = []
-        for p, st, gt in zip(w.params, dev.set_tensors, dev.grad_tensors):
-            if p.kind == gen.KIND_EMBED:
-                continue
-            for name, g in zip(("W_in", "W_rec", "bias"), gt):
-                if g is None:
-                    continue
-                cur = st[name]
-                if cur.dtype == torch.float32:
-                    self.tensors.append((cur, None, g))
-                else:
-                    self.tensors.append((cur.float(), cur, g))
-        if train_table:
-            self.tensors.append((dev.table.float(), dev.table if dev.bf16 else None, dev.d_table))
-            if not dev.bf16:
-                self.tensors[-1] = (dev.table, None, dev.d_table)
+        self.tensors = trained_tensors(dev, train_table)
         self.tensors += [(self.W_cls, None, self.dW_cls), (self.b_cls, None, self.db_cls)]
         self.moments = [(torch.zeros_like(m), torch.zeros_like(m)) for m, _, _ in self.tensors]
 
@@ -262,3 +262,81 @@ class TrainStep:
         for (master, low, grad), (m, v) in zip(self.tensors, self.moments):
             F.fold_adam_step(master.numel(), master, low, grad, m, v, lr, b1, b2, eps, self.t, dev.stream)
         dev.packed.update(dev.set_tensors, dev.stream)
+
+
+class VocabStep:
+    """One training step of a workload whose nodes each name a token of a vocabulary, through the C ABI: zero the
+    gradients, fold_forward, fold_vocab_logits on the whole pool, fold_loss_distill (a teacher's top logits, labels, or
+    both; the gradient over the logits, in place), fold_vocab_backward (its d_states are fold_backward's dh_nodes),
+    fold_backward, fold_adam_step on every parameter tensor and the head, fold_pack_update.
+
+    labels [N], teacher_token and teacher_logit [N, num_teacher] are in node order; the loss is the mean over the nodes
+    that have a target.  tied: the leaf table is the head's W (a table of `hidden` columns; the vocabulary is its rows)
+    and the head's dW is added to the table's gradient.  score() gives the log probabilities of tokens under the current
+    weights."""
+
+    def __init__(self, w: gen.Workload, vocab: int, labels=None, teacher_token=None, teacher_logit=None,
+                 temperature: float = 1.0, soft_weight: float = 1.0, hard_weight: float = 0.0, train_table: bool = True,
+                 tied: bool = False, seed: int = 0, lr: float = 1e-3, beta1: float = 0.9, beta2: float = 0.999,
+                 eps: float = 1e-8):
+        self.dev = dev = DeviceRun(w)
+        if tied and (not train_table or w.leaf_table.shape != (vocab, w.hidden)):
+            raise ValueError("a tied head needs a trained leaf table [vocab, hidden]")
+        self.vocab, self.tied, self.hyper, self.t = vocab, tied, (lr, beta1, beta2, eps), 0
+        cuda = lambda a, dt: None if a is None else torch.from_numpy(np.ascontiguousarray(a)).to(dt).to(dev.device)
+        self.labels = cuda(labels, torch.int32)
+        self.teacher_token, self.teacher_logit = cuda(teacher_token, torch.int32), cuda(teacher_logit, torch.float32)
+        self.loss_args = dict(temperature=temperature, soft_weight=soft_weight, hard_weight=hard_weight)
+        have = np.zeros(dev.N, bool)
+        if labels is not None:
+            have |= (np.asarray(labels) >= 0) & (np.asarray(labels) < vocab)
+        if teacher_token is not None:
+            have |= ((np.asarray(teacher_token) >= 0) & (np.asarray(teacher_token) < vocab)).any(1)
+        self.scale = 1.0 / max(1, int(have.sum()))
+        dev.alloc_grads(train_table)
+        dev.set_upstream(np.zeros_like(w.dh_roots))
+        self.dh_nodes = dev.dh_nodes = torch.zeros((dev.N, dev.ld), dtype=torch.float32, device=dev.device)
+        self.tensors = trained_tensors(dev, train_table)
+        self.bias = torch.zeros(vocab, dtype=torch.float32, device=dev.device)
+        self.db = torch.zeros_like(self.bias)
+        if tied:
+            self.W, self.dW = dev.table, dev.d_table
+        else:
+            rng = np.random.default_rng(seed)
+            W = torch.from_numpy(pad_cols(0.1 * rng.standard_normal((vocab, w.hidden)), dev.ld)).to(dev.device)
+            self.W, self.dW = W.to(dev.tdtype), torch.zeros_like(W)
+            self.tensors.append((self.W.float(), self.W, self.dW) if dev.bf16 else (self.W, None, self.dW))
+        self.tensors.append((self.bias, None, self.db))
+        self.head = F.VocabHead(self.W, self.bias, w.hidden)
+        self.logits = torch.zeros((dev.N, F.fold_row_ld(vocab)), dtype=dev.tdtype, device=dev.device)
+        self.node_loss = None
+        self.moments = [(torch.zeros_like(m), torch.zeros_like(m)) for m, _, _ in self.tensors]
+
+    def gradients(self):
+        """Zero the gradients, forward, head, loss, both backward passes (kernel launches only)."""
+        dev, st = self.dev, self.dev.stream
+        dev.zero_grads()
+        dev.forward()
+        self.head.logits(dev.h_pool, out=self.logits, stream=st)
+        self.node_loss, _ = F.distill_loss(self.logits, self.vocab, self.teacher_token, self.teacher_logit, self.labels,
+                                           scale=self.scale, dlogits=self.logits, sched=dev.sched, stream=st,
+                                           **self.loss_args)
+        self.db.zero_()
+        self.head.backward(dev.h_pool, self.logits, self.dh_nodes, self.dW, self.db, accumulate=self.tied, stream=st)
+        dev.backward()
+
+    def step(self):
+        dev = self.dev
+        self.t += 1
+        self.gradients()
+        lr, b1, b2, eps = self.hyper
+        for (master, low, grad), (m, v) in zip(self.tensors, self.moments):
+            F.fold_adam_step(master.numel(), master, low, grad, m, v, lr, b1, b2, eps, self.t, dev.stream)
+        dev.packed.update(dev.set_tensors, dev.stream)
+
+    def score(self, tokens, top_k: int = 0):
+        """F.TokenLogprobs of `tokens` [N, num_tokens] (node order) under the current weights."""
+        dev = self.dev
+        dev.forward()
+        self.head.logits(dev.h_pool, out=self.logits, stream=dev.stream)
+        return F.token_logprobs(self.logits, self.vocab, tokens, top_k, sched=dev.sched, stream=dev.stream)

@@ -1,0 +1,583 @@
+"""Parity of the vocabulary head (products, distillation loss, token log probabilities) with the fp64 oracle.
+
+Bounds, from the arithmetic (u = 2^-24, fp32's half step; a sum of n terms in any order is within n u of the sum of its
+terms' magnitudes, to first order):
+  * products: (K + 8) u of sum |a| |b| per output (K products, the bias, the pieces), and for bf16 logits half a step of
+    bf16 (2^-8 of the value) on top;
+  * log p = ln 2 (x - log2 s): x is one fma (u |x|), 2^x one instruction and s a sum of V terms in threads of V / 256
+    terms and about 20 joins; a base-2 exponential and logarithm are within 2 ulp (4 u).  So p is within
+    rel = u (4 |log p| + V / 256 + 64) of itself, log p within that absolutely, the entropy sum within rel times the sum
+    of p |log p| plus rel;
+  * the distillation loss and its gradient: the same rel on p^T and p (|log p| counted at z / T), q within u (4 |t| / T +
+    300) (256 terms); dz is at most rel times the magnitudes it is made of, and half a step of its type (2^-8 of bf16).
+"""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import vocab as OV
+from paper_1702_02181_amd import fold as F
+from paper_1702_02181_amd import gen
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+NAN = float("nan")
+
+
+def _t(dtype):
+    import torch
+    return torch.float32 if dtype == "f32" else torch.bfloat16
+
+
+def _round(a, dtype):
+    a = np.asarray(a, np.float32)
+    return a if dtype == "f32" else gen.round_bf16(a)
+
+
+def _dev(a, dtype="f32", fill=0.0):
+    """[rows, fold_row_ld(width)] on the GPU; `fill` in the pad columns."""
+    import torch
+    a = np.asarray(a, np.float32)
+    out = torch.full((a.shape[0], F.fold_row_ld(a.shape[1])), fill, dtype=torch.float32)
+    out[:, :a.shape[1]] = torch.from_numpy(a)
+    return out.to(_t(dtype)).cuda()
+
+
+def _ints(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, np.int32)).cuda()
+
+
+def _floats(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, np.float32)).cuda()
+
+
+def _np(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def _within(got, want, bound, what):
+    """Elementwise; infinities and NaN have to be the same ones."""
+    got, want, bound = np.asarray(got), np.asarray(want), np.broadcast_to(bound, np.shape(want))
+    # results are fp32 at most: from 2^128 (1 - 2^-25) on a value rounds to infinity (a loss of 5.1e38, say)
+    want = np.where(np.abs(want) >= 2.0 ** 128 * (1 - 2.0 ** -25), np.copysign(np.inf, want), want)
+    fine = np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want)), what
+    assert np.array_equal(got[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)]), what
+    off = np.abs(got[fine] - want[fine]) - bound[fine]
+    assert not (off > 0).any(), (what, float(off.max()), int((off > 0).sum()), off.size)
+
+
+# ---- products -------------------------------------------------------------------------------------------------------
+
+PRODUCTS = [(1, 1, 1, "f32"), (1, 64, 7, "bf16"), (3, 300, 129, "bf16"), (130, 65, 257, "f32"), (257, 1000, 500, "f32"),
+            (128, 128, 128, "bf16"), (33, 4096, 70, "bf16"), (2, 17, 20001, "f32"), (300, 96, 1111, "bf16"),
+            (16, 1024, 3000, "bf16"), (17, 256, 640, "f32"), (64, 520, 999, "bf16"), (1, 1024, 4097, "f32")]
+
+
+def _product_case(M, H, V, dtype, seed):
+    rng = np.random.default_rng(seed)
+    s = _round(np.tanh(rng.standard_normal((M, H))), dtype)
+    W = _round(rng.standard_normal((V, H)) / math.sqrt(H), dtype)
+    b = (0.3 * rng.standard_normal(V)).astype(np.float32)
+    dz = _round(rng.standard_normal((M, V)) / M, dtype)
+    dz[M // 2] = 0
+    return s, W, b, dz
+
+
+@pytest.mark.parametrize("M,H,V,dtype", PRODUCTS)
+@pytest.mark.parametrize("biased", [True, False])
+def test_logits(M, H, V, dtype, biased):
+    import torch
+    s, W, b, _ = _product_case(M, H, V, dtype, M + H + V)
+    if biased:
+        b[V // 2] = -np.inf  # a token taken out
+    head = F.VocabHead(_dev(W, dtype), _floats(b) if biased else None, H)
+    want = OV.head(s, W, b if biased else None)
+    mag = np.abs(s.astype(np.float64)) @ np.abs(W.astype(np.float64)).T + (np.abs(np.where(np.isinf(b), 0, b)) if biased else 0)
+    sd = _dev(s, dtype)
+    for out in ("f32", "bf16") if dtype == "bf16" else ("f32",):
+        z = torch.full((M, F.fold_row_ld(V)), NAN, dtype=_t(out), device="cuda")
+        assert head.logits(sd, out=z) is z
+        got = _np(z)
+        assert not got[:, V:].any()
+        _within(got[:, :V], want, (H + 8) * U * mag + (2.0 ** -8 * np.abs(np.where(np.isinf(want), 0, want)) if out == "bf16" else 0), out)
+        assert torch.equal(head.logits(sd, dtype=_t(out)), z)
+
+
+@pytest.mark.parametrize("M,H,V,dtype", PRODUCTS)
+def test_backward(M, H, V, dtype):
+    import torch
+    s, W, _, dz = _product_case(M, H, V, dtype, 7 * M + H + V)
+    head = F.VocabHead(_dev(W, dtype), None, H)
+    sd, dzd = _dev(s, dtype), _dev(dz, dtype)
+    want = OV.head_backward(s, W, dz)
+    a = [np.abs(x.astype(np.float64)) for x in (s, W, dz)]
+    mag = (a[2] @ a[1], a[2].T @ a[0], a[2].sum(0))
+    bound = [(n + 72) * U * m for n, m in zip((V, M, M), mag)]
+    ld = F.fold_row_ld(H)
+    full = lambda *shape: torch.full(shape, NAN, dtype=torch.float32, device="cuda")  # noqa: E731
+    ds, dW, db = head.backward(sd, dzd, full(M, ld), full(V, ld), full(V))
+    for name, got, w, bd in (("ds", _np(ds), want[0], bound[0]), ("dW", _np(dW), want[1], bound[1])):
+        assert not got[:, H:].any(), name
+        _within(got[:, :H], w, bd, name)
+    _within(_np(db), want[2], bound[2], "db")
+    # one at a time: the same bits
+    assert torch.equal(head.backward(sd, dzd, True, None, None)[0], ds)
+    assert torch.equal(head.backward(sd, dzd, None, True, None)[1], dW)
+    assert torch.equal(head.backward(sd, dzd, None, None, True)[2], db)
+    # added to what is there, whose pad columns stay
+    rng = np.random.default_rng(1)
+    W0, b0 = rng.standard_normal((V, H)).astype(np.float32), rng.standard_normal(V).astype(np.float32)
+    dW0, db0 = _dev(W0, fill=5.0), _floats(b0)
+    _, dW1, db1 = head.backward(sd, dzd, None, dW0, db0, accumulate=True)
+    got = _np(dW1)
+    assert dW1 is dW0 and (got[:, H:] == 5).all()
+    _within(got[:, :H], W0 + want[1], bound[1] + U * np.abs(W0 + want[1]), "dW +=")
+    _within(_np(db1), b0 + want[2], bound[2] + U * np.abs(b0 + want[2]), "db +=")
+
+
+def test_backward_of_no_rows():
+    import torch
+    head = F.VocabHead(_dev(np.ones((100, 70))), None, 70)
+    none = torch.zeros((0, 128), device="cuda")
+    ds, dW, db = head.backward(none, none, dW=torch.full((100, 128), NAN, device="cuda"),
+                               dbias=torch.full((100,), NAN, device="cuda"))
+    assert ds.shape == (0, 128) and not dW.any() and not db.any()
+    assert head.logits(none).shape == (0, 128)
+
+
+def test_products_read_nothing_past_their_matrices():
+    """States, weights and gradients that end where the next tensor's NaN begins."""
+    import torch
+    M, H, V = 5, 70, 131
+    s, W, b, dz = _product_case(M, H, V, "f32", 3)
+
+    def walled(a):
+        p = _dev(a)
+        wall = torch.full((p.shape[0] + 256, p.shape[1]), NAN, device="cuda")
+        wall[128:128 + p.shape[0]] = p
+        return wall[128:128 + p.shape[0]]
+    head = F.VocabHead(walled(W), _floats(b), H)
+    z = head.logits(walled(s))
+    ds, dW, db = head.backward(walled(s), walled(dz))
+    for x in (z, ds, dW, db):
+        assert torch.isfinite(x).all()
+
+
+# ---- rows of logits -------------------------------------------------------------------------------------------------
+
+def _logits(rng, M, V, dtype, spread=2.5):
+    return _round(spread * rng.standard_normal((M, V)), dtype)
+
+
+def _rel(z, T, V):
+    """The bound's rel for every logit of fine rows."""
+    z = np.asarray(z, np.float64) / T
+    with np.errstate(all="ignore"):
+        m = np.where(np.isfinite(z), z, -np.inf).max(1, keepdims=True)
+        far = np.where(np.isfinite(z - m), np.abs(z - m), 0.0)
+    return U * (4 * np.minimum(far + math.log(V), 300.0) + V / 256 + 64)
+
+
+ROWS = [(1, 1, "f32"), (3, 2, "bf16"), (5, 63, "f32"), (7, 64, "bf16"), (4, 1000, "bf16"), (9, 2049, "f32"),
+        (2, 20001, "f32"), (2, 33333, "bf16"), (1, 131073, "bf16"), (1040, 130, "f32"), (1030, 77, "bf16")]
+
+
+def _check_tokens(z, dtype, tokens, K, fill=NAN):
+    import torch
+    M, V = z.shape
+    zd = _dev(z, dtype, fill)
+    r = F.token_logprobs(zd, V, _ints(tokens), K)
+    logp, ent, top, top_lp = OV.token_logprobs(z, tokens, K)
+    rel = _rel(z, 1.0, V)
+    at = np.clip(tokens, 0, V - 1)
+    size = np.where(np.isfinite(logp), np.abs(logp), 0)
+    _within(_np(r.logp), logp, np.take_along_axis(rel, at, 1) + 2 * U * size, "logp")
+    big = rel[:, 0:1] * 0 + U * (V / 256 + 64)
+    _within(_np(r.entropy), ent, 4 * big[:, 0] * (1 + np.where(np.isfinite(ent), ent, 0)) + 16 * U * np.where(np.isfinite(ent), ent, 0) ** 2, "entropy")
+    assert np.array_equal(r.top_token.cpu().numpy(), top), "top tokens"
+    with np.errstate(all="ignore"):
+        b = U * (4 * np.where(np.isfinite(top_lp), np.abs(top_lp), 0) * 1.5 + V / 256 + 64 + 4 * math.log(V))
+    _within(_np(r.top_logp), top_lp, b, "top log probabilities")
+    again = F.token_logprobs(zd, V, _ints(tokens), K)
+    assert all(torch.equal(torch.nan_to_num(x.float(), 7.0), torch.nan_to_num(y.float(), 7.0)) for x, y in zip(r, again))
+    return r
+
+
+@pytest.mark.parametrize("M,V,dtype", ROWS)
+@pytest.mark.parametrize("K,J", [(0, 1), (5, 3), (32, 0)])
+def test_token_logprobs(M, V, dtype, K, J):
+    rng = np.random.default_rng(M + V + K)
+    tok = rng.integers(-1, V + 1, (M, J))
+    _check_tokens(_logits(rng, M, V, dtype), dtype, tok, K)
+
+
+def _hard_rows(dtype, V, rng):
+    """Rows whose masks and values are not a plain model's."""
+    low = float(np.finfo(np.float32).min) if dtype == "f32" else float(np.float32(-3.3895313892515355e38))
+    z = _logits(rng, 20, V, dtype)
+    z[1] = -np.inf                     # the mask leaves nothing
+    z[2, 1:] = -np.inf                 # ... one token
+    z[3, :V - 1] = -np.inf
+    z[4] = low                         # the type's lowest value everywhere: uniform
+    z[5, V // 3:] = low
+    z[6, ::2] = -np.inf
+    z[7, V // 2] = np.nan
+    z[8, V - 1] = np.inf
+    z[9] = 0.0                         # equal logits
+    z[10] = -0.0
+    z[10, ::3] = 0.0
+    z[11] = np.round(z[11])            # few different values
+    z[12] = -low                       # the type's largest
+    z[13, V // 4] = -low
+    z[14, V // 2] = 80.0               # one token takes all
+    z[15] = _round(np.linspace(-9, 9, V), dtype)
+    z[16] = z[15, ::-1]
+    z[17, 1:] = low
+    z[17, 0] = -np.inf
+    z[18, :] = np.nan
+    z[19, 0] = np.nan
+    z[19, 1:] = -np.inf
+    return z
+
+
+@pytest.mark.parametrize("V", [3, 300, 9000, 70001])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_token_logprobs_of_hard_rows(V, dtype):
+    rng = np.random.default_rng(V)
+    z = _hard_rows(dtype, V, rng)
+    _check_tokens(z, dtype, np.stack([np.zeros(20, int), np.full(20, V - 1), np.full(20, V // 2), np.full(20, -1)], 1), 8)
+
+
+@pytest.mark.parametrize("M", [2, 1100])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_top_lists_of_crowded_rows(M, dtype):
+    """Many logits at or above any threshold that a few of them give: equal logits, and the largest ones all in columns
+    that one thread reads."""
+    rng = np.random.default_rng(M)
+    V = 20000
+    z = _logits(rng, M, V, dtype)
+    z[0] = 1.5
+    vec = 4 if dtype == "f32" else 8
+    crowd = (np.arange(V) // vec) % 256 < 2
+    z[1, crowd] = _round(20 + rng.standard_normal(int(crowd.sum())), dtype)
+    for r in range(2, min(M, 6)):
+        z[r, rng.integers(0, V, 3000)] = 9.0
+    _check_tokens(z[:min(M, 6)] if M < 100 else z, dtype, np.zeros((min(M, 6) if M < 100 else M, 1), int), 32)
+
+
+def _check_distill(z, dtype, grad, tok, t, y, T, soft, hard, scale=0.7, inplace=False, sched=None, order=None):
+    """order: node of every row (targets and losses by node)."""
+    import torch
+    M, V = z.shape
+    o = np.arange(M) if order is None else order
+    loss, dz = OV.distill(z, None if tok is None else tok[o], None if t is None else t[o], None if y is None else y[o],
+                          T, soft, hard, scale)
+    zd = _dev(z, dtype, NAN)
+    out = zd if inplace else torch.full((M, F.fold_row_ld(V)), NAN, dtype=_t(grad), device="cuda")
+    args = [None if a is None else f(a) for a, f in ((tok, _ints), (t, _floats), (y, _ints))]
+    alone, none = F.distill_loss(zd, V, *args, temperature=T, soft_weight=soft, hard_weight=hard, scale=scale,
+                                 dlogits=None, sched=sched)
+    got, d = F.distill_loss(zd, V, *args, temperature=T, soft_weight=soft, hard_weight=hard, scale=scale, dlogits=out,
+                            sched=sched)
+    assert none is None and d is out
+    assert torch.equal(torch.nan_to_num(alone, 7.0), torch.nan_to_num(got, 7.0))
+    k = 0 if tok is None else tok.shape[1]
+    relT, rel1 = _rel(z, T, V), _rel(z, 1.0, V)
+    # the magnitudes: p^T and p are at most 1, log p^T of a target at most |z - m| / T + log V
+    with np.errstate(all="ignore"):
+        m = np.where(np.isfinite(z), z, -np.inf).max(1).astype(np.float64)
+    big = np.zeros(M)
+    relq = U * 300
+    tmax = 0.0 if t is None else float(np.abs(t[np.isfinite(t)]).max(initial=0)) / T
+    relq += U * 8 * tmax
+    for r in range(M):
+        cols = [i for i in ([] if tok is None else tok[o[r]]) if 0 <= i < V]
+        worst = max([abs(float(z[r, i]) - m[r]) / T for i in cols if np.isfinite(z[r, i])] + [0.0])
+        big[r] = soft * T * T * ((2 * tmax + 8) * relq + (worst + 20) * 8 * U + U * (V / 256 + 64) + relq * (worst + 20))
+        yy = -1 if y is None else y[o[r]]
+        if 0 <= yy < V and np.isfinite(z[r, yy]):
+            big[r] += hard * (U * (V / 256 + 64) + 8 * U * (abs(float(z[r, yy]) - m[r]) + 20))
+    want = np.empty(M)
+    want[o] = loss
+    bound = np.empty(M)
+    bound[o] = big
+    _within(got.cpu().numpy().astype(np.float64), want, bound + 4 * U * np.abs(np.where(np.isfinite(want), want, 0)), "loss")
+    gd = _np(d)
+    assert not gd[:, V:].any()
+    with np.errstate(all="ignore"):
+        e = z.astype(np.float64) - m[:, None]
+        pT, p1 = np.exp(e / T), np.exp(e)
+        pT, p1 = (np.nan_to_num(p / np.nansum(p, 1, keepdims=True)) for p in (pT, p1))
+    mass = np.zeros((M, V))
+    for r in range(M):
+        for j in range(k):
+            if 0 <= tok[o[r], j] < V:
+                mass[r, tok[o[r], j]] = 1.0
+        if y is not None and 0 <= y[o[r]] < V:
+            mass[r, y[o[r]]] = 1.0
+    db = abs(scale) * (soft * T * (2 * relT * pT + 2 * relq * mass) + hard * (2 * rel1 * p1 + 4 * U * mass)) + 1e-37
+    step = 2.0 ** -8 if (dtype if inplace else grad) == "bf16" else 2 * U
+    # a value rounded to bf16 is at most half a step from what was rounded, itself within db of the truth
+    _within(gd[:, :V], dz, db * (1 + step) + step * np.abs(np.where(np.isfinite(dz), dz, 0)), "dz")
+    return got, d
+
+
+def _targets(rng, M, V, k):
+    tok = rng.integers(0, V, (M, k))
+    t = (3 * rng.standard_normal((M, k))).astype(np.float32)
+    if k > 2:
+        tok[:, 1] = np.where(rng.random(M) < 0.5, tok[:, 0], tok[:, 1])  # the same token twice
+        t[0::3, 2] = -np.inf
+        tok[1::4, k // 2:] = -1
+        tok[2::5, 0] = V
+    y = rng.integers(-1, V, M)
+    y[::3] = tok[::3, 0] if k else y[::3]
+    return tok, t, y
+
+
+@pytest.mark.parametrize("M,V,dtype", ROWS)
+@pytest.mark.parametrize("k,T,soft,hard", [(4, 1.0, 1.0, 0.0), (7, 2.0, 0.6, 0.4), (1, 0.5, 0.0, 1.0), (256, 4.0, 1.0, 1.0)])
+def test_distill(M, V, dtype, k, T, soft, hard):
+    rng = np.random.default_rng(M + V + k)
+    if M > 1000 and k > 7:
+        k = 9
+    tok, t, y = _targets(rng, M, V, k)
+    _check_distill(_logits(rng, M, V, dtype), dtype, dtype, tok, t, y, T, soft, hard)
+
+
+@pytest.mark.parametrize("M,V", [(3, 1000), (2, 70001), (1030, 65)])
+def test_distill_variants(M, V):
+    """fp32 logits with a bf16 gradient; labels alone, a teacher alone; in place for either type."""
+    rng = np.random.default_rng(M * V)
+    tok, t, y = _targets(rng, M, V, 6)
+    z = _logits(rng, M, V, "f32")
+    _check_distill(z, "f32", "bf16", tok, t, y, 2.0, 0.5, 0.5)
+    _check_distill(z, "f32", "f32", None, None, y, 1.0, 1.0, 1.0)
+    _check_distill(z, "f32", "bf16", tok, t, None, 1.0, 1.0, 1.0)
+    _check_distill(z, "f32", "f32", tok, t, y, 2.0, 0.5, 0.5, inplace=True)
+    _check_distill(_round(z, "bf16"), "bf16", "bf16", tok, t, y, 3.0, 0.5, 0.5, inplace=True)
+    _check_distill(z, "f32", "f32", None, None, None, 1.0, 1.0, 1.0)
+
+
+@pytest.mark.parametrize("V", [3, 300, 9000, 70001])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1.0, 2.0])
+def test_distill_of_hard_rows(V, dtype, T):
+    rng = np.random.default_rng(V)
+    z = _hard_rows(dtype, V, rng)
+    tok, t, y = _targets(rng, 20, V, 3)
+    tok[4:7] = V // 5  # also where a row is masked
+    _check_distill(z, dtype, dtype, tok, t, y, T, 0.5, 0.5)
+    # the same rows without a target: nothing, whatever they hold
+    none = np.full((20, 3), -1)
+    loss, dz = _check_distill(z, dtype, dtype, none, t, np.full(20, -1), T, 0.5, 0.5)
+    assert not loss.any() and not dz.any()
+
+
+def test_distill_gradient_by_differences():
+    """Against differences of the library's own losses, in fp32: a step of h = 1/8 along a direction, the error term of
+    central differences h^2 / 6 |f'''| and the losses' own rounding."""
+    import torch
+    rng = np.random.default_rng(8)
+    M, V, k, T = 6, 900, 5, 2.0
+    tok, t, y = _targets(rng, M, V, k)
+    z = _logits(rng, M, V, "f32")
+    a = (_ints(tok), _floats(t), _ints(y))
+    kw = dict(temperature=T, soft_weight=0.5, hard_weight=0.5)
+    loss, dz = F.distill_loss(_dev(z), V, *a, **kw)
+    h = 0.125
+    d = rng.choice([-1.0, 1.0], (M, V)).astype(np.float32)
+    up, _ = F.distill_loss(_dev(z + h * d), V, *a, dlogits=None, **kw)
+    down, _ = F.distill_loss(_dev(z - h * d), V, *a, dlogits=None, **kw)
+    slope = _np(up - down) / (2 * h)
+    want = (_np(dz)[:, :V] * d).sum(1)
+    # third derivative of log sum exp along a direction of entries +-1: at most 2 (a third central moment of values in
+    # [-1, 1]); T^2 (1 / T^3) of it for the soft term
+    bound = h * h / 6 * 2 * (0.5 / T + 0.5) + 64 * U * (np.abs(_np(loss)) + 20) / h
+    assert (np.abs(slope - want) <= bound).all(), (slope - want, bound)
+
+
+# ---- order, streams, graphs -----------------------------------------------------------------------------------------
+
+def _model(dtype, H=64, vocab=300):
+    if dtype == "f32":
+        return gen.config2(seed=11, num_graphs=6, leaves=20, hidden=H)
+    return gen.config3(seed=12, num_graphs=30, hidden=H, vocab=vocab, emb_dim=H, leaf_range=(2, 30))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_node_order(dtype):
+    from paper_1702_02181_amd.runner import DeviceRun
+    import torch
+    w = _model(dtype)
+    dev = DeviceRun(w, with_backward=False)
+    order = dev.sched_arrays()["pos_node"]
+    rng = np.random.default_rng(2)
+    N, V = dev.N, 333
+    z = _logits(rng, N, V, dtype)
+    tok, t, y = _targets(rng, N, V, 4)
+    _check_distill(z, dtype, dtype, tok, t, y, 2.0, 0.5, 0.5, sched=dev.sched, order=order)
+    zd = _dev(z, dtype)
+    by_node = F.token_logprobs(zd, V, _ints(tok), 3, sched=dev.sched)
+    by_row = F.token_logprobs(zd, V, _ints(tok[order]), 3)
+    at = torch.from_numpy(order.astype(np.int64)).cuda()
+    assert all(torch.equal(a[at], b) for a, b in zip(by_node, by_row))
+    with pytest.raises(F.FoldError) as e:
+        F.token_logprobs(zd[:-1], V, _ints(tok[:-1]), 3, sched=dev.sched)
+    assert e.value.code == F.FOLD_E_MISMATCH
+
+
+def _chain(head, s, y, tok, t, vocab, stream=None):
+    z = head.logits(s, stream=stream)
+    r = F.token_logprobs(z, vocab, tok, 5, stream=stream)
+    loss, dz = F.distill_loss(z, vocab, tok, t, y, temperature=2.0, soft_weight=0.5, hard_weight=0.5, dlogits=z,
+                              stream=stream)
+    return [*r, loss, dz, *head.backward(s, dz, stream=stream)]
+
+
+@pytest.mark.parametrize("M,H,V,dtype", [(40, 96, 9001, "bf16"), (300, 64, 1000, "f32")])
+def test_streams_and_graphs(M, H, V, dtype):
+    """The chain on a stream of its own, and captured: every replay, with eager work between, equals the eager results
+    of the inputs it finds."""
+    import torch
+    s, W, b, _ = _product_case(M, H, V, dtype, 5)
+    rng = np.random.default_rng(9)
+    tok, t, y = _targets(rng, M, V, 4)
+    head = F.VocabHead(_dev(W, dtype), _floats(b), H)
+    sd, a = _dev(s, dtype), (_ints(y), _ints(tok), _floats(t))
+    eager = [x.clone() for x in _chain(head, sd, *a, V)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    other = _chain(head, sd, *a, V, stream=side)
+    side.synchronize()
+    assert all(torch.equal(x, z) for x, z in zip(eager, other))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = _chain(head, sd, *a, V)
+    for it in range(3):
+        new = _dev(_round(np.roll(s, it, axis=0), dtype), dtype)
+        want = [x.clone() for x in _chain(head, new, *a, V)]
+        sd.copy_(new)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, z) for x, z in zip(want, out)), it
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each: what either gives alone."""
+    import torch
+    rng = np.random.default_rng(10)
+    V, M = 50001, 6
+    zs = [_dev(_logits(rng, M, V, "f32")) for _ in range(2)]
+    tok, t, y = _targets(rng, M, V, 5)
+    a = (_ints(tok), _floats(t), _ints(y))
+    want = [F.distill_loss(z, V, *a, hard_weight=1.0) + tuple(F.token_logprobs(z, V, a[0], 9)) for z in zs]
+    streams = [torch.cuda.Stream() for _ in zs]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = [F.distill_loss(z, V, *a, hard_weight=1.0, stream=st) + tuple(F.token_logprobs(z, V, a[0], 9, stream=st))
+               for z, st in zip(zs, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, z) for g, w in zip(got, want) for x, z in zip(g, w))
+
+
+def test_wrappers_refuse():
+    import torch
+    W = torch.zeros((10, 64), device="cuda")
+    head = F.VocabHead(W, None, 33)
+    s, z = torch.zeros((4, 64), device="cuda"), torch.zeros((4, 64), device="cuda")
+    i4 = torch.zeros((4, 2), dtype=torch.int32, device="cuda")
+    for bad in (lambda: F.VocabHead(W[:, :32]), lambda: F.VocabHead(W.half()), lambda: F.VocabHead(W, torch.zeros(9, device="cuda")),
+                lambda: head.logits(s[:, :48].contiguous()), lambda: head.logits(s.bfloat16()), lambda: head.logits(s.t()),
+                lambda: head.backward(s, z[:3]), lambda: head.backward(s, z, accumulate=True),
+                lambda: head.backward(s, z, d_states=torch.zeros((4, 32), device="cuda")),
+                lambda: F.distill_loss(z, 100), lambda: F.distill_loss(z, 10, i4), lambda: F.distill_loss(z, 10, i4.long(), z[:, :2].contiguous()),
+                lambda: F.distill_loss(z, 10, labels=torch.zeros(3, dtype=torch.int32, device="cuda")),
+                lambda: F.token_logprobs(z, 10, i4[:2]), lambda: F.token_logprobs(z, 10, i4.t())):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(F.FoldError):
+        F.token_logprobs(z, 10, i4, top_k=33)
+
+
+# ---- with the batched path ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,tied", [("f32", False), ("bf16", False), ("bf16", True)])
+def test_training_step_with_a_vocabulary(dtype, tied):
+    """runner.VocabStep: forward, head, distillation on every node, both backward passes, against the oracle's chain."""
+    import torch
+    from oracle import compare, evaluate as EV
+    from paper_1702_02181_amd.runner import VocabStep
+    from tests import gpu_common as C
+    from tests._helpers import oracle_batch, oracle_params
+    w = _model(dtype)
+    rng = np.random.default_rng(21)
+    V = w.leaf_table.shape[0] if tied else 210
+    N, H = w.num_nodes, w.hidden
+    tok, t, y = _targets(rng, N, V, 5)
+    step = VocabStep(w, V, y, tok, t, temperature=2.0, soft_weight=0.5, hard_weight=0.5, tied=tied, seed=3)
+    step.gradients()
+    torch.cuda.synchronize()
+    grads, d_table = step.dev.weight_grads()
+    dW, db, loss = (_np(x) for x in (step.dW, step.db, step.node_loss))
+    ob, P = oracle_batch(w), oracle_params(w)
+    f = EV.forward(ob, P, H, w.leaf_table)
+    W = w.leaf_table if tied else _np(step.W)[:, :H]
+    o_loss, dz = OV.distill(OV.head(f["h"], W, np.zeros(V)), tok, t, y, 2.0, 0.5, 0.5, step.scale)
+    dh, o_dW, o_db = OV.head_backward(f["h"], W, dz)
+    bw = EV.backward(ob, P, H, w.leaf_table, f, np.zeros_like(w.dh_roots, dtype=np.float64), dh, want_table_grad=True)
+    errs = {"loss": compare.rel_err(loss, o_loss), "db": compare.rel_err(db, o_db, whole=True)}
+    errs["d_table"] = compare.rel_err(d_table, bw["d_table"] + (o_dW if tied else 0), whole=True)
+    if not tied:
+        errs["dW"] = compare.rel_err(dW[:, :H], o_dW, whole=True)
+    for s, (gg, oo) in enumerate(zip(grads, bw["grads"])):
+        for name in ("W_in", "W_rec", "bias"):
+            if gg.get(name) is not None and oo.get(name) is not None:
+                errs[f"set{s}.{name}"] = compare.rel_err(gg[name], oo[name], whole=True)
+    assert all(v <= C.TOL[dtype] for v in errs.values()), errs
+    # the steps run and the score reads the new weights
+    before = step.score(_ints(y[:, None].clip(0)), 4)
+    step.step()
+    after = step.score(_ints(y[:, None].clip(0)), 4)
+    assert torch.isfinite(after.logp).all() and not torch.equal(before.logp, after.logp)
+
+
+def test_roots_through_the_head():
+    """roots_out through the head, its d_states as dh_roots: the gradients of the batched path against the oracle's."""
+    import torch
+    from oracle import compare, evaluate as EV
+    from paper_1702_02181_amd.runner import DeviceRun
+    from tests import gpu_common as C
+    from tests._helpers import oracle_batch, oracle_params
+    w = _model("f32")
+    dev = DeviceRun(w)
+    dev.forward()
+    rng = np.random.default_rng(31)
+    V, H, R = 500, w.hidden, dev.R
+    W = (rng.standard_normal((V, H)) / 8).astype(np.float32)
+    y = rng.integers(0, V, R)
+    head = F.VocabHead(_dev(W), None, H)
+    roots = dev.roots[:R].contiguous()
+    z = head.logits(roots)
+    loss, dz = F.distill_loss(z, V, labels=_ints(y), soft_weight=0.0, hard_weight=1.0, scale=1.0 / R)
+    dev.alloc_grads(True)
+    dev.dh_roots, dW, _ = head.backward(roots, dz)
+    dev.backward()
+    torch.cuda.synchronize()
+    grads, d_table = dev.weight_grads()
+    ob, P = oracle_batch(w), oracle_params(w)
+    f = EV.forward(ob, P, H, w.leaf_table)
+    h = f["h"][EV.roots(ob)]
+    o_loss, o_dz = OV.distill(OV.head(h, W), y=y, soft=0.0, hard=1.0, scale=1.0 / R)
+    o_ds, o_dW, _ = OV.head_backward(h, W, o_dz)
+    bw = EV.backward(ob, P, H, w.leaf_table, f, o_ds, None, want_table_grad=True)
+    errs = {"loss": compare.rel_err(_np(loss), o_loss), "dW": compare.rel_err(_np(dW)[:, :H], o_dW, whole=True),
+            "d_table": compare.rel_err(d_table, bw["d_table"], whole=True),
+            "W_rec": compare.rel_err(grads[0]["W_rec"], bw["grads"][0]["W_rec"], whole=True)}
+    assert all(v <= C.TOL["f32"] for v in errs.values()), errs
