@@ -3,29 +3,29 @@
 //     states   ds = dz W          K = V: dz runs along K, W across it
 //     weights  dW (+)= dz^T s     K = M: both operands run across K
 //     bias     db (+)= sum_m dz
-// One kernel, k_product, computes C[m][n] = sum_k A(m, k) B(n, k) in 128 x 128 tiles for operands of either direction.
+// One kernel, k_product, computes C[m][n] = sum_k A(m, k) B(n, k) for operands of either direction.
 
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 #include "common.h"
 #include "dma.h"
 #include "internal.h"
 #include "mfma.h"
+#include "wide.h"
 
 namespace fold {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kTile = 128;            // rows and columns of a workgroup's tile (waves 2 x 2, each 64 x 64)
-constexpr int kStage = kTile * 128;   // bytes of one operand's stage: 64 bf16 or 32 fp32 values of K
+constexpr int kThreads = 256;  // four waves, 2 x 2, each 32 WM rows x 32 WN columns of the tile
 
-// what every operand element outside its matrix is read from
+// what the K values past an operand's last line are read from
 __device__ __attribute__((aligned(16))) uint32_t g_zero[4];
 
-// An operand as it lies in memory: `rows` lines of `ld` elements.  kAlong: line i holds element i's K values (and the
+// An operand as it lies in memory: `lines` lines of `ld` elements.  kAlong: line i holds element i's K values (and the
 // pad columns up to ld are zero or meet zeros); kAcross: line k holds the K value k of every element.
 enum { kAlong = 0, kAcross = 1 };
 struct Operand {
@@ -34,121 +34,119 @@ struct Operand {
   int ld;
 };
 
-// A stage in LDS.  kAlong: the row tiles of dma.h (row r's 16-byte unit u in slot 8 r + (u ^ swz(r))).  kAcross: K lines
-// of 128 elements; bf16 fragments come from the transposing read, which takes 4 lines x 16 columns at a time, so line
-// k's units are permuted by ^ 4 (k & 3) to put the 4 lines into different 64-byte bank ranges; fp32 fragments are one
-// dword a lane, the two half waves read lines k and k + 16, whose units are permuted apart by ^ 8.
+// A stage is KB bytes of K, 128 or 64: NS = KB / 32 steps of 16 bf16 or 8 fp32 values.  In LDS, kAlong: KB bytes an
+// element, the 16-byte units permuted as in dma.h (128) or wide.h (64) so that 16 neighbouring elements' units fall in 16
+// bank groups.  kAcross: lines of ELEMS elements; bf16 fragments come from the transposing read, which takes 4 lines x 16
+// columns at a time, so line k's units are permuted by ^ 4 (k & 3) to put the 4 lines into different 64-byte bank ranges;
+// fp32 fragments are one dword a lane, the two half waves read lines k and k + 4 NS, whose units are permuted apart by
+// ^ 8.
 typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4_t;
 #define FOLD_LDS_AS __attribute__((address_space(3)))
 
-template <typename T>
+template <typename T, int ELEMS, int NS>
+__device__ __forceinline__ int across_unit(int k, int u) {
+  return u ^ (sizeof(T) == 2 ? 4 * (k & 3) % (ELEMS / 8) : 8 * ((k / (4 * NS)) & 1));
+}
+template <typename T, int ELEMS, int NS>
 __device__ __forceinline__ int across_off(int k, int col) {
-  if constexpr (sizeof(T) == 2) return k * 256 + (((col >> 3) ^ (4 * (k & 3))) << 4) + (col & 7) * 2;
-  else return k * 512 + (((col >> 2) ^ (8 * ((k >> 4) & 1))) << 4) + (col & 3) * 4;
+  constexpr int VEC = 16 / (int)sizeof(T);
+  return k * (ELEMS * (int)sizeof(T)) + across_unit<T, ELEMS, NS>(k, col / VEC) * 16 + col % VEC * (int)sizeof(T);
+}
+template <int KB>
+__device__ __forceinline__ int along_off(int r, int u) {
+  return KB == 128 ? rt_off(r, u) : wide::off(r, u);
 }
 
-// One wave's loads of an operand's stages (4 instructions a stage).  e0: the tile's first element.
-template <typename T, int DIR>
+// lane l of the wave copies 16 bytes from base + off (its own offset) to lds + 16 l; not tracked by the compiler (see
+// dma16_untracked)
+__device__ __forceinline__ void dma16_at(const char* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ uint32_t lds_of(const char* p) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const FOLD_LDS_AS char*)p);
+}
+
+// One wave's loads of an operand's stages: NI instructions of 1 KB a stage, instruction t of the workgroup (NI a wave).  e0: the tile's first element.  Elements past
+// the operand's last one are read from a clamped place: they reach results that are not stored.
+template <typename T, int DIR, int ELEMS, int KB>
 struct Loader {
-  const char* base[4];
-  int line[4];
-  bool in[4];
+  static constexpr int NI = ELEMS * KB / 4096;
+  static constexpr int LINES = KB / (int)sizeof(T);  // K values of a stage
+  static constexpr int LL = ELEMS * sizeof(T) / 16;  // lanes of a line (kAcross)
+  const char* p;      // the tile's corner at K = 0
   int64_t lines;
-  size_t step;  // bytes from a stage to the next
+  size_t step;        // bytes from a stage to the next
+  uint32_t off[NI];
+  int line0;
   __device__ __forceinline__ Loader(const Operand& o, int64_t e0, int wave, int lane) {
     lines = o.lines;
-    const char* p = static_cast<const char*>(o.p);
     const size_t lb = (size_t)o.ld * sizeof(T);
+    p = static_cast<const char*>(o.p) + (DIR == kAlong ? (size_t)e0 * lb : (size_t)e0 * sizeof(T));
+    step = DIR == kAlong ? (size_t)KB : LINES * lb;
+    line0 = wave * NI * (64 / LL) + lane / LL;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = 4 * wave + i;
+    for (int i = 0; i < NI; ++i) {
+      const int t = wave * NI + i;
       if constexpr (DIR == kAlong) {
-        // elements behind the last are computed from the last one's values and never stored
-        const int64_t e = min(e0 + 8 * t + row_of_lane(lane), o.lines - 1);
-        base[i] = p + (size_t)e * lb + unit_of_lane(lane, t) * 16;
-        line[i] = 0;
-        in[i] = true;
-        step = 128;
-      } else if constexpr (sizeof(T) == 2) {
-        line[i] = 4 * t + (lane >> 4);
-        const int64_t col = e0 + 8 * ((lane & 15) ^ (4 * (line[i] & 3)));
-        in[i] = col < o.ld;
-        base[i] = p + (size_t)line[i] * lb + (size_t)col * 2;
-        step = 64 * lb;
+        const int r = KB == 128 ? 8 * t + row_of_lane(lane) : 16 * t + wide::lane_row(lane);
+        const int u = KB == 128 ? unit_of_lane(lane, t) : wide::lane_unit(lane);
+        const int64_t e = min(e0 + r, o.lines - 1) - e0;
+        off[i] = (uint32_t)(e * (int64_t)lb) + u * 16;
       } else {
-        line[i] = 2 * t + (lane >> 5);
-        const int64_t col = e0 + 4 * ((lane & 31) ^ (8 * ((line[i] >> 4) & 1)));
-        in[i] = col < o.ld;
-        base[i] = p + (size_t)line[i] * lb + (size_t)col * 4;
-        step = 32 * lb;
+        const int line = t * (64 / LL) + lane / LL;
+        const int u = across_unit<T, ELEMS, KB / 32>(line, lane % LL);
+        const int64_t col = min(e0 + u * (int)(16 / sizeof(T)), (int64_t)o.ld - (int)(16 / sizeof(T))) - e0;
+        off[i] = (uint32_t)(line * (int64_t)lb + col * (int64_t)sizeof(T));
       }
     }
   }
-  __device__ __forceinline__ void issue(int64_t c, int wave, char* lds) const {
-    constexpr int kLines = 128 / sizeof(T);  // K values of a stage
+  // the stages whose lines are all there
+  __device__ __forceinline__ int64_t whole() const { return DIR == kAlong ? INT64_MAX : lines / LINES; }
+  __device__ __forceinline__ void issue(int64_t c, int wave, uint32_t lds) const {
+    const char* src = p + (size_t)c * step;
+    if (c < whole()) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const char* src = base[i] + (size_t)c * step;
-      if constexpr (DIR == kAcross)
-        src = in[i] && c * kLines + line[i] < lines ? src : reinterpret_cast<const char*>(g_zero);
-      dma16(src, lds + (4 * wave + i) * 1024);
+      for (int i = 0; i < NI; ++i) dma16_at(src, off[i], lds + (wave * NI + i) * 1024);
+    } else {  // the last lines: zeros behind them
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const bool in = c * (int64_t)LINES + line0 + i * (64 / LL) < lines;
+        const char* at = in ? src + off[i] : reinterpret_cast<const char*>(g_zero);
+        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds + (wave * NI + i) * 1024), "v"(at)
+                     : "memory", "m0");
+      }
     }
   }
 };
 
-// The fragment of 32 elements from e0 of step s: bf16 K = 16 s + 8 (lane / 32) + 0 .. 7 (s < 4); fp32, four K values in
-// one, K = 4 s + 16 (lane / 32) + 0 .. 3 (s < 4).
-template <typename T, int DIR>
+// The fragment of 32 elements from e0 of step s < NS: bf16 K = 16 s + 8 (lane / 32) + 0 .. 7; fp32, four K values in one,
+// K = 4 s + 4 NS (lane / 32) + 0 .. 3.
+template <typename T, int DIR, int ELEMS, int KB>
 __device__ __forceinline__ uint4 fragment(const char* lds, int e0, int s, int lane) {
+  constexpr int NS = KB / 32;
   const int h = lane >> 5, l32 = lane & 31;
   if constexpr (DIR == kAlong) {
-    return *reinterpret_cast<const uint4*>(lds + rt_off(e0 + l32, sizeof(T) == 2 ? 2 * s + h : 4 * h + s));
+    return *reinterpret_cast<const uint4*>(lds + along_off<KB>(e0 + l32, sizeof(T) == 2 ? 2 * s + h : NS * h + s));
   } else if constexpr (sizeof(T) == 2) {
     const int g = lane >> 4, gi = lane & 15;
     const int col = e0 + 16 * (g & 1) + 4 * (gi & 3), k = 16 * s + 8 * (g >> 1) + (gi >> 2);
-    const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FOLD_LDS_AS bf16x4_t*)(lds + across_off<T>(k, col)));
+    const bf16x4_t lo =
+        __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FOLD_LDS_AS bf16x4_t*)(lds + across_off<T, ELEMS, NS>(k, col)));
     const bf16x4_t hi =
-        __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FOLD_LDS_AS bf16x4_t*)(lds + across_off<T>(k + 4, col)));
+        __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FOLD_LDS_AS bf16x4_t*)(lds + across_off<T, ELEMS, NS>(k + 4, col)));
     const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
     return make_uint4(a.x, a.y, b.x, b.y);
   } else {
-    uint4 r;
-    uint32_t* w = &r.x;
+    uint32_t w[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      w[e] = *reinterpret_cast<const uint32_t*>(lds + across_off<T>(4 * s + 16 * h + e, e0 + l32));
-    return r;
+      w[e] = *reinterpret_cast<const uint32_t*>(lds + across_off<T, ELEMS, NS>(4 * s + 4 * NS * h + e, e0 + l32));
+    return make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
-template <typename T, int AD, int BD>
-__device__ __forceinline__ void product_stage(const char* As, const char* Bs, f32x16 (&acc)[2][2], int a0, int b0,
-                                              int lane) {
-#pragma unroll
-  for (int s = 0; s < 4; ++s) {
-    uint4 a[2], b[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) a[i] = fragment<T, AD>(As, a0 + 32 * i, s, lane);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) b[i] = fragment<T, BD>(Bs, b0 + 32 * i, s, lane);
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a[i]),
-                                                              __builtin_bit_cast(bf16x8, b[j]), acc[i][j], 0, 0, 0);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float((&a[i].x)[e]),
-                                                             __uint_as_float((&b[j].x)[e]), acc[i][j], 0, 0, 0);
-    }
-  }
+__device__ __forceinline__ float word(const uint4& v, int e) {
+  return __uint_as_float(e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w);
 }
 
 struct ProductArgs {
@@ -163,116 +161,515 @@ struct ProductArgs {
   int add;            // out += C, the pad columns left alone
 };
 
-// OUT: the element type of out; partial sums of a split go to out + piece * M * ld
-template <typename T, int AD, int BD, typename OUT>
-__global__ __launch_bounds__(kThreads) void k_product(ProductArgs g) {
-  __shared__ __attribute__((aligned(16))) char A0[kStage], A1[kStage], B0[kStage], B1[kStage];
+// a value that is the same in all lanes, on the scalar unit (divisions leave it)
+__device__ __forceinline__ unsigned uniform(unsigned v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Tiles go to the XCDs in runs, each run walking groups of 8 tile rows column by column: the workgroups that an XCD has
+// at once then share their operands' stages in its L2 (32 of them: 8 x 4 tiles).
+// (In 32 bits: a launch has fewer than 2^24 tiles.)
+__device__ __forceinline__ void tile_at(const ProductArgs& g, unsigned t, unsigned& mt, unsigned& nt) {
+  const unsigned whole = 8 * (unsigned)g.nt, group = uniform(t / whole), in = t - group * whole;
+  const unsigned rows = min(8u, (unsigned)g.mt - 8 * group);
+  nt = uniform(in / rows);
+  mt = 8 * group + (in - nt * rows);
+}
+__device__ __forceinline__ bool tile_of(const ProductArgs& g, unsigned& mt, unsigned& nt, unsigned& piece) {
+  const unsigned one = (unsigned)g.mt * (unsigned)g.nt, total = one * (unsigned)g.split, per = (total + 7) >> 3;
+  const unsigned slot = blockIdx.x >> 3, at = (blockIdx.x & 7) * per + slot;
+  if (slot >= per || at >= total) return false;
+  piece = uniform(at / one);
+  tile_at(g, at - piece * one, mt, nt);
+  return true;
+}
+
+// One wave's part of a tile, WM x WN accumulators from row m0, column n0 (32 WN columns of the bias at `bias`), to out.
+// C's columns are on the accumulators' rows: a lane holds four neighbouring columns of one row.  They go through an image
+// in LDS of 32 rows by 128 bytes (rows 16 bytes apart in their banks), so that whole 128-byte pieces of rows are stored.
+constexpr int kImageRow = 128 + 16, kImage = 32 * kImageRow;
+
+template <typename OUT>
+__device__ __forceinline__ OUT* out_of(const ProductArgs& g, unsigned piece) {
+  return static_cast<OUT*>(g.out) + (size_t)piece * g.M * g.ld;
+}
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {  // rounded to nearest even, one instruction
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
+}
+
+// what a wave's lanes have written to LDS is there for its other lanes (LDS keeps a wave's order: nothing to wait for)
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+template <typename OUT, int WM, int WN>
+__device__ __forceinline__ void store_tile(const ProductArgs& g, OUT* out, const f32x16 (&acc)[WM][WN], int64_t m0,
+                                           int64_t n0, const float* bias, char* img, int lane) {
+  constexpr int VEC = 16 / (int)sizeof(OUT), COLS = 128 / (int)sizeof(OUT), JG = COLS / 32;
+  static_assert(WN % JG == 0, "whole images");
+  const int h = lane >> 5, l32 = lane & 31;
+  // what of the part exists: rows, columns with a value, columns that are written
+  const int rows = (int)min(g.M - m0, (int64_t)(32 * WM)), vals = (int)min(g.N - n0, (int64_t)(32 * WN));
+  const int cols = (int)min(g.cols - n0, (int64_t)(32 * WN));
+  out += (size_t)m0 * g.ld + n0;
+#pragma unroll
+  for (int i = 0; i < WM; ++i)
+#pragma unroll
+    for (int j0 = 0; j0 < WN; j0 += JG) {
+#pragma unroll
+      for (int j = j0; j < j0 + JG; ++j) {
+        f32x16 c = acc[i][j];
+        if constexpr (WM * WN >= 16) asm volatile("" : "+a"(c));  // stays in its accumulator registers until here
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int col = 32 * j + 8 * q + 4 * h;
+          const float4 b4 = *reinterpret_cast<const float4*>(bias + col);
+          const float b[4] = {b4.x, b4.y, b4.z, b4.w};
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = c[4 * q + e] + b[e];
+          char* o = img + l32 * kImageRow + (col - 32 * j0) * (int)sizeof(OUT);
+          if constexpr (sizeof(OUT) == 4) *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+          else *reinterpret_cast<uint2*>(o) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+        }
+      }
+      wave_fence();
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int row = x * 8 + (lane >> 3), col = (lane & 7) * VEC, n = 32 * j0 + col;
+        uint4 v = *reinterpret_cast<const uint4*>(img + row * kImageRow + col * (int)sizeof(OUT));
+        if (32 * i + row >= rows || n >= cols) continue;
+        v = mask_tail<OUT>(v, max(vals - n, 0));
+        OUT* o = out + (size_t)(32 * i + row) * g.ld + n;
+        if constexpr (sizeof(OUT) == 4) {
+          if (g.add) {  // + 0 in the pad columns
+            const float4 old = *reinterpret_cast<const float4*>(o);
+            v.x = __float_as_uint(old.x + __uint_as_float(v.x));
+            v.y = __float_as_uint(old.y + __uint_as_float(v.y));
+            v.z = __float_as_uint(old.z + __uint_as_float(v.z));
+            v.w = __float_as_uint(old.w + __uint_as_float(v.w));
+          }
+        }
+        *reinterpret_cast<uint4*>(o) = v;
+      }
+      wave_fence();  // one image after the other
+    }
+}
+
+// OUT: the element type of out; partial sums of a split go to out + piece * M * ld.
+// The K loop keeps SLOTS stages in LDS and the fragments of two steps (16 bytes of K a lane) in registers: a step's
+// multiplications run while the next step's fragments are read.  At a stage's last step its fragments are in registers
+// already, so the workgroup meets there: the next stage has landed, its first fragments are read, and the loads of a new
+// stage go out into the slot that nobody reads any more.
+template <typename T, int AD, int BD, typename OUT, int WM, int WN, int KB, int SLOTS>
+__global__ __launch_bounds__(kThreads, WM * WN >= 16 ? 1 : 2) void k_product(ProductArgs g) {
+  constexpr int EA = 64 * WM, EB = 64 * WN, STAGE = (EA + EB) * KB, NS = KB / 32;
+  using LA = Loader<T, AD, EA, KB>;
+  using LB = Loader<T, BD, EB, KB>;
+  __shared__ __attribute__((aligned(16))) char lds[SLOTS * STAGE];
+  static_assert(SLOTS * STAGE >= 4 * kImage, "the images lie where the stages were");
+  __shared__ __attribute__((aligned(16))) float bias[EB];
+  static_assert(EB <= kThreads, "one bias a thread");
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   const int wm = wave & 1, wn = wave >> 1;
-  const int64_t tile = blockIdx.x / g.split;
-  const int piece = (int)(blockIdx.x % g.split);
-  const int64_t m0 = tile % g.mt * kTile, n0 = tile / g.mt * kTile;
+  unsigned mt, nt, piece;
+  if (!tile_of(g, mt, nt, piece)) return;
+  const int64_t m0 = (int64_t)mt * EA, n0 = (int64_t)nt * EB;
   const int per = (g.nstage + g.split - 1) / g.split;
-  const int c0 = min(piece * per, g.nstage), c1 = min(c0 + per, g.nstage);
-  const Loader<T, AD> la(g.a, m0, wave, lane);
-  const Loader<T, BD> lb(g.b, n0, wave, lane);
-  f32x16 acc[2][2];
+  const int c0 = min((int)piece * per, g.nstage), c1 = min(c0 + per, g.nstage);
+  const LA la(g.a, m0, wave, lane);
+  const LB lb(g.b, n0, wave, lane);
+  const uint32_t base = lds_of(lds);
+  f32x16 acc[WM][WN];
   zero_acc(acc);
-  auto issue = [&](int c, char* A, char* B) {
-    la.issue(c, wave, A);
-    lb.issue(c, wave, B);
+  if (tid < EB) bias[tid] = g.bias && n0 + tid < g.N ? g.bias[n0 + tid] : 0.f;
+  auto issue = [&](int c) {
+    const uint32_t to = base + (c - c0) % SLOTS * STAGE;
+    la.issue(c, wave, to);
+    lb.issue(c, wave, to + EA * KB);
+  };
+  uint4 fa[2][WM], fb[2][WN];
+  // the f-th fragment of step s of a slot into register set `set`
+  auto load = [&](const char* slot, int s, int set, int f) {
+    if (f < WM) fa[set][f] = fragment<T, AD, EA, KB>(slot, (wm * WM + f) * 32, s, lane);
+    else fb[set][f - WM] = fragment<T, BD, EB, KB>(slot + EA * KB, (wn * WN + f - WM) * 32, s, lane);
+  };
+  // the k-th multiplication of a step.  C's columns are on the accumulators' rows: a lane holds four neighbouring
+  // columns of one row of C
+  constexpr int FRAGS = WM + WN, MULS = WM * WN * (sizeof(T) == 2 ? 1 : 4), LOADS = LA::NI + LB::NI;
+  constexpr int FPM = (FRAGS + MULS - 1) / MULS, LPM = (LOADS + MULS - 1) / MULS;  // of each beside one multiplication
+  auto multiply = [&](int set, int k) {
+    const int e = k / (WM * WN), i = k / WN % WM, j = k % WN;
+    if constexpr (sizeof(T) == 2)
+      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fb[set][j]),
+                                                          __builtin_bit_cast(bf16x8, fa[set][i]), acc[i][j], 0, 0, 0);
+    else
+      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(word(fb[set][j], e), word(fa[set][i], e), acc[i][j], 0, 0, 0);
+  };
+  // waits until stage c is in LDS: at most the loads of the stages after it, of those that were issued, are outstanding
+  static_assert(SLOTS == 2 || SLOTS == 4, "the waits below");
+  auto landed = [&](int c, int issued) {
+    const int behind = issued - 1 - c;
+    if (SLOTS == 4 && behind >= 3) vm_wait_n<3 * LOADS>();
+    else if (SLOTS == 4 && behind == 2) vm_wait_n<2 * LOADS>();
+    else if (behind == 1) vm_wait_n<LOADS>();
+    else vm_wait();
   };
   if (c0 < c1) {
-    issue(c0, A0, B0);
-    vm_wait();
-    __syncthreads();
+    int issued = min(c0 + SLOTS, c1);
+    for (int c = c0; c < issued; ++c) issue(c);
+    landed(c0, issued);
+    wg_barrier();
+#pragma unroll
+    for (int f = 0; f < FRAGS; ++f) load(lds, 0, 0, f);
     int c = c0;
-    for (; c + 2 <= c1; c += 2) {
-      issue(c + 1, A1, B1);
-      __builtin_amdgcn_sched_barrier(0);
-      product_stage<T, AD, BD>(A0, B0, acc, wm * 64, wn * 64, lane);
-      vm_wait();
-      __syncthreads();
-      if (c + 2 < c1) issue(c + 2, A0, B0);
-      __builtin_amdgcn_sched_barrier(0);
-      product_stage<T, AD, BD>(A1, B1, acc, wm * 64, wn * 64, lane);
-      vm_wait();
-      __syncthreads();
-    }
-    if (c < c1) product_stage<T, AD, BD>(A0, B0, acc, wm * 64, wn * 64, lane);
-  }
-  OUT* out = static_cast<OUT*>(g.out) + (size_t)piece * g.M * g.ld;
+    // stages with SLOTS more whole ones behind them: one multiplication, then the fragments and loads placed beside it
+    const int cw = (int)min((int64_t)c1, min(la.whole(), lb.whole())) - SLOTS;
+    const char *pa = la.p + (size_t)(c0 + SLOTS) * la.step, *pb = lb.p + (size_t)(c0 + SLOTS) * lb.step;
+    for (; c < cw; ++c) {
+      const int at = (c - c0) % SLOTS * STAGE, next = (c + 1 - c0) % SLOTS * STAGE;
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int64_t n = n0 + wn * 64 + j * 32 + (lane & 31);
-    if (n >= g.cols || (g.add && n >= g.N)) continue;
-    const float b = g.bias && n < g.N ? g.bias[n] : 0.f;
+      for (int s = 0; s < NS; ++s) {
+        if (s == NS - 1) {
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * LOADS) : "memory");
+          wg_barrier();
+        }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+        for (int k = 0; k < MULS; ++k) {
+          multiply(s & 1, k);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int64_t m = m0 + wm * 64 + i * 32 + acc_row(r, lane);
-        if (m >= g.M) continue;
-        OUT* o = out + (size_t)m * g.ld + n;
-        float v = n < g.N ? acc[i][j][r] + b : 0.f;
-        if constexpr (sizeof(OUT) == 4) v += g.add ? *o : 0.f;
-        *o = from_f32<OUT>(v);
+          for (int f = k * FPM; f < (k + 1) * FPM && f < FRAGS; ++f)
+            load(lds + (s < NS - 1 ? at : next), (s + 1) % NS, (s + 1) & 1, f);
+          if (s == NS - 1)
+#pragma unroll
+            for (int d = k * LPM; d < (k + 1) * LPM && d < LOADS; ++d) {
+              if (d < LA::NI) dma16_at(pa, la.off[d], base + at + (wave * LA::NI + d) * 1024);
+              else dma16_at(pb, lb.off[d - LA::NI], base + at + EA * KB + (wave * LB::NI + d - LA::NI) * 1024);
+            }
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-  }
-}
-
-// out (+)= the sum of the pieces, in their order
-__global__ __launch_bounds__(256) void k_join(const float* part, int pieces, size_t n, float* out) {
-  const size_t step = (size_t)gridDim.x * 256 * 4;
-  for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4; i < n; i += step) {
-    float4 s = *reinterpret_cast<const float4*>(part + i);
-    for (int p = 1; p < pieces; ++p) {
-      const float4 v = *reinterpret_cast<const float4*>(part + (size_t)p * n + i);
-      s.x += v.x;
-      s.y += v.y;
-      s.z += v.z;
-      s.w += v.w;
+      pa += la.step;
+      pb += lb.step;
     }
-    *reinterpret_cast<float4*>(out + i) = s;
+    issued = max(issued, min(c + SLOTS, c1));
+    for (; c < c1; ++c) {
+      const char *at = lds + (c - c0) % SLOTS * STAGE, *next = lds + (c + 1 - c0) % SLOTS * STAGE;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        if (s == NS - 1 && c + 1 < c1) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          landed(c + 1, issued);
+          wg_barrier();
+          if (issued < c1) issue(issued++);
+        }
+        if (s < NS - 1 || c + 1 < c1)
+#pragma unroll
+          for (int f = 0; f < FRAGS; ++f) load(s < NS - 1 ? at : next, (s + 1) % NS, (s + 1) & 1, f);
+#pragma unroll
+        for (int k = 0; k < MULS; ++k) multiply(s & 1, k);
+      }
+    }
   }
-}
-
-// db: sums over the rows, a workgroup per 64 columns; its four waves take every fourth row
-template <typename T>
-__global__ __launch_bounds__(256) void k_column_sums(const T* dz, int64_t M, int V, size_t ld, float* db, int add) {
-  __shared__ float red[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int col = blockIdx.x * 64 + lane;
-  float s = 0.f;
-  for (int64_t m = wave; m < M; m += 4) s += to_f32<T>(dz[(size_t)m * ld + col]);
-  red[wave][lane] = s;
   __syncthreads();
-  if (wave == 0 && col < V) {
-    s = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
-    db[col] = add ? db[col] + s : s;
+  store_tile<OUT, WM, WN>(g, out_of<OUT>(g, piece), acc, m0 + wm * 32 * WM, n0 + wn * 32 * WN, bias + wn * 32 * WN,
+                          lds + wave * kImage, lane);
+}
+
+// The same product where both operands run along a short K (the logits: K = H) and there are many tiles: a workgroup per
+// compute unit walks its tiles, and the stages of all of them are one stream through the slots.  While a tile's last
+// SLOTS stages are multiplied the first of the next tile are loaded, and they land while the tile is stored, so neither
+// the first loads' latency nor the store is waited for (a tile of K = 1,024 bf16 is 28 us of multiplication, and took
+// 16 us more alone).  Needs at least SLOTS stages.
+template <typename T, typename OUT>
+__global__ __launch_bounds__(kThreads, 1) void k_product_chain(ProductArgs g) {
+  constexpr int WM = 4, WN = 4, KB = 64, SLOTS = 4;
+  constexpr int EA = 64 * WM, EB = 64 * WN, STAGE = (EA + EB) * KB, NS = KB / 32;
+  using LA = Loader<T, kAlong, EA, KB>;
+  using LB = Loader<T, kAlong, EB, KB>;
+  __shared__ __attribute__((aligned(16))) char lds[SLOTS * STAGE];
+  __shared__ __attribute__((aligned(16))) char image[4 * kImage];
+  __shared__ __attribute__((aligned(16))) float bias[EB];
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
+  const int wm = wave & 1, wn = wave >> 1;
+  const unsigned total = (unsigned)g.mt * (unsigned)g.nt, per = (total + 7) >> 3;
+  const unsigned first = (blockIdx.x & 7) * per, slots = gridDim.x >> 3;
+  unsigned slot = blockIdx.x >> 3, mt, nt;
+  auto there = [&](unsigned s) { return s < per && first + s < total; };
+  if (!there(slot)) return;
+  const uint32_t base = lds_of(lds);
+  tile_at(g, first + slot, mt, nt);
+  int64_t m0 = (int64_t)mt * EA, n0 = (int64_t)nt * EB;
+  LA la(g.a, m0, wave, lane);
+  LB lb(g.b, n0, wave, lane);
+  const int n = g.nstage;
+  uint4 fa[2][WM], fb[2][WN];
+  auto load = [&](const char* at, int s, int set, int f) {
+    if (f < WM) fa[set][f] = fragment<T, kAlong, EA, KB>(at, (wm * WM + f) * 32, s, lane);
+    else fb[set][f - WM] = fragment<T, kAlong, EB, KB>(at + EA * KB, (wn * WN + f - WM) * 32, s, lane);
+  };
+  constexpr int FRAGS = WM + WN, MULS = WM * WN * (sizeof(T) == 2 ? 1 : 4), LOADS = LA::NI + LB::NI;
+  f32x16 acc[WM][WN];
+  auto multiply = [&](int set, int k) {
+    const int e = k / (WM * WN), i = k / WN % WM, j = k % WN;
+    if constexpr (sizeof(T) == 2)
+      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fb[set][j]),
+                                                          __builtin_bit_cast(bf16x8, fa[set][i]), acc[i][j], 0, 0, 0);
+    else
+      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x2f32(word(fb[set][j], e), word(fa[set][i], e), acc[i][j], 0, 0, 0);
+  };
+  const char *pa = la.p, *pb = lb.p;
+  size_t step = la.step;  // of either operand
+  auto put = [&](int d, uint32_t to) {
+    if (d < LA::NI) dma16_at(pa, la.off[d], to + (wave * LA::NI + d) * 1024);
+    else dma16_at(pb, lb.off[d - LA::NI], to + EA * KB + (wave * LB::NI + d - LA::NI) * 1024);
+  };
+  static_assert(FRAGS <= MULS && LOADS <= MULS, "one of each beside a multiplication");
+#pragma unroll
+  for (int c = 0; c < SLOTS; ++c) {
+#pragma unroll
+    for (int d = 0; d < LOADS; ++d) put(d, base + c * STAGE);
+    pa += step;
+    pb += step;
+  }
+  vm_wait_n<(SLOTS - 1) * LOADS>();
+  wg_barrier();
+#pragma unroll
+  for (int f = 0; f < FRAGS; ++f) load(lds, 0, 0, f);
+  bool more = true;
+  int loads = n - SLOTS, at = 0;  // stages still to load of the tile that is loaded; the slot that is read
+  for (;;) {
+    const int64_t m = m0, nn = n0;  // of the tile that is multiplied
+    bias[tid] = g.bias && nn + tid < g.N ? g.bias[nn + tid] : 0.f;  // read behind the stages' barriers
+    zero_acc(acc);
+    for (int c = 0; c < n; ++c) {
+      if (loads == 0) {
+        slot += slots;
+        more = there(slot);
+        if (more) {
+          tile_at(g, first + slot, mt, nt);
+          m0 = (int64_t)mt * EA;
+          n0 = (int64_t)nt * EB;
+          la = LA(g.a, m0, wave, lane);
+          lb = LB(g.b, n0, wave, lane);
+          pa = la.p;
+          pb = lb.p;
+          loads = n;
+        } else {  // nothing is left: the last stage's place again, which nobody reads
+          pa -= step;
+          pb -= step;
+          step = 0;
+          loads = SLOTS + 1;
+        }
+      }
+      --loads;
+      const int next = at == (SLOTS - 1) * STAGE ? 0 : at + STAGE;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        if (s == NS - 1) {
+          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * LOADS) : "memory");
+          wg_barrier();
+        }
+#pragma unroll
+        for (int k = 0; k < MULS; ++k) {
+          multiply(s & 1, k);
+          if (k < FRAGS) load(lds + (s < NS - 1 ? at : next), (s + 1) % NS, (s + 1) & 1, k);
+          if (s == NS - 1 && k < LOADS) put(k, base + at);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      pa += step;
+      pb += step;
+      at = next;
+    }
+    store_tile<OUT, WM, WN>(g, static_cast<OUT*>(g.out), acc, m + wm * 32 * WM, nn + wn * 32 * WN, bias + wn * 32 * WN,
+                            image + wave * kImage, lane);
+    if (!more) break;
+    wg_barrier();  // this tile's bias is read
+  }
+  vm_wait();  // no load outlives the workgroup's LDS
+}
+
+// out = the sum of the pieces, in an order that does not depend on scheduling: G thread groups of a workgroup take every
+// G-th piece (eight loads in flight each) of 1,024 / G neighbouring values and meet in LDS.  G = 4 for many pieces, which
+// few values are cut into (33 x 320 in 16 pieces: 1.7 us, 11 us with G = 1 and a load at a time), else 1 (8,192 x 1,024 in
+// 2 pieces: 15 us, 23 us with G = 4).  VEC: out is 16-byte aligned and n = stride; otherwise n of the pieces' `stride`
+// values are written, one by one, and added to out if `add`.
+template <bool VEC, int G>
+__global__ __launch_bounds__(256) void k_join(const float* part, int pieces, size_t stride, size_t n, float* out,
+                                              int add) {
+  constexpr int W = 256 / G, U = 8;
+  __shared__ float4 red[G][W];
+  const int at = threadIdx.x % W, group = threadIdx.x / W;
+  const size_t i = ((size_t)blockIdx.x * W + at) * 4;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto take = [&](const float4& v, bool in) {  // a piece that is not there adds an exact 0
+    s.x += in ? v.x : 0.f;
+    s.y += in ? v.y : 0.f;
+    s.z += in ? v.z : 0.f;
+    s.w += in ? v.w : 0.f;
+  };
+  if (i < stride) {
+    if (G == 1 && pieces <= 2) {
+      take(*reinterpret_cast<const float4*>(part + i), true);
+      if (pieces == 2) take(*reinterpret_cast<const float4*>(part + stride + i), true);
+    } else {
+      for (int p0 = group; p0 < pieces; p0 += G * U) {
+        float4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          v[u] = *reinterpret_cast<const float4*>(part + (size_t)min(p0 + G * u, pieces - 1) * stride + i);
+#pragma unroll
+        for (int u = 0; u < U; ++u) take(v[u], p0 + G * u < pieces);
+      }
+    }
+  }
+  if constexpr (G > 1) {
+    red[group][at] = s;
+    __syncthreads();
+    if (group == 0)
+#pragma unroll
+      for (int w = 1; w < G; ++w) take(red[w][at], true);
+  }
+  if (group != 0 || i >= n) return;
+  if constexpr (VEC) {
+    *reinterpret_cast<float4*>(out + i) = s;
+  } else {
+    const float t[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (i + e < n) out[i + e] = add ? out[i + e] + t[e] : t[e];
   }
 }
 
-int64_t tiles(int64_t n) { return (n + kTile - 1) / kTile; }
+template <bool VEC>
+void join(const float* part, int pieces, size_t stride, size_t n, float* out, int add, hipStream_t st) {
+  if (pieces > 8)
+    hipLaunchKernelGGL((k_join<VEC, 4>), dim3((unsigned)((stride + 255) / 256)), dim3(256), 0, st, part, pieces, stride,
+                       n, out, add);
+  else
+    hipLaunchKernelGGL((k_join<VEC, 1>), dim3((unsigned)((stride + 1023) / 1024)), dim3(256), 0, st, part, pieces,
+                       stride, n, out, add);
+}
 
-// Pieces of K for the states' gradient: few tiles with a long K are cut until the chip has two workgroups a compute
-// unit, each with at least 8 stages.
-int split_of(int64_t M, int H, int V, int esize) {
-  const int64_t t = std::max<int64_t>(1, tiles(M) * tiles(row_ld(H)));
-  const int64_t nst = ((int64_t)row_ld(V) * esize + 127) / 128;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / t, nst / 8, 64}));
+// db: column sums.  A workgroup takes 64 16-byte vectors of columns of one of `chunks` pieces of the rows; its four waves
+// take every fourth row, eight loads in flight each.  One piece writes db itself, more their sums to part [chunks][ld].
+template <typename T>
+__global__ __launch_bounds__(256) void k_column_sums(const T* dz, int64_t M, int V, size_t ld, int chunks, float* part,
+                                                     float* db, int add) {
+  constexpr int VEC = 16 / (int)sizeof(T), U = 8;
+  __shared__ float red[4][64 * VEC + 4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const size_t col = ((size_t)(blockIdx.x / chunks) * 64 + lane) * VEC;
+  const int chunk = (int)(blockIdx.x % chunks);
+  const int64_t per = (M + chunks - 1) / chunks, lo = min(chunk * per, M), hi = min(lo + per, M);
+  float s[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) s[e] = 0.f;
+  if (col < ld)
+    for (int64_t m = lo + wave; m < hi; m += 4 * U) {
+      uint4 r[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) r[u] = *reinterpret_cast<const uint4*>(dz + (size_t)min(m + 4 * u, hi - 1) * ld + col);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool in = m + 4 * u < hi;
+        const T* x = reinterpret_cast<const T*>(&r[u]);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s[e] += in ? to_f32<T>(x[e]) : 0.f;
+      }
+    }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) red[wave][lane * VEC + e] = s[e];
+  __syncthreads();
+  const size_t c0 = (size_t)(blockIdx.x / chunks) * 64 * VEC;
+  for (int i = threadIdx.x; i < 64 * VEC; i += 256) {
+    if (c0 + i >= ld) break;
+    const float t = (red[0][i] + red[1][i]) + (red[2][i] + red[3][i]);
+    if (chunks > 1) part[(size_t)chunk * ld + c0 + i] = t;
+    else if (c0 + i < (size_t)V) db[c0 + i] = add ? db[c0 + i] + t : t;
+  }
+}
+
+// pieces of the rows for db: enough workgroups for the chip, each with at least 64 rows
+int bias_chunks(int64_t M, int V, int esize) {
+  const int64_t groups = ((int64_t)row_ld(V) * esize + 1023) / 1024;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({1024 / groups, M / 64, 64}));
+}
+
+// How a product is cut: tiles of 64 WM x 64 WN, and K into pieces.
+struct Shape {
+  int wm, wn, split;
+  int64_t mt, nt;
+};
+int64_t tiles_of(int64_t n, int w) { return (n + 64 * w - 1) / (64 * w); }
+constexpr int kPieces = 64;
+constexpr int kUnits = 256;  // compute units
+
+// The cut with the least expected time.  A compute unit gets ceil(tiles * pieces / 256) workgroups, whose time goes with
+// their area and their share of K; a stage of 64 x 64 takes 0.11 us (bf16) or 0.49 us (fp32) at the rate of the largest
+// tiles, and the smaller ones' operands cost more of LDS's bandwidth.  Measured at 8,192 x 1,024 x 32,000 bf16 against
+// 256 x 256 tiles: 1.2 times the time for 128 x 128, 1.55 for 64 x 128, 2.2 for 64 x 64; in fp32 (2,048 rows), where the
+// matrix cores bound all of them, 1.0, 1.03 and 1.06.  A workgroup's first loads and its store take about 2 us; pieces
+// cost their sums' way through memory (4 TB/s) and a second launch (3 us).  What the rule gets (best and worst cut tried):
+// states' gradient of 33 x 300 x 20,000 bf16 13 us (335), of 257 x 300 x 20,001 fp32 49 us (4,512), weights' gradient of
+// 2,048 x 256 x 10,000 fp32 95 us (486).
+// small: the smallest tile's columns / 64 (1 or 2)
+Shape shape_of(int64_t M, int64_t N, int64_t nstage, int esize, int small, int pieces) {
+  static constexpr struct { int wm, wn; double bf16, f32; } kTiles[] = {
+      {4, 4, 1.0, 1.0}, {2, 2, 1.2, 1.0}, {1, 2, 1.55, 1.03}, {1, 1, 2.2, 1.06}};
+  Shape best{0, 0, 0, 0, 0};
+  double least = 0;
+  for (const auto& t : kTiles) {
+    if (t.wm == 1 && t.wn != small) continue;
+    const int64_t mt = tiles_of(M, t.wm), nt = tiles_of(N, t.wn);
+    for (int p = 1; p <= pieces && (p == 1 || nstage / p >= 4); p *= 2) {
+      const double rounds = (double)((mt * nt * p + kUnits - 1) / kUnits);
+      const double stage = t.wm * t.wn * (esize == 2 ? 0.11 * t.bf16 : 0.49 * t.f32);
+      double us = rounds * (stage * (double)((nstage + p - 1) / p) + 2.0 / (t.wm == 4 ? 1 : 2));
+      if (p > 1) us += 3.0 + (double)(p + 1) * M * N * 4 / 4e6;
+      if (best.wm == 0 || us < least) {
+        least = us;
+        best = Shape{t.wm, t.wn, p, mt, nt};
+      }
+    }
+  }
+  return best;
+}
+Shape states_shape(int64_t M, int H, int V, int esize) {
+  return shape_of(std::max<int64_t>(M, 1), row_ld(H), (int64_t)row_ld(V) * esize / 128, esize, 1, kPieces);
 }
 
 template <typename T, int AD, int BD, typename OUT>
-void launch(const ProductArgs& g, hipStream_t st) {
-  hipLaunchKernelGGL((k_product<T, AD, BD, OUT>), dim3((unsigned)(g.mt * g.nt * g.split)), dim3(kThreads), 0, st, g);
+void launch(ProductArgs g, const Shape& sh, hipStream_t st) {
+  g.mt = sh.mt;
+  g.nt = sh.nt;
+  g.split = sh.split;
+  const dim3 grid((unsigned)((g.mt * g.nt * g.split + 7) / 8 * 8));
+  if (sh.wm == 4) {
+    g.nstage *= 2;
+    if constexpr (AD == kAlong && BD == kAlong)
+      if (g.nstage >= 4 && g.mt * g.nt > kUnits) {
+        hipLaunchKernelGGL((k_product_chain<T, OUT>), dim3(kUnits), dim3(kThreads), 0, st, g);
+        return;
+      }
+    hipLaunchKernelGGL((k_product<T, AD, BD, OUT, 4, 4, 64, 4>), grid, dim3(kThreads), 0, st, g);
+  } else if (sh.wm == 2) {
+    hipLaunchKernelGGL((k_product<T, AD, BD, OUT, 2, 2, 128, 2>), grid, dim3(kThreads), 0, st, g);
+  } else if constexpr (AD == kAlong && BD == kAlong) {
+    hipLaunchKernelGGL((k_product<T, AD, BD, OUT, 1, 2, 128, 2>), grid, dim3(kThreads), 0, st, g);
+  } else {
+    hipLaunchKernelGGL((k_product<T, AD, BD, OUT, 1, 1, 128, 2>), grid, dim3(kThreads), 0, st, g);
+  }
 }
 
 }  // namespace
 
 int64_t vocab_tiles(int64_t M, int H, int V) {
-  const int64_t h = tiles(row_ld(H)), v = tiles(row_ld(V)), m = std::max<int64_t>(tiles(M), 1);
-  return std::max(m * v, std::max(v * h, m * h * 64));
+  const int64_t h = tiles_of(row_ld(H), 1), v = tiles_of(row_ld(V), 1), m = std::max<int64_t>(tiles_of(M, 1), 1);
+  return std::max((m * v + 1) / 2, std::max(v * h, m * h * kPieces));
 }
 
 void launch_vocab_logits(int dtype, int64_t M, int H, int V, const void* s, const void* W, const float* bias,
@@ -280,15 +677,18 @@ void launch_vocab_logits(int dtype, int64_t M, int H, int V, const void* s, cons
   if (M <= 0) return;
   ProfScope prof("vocab_logits", st);
   const int es = dtype == FOLD_BF16 ? 2 : 4, ldh = row_ld(H), ldv = row_ld(V);
-  ProductArgs g{{s, M, ldh}, {W, V, ldh}, M, V, tiles(M), tiles(ldv), ldh * es / 128, 1, z, (size_t)ldv, ldv, bias, 0};
-  if (dtype == FOLD_F32) launch<float, kAlong, kAlong, float>(g, st);
-  else if (out_dtype == FOLD_F32) launch<uint16_t, kAlong, kAlong, float>(g, st);
-  else launch<uint16_t, kAlong, kAlong, uint16_t>(g, st);
+  const Shape sh = shape_of(M, ldv, ldh * es / 128, es, 2, 1);
+  const ProductArgs g{{s, M, ldh}, {W, V, ldh}, M, V, 0, 0, ldh * es / 128, 1, z, (size_t)ldv, ldv, bias, 0};
+  if (dtype == FOLD_F32) launch<float, kAlong, kAlong, float>(g, sh, st);
+  else if (out_dtype == FOLD_F32) launch<uint16_t, kAlong, kAlong, float>(g, sh, st);
+  else launch<uint16_t, kAlong, kAlong, uint16_t>(g, sh, st);
 }
 
 size_t vocab_backward_bytes(int dtype, int64_t M, int H, int V) {
-  const int n = split_of(M, H, V, dtype == FOLD_BF16 ? 2 : 4);
-  return n == 1 ? 0 : (size_t)n * M * row_ld(H) * sizeof(float);
+  const int es = dtype == FOLD_BF16 ? 2 : 4;
+  const int n = states_shape(M, H, V, es).split, c = bias_chunks(M, V, es);
+  // the two follow each other on the stream: one region serves both
+  return std::max(n == 1 ? 0 : (size_t)n * M * row_ld(H), c == 1 ? 0 : (size_t)c * row_ld(V)) * sizeof(float);
 }
 
 void launch_vocab_backward(int dtype, int64_t M, int H, int V, const void* s, const void* W, const void* dz, float* ds,
@@ -297,33 +697,34 @@ void launch_vocab_backward(int dtype, int64_t M, int H, int V, const void* s, co
   const int kst = 128 / es;
   if (ds && M > 0) {
     ProfScope prof("vocab_dstates", st);
-    const int n = split_of(M, H, V, es);
-    ProductArgs g{{dz, M, ldv}, {W, V, ldh}, M, H, tiles(M), tiles(ldh), ldv * es / 128, n,
-                  n > 1 ? ws : ds, (size_t)ldh, ldh, nullptr, 0};
-    if (dtype == FOLD_F32) launch<float, kAlong, kAcross, float>(g, st);
-    else launch<uint16_t, kAlong, kAcross, float>(g, st);
-    if (n > 1) {
-      const size_t total = (size_t)M * ldh;
-      hipLaunchKernelGGL(k_join, dim3((unsigned)std::min<size_t>((total + 1023) / 1024, 4096)), dim3(256), 0, st,
-                         static_cast<const float*>(ws), n, total, ds);
-    }
+    const Shape sh = states_shape(M, H, V, es);
+    const ProductArgs g{{dz, M, ldv}, {W, V, ldh}, M, H, 0, 0, ldv * es / 128, 1, sh.split > 1 ? ws : ds, (size_t)ldh,
+                        ldh, nullptr, 0};
+    if (dtype == FOLD_F32) launch<float, kAlong, kAcross, float>(g, sh, st);
+    else launch<uint16_t, kAlong, kAcross, float>(g, sh, st);
+    if (sh.split > 1)
+      join<true>(static_cast<const float*>(ws), sh.split, (size_t)M * ldh, (size_t)M * ldh, ds, 0, st);
   }
   if (dW) {
     ProfScope prof("vocab_dweights", st);
-    ProductArgs g{{dz, M, ldv}, {s, M, ldh}, V, H, tiles(V), tiles(ldh), (int)((M + kst - 1) / kst), 1,
-                  dW, (size_t)ldh, ldh, nullptr, add};
-    if (dtype == FOLD_F32) launch<float, kAcross, kAcross, float>(g, st);
-    else launch<uint16_t, kAcross, kAcross, float>(g, st);
+    const ProductArgs g{{dz, M, ldv}, {s, M, ldh}, V, H, 0, 0, (int)((M + kst - 1) / kst), 1,
+                        dW, (size_t)ldh, ldh, nullptr, add};
+    const Shape sh = shape_of(V, ldh, g.nstage, es, 1, 1);
+    if (dtype == FOLD_F32) launch<float, kAcross, kAcross, float>(g, sh, st);
+    else launch<uint16_t, kAcross, kAcross, float>(g, sh, st);
   }
   if (db) {
     ProfScope prof("vocab_dbias", st);
-    const dim3 grid((unsigned)(ldv / 64));
+    const int c = bias_chunks(M, V, es);
+    float* part = static_cast<float*>(ws);
+    const dim3 grid((unsigned)(((int64_t)ldv * es + 1023) / 1024 * c));
     if (dtype == FOLD_F32)
       hipLaunchKernelGGL(k_column_sums<float>, grid, dim3(256), 0, st, static_cast<const float*>(dz), M, V,
-                         (size_t)ldv, db, add);
+                         (size_t)ldv, c, part, db, add);
     else
       hipLaunchKernelGGL(k_column_sums<uint16_t>, grid, dim3(256), 0, st, static_cast<const uint16_t*>(dz), M, V,
-                         (size_t)ldv, db, add);
+                         (size_t)ldv, c, part, db, add);
+    if (c > 1) join<false>(part, c, (size_t)ldv, (size_t)V, db, add, st);
   }
 }
 

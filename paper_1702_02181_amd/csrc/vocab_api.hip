@@ -31,7 +31,8 @@ int32_t guarded(F&& body) {
   }
 }
 
-constexpr int kMaxVocab = 1 << 30;    // columns and their keys are counted in 31 bits
+constexpr int kMaxVocab = 1 << 30;      // columns and their keys are counted in 31 bits
+constexpr int kMaxHeadVocab = 1 << 21;  // a tile of a product is addressed by 32-bit offsets (256 lines of the logits)
 constexpr int64_t kMaxTiles = 1 << 24;  // workgroups of one launch of 256 threads each
 
 bool known_type(int dtype) { return dtype == FOLD_F32 || dtype == FOLD_BF16; }
@@ -50,6 +51,7 @@ int check_rows(const std::string& who, int dtype, int64_t rows, int vocab) {
 int check_product(const std::string& who, int dtype, int64_t rows, int hidden, int vocab) {
   const int rc = check_rows(who, dtype, rows, vocab);
   if (rc != FOLD_OK) return rc;
+  if (vocab > kMaxHeadVocab) return vfail(FOLD_E_INVALID, who + ": vocabulary size out of range (1 .. 2^21)");
   if (hidden < 1 || hidden > kMaxHidden) return vfail(FOLD_E_INVALID, who + ": hidden size out of range");
   if (vocab_tiles(rows, hidden, vocab) >= kMaxTiles)
     return vfail(FOLD_E_INVALID, who + ": rows * vocabulary too large for one call");

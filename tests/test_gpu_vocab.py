@@ -78,6 +78,11 @@ PRODUCTS = [(1, 1, 1, "f32"), (1, 64, 7, "bf16"), (3, 300, 129, "bf16"), (130, 6
             (16, 1024, 3000, "bf16"), (17, 256, 640, "f32"), (64, 520, 999, "bf16"), (1, 1024, 4097, "f32")]
 
 
+# more tiles than compute units, edges in both directions, K of 6, 8 and 10 stages; long products cut into pieces
+MANY = [(1300, 130, 20011, "bf16"), (1100, 70, 20011, "f32"), (2309, 300, 9000, "bf16"), (1030, 260, 30011, "bf16"),
+        (1030, 260, 30011, "f32")]
+
+
 def _product_case(M, H, V, dtype, seed):
     rng = np.random.default_rng(seed)
     s = _round(np.tanh(rng.standard_normal((M, H))), dtype)
@@ -88,7 +93,7 @@ def _product_case(M, H, V, dtype, seed):
     return s, W, b, dz
 
 
-@pytest.mark.parametrize("M,H,V,dtype", PRODUCTS)
+@pytest.mark.parametrize("M,H,V,dtype", PRODUCTS + MANY)
 @pytest.mark.parametrize("biased", [True, False])
 def test_logits(M, H, V, dtype, biased):
     import torch
@@ -108,7 +113,7 @@ def test_logits(M, H, V, dtype, biased):
         assert torch.equal(head.logits(sd, dtype=_t(out)), z)
 
 
-@pytest.mark.parametrize("M,H,V,dtype", PRODUCTS)
+@pytest.mark.parametrize("M,H,V,dtype", PRODUCTS + MANY)
 def test_backward(M, H, V, dtype):
     import torch
     s, W, _, dz = _product_case(M, H, V, dtype, 7 * M + H + V)

@@ -144,7 +144,7 @@ def test_refusals_of_the_products(F):
         F.fold_vocab_logits(dtype, rows, hidden, vocab, s, W, bias, out, z, NULL_STREAM)
 
     for kw in (dict(dtype=2), dict(dtype=-1), dict(rows=-1), dict(rows=1 << 31), dict(hidden=0), dict(hidden=4097),
-               dict(vocab=0), dict(vocab=(1 << 30) + 1), dict(out=1), dict(dtype=1, out=7), dict(s=None), dict(W=None),
+               dict(vocab=0), dict(vocab=(1 << 21) + 1), dict(out=1), dict(dtype=1, out=7), dict(s=None), dict(W=None),
                dict(z=None), dict(s=odd), dict(W=odd), dict(z=odd), dict(rows=(1 << 31) - 1, vocab=1 << 20)):
         _refused(F, F.FOLD_E_INVALID, logits, **kw)
     logits(rows=0, s=None, W=None, z=None)
