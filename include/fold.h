@@ -595,7 +595,8 @@ int32_t fold_vocab_backward(int32_t dtype, int64_t rows, int32_t hidden, int32_t
  *   dlogits     device [rows, fold_row_ld(vocab)], written whole (pad columns
  *               zero); may be `logits` itself if the types are equal, must not
  *               overlap it otherwise; NULL: the losses alone
- *   ws          device workspace of >= fold_distill_workspace_size bytes
+ *   ws          device workspace of >= fold_distill_workspace_size bytes (may be
+ *               NULL where that is 0: rows that fit LDS)
  * Sums are fp32.  Logits of -inf (masked) have probability 0; a target there
  * has loss +inf.  A row with a target whose logits are all -inf has loss +inf
  * and gradient 0; one with NaN or +inf has loss and gradient NaN. */
@@ -621,7 +622,7 @@ int32_t fold_loss_distill(const fold_sched* sched, int32_t dtype, int64_t rows, 
  *   entropy     device [rows] fp32, or NULL
  *   top_token, top_logp  device [rows, top_k] int32, fp32; top_k 0 .. 32
  *   ws          device workspace of >= fold_token_workspace_size bytes (may be
- *               NULL where that is 0: many rows)
+ *               NULL where that is 0: many rows, or short ones)
  * Sums are fp32.  A row of -inf alone has log probabilities -inf and entropy
  * 0; one with NaN or +inf has NaN for all of them and top tokens -1.
  * Errors of both calls: FOLD_E_INVALID for sizes out of range, NULL or

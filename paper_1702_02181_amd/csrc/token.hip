@@ -18,6 +18,7 @@
 
 #include "common.h"
 #include "internal.h"
+#include "dma.h"
 #include "mfma.h"
 
 namespace fold {
@@ -27,9 +28,10 @@ namespace {
 constexpr float kL2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kFar = 1e35f;      // |m| from here on: see above (z / T stays finite for T >= 1e-3)
 constexpr float kFloor = -200.f;   // 2^-200 is 0 in fp32: bounds x where it is multiplied by 2^x
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = 256, kWaves = kThreads / 64;  // of a workgroup, where nothing else is said
 constexpr int kUnroll = 4;         // vectors a thread has in flight
 constexpr int kCap = 1024;         // candidates of a segment's top list held in LDS
+constexpr int kMaxSegments = 64;   // of a row: a lane each
 
 __device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -60,26 +62,24 @@ __device__ __forceinline__ float wave_add(float v) {
   for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
   return v;
 }
-// over the workgroup; red holds kWaves floats and is free again after the next barrier
-__device__ __forceinline__ float block_max(float v, float* red) {
-  v = wave_max(v);
+// over a workgroup of NW waves; red holds NW floats and is free again after the next barrier
+template <int NW, class OP>
+__device__ __forceinline__ float block_fold(float v, float* red, OP op) {
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
   float r = red[0];
 #pragma unroll
-  for (int w = 1; w < kWaves; ++w) r = fmaxf(r, red[w]);
+  for (int w = 1; w < NW; ++w) r = op(r, red[w]);
   return r;
 }
+template <int NW>
+__device__ __forceinline__ float block_max(float v, float* red) {
+  return block_fold<NW>(wave_max(v), red, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int NW>
 __device__ __forceinline__ float block_add(float v, float* red) {
-  v = wave_add(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float r = red[0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) r += red[w];
-  return r;
+  return block_fold<NW>(wave_add(v), red, [](float a, float b) { return a + b; });
 }
 
 // Order of the logits as whole numbers: larger is larger, -0 equals +0; with the column below it, the lowest index of
@@ -102,7 +102,8 @@ struct Segment {
   const uint4* row;
   int v0, v1, V;
 
-  // f(vector index, its values, the number of them that are real): kUnroll loads in flight, from clamped addresses
+  // f(vector index, its values, the number of them that are real), for every vector a thread has: kUnroll loads in flight,
+  // from clamped addresses
   template <class F>
   __device__ __forceinline__ void each(F&& f) const {
     for (int b = v0; b < v1; b += kThreads * kUnroll) {
@@ -118,7 +119,45 @@ struct Segment {
       }
     }
   }
+
+  // f(first vector, group of `kUnroll` vectors' values) while whole groups are left, then f1(vector, values) for the rest
+  // one vector at a time, columns that are not there as -inf.  The groups need no test for the end.
+  template <class F, class F1>
+  __device__ __forceinline__ void groups(F&& f, F1&& f1) const {
+    int b = v0;
+    for (; b + kThreads * kUnroll < v1; b += kThreads * kUnroll) {
+      uint4 raw[kUnroll];
+      float v[kUnroll][VEC];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) raw[u] = row[b + u * kThreads + (int)threadIdx.x];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) unpack<T>(raw[u], v[u]);
+      f(b + (int)threadIdx.x, v);
+    }
+    uint4 raw[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (b + u * kThreads < v1) raw[u] = row[min(b + u * kThreads + (int)threadIdx.x, v1 - 1)];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (b + u * kThreads >= v1) continue;
+      const int i = b + u * kThreads + (int)threadIdx.x, have = i < v1 ? V - i * VEC : 0;
+      float v[VEC];
+      unpack<T>(raw[u], v);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[e] = e < have ? v[e] : neg_inf();
+      f1(i, v);
+    }
+  }
 };
+
+template <int N>
+__device__ __forceinline__ float max_of(const float (&v)[N]) {
+  float m = v[0];
+#pragma unroll
+  for (int e = 1; e < N; ++e) m = fmaxf(m, v[e]);
+  return m;
+}
 
 __host__ __device__ inline int vectors_of(int V, int vec) { return (V + vec - 1) / vec; }
 
@@ -126,7 +165,7 @@ template <typename T>
 __device__ __forceinline__ Segment<T> segment_of(const T* z, size_t ld, int64_t p, int seg, int nseg, int V) {
   // pieces of whole 64-column blocks, so that a gradient of another type splits at the same columns; the last ones may
   // be empty
-  const int nv = vectors_of(V, Segment<T>::VEC), block = 64 / Segment<T>::VEC;
+  const int nv = vectors_of(V, (16 / (int)sizeof(T))), block = 64 / (16 / (int)sizeof(T));
   const int per = ((nv + nseg - 1) / nseg + block - 1) / block * block;
   Segment<T> s;
   s.row = reinterpret_cast<const uint4*>(z + (size_t)p * ld);
@@ -141,7 +180,12 @@ struct Stat {
   float m, m2, s, t;
 };
 
-__device__ __forceinline__ float ref_of(float m, float c) { return fminf(fmaxf(m, -kFar), kFar) * c; }
+// Rounded here: fused into the subtraction that follows, two references of the same maximum would differ by the product's
+// rounding, which is 1e28 at kFar.
+__device__ __forceinline__ float ref_of(float m, float c) {
+#pragma clang fp contract(off)
+  return fminf(fmaxf(m, -kFar), kFar) * c;
+}
 __device__ __forceinline__ bool is_far(float m) { return fabsf(m) >= kFar && m != neg_inf(); }
 
 // s and t seen from the reference m2
@@ -190,12 +234,27 @@ __device__ __forceinline__ void rank_keys(const uint64_t* cand, int n, int K, ui
   __syncthreads();
 }
 
+// What a thread keeps of its vectors for the top list: its largest logit, the first vector of the group that holds it, and
+// the largest of its other groups.
+struct Best {
+  float m, second;
+  int first;
+  __device__ __forceinline__ void meet(int i, float v) {
+    const bool more = v > m;
+    second = fmaxf(second, more ? m : v);
+    first = more ? i : first;
+    m = more ? v : m;
+  }
+};
+
 struct TopLds {
-  uint64_t cand[kCap];
+  uint64_t cand[kCap + kMaxTopTokens];
   uint64_t out[kMaxTopTokens];
   uint32_t key[kThreads];
   unsigned hist[256];
-  int n, bin, left;
+  int vec[kCap];
+  uint32_t tau;
+  int n, vectors, bin, left;
 };
 
 // Adds one to hist[b] for every lane with `in`; lanes that all have the same bin add once (a row of equal logits).
@@ -210,55 +269,147 @@ __device__ __forceinline__ void count_bin(unsigned* hist, int b, bool in) {
   }
 }
 
-// The K largest keys of a segment, in order, in s.out.  m: the thread's own largest logit.  A threshold first: the K-th
-// largest of the 256 threads' maxima cannot exceed the K-th largest logit, and few logits reach it (about K where the
-// large ones are spread over the threads); they are found again in the segment, now in a cache, by the threads whose
-// maximum reaches it.  Where more than kCap do (many equal logits, or all the large ones in few threads' columns), the
-// K-th largest key is found digit by digit instead, with one read of the segment a digit.
+// The K largest keys of a segment, in order, in s.out.  A threshold first: the K-th largest of the 256 threads' maxima
+// cannot exceed the K-th largest logit, and few logits reach it (about K where the large ones are spread over the
+// threads).  They are found again by the threads whose maximum reaches it, mostly in the one group of vectors that holds
+// it; a thread whose other groups reach it too reads all its vectors again (eight loads in flight).
+// Where more than kCap do, either many equal the threshold: then the logits above it are the list's head and the rest is
+// filled with the first ones that equal it, in the columns' order, which ends as soon as the list is full.  Or more than
+// kCap are above it (all the large ones in few threads' columns): then the K-th largest key is found digit by digit, with
+// one read of the segment a digit.
 template <typename T>
-__device__ void top_of_segment(const Segment<T>& seg, float m, int K, TopLds& s) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  s.key[tid] = m > neg_inf() ? order_of(m) : 0u;
-  if (tid == 0) s.n = 0;
+__device__ void top_of_segment(const Segment<T>& seg, const Best& best, int K, TopLds& s) {
+  constexpr int VEC = 16 / (int)sizeof(T), NW = kWaves;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t key = best.m > neg_inf() ? order_of(best.m) : 0u;
+  s.key[tid] = key;
   __syncthreads();
-  uint32_t k[kWaves], tau = 0;
+  if (wave == 0) {
+    uint32_t k[4], t = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) k[w] = s.key[w * 64 + lane];
-  for (int b = 31; b >= 0; --b) {
-    const uint32_t c = tau | (1u << b);
-    int n = 0;
+    for (int w = 0; w < 4; ++w) k[w] = s.key[w * 64 + lane];
+    for (int b = 31; b >= 0; --b) {
+      const uint32_t c = t | (1u << b);
+      int n = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) n += __popcll(__ballot(k[w] >= c));
-    if (n >= K) {
-      tau = c;
-      if (n == K) break;
+      for (int w = 0; w < 4; ++w) n += __popcll(__ballot(k[w] >= c));
+      if (n >= K) {
+        t = c;
+        if (n == K) break;
+      }
     }
+    if (lane == 0) s.tau = t;
   }
-  if (s.key[tid] >= tau && s.key[tid] != 0) {
-    for (int i = seg.v0 + tid; i < seg.v1; i += kThreads) {
-      float v[Segment<T>::VEC];
+  __syncthreads();
+  const uint32_t tau = s.tau;
+  const bool mine = key >= tau && key != 0;
+  const bool others = best.second > neg_inf() && order_of(best.second) >= tau;
+  // The logits above the threshold, or that reach it, into s.cand [s.n]: first the vectors that hold one, found by the
+  // threads whose maximum reaches it, then their logits, a vector a thread.  False if there is no room for all.
+  auto collect = [&](bool above) {
+    __syncthreads();
+    if (tid == 0) s.n = s.vectors = 0;
+    __syncthreads();
+    auto look = [&](int i, const uint4& raw) __attribute__((always_inline)) {
+      float v[VEC];
+      unpack<T>(raw, v);
+      float vm = neg_inf();
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) vm = fmaxf(vm, i * VEC + e < seg.V ? v[e] : neg_inf());
+      const uint32_t o = order_of(vm);
+      if (i < seg.v1 && vm > neg_inf() && (above ? o > tau : o >= tau)) {
+        const int at = atomicAdd(&s.vectors, 1);
+        if (at < kCap) s.vec[at] = i;
+      }
+    };
+    if (mine && !others) {
+      // a group of the main part, or one vector of the rest (the others looked at with it do not reach the threshold)
+      uint4 raw[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) raw[u] = seg.row[min(best.first + u * kThreads, seg.v1 - 1)];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) look(best.first + u * kThreads, raw[u]);
+    }
+    if (mine && others) {
+      constexpr int U = 8;
+      for (int b = seg.v0 + tid; b < seg.v1; b += kThreads * U) {
+        uint4 raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = seg.row[min(b + u * kThreads, seg.v1 - 1)];
+#pragma unroll
+        for (int u = 0; u < U; ++u) look(b + u * kThreads, raw[u]);
+      }
+    }
+    __syncthreads();
+    const int n = s.vectors;
+    if (n > kCap) return false;
+    for (int j = tid; j < n; j += kThreads) {
+      const int i = s.vec[j];
+      float v[VEC];
       unpack<T>(seg.row[i], v);
 #pragma unroll
-      for (int e = 0; e < Segment<T>::VEC; ++e) {
-        const int col = i * Segment<T>::VEC + e;
-        if (col < seg.V && v[e] > neg_inf() && order_of(v[e]) >= tau) {
+      for (int e = 0; e < VEC; ++e) {
+        const uint32_t o = order_of(v[e]);
+        if (i * VEC + e < seg.V && v[e] > neg_inf() && (above ? o > tau : o >= tau)) {
           const int at = atomicAdd(&s.n, 1);
-          if (at < kCap) s.cand[at] = key_of(v[e], col);
+          if (at < kCap) s.cand[at] = key_of(v[e], i * VEC + e);
         }
       }
     }
-  }
-  __syncthreads();
-  if (s.n > kCap) {  // the same for every thread
+    __syncthreads();
+    return s.n <= kCap;
+  };
+  if (collect(false)) {  // the same for every thread, as below
+  } else if (collect(true)) {
+    const int above = s.n;
+    int need = K - above;  // of the logits that equal the threshold
+    for (int b = seg.v0; b < seg.v1 && need > 0; b += kThreads) {
+      const int i = b + tid;
+      float v[VEC];
+      unpack<T>(seg.row[min(i, seg.v1 - 1)], v);
+      int c = 0;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        c += i < seg.v1 && i * VEC + e < seg.V && v[e] > neg_inf() && order_of(v[e]) == tau;
+      // place among the chunk's: inclusive sums over the wave, then the waves before
+      int before = c;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(before, d);
+        before += lane >= d ? o : 0;
+      }
+      __syncthreads();
+      if (lane == 63) s.hist[wave] = before;
+      __syncthreads();
+      int total = 0;
+      before -= c;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        before += w < wave ? (int)s.hist[w] : 0;
+        total += (int)s.hist[w];
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (i < seg.v1 && i * VEC + e < seg.V && v[e] > neg_inf() && order_of(v[e]) == tau) {
+          if (before < need) s.cand[above + (K - above - need) + before] = key_of(v[e], i * VEC + e);
+          ++before;
+        }
+      need -= min(need, total);
+    }
+    __syncthreads();
+    if (tid == 0) s.n = max(above, K - need);
+    __syncthreads();
+  } else {
+    __syncthreads();
     uint64_t prefix = 0;
     int left = K;
     for (int byte = 7; byte >= 0; --byte) {
       s.hist[tid] = 0;
       __syncthreads();
-      seg.each([&](int i, float (&v)[Segment<T>::VEC], int nv) {
+      seg.each([&](int i, float (&v)[VEC], int nv) {
 #pragma unroll
-        for (int e = 0; e < Segment<T>::VEC; ++e) {
-          const uint64_t q = key_of(v[e], i * Segment<T>::VEC + e);
+        for (int e = 0; e < VEC; ++e) {
+          const uint64_t q = key_of(v[e], i * VEC + e);
           const bool same = byte == 7 || (q >> (8 * byte + 8)) == (prefix >> (8 * byte + 8));
           count_bin(s.hist, (int)(q >> (8 * byte)) & 255, e < nv && v[e] > neg_inf() && same);
         }
@@ -279,10 +430,10 @@ __device__ void top_of_segment(const Segment<T>& seg, float m, int K, TopLds& s)
     }
     if (tid == 0) s.n = 0;
     __syncthreads();
-    seg.each([&](int i, float (&v)[Segment<T>::VEC], int nv) {
+    seg.each([&](int i, float (&v)[VEC], int nv) {
 #pragma unroll
-      for (int e = 0; e < Segment<T>::VEC; ++e) {
-        const uint64_t q = key_of(v[e], i * Segment<T>::VEC + e);
+      for (int e = 0; e < VEC; ++e) {
+        const uint64_t q = key_of(v[e], i * VEC + e);
         if (e < nv && v[e] > neg_inf() && q >= prefix) {
           const int at = atomicAdd(&s.n, 1);
           if (at < kCap) s.cand[at] = q;
@@ -332,35 +483,45 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void k_token(TokenArgs a) {
   __shared__ float red[kWaves];
   __shared__ TopLds top;
-  constexpr int VEC = Segment<T>::VEC;
+  constexpr int VEC = 16 / (int)sizeof(T);
   const int64_t p = a.row0 + blockIdx.x / a.nseg;
   const int g = (int)(blockIdx.x % a.nseg);
   const Segment<T> seg = segment_of<T>(static_cast<const T*>(a.logits), a.ld, p, g, a.nseg, a.V);
   Stat st{neg_inf(), -kFar * kL2E, 0.f, 0.f};
-  seg.each([&](int, float (&v)[VEC], int nv) {
-    if (nv < VEC)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) v[e] = e < nv ? v[e] : neg_inf();
-    float vm = v[0];
-#pragma unroll
-    for (int e = 1; e < VEC; ++e) vm = fmaxf(vm, v[e]);
-    st.m = fmaxf(st.m, vm);
-    const float m2 = ref_of(st.m, kL2E);
-    if (m2 > st.m2) rebase(st, m2);
+  Best best{neg_inf(), neg_inf(), seg.v0 + (int)threadIdx.x};
+  auto add = [&](const float (&v)[VEC]) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       const float x = __builtin_fmaf(v[e], kL2E, -st.m2), y = exp2_(x);
       st.s += y;
       st.t = __builtin_fmaf(y, fmaxf(x, kFloor), st.t);
     }
-  });
-  const float mine = st.m;
+  };
+  auto meet = [&](int i, float m) __attribute__((always_inline)) {
+    best.meet(i, m);
+    const float m2 = ref_of(best.m, kL2E);
+    if (m2 > st.m2) rebase(st, m2);
+  };
+  seg.groups(
+      [&](int i, float (&v)[kUnroll][VEC]) __attribute__((always_inline)) {
+        float m[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) m[u] = max_of(v[u]);
+        meet(i, max_of(m));
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) add(v[u]);
+      },
+      [&](int i, float (&v)[VEC]) __attribute__((always_inline)) {
+        meet(i, max_of(v));
+        add(v);
+      });
+  st.m = best.m;
   RowState r;
-  r.m = block_max(st.m, red);
+  r.m = block_max<kWaves>(st.m, red);
   r.m2 = ref_of(r.m, kL2E);
   rebase(st, r.m2);
-  r.s = block_add(st.s, red);
-  r.t = block_add(st.t, red);
+  r.s = block_add<kWaves>(st.s, red);
+  r.t = block_add<kWaves>(st.t, red);
   if (is_far(r.m)) {
     float n = 0.f;
     seg.each([&](int, float (&v)[VEC], int nv) {
@@ -368,10 +529,10 @@ __global__ __launch_bounds__(kThreads) void k_token(TokenArgs a) {
       for (int e = 0; e < VEC; ++e)
         if (e < nv) n += v[e] == r.m ? 1.f : v[e] == v[e] ? 0.f : v[e];
     });
-    r.s = block_add(n, red);
+    r.s = block_add<kWaves>(n, red);
     r.t = 0.f;
   }
-  if (a.K > 0) top_of_segment<T>(seg, mine, a.K, top);
+  if (a.K > 0) top_of_segment<T>(seg, best, a.K, top);
   if (a.nseg == 1) {
     r.close();
     write_row<T>(a, p, r, top.out);
@@ -401,8 +562,8 @@ __device__ __forceinline__ RowState join(const Stat* part, int nseg) {
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_token_join(TokenArgs a) {
-  __shared__ uint64_t cand[64 * kMaxTopTokens], out[kMaxTopTokens];
-  __shared__ uint64_t first[64];
+  __shared__ uint64_t cand[kMaxSegments * kMaxTopTokens], out[kMaxTopTokens];
+  __shared__ uint64_t first[kMaxSegments];
   __shared__ int n;
   const int64_t p = a.row0 + blockIdx.x;
   const RowState r = join(a.part + (size_t)p * a.nseg, a.nseg);
@@ -438,6 +599,11 @@ __global__ __launch_bounds__(kThreads) void k_token_join(TokenArgs a) {
 }
 
 // ---------------------------------------------------------------- distillation
+// The gradient needs the softmax's sums before its first value, so a row is read twice or held.  k_distill_row holds a
+// row of up to 144 KB in LDS and so reads and writes memory once; longer rows go through k_distill_stats (sums of
+// segments) and k_distill_grad (joins them, reads its segment again, mostly from a cache).  TWO: the loss has both terms
+// at different temperatures, so a row has two sums; otherwise one serves, at T where there are soft targets and at 1
+// where there are none.
 
 struct DistillArgs {
   int64_t row0;  // first row of this launch
@@ -449,20 +615,21 @@ struct DistillArgs {
   const float* teacher_logit;
   const int* labels;          // [rows] or NULL
   float T, soft, hard, scale;
+  float c;      // log2 e / the temperature of the soft term (of the only one, if there is one)
   float* row_loss;
   void* grad;   // [rows][ld] or NULL
-  Stat* part;   // [rows][nseg]: t holds the sum at temperature T
+  Stat* part;   // [rows][nseg]: s the sum at c, t the sum at temperature 1 (TWO)
   float* at;    // [rows][k + 1]: the logits of the teacher's tokens and of the label
 };
 
-static_assert(kMaxTeacherTokens == kThreads, "one entry a thread");
+static_assert(kMaxTeacherTokens == 256, "one entry a thread of the smallest workgroup");
 
-// a row's targets: which entries count
+// a row's targets: this thread's teacher entry, the label
 struct Target {
-  bool have;      // this thread's teacher entry counts
-  int tok;        // its token
-  float t;        // the teacher's logit
-  int y;          // the label, or -1
+  bool have;       // the entry counts
+  int tok;         // its token
+  float t;         // the teacher's logit
+  int y;           // the label, or -1
   bool soft, any;  // the row has a teacher's entry; a target at all
 };
 __device__ __forceinline__ Target target_of(const DistillArgs& a, size_t q) {
@@ -481,11 +648,232 @@ __device__ __forceinline__ Target target_of(const DistillArgs& a, size_t q) {
   return g;
 }
 
-// One segment's maximum and its sums at temperature 1 and T
-template <typename T>
+// What a row's gradient and loss are made of, from its maximum and sums.
+template <bool TWO>
+struct RowGrad {
+  float m, mc, m1, s, s1;  // the maximum; the references and sums at c and (TWO) at temperature 1
+  float c, invT;
+  float wa, wb, ga, gb;    // weights of the soft and hard term, and of 2^x in the gradient
+  bool far, bad, empty;
+  __device__ __forceinline__ void close(const DistillArgs& a, const Target& t) {
+    c = a.c;
+    invT = 1.f / a.T;
+    far = is_far(m);
+    bad = !(s == s) || m == __builtin_inff();
+    empty = !bad && m == neg_inf();
+    if (!TWO) s1 = s;
+    wa = t.soft ? a.scale * a.soft * a.T : 0.f;
+    wb = t.y >= 0 ? a.scale * a.hard : 0.f;
+    const float nan = __builtin_nanf("");
+    ga = bad ? nan : empty ? 0.f : TWO ? wa / s : (wa + wb) / s;
+    gb = TWO ? (bad ? nan : empty ? 0.f : wb / s1) : 0.f;
+  }
+  // the gradient of a logit that is no target: 0 for -inf, in rows that are not bad
+  __device__ __forceinline__ float dense(float z) const {
+    const float d = ga * exp2_(__builtin_fmaf(z, c, -mc));
+    return TWO ? __builtin_fmaf(gb, exp2_(__builtin_fmaf(z, kL2E, -m1)), d) : d;
+  }
+  // the same in a row that is far or bad
+  __device__ __forceinline__ float odd(float z) const { return bad ? ga : z == m ? ga + gb : 0.f; }
+  __device__ __forceinline__ bool is_odd() const { return bad || (far && !empty); }
+  // the gradient of a target: soft and hard mass on it
+  __device__ __forceinline__ float target(float z, float soft_mass, float hard_mass) const {
+    if (empty) return 0.f;
+    if (bad) return ga;
+    const float pc = far ? (z == m ? 1.f : 0.f) : exp2_(__builtin_fmaf(z, c, -mc));
+    const float p1 = !TWO || far ? pc : exp2_(__builtin_fmaf(z, kL2E, -m1));
+    return wa * (pc / s - soft_mass) + wb * (p1 / s1 - hard_mass);
+  }
+  // log p at a temperature (its factor, reference and sum)
+  __device__ __forceinline__ float logp(float z, float f, float ref, float sum, float inv) const {
+    if (bad) return __builtin_nanf("");
+    if (empty) return neg_inf();
+    if (far || z < -1e30f) return (z - m) * inv - kLn2 * log2_(sum);
+    return kLn2 * (__builtin_fmaf(z, f, -ref) - log2_(sum));
+  }
+  __device__ __forceinline__ float logp_soft(float z) const { return logp(z, c, mc, s, invT); }
+  __device__ __forceinline__ float logp_hard(float z) const {
+    return TWO ? logp(z, kL2E, m1, s1, 1.f) : logp(z, c, mc, s, 1.f);
+  }
+};
+
+// this thread's share of the soft term: q (log q - log p), q = e / es with e = exp(dt)
+template <bool TWO>
+__device__ __forceinline__ float soft_loss(const DistillArgs& a, const RowGrad<TWO>& r, const Target& t, float q,
+                                           float dt, float es, float z) {
+  return t.have && q != 0.f && a.soft != 0.f ? q * (dt - logf(es) - r.logp_soft(z)) : 0.f;
+}
+// the row's loss from the sum of the shares
+template <bool TWO>
+__device__ __forceinline__ float row_loss(const DistillArgs& a, const RowGrad<TWO>& r, const Target& t, float soft,
+                                          float zy) {
+  float loss = t.soft && a.soft != 0.f ? a.soft * a.T * a.T * soft : 0.f;
+  if (t.y >= 0 && a.hard != 0.f) loss -= a.hard * r.logp_hard(zy);
+  return loss;
+}
+
+// The targets' columns inside [lo, hi), written whole after everything else: the first entry of a token takes the mass of
+// all its entries.  tok, mass: every entry's token (-1: does not count) and q.
+template <typename G, bool TWO>
+__device__ __forceinline__ void write_targets(const DistillArgs& a, const RowGrad<TWO>& r, const Target& t,
+                                              const int* tok, const float* mass, float zj, float zy, G* out, int lo,
+                                              int hi) {
+  if (t.have && t.tok >= lo && t.tok < hi) {
+    float sum = 0.f;
+    bool lead = true;
+    for (int j = 0; j < a.k; ++j) {
+      const bool same = tok[j] == t.tok;
+      sum += same ? mass[j] : 0.f;
+      lead = lead && !(same && j < (int)threadIdx.x);
+    }
+    if (lead) out[t.tok] = from_f32<G>(r.target(zj, sum, t.tok == t.y ? 1.f : 0.f));
+  }
+  if (threadIdx.x == 0 && t.y >= lo && t.y < hi) {
+    bool seen = false;
+    for (int j = 0; j < a.k; ++j) seen = seen || tok[j] == t.y;
+    if (!seen) out[t.y] = from_f32<G>(r.target(zy, 0.f, 1.f));
+  }
+}
+
+template <typename G>
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{a, b}), b2));  // to nearest even
+}
+// N neighbouring gradients
+template <typename G, int N>
+__device__ __forceinline__ void store_grad(G* p, const float (&v)[N]) {
+  if constexpr (sizeof(G) == 4) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+  } else if constexpr (N == 8) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack2<G>(v[0], v[1]), pack2<G>(v[2], v[3]), pack2<G>(v[4], v[5]),
+                                              pack2<G>(v[6], v[7]));
+  } else {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack2<G>(v[0], v[1]), pack2<G>(v[2], v[3]));
+  }
+}
+
+// A whole row by one workgroup, in LDS: loaded there directly, its missing columns set to -inf (probability 0, gradient 0),
+// then read three times (maximum, sums, gradient).  LDS holds BYTES >= the row rounded up to a vector a thread.
+template <typename T, typename G, bool TWO, int TH, int BYTES>
+__global__ __launch_bounds__(TH) void k_distill_row(DistillArgs a) {
+  constexpr int VEC = 16 / (int)sizeof(T), NW = TH / 64;
+  static_assert(BYTES % (TH * 16) == 0, "the row rounded up to a vector a thread fits");
+  __shared__ __attribute__((aligned(16))) char lds[BYTES];
+  __shared__ float red[6][NW];
+  __shared__ int tok[kMaxTeacherTokens];
+  __shared__ float mass[kMaxTeacherTokens];
+  const int tid = threadIdx.x, wave = wave_id();
+  const int64_t p = a.row0 + blockIdx.x;
+  const size_t q = a.order ? (size_t)a.order[p] : (size_t)p;
+  const Target t = target_of(a, q);
+  const T* row = static_cast<const T*>(a.logits) + (size_t)p * a.ld;
+  G* out = a.grad ? static_cast<G*>(a.grad) + (size_t)p * a.ld : nullptr;
+  const int nv = (int)(a.ld / VEC), nr = (nv + TH - 1) / TH * TH;
+  if (!t.any) {
+    if (tid == 0) a.row_loss[q] = 0.f;
+    if (out) {
+      const float z[VEC] = {};
+      for (int i = tid; i < nv; i += TH) store_grad<G>(out + (size_t)i * VEC, z);
+    }
+    return;
+  }
+  for (int i = 0; i < nr; i += TH) dma16(row + (size_t)min(i + tid, nv - 1) * VEC, lds + (i + wave * 64) * 16);
+  vm_wait();
+  __syncthreads();
+  T* held = reinterpret_cast<T*>(lds);
+  for (int col = a.V + tid; col < nr * VEC; col += TH) held[col] = from_f32<T>(neg_inf());
+  __syncthreads();
+  const float zj = t.have ? to_f32<T>(held[t.tok]) : 0.f, zy = t.y >= 0 ? to_f32<T>(held[t.y]) : 0.f;
+  auto all = [&](const float* x, bool max) {
+    float r = x[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) r = max ? fmaxf(r, x[w]) : r + x[w];
+    return r;
+  };
+  auto put = [&](float* x, float v) {
+    if ((tid & 63) == 0) x[wave] = v;
+  };
+  // f(vector of the row, its values)
+  auto pass = [&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll 4
+    for (int i = tid; i < nr; i += TH) {
+      float v[VEC];
+      unpack<T>(*reinterpret_cast<const uint4*>(lds + i * 16), v);
+      f(i, v);
+    }
+  };
+  float m = neg_inf();
+  pass([&](int, float (&v)[VEC]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) m = fmaxf(m, v[e]);
+  });
+  put(red[0], wave_max(m));
+  put(red[1], wave_max(t.have ? t.t : neg_inf()));
+  __syncthreads();
+  RowGrad<TWO> r;
+  r.m = all(red[0], true);
+  r.mc = ref_of(r.m, a.c);
+  r.m1 = ref_of(r.m, kL2E);
+  float s = 0.f, s1 = 0.f;
+  if (is_far(r.m)) {
+    pass([&](int, float (&v)[VEC]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s += v[e] == r.m ? 1.f : v[e] == v[e] ? 0.f : v[e];
+    });
+    s1 = s;
+  } else {
+    pass([&](int, float (&v)[VEC]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        s += exp2_(__builtin_fmaf(v[e], a.c, -r.mc));
+        if constexpr (TWO) s1 += exp2_(__builtin_fmaf(v[e], kL2E, -r.m1));
+      }
+    });
+  }
+  // teacher: q_j = softmax(t / T) over the entries that count
+  const float dt = (t.t - all(red[1], true)) / a.T;
+  const float ej = t.have ? expf(dt) : 0.f;
+  put(red[2], wave_add(s));
+  if constexpr (TWO) put(red[3], wave_add(s1));
+  put(red[4], wave_add(ej));
+  __syncthreads();
+  r.s = all(red[2], false);
+  r.s1 = TWO ? all(red[3], false) : r.s;
+  r.close(a, t);
+  const float es = all(red[4], false), qj = t.have ? ej / es : 0.f;
+  if (tid < a.k) {
+    tok[tid] = t.have ? t.tok : -1;
+    mass[tid] = qj;
+  }
+  put(red[5], wave_add(soft_loss(a, r, t, qj, dt, es, zj)));
+  if (out) {
+    if (r.is_odd()) {
+      pass([&](int i, float (&v)[VEC]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] = i * VEC + e < a.V ? r.odd(v[e]) : 0.f;
+        if (i < nv) store_grad<G>(out + (uint32_t)(i * VEC), v);
+      });
+    } else {
+      pass([&](int i, float (&v)[VEC]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[e] = r.dense(v[e]);
+        if (i < nv) store_grad<G>(out + (uint32_t)(i * VEC), v);
+      });
+    }
+  }
+  __syncthreads();
+  if (tid == 0) a.row_loss[q] = row_loss(a, r, t, all(red[5], false), zy);
+  if (out) write_targets(a, r, t, tok, mass, zj, zy, out, 0, a.V);
+}
+
+// One segment's maximum and its sums
+template <typename T, bool TWO>
 __global__ __launch_bounds__(kThreads) void k_distill_stats(DistillArgs a) {
   __shared__ float red[kWaves];
-  constexpr int VEC = Segment<T>::VEC;
+  constexpr int VEC = 16 / (int)sizeof(T);
   const int64_t p = a.row0 + blockIdx.x / a.nseg;
   const int g = (int)(blockIdx.x % a.nseg);
   const size_t q = a.order ? (size_t)a.order[p] : (size_t)p;
@@ -498,32 +886,42 @@ __global__ __launch_bounds__(kThreads) void k_distill_stats(DistillArgs a) {
     if (tg.have) at[threadIdx.x] = to_f32<T>(row[tg.tok]);
     if (threadIdx.x == 0) at[a.k] = tg.y >= 0 ? to_f32<T>(row[tg.y]) : 0.f;
   }
-  const float c = kL2E / a.T;
-  float m = neg_inf(), s1 = 0.f, sT = 0.f;
-  float r1 = -kFar * kL2E, rT = -kFar * c;
-  seg.each([&](int, float (&v)[VEC], int nv) {
-    if (nv < VEC)
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) v[e] = e < nv ? v[e] : neg_inf();
-    float vm = v[0];
-#pragma unroll
-    for (int e = 1; e < VEC; ++e) vm = fmaxf(vm, v[e]);
+  float m = neg_inf(), s = 0.f, s1 = 0.f, rc = ref_of(m, a.c), r1 = ref_of(m, kL2E);
+  auto meet = [&](float vm) __attribute__((always_inline)) {
     if (vm > m) {
       m = vm;
-      const float n1 = ref_of(m, kL2E), nT = ref_of(m, c);
-      s1 *= exp2_(r1 - n1);
-      sT *= exp2_(rT - nT);
-      r1 = n1;
-      rT = nT;
+      const float nc = ref_of(m, a.c), n1 = ref_of(m, kL2E);
+      s *= exp2_(rc - nc);
+      rc = nc;
+      if constexpr (TWO) {
+        s1 *= exp2_(r1 - n1);
+        r1 = n1;
+      }
     }
+  };
+  auto add = [&](const float (&v)[VEC]) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      s1 += exp2_(__builtin_fmaf(v[e], kL2E, -r1));
-      sT += exp2_(__builtin_fmaf(v[e], c, -rT));
+      s += exp2_(__builtin_fmaf(v[e], a.c, -rc));
+      if constexpr (TWO) s1 += exp2_(__builtin_fmaf(v[e], kL2E, -r1));
     }
-  });
-  const float M = block_max(m, red), M1 = ref_of(M, kL2E), MT = ref_of(M, c);
-  float S1 = block_add(s1 * exp2_(r1 - M1), red), ST = block_add(sT * exp2_(rT - MT), red);
+  };
+  seg.groups(
+      [&](int, float (&v)[kUnroll][VEC]) __attribute__((always_inline)) {
+        float vm[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) vm[u] = max_of(v[u]);
+        meet(max_of(vm));
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) add(v[u]);
+      },
+      [&](int, float (&v)[VEC]) __attribute__((always_inline)) {
+        meet(max_of(v));
+        add(v);
+      });
+  const float M = block_max<kWaves>(m, red);
+  float S = block_add<kWaves>(s * exp2_(rc - ref_of(M, a.c)), red);
+  float S1 = TWO ? block_add<kWaves>(s1 * exp2_(r1 - ref_of(M, kL2E)), red) : 0.f;
   if (is_far(M)) {
     float n = 0.f;
     seg.each([&](int, float (&v)[VEC], int nv) {
@@ -531,32 +929,18 @@ __global__ __launch_bounds__(kThreads) void k_distill_stats(DistillArgs a) {
       for (int e = 0; e < VEC; ++e)
         if (e < nv) n += v[e] == M ? 1.f : v[e] == v[e] ? 0.f : v[e];
     });
-    S1 = ST = block_add(n, red);
+    S = S1 = block_add<kWaves>(n, red);
   }
-  if (threadIdx.x == 0) a.part[(size_t)p * a.nseg + g] = Stat{M, M1, S1, ST};
-}
-
-template <typename T>
-__device__ __forceinline__ void store_grad(T* p, const float (&v)[16 / sizeof(T)]) {
-  uint4 w;
-  if constexpr (sizeof(T) == 4) {
-    w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-  } else {
-    uint32_t u[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = (uint32_t)f2bf(v[2 * i]) | ((uint32_t)f2bf(v[2 * i + 1]) << 16);
-    w = make_uint4(u[0], u[1], u[2], u[3]);
-  }
-  *reinterpret_cast<uint4*>(p) = w;
+  if (threadIdx.x == 0) a.part[(size_t)p * a.nseg + g] = Stat{M, 0.f, S, S1};
 }
 
 // The loss of a row and one segment of its gradient
-template <typename T, typename G>
-__global__ __launch_bounds__(kThreads) void k_distill(DistillArgs a) {
+template <typename T, typename G, bool TWO>
+__global__ __launch_bounds__(kThreads) void k_distill_grad(DistillArgs a) {
   __shared__ float red[kWaves];
   __shared__ int tok[kMaxTeacherTokens];
   __shared__ float mass[kMaxTeacherTokens];
-  constexpr int VEC = Segment<T>::VEC, GV = 16 / sizeof(G);
+  constexpr int VEC = 16 / (int)sizeof(T);
   const int64_t p = a.row0 + blockIdx.x / a.nseg;
   const int g = (int)(blockIdx.x % a.nseg);
   const size_t q = a.order ? (size_t)a.order[p] : (size_t)p;
@@ -564,35 +948,30 @@ __global__ __launch_bounds__(kThreads) void k_distill(DistillArgs a) {
   const Segment<T> seg = segment_of<T>(static_cast<const T*>(a.logits), a.ld, p, g, a.nseg, a.V);
   G* out = a.grad ? static_cast<G*>(a.grad) + (size_t)p * a.ld : nullptr;
   // the segment that holds column V - 1 writes the pad columns too; the empty ones behind it write nothing
-  const int last = seg.v0 == seg.v1 ? 0 : seg.v1 * VEC >= a.V ? (int)a.ld : seg.v1 * VEC;
+  const int first = seg.v0 * VEC, last = seg.v0 == seg.v1 ? 0 : seg.v1 * VEC >= a.V ? (int)a.ld : seg.v1 * VEC;
   if (!tg.any) {
     if (g == 0 && threadIdx.x == 0) a.row_loss[q] = 0.f;
-    if (out)
-      for (int col = seg.v0 * VEC + (int)threadIdx.x * GV; col < last; col += kThreads * GV)
-        *reinterpret_cast<uint4*>(out + col) = make_uint4(0, 0, 0, 0);
+    if (out) {
+      const float z[8] = {};
+      for (int col = first + (int)threadIdx.x * 8; col < last; col += kThreads * 8) store_grad<G>(out + col, z);
+    }
     return;
   }
-  // the row's sums at temperature 1 (s) and T (sT)
-  const float c = kL2E / a.T;
   const int lane = threadIdx.x & 63;
   Stat st{neg_inf(), 0.f, 0.f, 0.f};
   if (lane < a.nseg) st = a.part[(size_t)p * a.nseg + lane];
-  RowState r;
+  RowGrad<TWO> r;
   r.m = wave_max(st.m);
-  r.m2 = ref_of(r.m, kL2E);
-  const float mT = ref_of(r.m, c);
-  float f1 = exp2_(st.m2 - r.m2), fT = exp2_(ref_of(st.m, c) - mT);
-  if (is_far(r.m)) f1 = fT = st.m == r.m ? 1.f : 0.f;
-  r.s = wave_add(lane < a.nseg ? st.s * f1 : 0.f);
-  const float sT = wave_add(lane < a.nseg ? st.t * fT : 0.f);
-  r.t = 0.f;
-  r.close();
-  // teacher: q_j = softmax(t / T) over the entries that count
-  const float tm = block_max(tg.have ? tg.t : neg_inf(), red);
-  const float dt = (tg.t - tm) / a.T;
-  const float e = tg.have ? expf(dt) : 0.f;
-  const float es = block_add(e, red);
-  const float qj = tg.have ? e / es : 0.f;
+  r.mc = ref_of(r.m, a.c);
+  r.m1 = ref_of(r.m, kL2E);
+  float fc = exp2_(ref_of(st.m, a.c) - r.mc), f1 = exp2_(ref_of(st.m, kL2E) - r.m1);
+  if (is_far(r.m)) fc = f1 = st.m == r.m ? 1.f : 0.f;
+  r.s = wave_add(st.s * fc);
+  r.s1 = wave_add(st.t * f1);
+  r.close(a, tg);
+  const float tm = block_max<kWaves>(tg.have ? tg.t : neg_inf(), red);
+  const float dt = (tg.t - tm) / a.T, ej = tg.have ? expf(dt) : 0.f, es = block_add<kWaves>(ej, red);
+  const float qj = tg.have ? ej / es : 0.f;
   const float* at = a.at + (size_t)p * (a.k + 1);
   const float zj = tg.have ? at[threadIdx.x] : 0.f, zy = at[a.k];
   if ((int)threadIdx.x < a.k) {
@@ -600,81 +979,93 @@ __global__ __launch_bounds__(kThreads) void k_distill(DistillArgs a) {
     mass[threadIdx.x] = qj;
   }
   if (g == 0) {
-    float lossj = 0.f;
-    if (tg.have && qj != 0.f) {
-      float lp;
-      if (r.bad) lp = __builtin_nanf("");
-      else if (r.empty) lp = neg_inf();
-      else if (r.far || zj < -1e30f) lp = (zj - r.m) / a.T - kLn2 * log2_(sT);
-      else lp = kLn2 * (__builtin_fmaf(zj, c, -mT) - log2_(sT));
-      lossj = qj * (dt - logf(es) - lp);
-    }
-    float loss = a.soft * a.T * a.T * block_add(lossj, red);
-    if (!tg.soft || a.soft == 0.f) loss = 0.f;
-    if (tg.y >= 0 && a.hard != 0.f) loss -= a.hard * r.logp(zy);
-    if (threadIdx.x == 0) a.row_loss[q] = loss;
+    const float soft = block_add<kWaves>(soft_loss(a, r, tg, qj, dt, es, zj), red);
+    if (threadIdx.x == 0) a.row_loss[q] = row_loss(a, r, tg, soft, zy);
   }
   if (!out) return;
-  const float wa = tg.soft ? a.scale * a.soft * a.T : 0.f, wb = tg.y >= 0 ? a.scale * a.hard : 0.f;
-  // weights of 2^x in the gradient; an empty row has none
-  const float nan = __builtin_nanf("");
-  const float ga = r.bad ? nan : r.empty ? 0.f : wa / sT, gb = r.bad ? nan : r.empty ? 0.f : wb / r.s;
-  auto p1 = [&](float z) { return r.far ? (z == r.m ? 1.f : 0.f) : exp2_(__builtin_fmaf(z, kL2E, -r.m2)); };
-  auto pT = [&](float z) { return r.far ? (z == r.m ? 1.f : 0.f) : exp2_(__builtin_fmaf(z, c, -mT)); };
-  auto dense = [&](float z) { return ga * pT(z) + gb * p1(z); };
   const T* row = static_cast<const T*>(a.logits) + (size_t)p * a.ld;
-  for (int col = seg.v0 * VEC + (int)threadIdx.x * 8; col < last; col += kThreads * 8) {
-    float v[8];
+  auto write = [&](auto&& value) __attribute__((always_inline)) {
+    constexpr int U = 4;  // groups of 8 columns in flight
+    for (int b = first + (int)threadIdx.x * 8; b < last; b += kThreads * 8 * U) {
+      uint4 raw[U][8 / VEC];
 #pragma unroll
-    for (int h = 0; h < 8 / VEC; ++h) {
-      float u[VEC];
-      unpack<T>(*reinterpret_cast<const uint4*>(row + col + h * VEC), u);
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) v[h * VEC + i] = col + h * VEC + i < a.V ? dense(u[i]) : 0.f;
+        for (int h = 0; h < 8 / VEC; ++h)
+          raw[u][h] = *reinterpret_cast<const uint4*>(row + min(b + u * kThreads * 8, last - 8) + h * VEC);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int col = b + u * kThreads * 8;
+        if (col >= last) continue;
+        float v[8];
+#pragma unroll
+        for (int h = 0; h < 8 / VEC; ++h) {
+          float w[VEC];
+          unpack<T>(raw[u][h], w);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) v[h * VEC + e] = col + h * VEC + e < a.V ? value(w[e]) : 0.f;
+        }
+        store_grad<G>(out + col, v);
+      }
     }
-#pragma unroll
-    for (int h = 0; h < 8 / GV; ++h) {
-      float u[GV];
-#pragma unroll
-      for (int i = 0; i < GV; ++i) u[i] = v[h * GV + i];
-      store_grad<G>(out + col + h * GV, u);
-    }
-  }
-  // the targets' columns once more, whole: the first entry of a token takes the mass of all its entries
-  __syncthreads();
-  const bool empty = r.empty;
-  auto sparse = [&](int col, float z, float soft_mass, float hard_mass) {
-    if (col < seg.v0 * VEC || col >= last) return;
-    const float d = empty ? 0.f : r.bad ? nan
-        : (wa / sT * pT(z) - wa * soft_mass) + (wb / r.s * p1(z) - wb * hard_mass);
-    out[col] = from_f32<G>(d);
   };
-  if (tg.have) {
-    float sum = 0.f;
-    bool lead = true;
-    for (int j = 0; j < a.k; ++j) {
-      if (tok[j] != tg.tok) continue;
-      sum += mass[j];
-      lead = lead && j >= (int)threadIdx.x;
-    }
-    if (lead) sparse(tg.tok, zj, sum, tg.tok == tg.y ? 1.f : 0.f);
-  }
-  if (threadIdx.x == 0 && tg.y >= 0) {
-    bool seen = false;
-    for (int j = 0; j < a.k; ++j) seen = seen || tok[j] == tg.y;
-    if (!seen) sparse(tg.y, zy, 0.f, 1.f);
-  }
+  if (r.is_odd()) write([&](float z) __attribute__((always_inline)) { return r.odd(z); });
+  else write([&](float z) __attribute__((always_inline)) { return r.dense(z); });
+  __syncthreads();
+  write_targets(a, r, tg, tok, mass, zj, zy, out, first, last);
 }
 
-// Segments of a row: rows alone fill the chip from kRowsFull on; below, a row is cut into pieces of at least kSegMin
-// bytes, at most 64.
-constexpr int kRowsFull = 1024, kSegMin = 16384;
-constexpr int64_t kRowsLaunch = 1 << 22;  // rows of one launch: its threads are counted in 32 bits
+// Segments of a row.  A workgroup takes about 11 us for a row of 200 KB, which is what a row in segments and their join
+// take together, so shorter rows stay whole; longer ones are cut into pieces of 32 KB, unless there are rows enough to
+// fill the chip several times (one row of 131,072 fp32: 32 us whole, 12 us in 16; 64 rows: 34 and 16 us; 1,500 rows: 162
+// and 154 us; at 16,384 rows of 50,000 two segments cost more than they save).
+constexpr int kSegmentBytes = 32 * 1024, kWholeBytes = 224 * 1024, kRowsFull = 2048;
 int segments(int64_t rows, int V, int esize) {
-  if (rows >= kRowsFull) return 1;
-  const int64_t want = (kRowsFull + rows - 1) / std::max<int64_t>(rows, 1);
-  const int64_t most = ((int64_t)V * esize + kSegMin - 1) / kSegMin;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, most), 64));
+  const int64_t bytes = (int64_t)V * esize;
+  if (bytes < kWholeBytes || rows >= kRowsFull) return 1;
+  return (int)std::min<int64_t>((bytes + kSegmentBytes - 1) / kSegmentBytes, kMaxSegments);
+}
+constexpr int64_t kRowsLaunch = 1 << 22;  // rows of one launch: its threads are counted in 32 bits
+int distill_segments(int64_t rows, int V, int esize) {
+  const int64_t bytes = (int64_t)V * esize;
+  return (int)std::min<int64_t>((bytes + kSegmentBytes - 1) / kSegmentBytes, kMaxSegments);
+}
+
+// Rows that a workgroup holds in LDS.
+constexpr int kHeldBytes = 144 * 1024;
+bool held(int V, int esize) { return (size_t)row_ld(V) * esize <= (size_t)kHeldBytes; }
+
+template <typename T>
+void launch_token_rows(const TokenArgs& a, unsigned rows, hipStream_t st) {
+  hipLaunchKernelGGL(k_token<T>, dim3(rows * a.nseg), dim3(kThreads), 0, st, a);
+  if (a.nseg > 1) hipLaunchKernelGGL(k_token_join<T>, dim3(rows), dim3(kThreads), 0, st, a);
+}
+
+template <typename T, typename G, bool TWO>
+void launch_distill_form(const DistillArgs& a, unsigned rows, hipStream_t st) {
+  if (a.nseg == 0) {
+    // the smallest size that holds the row: LDS decides how many rows a compute unit has at once
+    const size_t bytes = a.ld * sizeof(T);
+    const dim3 grid(rows);
+    if (bytes <= 8 * 1024)
+      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 256, 8 * 1024>), grid, dim3(256), 0, st, a);
+    else if (bytes <= 24 * 1024)
+      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 512, 24 * 1024>), grid, dim3(512), 0, st, a);
+    else if (bytes <= 48 * 1024)
+      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 512, 48 * 1024>), grid, dim3(512), 0, st, a);
+    else if (bytes <= 72 * 1024)
+      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 512, 72 * 1024>), grid, dim3(512), 0, st, a);
+    else
+      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 1024, kHeldBytes>), grid, dim3(1024), 0, st, a);
+    return;
+  }
+  hipLaunchKernelGGL((k_distill_stats<T, TWO>), dim3(rows * a.nseg), dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL((k_distill_grad<T, G, TWO>), dim3(rows * a.nseg), dim3(kThreads), 0, st, a);
+}
+template <typename T, typename G>
+void launch_distill_rows(const DistillArgs& a, bool two, unsigned rows, hipStream_t st) {
+  if (two) launch_distill_form<T, G, true>(a, rows, st);
+  else launch_distill_form<T, G, false>(a, rows, st);
 }
 
 }  // namespace
@@ -685,8 +1076,9 @@ size_t token_workspace_bytes(int dtype, int64_t rows, int V, int K) {
 }
 
 size_t distill_workspace_bytes(int dtype, int64_t rows, int V, int k) {
-  const int n = segments(rows, V, dtype == FOLD_BF16 ? 2 : 4);
-  return (size_t)rows * (n * sizeof(Stat) + (size_t)(k + 1) * sizeof(float));
+  const int es = dtype == FOLD_BF16 ? 2 : 4;
+  if (held(V, es)) return 0;
+  return (size_t)rows * (distill_segments(rows, V, es) * sizeof(Stat) + (size_t)(k + 1) * sizeof(float));
 }
 
 void launch_token(int dtype, const int* order, int64_t rows, int V, const void* logits, int J, const int* tokens,
@@ -698,13 +1090,8 @@ void launch_token(int dtype, const int* order, int64_t rows, int V, const void* 
               static_cast<Stat*>(ws), reinterpret_cast<uint64_t*>(static_cast<Stat*>(ws) + (size_t)rows * n)};
   for (; a.row0 < rows; a.row0 += kRowsLaunch) {
     const unsigned r = (unsigned)std::min<int64_t>(rows - a.row0, kRowsLaunch);
-    if (dtype == FOLD_BF16) {
-      hipLaunchKernelGGL(k_token<uint16_t>, dim3(r * n), dim3(kThreads), 0, st, a);
-      if (n > 1) hipLaunchKernelGGL(k_token_join<uint16_t>, dim3(r), dim3(kThreads), 0, st, a);
-    } else {
-      hipLaunchKernelGGL(k_token<float>, dim3(r * n), dim3(kThreads), 0, st, a);
-      if (n > 1) hipLaunchKernelGGL(k_token_join<float>, dim3(r), dim3(kThreads), 0, st, a);
-    }
+    if (dtype == FOLD_BF16) launch_token_rows<uint16_t>(a, r, st);
+    else launch_token_rows<float>(a, r, st);
   }
 }
 
@@ -713,22 +1100,19 @@ void launch_distill(int dtype, const int* order, int64_t rows, int V, const void
                     float hard, float scale, float* row_loss, int grad_dtype, void* grad, void* ws, hipStream_t st) {
   if (rows <= 0) return;
   ProfScope prof("loss_distill", st);
-  const int n = segments(rows, V, dtype == FOLD_BF16 ? 2 : 4);
+  const int es = dtype == FOLD_BF16 ? 2 : 4;
+  const int n = held(V, es) ? 0 : distill_segments(rows, V, es);
+  // one temperature serves unless both terms are there and differ
+  const bool uses_soft = soft != 0.f && k > 0, uses_hard = hard != 0.f && labels;
+  const bool two = uses_soft && uses_hard && T != 1.f;
   DistillArgs a{0, order, logits, (size_t)row_ld(V), V, k, n, teacher_token, teacher_logit, labels, T, soft, hard,
-                scale, row_loss, grad, static_cast<Stat*>(ws),
+                scale, kL2E / (uses_soft ? T : 1.f), row_loss, grad, static_cast<Stat*>(ws),
                 reinterpret_cast<float*>(static_cast<Stat*>(ws) + (size_t)rows * n)};
   for (; a.row0 < rows; a.row0 += kRowsLaunch) {
-    const dim3 grid((unsigned)std::min<int64_t>(rows - a.row0, kRowsLaunch) * n);
-    if (dtype == FOLD_BF16) {
-      hipLaunchKernelGGL(k_distill_stats<uint16_t>, grid, dim3(kThreads), 0, st, a);
-      hipLaunchKernelGGL((k_distill<uint16_t, uint16_t>), grid, dim3(kThreads), 0, st, a);
-    } else {
-      hipLaunchKernelGGL(k_distill_stats<float>, grid, dim3(kThreads), 0, st, a);
-      if (grad_dtype == FOLD_BF16)
-        hipLaunchKernelGGL((k_distill<float, uint16_t>), grid, dim3(kThreads), 0, st, a);
-      else
-        hipLaunchKernelGGL((k_distill<float, float>), grid, dim3(kThreads), 0, st, a);
-    }
+    const unsigned r = (unsigned)std::min<int64_t>(rows - a.row0, kRowsLaunch);
+    if (dtype == FOLD_BF16) launch_distill_rows<uint16_t, uint16_t>(a, two, r, st);
+    else if (grad_dtype == FOLD_BF16) launch_distill_rows<float, uint16_t>(a, two, r, st);
+    else launch_distill_rows<float, float>(a, two, r, st);
   }
 }
 

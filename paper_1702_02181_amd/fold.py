@@ -15,7 +15,9 @@ The functions keep the ABI's names:
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
+import functools
 import os
 from ctypes import POINTER, byref, c_int32, c_int64, c_size_t, c_void_p
 from typing import NamedTuple
@@ -751,12 +753,32 @@ def _here(name, t):
         raise ValueError(f"{name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
 
 
+_HERE_STREAM = contextlib.nullcontext()
+
+
 def _on(stream):
     """New tensors belong to the stream that the call runs on."""
-    import contextlib
-
     import torch
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return _HERE_STREAM if stream is None else torch.cuda.stream(stream)
+
+
+class _Raw:
+    """The current stream as the calls take it, without the object that torch.cuda.current_stream() makes (3 us, where a
+    whole call on one row takes 15)."""
+
+    @property
+    def cuda_stream(self):
+        import torch
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+_CURRENT = _Raw()
+
+
+# sizes by sizes: pure functions of their arguments
+_vocab_ws = functools.lru_cache(256)(fold_vocab_workspace_size)
+_distill_ws = functools.lru_cache(256)(fold_distill_workspace_size)
+_token_ws = functools.lru_cache(256)(fold_token_workspace_size)
 
 
 class VocabHead:
@@ -784,7 +806,7 @@ class VocabHead:
             else:
                 _matrix("out", out, self.vocab, dtype, rows)
             fold_vocab_logits(self.code, rows, self.hidden, self.vocab, states, self.weight, self.bias,
-                              _code(out.dtype), out, stream)
+                              _code(out.dtype), out, stream or _CURRENT)
         return out
 
     def backward(self, states, dlogits, d_states=True, dW=True, dbias=True, accumulate=False, stream=None):
@@ -810,10 +832,10 @@ class VocabHead:
                 dbias = torch.empty(self.vocab, **f32)
             elif dbias is not None:
                 _vector("dbias", dbias, torch.float32, self.vocab)
-            n = fold_vocab_workspace_size(self.code, rows, self.hidden, self.vocab)
+            n = _vocab_ws(self.code, rows, self.hidden, self.vocab)
             ws = torch.empty(n, dtype=torch.uint8, device=states.device) if n else None
             fold_vocab_backward(self.code, rows, self.hidden, self.vocab, states, self.weight, dlogits, d_states, dW,
-                                dbias, FOLD_VOCAB_ACCUMULATE if accumulate else 0, ws, n, stream)
+                                dbias, FOLD_VOCAB_ACCUMULATE if accumulate else 0, ws, n, stream or _CURRENT)
         return d_states, dW, dbias
 
 
@@ -841,23 +863,23 @@ def distill_loss(logits, vocab, teacher_token=None, teacher_logit=None, labels=N
         elif dlogits is not None:
             _matrix("dlogits", dlogits, vocab, grad_dtype, rows)
         loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
-        n = fold_distill_workspace_size(code, rows, vocab, k)
+        n = _distill_ws(code, rows, vocab, k)
         ws = torch.empty(n, dtype=torch.uint8, device=logits.device) if n else None
         fold_loss_distill(None if sched is None else sched.handle, code, rows, vocab, logits, k, teacher_token,
                           teacher_logit, labels, temperature, soft_weight, hard_weight, scale, loss,
-                          code if dlogits is None else _code(dlogits.dtype), dlogits, ws, n, stream)
+                          code if dlogits is None else _code(dlogits.dtype), dlogits, ws, n, stream or _CURRENT)
     return loss, dlogits
 
 
 class TokenLogprobs(NamedTuple):
-    """logp [rows, num_tokens], entropy [rows], top_token and top_logp [rows, top_k]."""
+    """logp [rows, num_tokens], entropy [rows], top_token and top_logp [rows, top_k]; None for what was not asked for."""
     logp: object
     entropy: object
     top_token: object
     top_logp: object
 
 
-def token_logprobs(logits, vocab, tokens=None, top_k=0, sched=None, stream=None) -> TokenLogprobs:
+def token_logprobs(logits, vocab, tokens=None, top_k=0, entropy=True, sched=None, stream=None) -> TokenLogprobs:
     """Log probabilities of `tokens` [rows, num_tokens] int32, the rows' entropy and their top_k alternatives
     (fold_token_logprobs).  sched: as in distill_loss."""
     import torch
@@ -866,11 +888,12 @@ def token_logprobs(logits, vocab, tokens=None, top_k=0, sched=None, stream=None)
     if tokens is not None:
         J = int(tokens.shape[-1])
         _vector("tokens", tokens, torch.int32, rows, J)
-    n = fold_token_workspace_size(code, rows, vocab, top_k)
+    n = _token_ws(code, rows, vocab, top_k)
     with _on(stream):
         new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
-        out = TokenLogprobs(new(rows, J), new(rows), new(rows, top_k, dtype=torch.int32), new(rows, top_k))
+        out = TokenLogprobs(new(rows, J) if J else None, new(rows) if entropy else None,
+                            new(rows, top_k, dtype=torch.int32) if top_k else None, new(rows, top_k) if top_k else None)
         ws = new(n, dtype=torch.uint8) if n else None
         fold_token_logprobs(None if sched is None else sched.handle, code, rows, vocab, logits, J, tokens, out.logp,
-                            out.entropy, top_k, out.top_token, out.top_logp, ws, n, stream)
+                            out.entropy, top_k, out.top_token, out.top_logp, ws, n, stream or _CURRENT)
     return out

@@ -201,16 +201,29 @@ def _check_tokens(z, dtype, tokens, K, fill=NAN):
     rel = _rel(z, 1.0, V)
     at = np.clip(tokens, 0, V - 1)
     size = np.where(np.isfinite(logp), np.abs(logp), 0)
-    _within(_np(r.logp), logp, np.take_along_axis(rel, at, 1) + 2 * U * size, "logp")
+    assert (r.logp is None) == (tokens.shape[1] == 0) and (r.top_token is None) == (r.top_logp is None) == (K == 0)
+    if r.logp is not None:
+        _within(_np(r.logp), logp, np.take_along_axis(rel, at, 1) + 2 * U * size, "logp")
     big = rel[:, 0:1] * 0 + U * (V / 256 + 64)
     _within(_np(r.entropy), ent, 4 * big[:, 0] * (1 + np.where(np.isfinite(ent), ent, 0)) + 16 * U * np.where(np.isfinite(ent), ent, 0) ** 2, "entropy")
-    assert np.array_equal(r.top_token.cpu().numpy(), top), "top tokens"
-    with np.errstate(all="ignore"):
-        b = U * (4 * np.where(np.isfinite(top_lp), np.abs(top_lp), 0) * 1.5 + V / 256 + 64 + 4 * math.log(V))
-    _within(_np(r.top_logp), top_lp, b, "top log probabilities")
+    if K:
+        assert np.array_equal(r.top_token.cpu().numpy(), top), "top tokens"
+        with np.errstate(all="ignore"):
+            b = U * (4 * np.where(np.isfinite(top_lp), np.abs(top_lp), 0) * 1.5 + V / 256 + 64 + 4 * math.log(V))
+        _within(_np(r.top_logp), top_lp, b, "top log probabilities")
     again = F.token_logprobs(zd, V, _ints(tokens), K)
-    assert all(torch.equal(torch.nan_to_num(x.float(), 7.0), torch.nan_to_num(y.float(), 7.0)) for x, y in zip(r, again))
+    assert all(_same(x, y) for x, y in zip(r, again))
+    alone = F.token_logprobs(zd, V, _ints(tokens), entropy=False)
+    assert _same(alone.logp, r.logp) and alone.entropy is None
     return r
+
+
+def _same(x, y):
+    """The same bits, or the same NaN, or both left out."""
+    import torch
+    if x is None or y is None:
+        return x is y
+    return torch.equal(torch.nan_to_num(x.float(), 7.0), torch.nan_to_num(y.float(), 7.0))
 
 
 @pytest.mark.parametrize("M,V,dtype", ROWS)

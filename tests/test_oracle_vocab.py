@@ -179,9 +179,10 @@ def test_refusals_of_the_distillation_loss(F):
                dict(grad=1, dz=b),                     # another type over the same memory
                dict(dz=_Buf(4096 + 256))):             # a row further on
         _refused(F, F.FOLD_E_INVALID, call, **kw)
-    n = F.fold_distill_workspace_size(0, 4, 16, 2)
-    _refused(F, F.FOLD_E_MISMATCH, call, n=n - 1)
-    _refused(F, F.FOLD_E_MISMATCH, call, ws=None)
+    n = F.fold_distill_workspace_size(0, 4, 100000, 2)
+    assert n > 0  # a row that no workgroup holds
+    _refused(F, F.FOLD_E_MISMATCH, call, vocab=100000, n=n - 1)
+    _refused(F, F.FOLD_E_MISMATCH, call, vocab=100000, ws=None)
     _refused(F, F.FOLD_E_INVALID, F.fold_distill_workspace_size, 0, 4, 16, 300)
     call(rows=0, z=None, loss=None, tok=None, t=None, dz=None, ws=None, n=0)
 
