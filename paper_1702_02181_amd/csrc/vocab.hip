@@ -62,8 +62,13 @@ __device__ __forceinline__ int along_off(int r, int u) {
 __device__ __forceinline__ void dma16_at(const char* base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory", "m0");
 }
-__device__ __forceinline__ uint32_t lds_of(const char* p) {
-  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const FOLD_LDS_AS char*)p);
+// the same with 4 bytes a lane, from its own address
+__device__ __forceinline__ void dma4_at(const float* src, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(src) : "memory", "m0");
+}
+template <typename P>
+__device__ __forceinline__ uint32_t lds_of(const P* p) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const FOLD_LDS_AS char*)reinterpret_cast<const char*>(p));
 }
 
 // One wave's loads of an operand's stages: NI instructions of 1 KB a stage, instruction t of the workgroup (NI a wave).  e0: the tile's first element.  Elements past
@@ -182,11 +187,6 @@ __device__ __forceinline__ bool tile_of(const ProductArgs& g, unsigned& mt, unsi
   return true;
 }
 
-// One wave's part of a tile, WM x WN accumulators from row m0, column n0 (32 WN columns of the bias at `bias`), to out.
-// C's columns are on the accumulators' rows: a lane holds four neighbouring columns of one row.  They go through an image
-// in LDS of 32 rows by 128 bytes (rows 16 bytes apart in their banks), so that whole 128-byte pieces of rows are stored.
-constexpr int kImageRow = 128 + 16, kImage = 32 * kImageRow;
-
 template <typename OUT>
 __device__ __forceinline__ OUT* out_of(const ProductArgs& g, unsigned piece) {
   return static_cast<OUT*>(g.out) + (size_t)piece * g.M * g.ld;
@@ -197,6 +197,25 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {  // rounded to
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
 }
 
+// The accumulators start from the bias of their columns (LDS, 32 WN of them): C's columns are on the accumulators' rows, so
+// register 4 q + e of lane l is column 8 q + 4 (l / 32) + e of row l % 32.
+template <int WM, int WN>
+__device__ __forceinline__ void start_acc(f32x16 (&acc)[WM][WN], const float* bias, int lane) {
+#pragma unroll
+  for (int j = 0; j < WN; ++j)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float4 b = *reinterpret_cast<const float4*>(bias + 32 * j + 8 * q + 4 * (lane >> 5));
+#pragma unroll
+      for (int i = 0; i < WM; ++i) {
+        acc[i][j][4 * q] = b.x;
+        acc[i][j][4 * q + 1] = b.y;
+        acc[i][j][4 * q + 2] = b.z;
+        acc[i][j][4 * q + 3] = b.w;
+      }
+    }
+}
+
 // what a wave's lanes have written to LDS is there for its other lanes (LDS keeps a wave's order: nothing to wait for)
 __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -204,16 +223,20 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-template <typename OUT, int WM, int WN>
-__device__ __forceinline__ void store_tile(const ProductArgs& g, OUT* out, const f32x16 (&acc)[WM][WN], int64_t m0,
-                                           int64_t n0, const float* bias, char* img, int lane) {
-  constexpr int VEC = 16 / (int)sizeof(OUT), COLS = 128 / (int)sizeof(OUT), JG = COLS / 32;
-  static_assert(WN % JG == 0, "whole images");
+// One wave's part of a tile, WM x WN accumulators from row m0, column n0, to out, through images in LDS of 32 rows by 128
+// bytes (rows 16 bytes apart in their banks), so that an instruction stores eight rows' whole lines.  Stored from the
+// registers, 32 rows by 32 bytes, logits whose rows are a power of two apart queued in a few of the memory's channels:
+// 8,192 x 32,768 bf16 at H = 1,024 took 980 us, at a vocabulary of 32,000 530 us.  For bf16 the half waves swap first: two
+// neighbouring groups of 8 columns, 4 in either half, become 8 columns of one group a lane.  WHOLE: the part lies inside
+// the matrix.
+constexpr int kImageRow = 128 + 16, kImage = 32 * kImageRow;
+
+template <typename OUT, int WM, int WN, bool WHOLE>
+__device__ __forceinline__ void store_part(const ProductArgs& g, OUT* out, const f32x16 (&acc)[WM][WN], int rows, int vals,
+                                           int cols, char* img, int lane) {
+  constexpr int VEC = 16 / (int)sizeof(OUT), COLS = 128 / (int)sizeof(OUT), JG = COLS / 32 < WN ? COLS / 32 : WN;
+  constexpr int LPR = 32 * JG / VEC;  // lanes of a row of the image
   const int h = lane >> 5, l32 = lane & 31;
-  // what of the part exists: rows, columns with a value, columns that are written
-  const int rows = (int)min(g.M - m0, (int64_t)(32 * WM)), vals = (int)min(g.N - n0, (int64_t)(32 * WN));
-  const int cols = (int)min(g.cols - n0, (int64_t)(32 * WN));
-  out += (size_t)m0 * g.ld + n0;
 #pragma unroll
   for (int i = 0; i < WM; ++i)
 #pragma unroll
@@ -223,25 +246,33 @@ __device__ __forceinline__ void store_tile(const ProductArgs& g, OUT* out, const
         f32x16 c = acc[i][j];
         if constexpr (WM * WN >= 16) asm volatile("" : "+a"(c));  // stays in its accumulator registers until here
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int col = 32 * j + 8 * q + 4 * h;
-          const float4 b4 = *reinterpret_cast<const float4*>(bias + col);
-          const float b[4] = {b4.x, b4.y, b4.z, b4.w};
-          float v[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = c[4 * q + e] + b[e];
-          char* o = img + l32 * kImageRow + (col - 32 * j0) * (int)sizeof(OUT);
-          if constexpr (sizeof(OUT) == 4) *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
-          else *reinterpret_cast<uint2*>(o) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+        for (int q = 0; q < 4; q += VEC / 4) {
+          uint4 v;
+          int n;
+          if constexpr (sizeof(OUT) == 4) {
+            n = 32 * (j - j0) + 8 * q + 4 * h;
+            v = make_uint4(__float_as_uint(c[4 * q]), __float_as_uint(c[4 * q + 1]), __float_as_uint(c[4 * q + 2]),
+                           __float_as_uint(c[4 * q + 3]));
+          } else {
+            n = 32 * (j - j0) + 8 * (q + h);
+            const auto lo = __builtin_amdgcn_permlane32_swap(bf16_pair(c[4 * q], c[4 * q + 1]),
+                                                             bf16_pair(c[4 * q + 4], c[4 * q + 5]), false, false);
+            const auto hi = __builtin_amdgcn_permlane32_swap(bf16_pair(c[4 * q + 2], c[4 * q + 3]),
+                                                             bf16_pair(c[4 * q + 6], c[4 * q + 7]), false, false);
+            v = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+          }
+          *reinterpret_cast<uint4*>(img + l32 * kImageRow + n * (int)sizeof(OUT)) = v;
         }
       }
       wave_fence();
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int row = x * 8 + (lane >> 3), col = (lane & 7) * VEC, n = 32 * j0 + col;
+      for (int x = 0; x < 32 * LPR / 64; ++x) {
+        const int row = x * (64 / LPR) + lane / LPR, col = lane % LPR * VEC, n = 32 * j0 + col;
         uint4 v = *reinterpret_cast<const uint4*>(img + row * kImageRow + col * (int)sizeof(OUT));
-        if (32 * i + row >= rows || n >= cols) continue;
-        v = mask_tail<OUT>(v, max(vals - n, 0));
+        if constexpr (!WHOLE) {
+          if (32 * i + row >= rows || n >= cols) continue;
+          v = mask_tail<OUT>(v, max(vals - n, 0));
+        }
         OUT* o = out + (size_t)(32 * i + row) * g.ld + n;
         if constexpr (sizeof(OUT) == 4) {
           if (g.add) {  // + 0 in the pad columns
@@ -254,22 +285,62 @@ __device__ __forceinline__ void store_tile(const ProductArgs& g, OUT* out, const
         }
         *reinterpret_cast<uint4*>(o) = v;
       }
-      wave_fence();  // one image after the other
+      wave_fence();
     }
+}
+
+template <typename OUT, int WM, int WN>
+__device__ __forceinline__ void store_tile(const ProductArgs& g, OUT* out, const f32x16 (&acc)[WM][WN], int64_t m0,
+                                           int64_t n0, char* img, int lane) {
+  // what of the part exists: rows, columns with a value, columns that are written
+  const int rows = (int)min(g.M - m0, (int64_t)(32 * WM)), vals = (int)min(g.N - n0, (int64_t)(32 * WN));
+  const int cols = (int)min(g.cols - n0, (int64_t)(32 * WN));
+  out += (size_t)m0 * g.ld + n0;
+  if (rows == 32 * WM && vals == 32 * WN) store_part<OUT, WM, WN, true>(g, out, acc, rows, vals, cols, img, lane);
+  else store_part<OUT, WM, WN, false>(g, out, acc, rows, vals, cols, img, lane);
+}
+
+// One stage of the K loop: NS steps of MULS multiplications, placed one by one with what runs beside them.
+//   load(s, f)   reads fragment f of the step after s (of the next stage after the last step)
+//   meet()       the workgroup meets: everybody has read its fragments of this stage, the next stage has landed
+//   put(d)       starts load d of a new stage
+// The fragments are spread over a step, so that four waves' reads do not queue in LDS, the first needed first; the new
+// stage's loads go out in the first step, into the slot that the last meeting freed (SLOTS > 2), or behind the meeting into
+// this stage's own slot (SLOTS = 2).  A meeting follows the first multiplications of its step, which need the fragments
+// read last.
+template <int MULS, int FRAGS, int LOADS, int NS, int SLOTS, class MUL, class LOAD, class MEET, class PUT>
+__device__ __forceinline__ void pipeline_stage(MUL&& multiply, LOAD&& load, MEET&& meet, PUT&& put) {
+  constexpr int K = MULS < 16 ? MULS : 16, EACH = MULS / K;  // places of a step, multiplications of each
+  constexpr int MEETING = K == 16 ? 4 : 0;
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    const bool last = s == NS - 1, loads = SLOTS > 2 ? s == 0 : last;
+    const int from = last ? MEETING : 0, pfrom = SLOTS > 2 ? 0 : MEETING;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (last && k == MEETING) meet();
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) multiply(s & 1, k * EACH + e);
+#pragma unroll
+      for (int f = 0; f < FRAGS; ++f)
+        if (from + f * (K - from) / FRAGS == k) load(s, f);
+#pragma unroll
+      for (int d = 0; d < LOADS; ++d)
+        if (loads && pfrom + (2 * d + 1) * (K - pfrom) / (2 * LOADS) == k) put(d);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
 }
 
 // OUT: the element type of out; partial sums of a split go to out + piece * M * ld.
 // The K loop keeps SLOTS stages in LDS and the fragments of two steps (16 bytes of K a lane) in registers: a step's
-// multiplications run while the next step's fragments are read.  At a stage's last step its fragments are in registers
-// already, so the workgroup meets there: the next stage has landed, its first fragments are read, and the loads of a new
-// stage go out into the slot that nobody reads any more.
+// multiplications run while the next step's fragments are read.
 template <typename T, int AD, int BD, typename OUT, int WM, int WN, int KB, int SLOTS>
 __global__ __launch_bounds__(kThreads, WM * WN >= 16 ? 1 : 2) void k_product(ProductArgs g) {
   constexpr int EA = 64 * WM, EB = 64 * WN, STAGE = (EA + EB) * KB, NS = KB / 32;
   using LA = Loader<T, AD, EA, KB>;
   using LB = Loader<T, BD, EB, KB>;
   __shared__ __attribute__((aligned(16))) char lds[SLOTS * STAGE];
-  static_assert(SLOTS * STAGE >= 4 * kImage, "the images lie where the stages were");
   __shared__ __attribute__((aligned(16))) float bias[EB];
   static_assert(EB <= kThreads, "one bias a thread");
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
@@ -283,7 +354,6 @@ __global__ __launch_bounds__(kThreads, WM * WN >= 16 ? 1 : 2) void k_product(Pro
   const LB lb(g.b, n0, wave, lane);
   const uint32_t base = lds_of(lds);
   f32x16 acc[WM][WN];
-  zero_acc(acc);
   if (tid < EB) bias[tid] = g.bias && n0 + tid < g.N ? g.bias[n0 + tid] : 0.f;
   auto issue = [&](int c) {
     const uint32_t to = base + (c - c0) % SLOTS * STAGE;
@@ -292,14 +362,15 @@ __global__ __launch_bounds__(kThreads, WM * WN >= 16 ? 1 : 2) void k_product(Pro
   };
   uint4 fa[2][WM], fb[2][WN];
   // the f-th fragment of step s of a slot into register set `set`
-  auto load = [&](const char* slot, int s, int set, int f) {
-    if (f < WM) fa[set][f] = fragment<T, AD, EA, KB>(slot, (wm * WM + f) * 32, s, lane);
-    else fb[set][f - WM] = fragment<T, BD, EB, KB>(slot + EA * KB, (wn * WN + f - WM) * 32, s, lane);
+  auto load = [&](const char* slot, int s, int set, int f) {  // in the order of their first use
+    const int i = f == 0 ? 0 : f - WN, j = f - 1;
+    if (f == 0 || f > WN) fa[set][i] = fragment<T, AD, EA, KB>(slot, (wm * WM + i) * 32, s, lane);
+    else fb[set][j] = fragment<T, BD, EB, KB>(slot + EA * KB, (wn * WN + j) * 32, s, lane);
   };
   // the k-th multiplication of a step.  C's columns are on the accumulators' rows: a lane holds four neighbouring
   // columns of one row of C
   constexpr int FRAGS = WM + WN, MULS = WM * WN * (sizeof(T) == 2 ? 1 : 4), LOADS = LA::NI + LB::NI;
-  constexpr int FPM = (FRAGS + MULS - 1) / MULS, LPM = (LOADS + MULS - 1) / MULS;  // of each beside one multiplication
+  constexpr int AHEAD = SLOTS > 2 ? SLOTS - 1 : SLOTS;  // stages loaded before the loop, and ahead in it
   auto multiply = [&](int set, int k) {
     const int e = k / (WM * WN), i = k / WN % WM, j = k % WN;
     if constexpr (sizeof(T) == 2)
@@ -317,53 +388,49 @@ __global__ __launch_bounds__(kThreads, WM * WN >= 16 ? 1 : 2) void k_product(Pro
     else if (behind == 1) vm_wait_n<LOADS>();
     else vm_wait();
   };
-  if (c0 < c1) {
-    int issued = min(c0 + SLOTS, c1);
+  if (c0 == c1) {
+    __syncthreads();
+    start_acc(acc, bias + wn * 32 * WN, lane);
+  } else {
+    int issued = min(c0 + AHEAD, c1);
     for (int c = c0; c < issued; ++c) issue(c);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the bias
     landed(c0, issued);
     wg_barrier();
+    start_acc(acc, bias + wn * 32 * WN, lane);
 #pragma unroll
     for (int f = 0; f < FRAGS; ++f) load(lds, 0, 0, f);
     int c = c0;
-    // stages with SLOTS more whole ones behind them: one multiplication, then the fragments and loads placed beside it
-    const int cw = (int)min((int64_t)c1, min(la.whole(), lb.whole())) - SLOTS;
-    const char *pa = la.p + (size_t)(c0 + SLOTS) * la.step, *pb = lb.p + (size_t)(c0 + SLOTS) * lb.step;
+    // the stages that start the load of a whole stage
+    const int cw = (int)min((int64_t)c1, min(la.whole(), lb.whole())) - AHEAD;
+    const char *pa = la.p + (size_t)(c0 + AHEAD) * la.step, *pb = lb.p + (size_t)(c0 + AHEAD) * lb.step;
     for (; c < cw; ++c) {
       const int at = (c - c0) % SLOTS * STAGE, next = (c + 1 - c0) % SLOTS * STAGE;
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        if (s == NS - 1) {
-          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * LOADS) : "memory");
-          wg_barrier();
-        }
-#pragma unroll
-        for (int k = 0; k < MULS; ++k) {
-          multiply(s & 1, k);
-#pragma unroll
-          for (int f = k * FPM; f < (k + 1) * FPM && f < FRAGS; ++f)
-            load(lds + (s < NS - 1 ? at : next), (s + 1) % NS, (s + 1) & 1, f);
-          if (s == NS - 1)
-#pragma unroll
-            for (int d = k * LPM; d < (k + 1) * LPM && d < LOADS; ++d) {
-              if (d < LA::NI) dma16_at(pa, la.off[d], base + at + (wave * LA::NI + d) * 1024);
-              else dma16_at(pb, lb.off[d - LA::NI], base + at + EA * KB + (wave * LB::NI + d - LA::NI) * 1024);
-            }
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
+      const uint32_t to = base + (c - c0 + AHEAD) % SLOTS * STAGE;
+      pipeline_stage<MULS, FRAGS, LOADS, NS, SLOTS>(
+          multiply, [&](int s, int f) { load(lds + (s < NS - 1 ? at : next), (s + 1) % NS, (s + 1) & 1, f); },
+          [&]() {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * LOADS) : "memory");
+            wg_barrier();
+          },
+          [&](int d) {
+            if (d < LA::NI) dma16_at(pa, la.off[d], to + (wave * LA::NI + d) * 1024);
+            else dma16_at(pb, lb.off[d - LA::NI], to + EA * KB + (wave * LB::NI + d - LA::NI) * 1024);
+          });
       pa += la.step;
       pb += lb.step;
     }
-    issued = max(issued, min(c + SLOTS, c1));
+    issued = max(issued, min(c + AHEAD, c1));
     for (; c < c1; ++c) {
       const char *at = lds + (c - c0) % SLOTS * STAGE, *next = lds + (c + 1 - c0) % SLOTS * STAGE;
+      if (SLOTS > 2 && issued < c1) issue(issued++);
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         if (s == NS - 1 && c + 1 < c1) {
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           landed(c + 1, issued);
           wg_barrier();
-          if (issued < c1) issue(issued++);
+          if (SLOTS == 2 && issued < c1) issue(issued++);
         }
         if (s < NS - 1 || c + 1 < c1)
 #pragma unroll
@@ -373,25 +440,26 @@ __global__ __launch_bounds__(kThreads, WM * WN >= 16 ? 1 : 2) void k_product(Pro
       }
     }
   }
+  static_assert(SLOTS * STAGE >= 4 * kImage, "the images lie where the stages were");
   __syncthreads();
-  store_tile<OUT, WM, WN>(g, out_of<OUT>(g, piece), acc, m0 + wm * 32 * WM, n0 + wn * 32 * WN, bias + wn * 32 * WN,
-                          lds + wave * kImage, lane);
+  store_tile<OUT, WM, WN>(g, out_of<OUT>(g, piece), acc, m0 + wm * 32 * WM, n0 + wn * 32 * WN, lds + wave * kImage, lane);
 }
 
 // The same product where both operands run along a short K (the logits: K = H) and there are many tiles: a workgroup per
-// compute unit walks its tiles, and the stages of all of them are one stream through the slots.  While a tile's last
-// SLOTS stages are multiplied the first of the next tile are loaded, and they land while the tile is stored, so neither
-// the first loads' latency nor the store is waited for (a tile of K = 1,024 bf16 is 28 us of multiplication, and took
-// 16 us more alone).  Needs at least SLOTS stages.
+// compute unit walks its tiles, and the stages of all of them are one stream through the slots.  While a tile's last stages
+// are multiplied the first of the next tile and its bias are loaded, and they land while the tile is stored, so neither
+// the first loads' latency nor the store's is waited for (8,192 x 1,024 x 32,000 bf16: 693 us with a workgroup a tile,
+// 490 us so).  Needs at least SLOTS stages.
 template <typename T, typename OUT>
 __global__ __launch_bounds__(kThreads, 1) void k_product_chain(ProductArgs g) {
+  g.add = 0;  // logits are written
   constexpr int WM = 4, WN = 4, KB = 64, SLOTS = 4;
   constexpr int EA = 64 * WM, EB = 64 * WN, STAGE = (EA + EB) * KB, NS = KB / 32;
   using LA = Loader<T, kAlong, EA, KB>;
   using LB = Loader<T, kAlong, EB, KB>;
   __shared__ __attribute__((aligned(16))) char lds[SLOTS * STAGE];
   __shared__ __attribute__((aligned(16))) char image[4 * kImage];
-  __shared__ __attribute__((aligned(16))) float bias[EB];
+  __shared__ __attribute__((aligned(16))) float bias[2][EB];  // of the tile that is multiplied and of the next
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   const int wm = wave & 1, wn = wave >> 1;
   const unsigned total = (unsigned)g.mt * (unsigned)g.nt, per = (total + 7) >> 3;
@@ -407,8 +475,9 @@ __global__ __launch_bounds__(kThreads, 1) void k_product_chain(ProductArgs g) {
   const int n = g.nstage;
   uint4 fa[2][WM], fb[2][WN];
   auto load = [&](const char* at, int s, int set, int f) {
-    if (f < WM) fa[set][f] = fragment<T, kAlong, EA, KB>(at, (wm * WM + f) * 32, s, lane);
-    else fb[set][f - WM] = fragment<T, kAlong, EB, KB>(at + EA * KB, (wn * WN + f - WM) * 32, s, lane);
+    const int i = f == 0 ? 0 : f - WN, j = f - 1;
+    if (f == 0 || f > WN) fa[set][i] = fragment<T, kAlong, EA, KB>(at, (wm * WM + i) * 32, s, lane);
+    else fb[set][j] = fragment<T, kAlong, EB, KB>(at + EA * KB, (wn * WN + j) * 32, s, lane);
   };
   constexpr int FRAGS = WM + WN, MULS = WM * WN * (sizeof(T) == 2 ? 1 : 4), LOADS = LA::NI + LB::NI;
   f32x16 acc[WM][WN];
@@ -426,24 +495,35 @@ __global__ __launch_bounds__(kThreads, 1) void k_product_chain(ProductArgs g) {
     if (d < LA::NI) dma16_at(pa, la.off[d], to + (wave * LA::NI + d) * 1024);
     else dma16_at(pb, lb.off[d - LA::NI], to + EA * KB + (wave * LB::NI + d - LA::NI) * 1024);
   };
-  static_assert(FRAGS <= MULS && LOADS <= MULS, "one of each beside a multiplication");
+  // columns that are not there get another one's bias, and are not stored; before a tile's first stage, so that it is there
+  // when that is
+  auto load_bias = [&](int buf) {
+    if (g.bias) dma4_at(g.bias + min(n0 + tid, g.N - 1), lds_of(bias[buf]) + wave * 256);
+  };
+  if (!g.bias) bias[0][tid] = bias[1][tid] = 0.f;
+  load_bias(0);
 #pragma unroll
-  for (int c = 0; c < SLOTS; ++c) {
+  for (int c = 0; c < SLOTS - 1; ++c) {
 #pragma unroll
     for (int d = 0; d < LOADS; ++d) put(d, base + c * STAGE);
     pa += step;
     pb += step;
   }
-  vm_wait_n<(SLOTS - 1) * LOADS>();
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * LOADS) : "memory");
   wg_barrier();
 #pragma unroll
   for (int f = 0; f < FRAGS; ++f) load(lds, 0, 0, f);
+  // A wait for stage c lets only the loads of later stages be outstanding, and loads and stores are counted together and
+  // complete in order.  After a tile that was stored whole, STORES store instructions lie between the loads of the next
+  // tile's first stages and what comes later, so the next SLOTS - 2 waits may leave that many more (the counter holds 63).
+  constexpr int STORES = WM * WN * 32 * 32 * (int)sizeof(OUT) / 1024;
+  constexpr int WAIT = (SLOTS - 2) * LOADS, RELAXED = WAIT + STORES < 63 ? WAIT + STORES : 63;
   bool more = true;
-  int loads = n - SLOTS, at = 0;  // stages still to load of the tile that is loaded; the slot that is read
-  for (;;) {
+  int loads = n - (SLOTS - 1), at = 0;  // stages still to load of the tile that is loaded; the slot that is read
+  int relaxed = 0;
+  for (int mine = 0;; mine ^= 1) {
     const int64_t m = m0, nn = n0;  // of the tile that is multiplied
-    bias[tid] = g.bias && nn + tid < g.N ? g.bias[nn + tid] : 0.f;  // read behind the stages' barriers
-    zero_acc(acc);
+    start_acc(acc, bias[mine] + wn * 32 * WN, lane);
     for (int c = 0; c < n; ++c) {
       if (loads == 0) {
         slot += slots;
@@ -457,6 +537,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_product_chain(ProductArgs g) {
           pa = la.p;
           pb = lb.p;
           loads = n;
+          load_bias(mine ^ 1);
         } else {  // nothing is left: the last stage's place again, which nobody reads
           pa -= step;
           pb -= step;
@@ -466,28 +547,27 @@ __global__ __launch_bounds__(kThreads, 1) void k_product_chain(ProductArgs g) {
       }
       --loads;
       const int next = at == (SLOTS - 1) * STAGE ? 0 : at + STAGE;
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        if (s == NS - 1) {
-          asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((SLOTS - 2) * LOADS) : "memory");
-          wg_barrier();
-        }
-#pragma unroll
-        for (int k = 0; k < MULS; ++k) {
-          multiply(s & 1, k);
-          if (k < FRAGS) load(lds + (s < NS - 1 ? at : next), (s + 1) % NS, (s + 1) & 1, k);
-          if (s == NS - 1 && k < LOADS) put(k, base + at);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
+      const uint32_t to = base + (at == 0 ? (SLOTS - 1) * STAGE : at - STAGE);
+      pipeline_stage<MULS, FRAGS, LOADS, NS, SLOTS>(
+          multiply, [&](int s, int f) { load(lds + (s < NS - 1 ? at : next), (s + 1) % NS, (s + 1) & 1, f); },
+          [&]() {
+            if (relaxed > 0) {
+              --relaxed;
+              asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(RELAXED) : "memory");
+            } else {
+              asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(WAIT) : "memory");
+            }
+            wg_barrier();
+          },
+          [&](int d) { put(d, to); });
       pa += step;
       pb += step;
       at = next;
     }
-    store_tile<OUT, WM, WN>(g, static_cast<OUT*>(g.out), acc, m + wm * 32 * WM, nn + wn * 32 * WN, bias + wn * 32 * WN,
-                            image + wave * kImage, lane);
+    store_tile<OUT, WM, WN>(g, static_cast<OUT*>(g.out), acc, m + wm * 32 * WM, nn + wn * 32 * WN, image + wave * kImage,
+                            lane);
     if (!more) break;
-    wg_barrier();  // this tile's bias is read
+    relaxed = m + EA <= g.M && nn + EB <= g.N ? SLOTS - 2 : 0;
   }
   vm_wait();  // no load outlives the workgroup's LDS
 }
