@@ -164,6 +164,7 @@ struct ProductArgs {
   int64_t cols;       // columns of out that are written (pad columns up to it as zero)
   const float* bias;  // [N] or NULL
   int add;            // out += C, the pad columns left alone
+  float* sums;        // [M] (+)= the sums over K of A's elements, or NULL; A across, K of at most SLOTS stages, no pieces
 };
 
 // a value that is the same in all lanes, on the scalar unit (divisions leave it)
@@ -178,9 +179,10 @@ __device__ __forceinline__ void tile_at(const ProductArgs& g, unsigned t, unsign
   nt = uniform(in / rows);
   mt = 8 * group + (in - nt * rows);
 }
-__device__ __forceinline__ bool tile_of(const ProductArgs& g, unsigned& mt, unsigned& nt, unsigned& piece) {
+__device__ __forceinline__ bool tile_of(const ProductArgs& g, unsigned block, unsigned& mt, unsigned& nt,
+                                        unsigned& piece) {
   const unsigned one = (unsigned)g.mt * (unsigned)g.nt, total = one * (unsigned)g.split, per = (total + 7) >> 3;
-  const unsigned slot = blockIdx.x >> 3, at = (blockIdx.x & 7) * per + slot;
+  const unsigned slot = block >> 3, at = (block & 7) * per + slot;
   if (slot >= per || at >= total) return false;
   piece = uniform(at / one);
   tile_at(g, at - piece * one, mt, nt);
@@ -335,24 +337,32 @@ __device__ __forceinline__ void pipeline_stage(MUL&& multiply, LOAD&& load, MEET
 // OUT: the element type of out; partial sums of a split go to out + piece * M * ld.
 // The K loop keeps SLOTS stages in LDS and the fragments of two steps (16 bytes of K a lane) in registers: a step's
 // multiplications run while the next step's fragments are read.
+// block: this workgroup's place among the product's.
+template <int WM, int WN, int KB, int SLOTS>
+struct ProductLds {
+  char stages[SLOTS * 64 * (WM + WN) * KB];
+  float bias[64 * WN];
+};
 template <typename T, int AD, int BD, typename OUT, int WM, int WN, int KB, int SLOTS>
-__global__ __launch_bounds__(kThreads, WM * WN >= 16 ? 1 : 2) void k_product(ProductArgs g) {
+__device__ __forceinline__ void product(const ProductArgs& g, unsigned block, ProductLds<WM, WN, KB, SLOTS>& shared) {
   constexpr int EA = 64 * WM, EB = 64 * WN, STAGE = (EA + EB) * KB, NS = KB / 32;
   using LA = Loader<T, AD, EA, KB>;
   using LB = Loader<T, BD, EB, KB>;
-  __shared__ __attribute__((aligned(16))) char lds[SLOTS * STAGE];
-  __shared__ __attribute__((aligned(16))) float bias[EB];
+  char* lds = shared.stages;
+  float* bias = shared.bias;
   static_assert(EB <= kThreads, "one bias a thread");
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_id();
   const int wm = wave & 1, wn = wave >> 1;
   unsigned mt, nt, piece;
-  if (!tile_of(g, mt, nt, piece)) return;
+  if (!tile_of(g, block, mt, nt, piece)) return;
   const int64_t m0 = (int64_t)mt * EA, n0 = (int64_t)nt * EB;
   const int per = (g.nstage + g.split - 1) / g.split;
   const int c0 = min((int)piece * per, g.nstage), c1 = min(c0 + per, g.nstage);
   const LA la(g.a, m0, wave, lane);
   const LB lb(g.b, n0, wave, lane);
   const uint32_t base = lds_of(lds);
+  const bool sums = AD == kAcross && g.sums && nt == 0;  // column tid % EA of the tile, every kThreads / EA-th line
+  float sum = 0.f;
   f32x16 acc[WM][WN];
   if (tid < EB) bias[tid] = g.bias && n0 + tid < g.N ? g.bias[n0 + tid] : 0.f;
   auto issue = [&](int c) {
@@ -424,6 +434,11 @@ __global__ __launch_bounds__(kThreads, WM * WN >= 16 ? 1 : 2) void k_product(Pro
     for (; c < c1; ++c) {
       const char *at = lds + (c - c0) % SLOTS * STAGE, *next = lds + (c + 1 - c0) % SLOTS * STAGE;
       if (SLOTS > 2 && issued < c1) issue(issued++);
+      if constexpr (AD == kAcross)
+        if (sums)
+#pragma unroll 8
+          for (int k = tid / EA; k < KB / (int)sizeof(T); k += kThreads / EA)
+            sum += to_f32<T>(*reinterpret_cast<const T*>(at + across_off<T, EA, NS>(k, tid % EA)));
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         if (s == NS - 1 && c + 1 < c1) {
@@ -440,9 +455,36 @@ __global__ __launch_bounds__(kThreads, WM * WN >= 16 ? 1 : 2) void k_product(Pro
       }
     }
   }
-  static_assert(SLOTS * STAGE >= 4 * kImage, "the images lie where the stages were");
+  static_assert(SLOTS * STAGE >= 4 * kImage + kThreads * 4, "the images and sums lie where the stages were");
   __syncthreads();
+  if constexpr (AD == kAcross)
+    if (sums) {
+      float* red = reinterpret_cast<float*>(lds + 4 * kImage);
+      red[tid] = sum;
+      __syncthreads();
+      if (tid < EA && m0 + tid < g.M) {
+        float t = red[tid];
+#pragma unroll
+        for (int w = 1; w < kThreads / EA; ++w) t += red[tid + w * EA];
+        g.sums[m0 + tid] = g.add ? g.sums[m0 + tid] + t : t;
+      }
+    }
   store_tile<OUT, WM, WN>(g, out_of<OUT>(g, piece), acc, m0 + wm * 32 * WM, n0 + wn * 32 * WN, lds + wave * kImage, lane);
+}
+
+template <typename T, int AD, int BD, typename OUT, int WM, int WN, int KB, int SLOTS>
+__global__ __launch_bounds__(kThreads, WM * WN >= 16 ? 1 : 2) void k_product(ProductArgs g) {
+  __shared__ __attribute__((aligned(16))) ProductLds<WM, WN, KB, SLOTS> lds;
+  product<T, AD, BD, OUT, WM, WN, KB, SLOTS>(g, blockIdx.x, lds);
+}
+
+// The states' and the weights' gradient of a small batch in one launch: `first` workgroups (a multiple of 8) for the
+// states', the rest for the weights'.  Apart, each leaves most of the chip idle and has a launch's start to itself.
+template <typename T>
+__global__ __launch_bounds__(kThreads, 2) void k_product_both(ProductArgs states, ProductArgs weights, unsigned first) {
+  __shared__ __attribute__((aligned(16))) ProductLds<1, 1, 128, 2> lds;
+  if (blockIdx.x < first) product<T, kAlong, kAcross, float, 1, 1, 128, 2>(states, blockIdx.x, lds);
+  else product<T, kAcross, kAcross, float, 1, 1, 128, 2>(weights, blockIdx.x - first, lds);
 }
 
 // The same product where both operands run along a short K (the logits: K = H) and there are many tiles: a workgroup per
@@ -696,14 +738,14 @@ constexpr int kUnits = 256;  // compute units
 // cost their sums' way through memory (4 TB/s) and a second launch (3 us).  What the rule gets (best and worst cut tried):
 // states' gradient of 33 x 300 x 20,000 bf16 13 us (335), of 257 x 300 x 20,001 fp32 49 us (4,512), weights' gradient of
 // 2,048 x 256 x 10,000 fp32 95 us (486).
-// small: the smallest tile's columns / 64 (1 or 2)
-Shape shape_of(int64_t M, int64_t N, int64_t nstage, int esize, int small, int pieces) {
+// small: the smallest tile's columns / 64 (1 or 2); smallest: that tile alone
+Shape shape_of(int64_t M, int64_t N, int64_t nstage, int esize, int small, int pieces, bool smallest = false) {
   static constexpr struct { int wm, wn; double bf16, f32; } kTiles[] = {
       {4, 4, 1.0, 1.0}, {2, 2, 1.2, 1.0}, {1, 2, 1.55, 1.03}, {1, 1, 2.2, 1.06}};
   Shape best{0, 0, 0, 0, 0};
   double least = 0;
   for (const auto& t : kTiles) {
-    if (t.wm == 1 && t.wn != small) continue;
+    if ((t.wm == 1 && t.wn != small) || (smallest && t.wm != 1)) continue;
     const int64_t mt = tiles_of(M, t.wm), nt = tiles_of(N, t.wn);
     for (int p = 1; p <= pieces && (p == 1 || nstage / p >= 4); p *= 2) {
       const double rounds = (double)((mt * nt * p + kUnits - 1) / kUnits);
@@ -718,16 +760,19 @@ Shape shape_of(int64_t M, int64_t N, int64_t nstage, int esize, int small, int p
   }
   return best;
 }
+// Rows up to which the two gradients of the backward share a launch (33 x 300 x 20,000 bf16, all three gradients: 26.6 us
+// in four launches, 19.0 us in two).
+constexpr int kBothRows = 128;
 Shape states_shape(int64_t M, int H, int V, int esize) {
-  return shape_of(std::max<int64_t>(M, 1), row_ld(H), (int64_t)row_ld(V) * esize / 128, esize, 1, kPieces);
+  return shape_of(std::max<int64_t>(M, 1), row_ld(H), (int64_t)row_ld(V) * esize / 128, esize, 1, kPieces,
+                  M <= kBothRows);
 }
+
+unsigned blocks_of(const ProductArgs& g) { return (unsigned)((g.mt * g.nt * g.split + 7) / 8 * 8); }
 
 template <typename T, int AD, int BD, typename OUT>
 void launch(ProductArgs g, const Shape& sh, hipStream_t st) {
-  g.mt = sh.mt;
-  g.nt = sh.nt;
-  g.split = sh.split;
-  const dim3 grid((unsigned)((g.mt * g.nt * g.split + 7) / 8 * 8));
+  const dim3 grid(blocks_of(g));
   if (sh.wm == 4) {
     g.nstage *= 2;
     if constexpr (AD == kAlong && BD == kAlong)
@@ -758,7 +803,8 @@ void launch_vocab_logits(int dtype, int64_t M, int H, int V, const void* s, cons
   ProfScope prof("vocab_logits", st);
   const int es = dtype == FOLD_BF16 ? 2 : 4, ldh = row_ld(H), ldv = row_ld(V);
   const Shape sh = shape_of(M, ldv, ldh * es / 128, es, 2, 1);
-  const ProductArgs g{{s, M, ldh}, {W, V, ldh}, M, V, 0, 0, ldh * es / 128, 1, z, (size_t)ldv, ldv, bias, 0};
+  const ProductArgs g{{s, M, ldh}, {W, V, ldh}, M, V, sh.mt, sh.nt, ldh * es / 128, 1, z, (size_t)ldv, ldv, bias, 0,
+                      nullptr};
   if (dtype == FOLD_F32) launch<float, kAlong, kAlong, float>(g, sh, st);
   else if (out_dtype == FOLD_F32) launch<uint16_t, kAlong, kAlong, float>(g, sh, st);
   else launch<uint16_t, kAlong, kAlong, uint16_t>(g, sh, st);
@@ -775,25 +821,38 @@ void launch_vocab_backward(int dtype, int64_t M, int H, int V, const void* s, co
                            float* dW, float* db, int add, void* ws, hipStream_t st) {
   const int es = dtype == FOLD_BF16 ? 2 : 4, ldh = row_ld(H), ldv = row_ld(V);
   const int kst = 128 / es;
-  if (ds && M > 0) {
-    ProfScope prof("vocab_dstates", st);
-    const Shape sh = states_shape(M, H, V, es);
-    const ProductArgs g{{dz, M, ldv}, {W, V, ldh}, M, H, 0, 0, ldv * es / 128, 1, sh.split > 1 ? ws : ds, (size_t)ldh,
-                        ldh, nullptr, 0};
-    if (dtype == FOLD_F32) launch<float, kAlong, kAcross, float>(g, sh, st);
-    else launch<uint16_t, kAlong, kAcross, float>(g, sh, st);
-    if (sh.split > 1)
-      join<true>(static_cast<const float*>(ws), sh.split, (size_t)M * ldh, (size_t)M * ldh, ds, 0, st);
+  const int64_t stages = (M + kst - 1) / kst;
+  // a few rows' sums come from the weights' product, whose tiles of the first column hold all of dz
+  float* sums = dW && stages <= 2 ? db : nullptr;
+  const Shape s1 = states_shape(M, H, V, es);
+  const bool both = ds && dW && M > 0 && M <= kBothRows;
+  const Shape s2 = shape_of(V, ldh, stages, es, 1, 1, both);
+  ProductArgs states{{dz, M, ldv}, {W, V, ldh}, M, H, s1.mt, s1.nt, ldv * es / 128, s1.split,
+                     s1.split > 1 ? ws : ds, (size_t)ldh, ldh, nullptr, 0, nullptr};
+  ProductArgs weights{{dz, M, ldv}, {s, M, ldh}, V, H, s2.mt, s2.nt, (int)stages, 1, dW, (size_t)ldh, ldh, nullptr, add,
+                      sums};
+  if (both) {
+    ProfScope prof("vocab_backward", st);
+    const unsigned n1 = blocks_of(states), n2 = blocks_of(weights);
+    if (dtype == FOLD_F32)
+      hipLaunchKernelGGL(k_product_both<float>, dim3(n1 + n2), dim3(kThreads), 0, st, states, weights, n1);
+    else
+      hipLaunchKernelGGL(k_product_both<uint16_t>, dim3(n1 + n2), dim3(kThreads), 0, st, states, weights, n1);
+  } else {
+    if (ds && M > 0) {
+      ProfScope prof("vocab_dstates", st);
+      if (dtype == FOLD_F32) launch<float, kAlong, kAcross, float>(states, s1, st);
+      else launch<uint16_t, kAlong, kAcross, float>(states, s1, st);
+    }
+    if (dW) {
+      ProfScope prof("vocab_dweights", st);
+      if (dtype == FOLD_F32) launch<float, kAcross, kAcross, float>(weights, s2, st);
+      else launch<uint16_t, kAcross, kAcross, float>(weights, s2, st);
+    }
   }
-  if (dW) {
-    ProfScope prof("vocab_dweights", st);
-    const ProductArgs g{{dz, M, ldv}, {s, M, ldh}, V, H, 0, 0, (int)((M + kst - 1) / kst), 1,
-                        dW, (size_t)ldh, ldh, nullptr, add};
-    const Shape sh = shape_of(V, ldh, g.nstage, es, 1, 1);
-    if (dtype == FOLD_F32) launch<float, kAcross, kAcross, float>(g, sh, st);
-    else launch<uint16_t, kAcross, kAcross, float>(g, sh, st);
-  }
-  if (db) {
+  if (ds && M > 0 && s1.split > 1)
+    join<true>(static_cast<const float*>(ws), s1.split, (size_t)M * ldh, (size_t)M * ldh, ds, 0, st);
+  if (db && !sums) {
     ProfScope prof("vocab_dbias", st);
     const int c = bias_chunks(M, V, es);
     float* part = static_cast<float*>(ws);
