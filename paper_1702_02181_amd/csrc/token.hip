@@ -600,7 +600,7 @@ __global__ __launch_bounds__(kThreads) void k_token_join(TokenArgs a) {
 
 // ---------------------------------------------------------------- distillation
 // The gradient needs the softmax's sums before its first value, so a row is read twice or held.  k_distill_row holds a
-// row of up to 144 KB in LDS and so reads and writes memory once; longer rows go through k_distill_stats (sums of
+// row of up to 144 KB (bf16: 72) in LDS and so reads and writes memory once; longer rows go through k_distill_stats (sums of
 // segments) and k_distill_grad (joins them, reads its segment again, mostly from a cache).  TWO: the loss has both terms
 // at different temperatures, so a row has two sums; otherwise one serves, at T where there are soft targets and at 1
 // where there are none.
@@ -1026,14 +1026,17 @@ int segments(int64_t rows, int V, int esize) {
   return (int)std::min<int64_t>((bytes + kSegmentBytes - 1) / kSegmentBytes, kMaxSegments);
 }
 constexpr int64_t kRowsLaunch = 1 << 22;  // rows of one launch: its threads are counted in 32 bits
+// Two passes over a row that is not held; a workgroup per 32 KB (2,048 rows of 130,001 fp32: 600 us whole, 495 in 32).
 int distill_segments(int64_t rows, int V, int esize) {
   const int64_t bytes = (int64_t)V * esize;
   return (int)std::min<int64_t>((bytes + kSegmentBytes - 1) / kSegmentBytes, kMaxSegments);
 }
 
-// Rows that a workgroup holds in LDS.
-constexpr int kHeldBytes = 144 * 1024;
-bool held(int V, int esize) { return (size_t)row_ld(V) * esize <= (size_t)kHeldBytes; }
+// Rows that a workgroup holds in LDS.  Above 72 KB a compute unit has one row at a time, and its loads and stores wait for
+// its arithmetic: bf16 rows, with twice the values a byte, are then faster in segments (8,192 x 40,000: 528 us held, 396
+// in segments; 50,000: 625 and 515; but 32,000, 64 KB: 272 and 329), fp32 rows are not (4,096 x 36,000: 300 and 335).
+constexpr int kHeldBytes = 144 * 1024, kHeldBf16 = 72 * 1024;
+bool held(int V, int esize) { return (size_t)row_ld(V) * esize <= (size_t)(esize == 2 ? kHeldBf16 : kHeldBytes); }
 
 template <typename T>
 void launch_token_rows(const TokenArgs& a, unsigned rows, hipStream_t st) {
@@ -1044,19 +1047,25 @@ void launch_token_rows(const TokenArgs& a, unsigned rows, hipStream_t st) {
 template <typename T, typename G, bool TWO>
 void launch_distill_form(const DistillArgs& a, unsigned rows, hipStream_t st) {
   if (a.nseg == 0) {
-    // the smallest size that holds the row: LDS decides how many rows a compute unit has at once
+    // the smallest size that holds the row: LDS decides how many rows a compute unit has at once (32,768 x 8,000 bf16:
+    // 352 us in 24 KB, 243 in 16; 16,384 x 9,000 fp32: 263 in 48 KB, 240 in 36; 8,192 x 20,000 bf16, 40 KB: 170 in
+    // 48 KB, 209 in 72)
     const size_t bytes = a.ld * sizeof(T);
     const dim3 grid(rows);
     if (bytes <= 8 * 1024)
       hipLaunchKernelGGL((k_distill_row<T, G, TWO, 256, 8 * 1024>), grid, dim3(256), 0, st, a);
+    else if (bytes <= 16 * 1024)
+      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 256, 16 * 1024>), grid, dim3(256), 0, st, a);
     else if (bytes <= 24 * 1024)
       hipLaunchKernelGGL((k_distill_row<T, G, TWO, 512, 24 * 1024>), grid, dim3(512), 0, st, a);
+    else if (bytes <= 36 * 1024)
+      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 256, 36 * 1024>), grid, dim3(256), 0, st, a);
     else if (bytes <= 48 * 1024)
       hipLaunchKernelGGL((k_distill_row<T, G, TWO, 512, 48 * 1024>), grid, dim3(512), 0, st, a);
     else if (bytes <= 72 * 1024)
       hipLaunchKernelGGL((k_distill_row<T, G, TWO, 512, 72 * 1024>), grid, dim3(512), 0, st, a);
-    else
-      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 1024, kHeldBytes>), grid, dim3(1024), 0, st, a);
+    else if constexpr (sizeof(T) == 4)
+      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 512, kHeldBytes>), grid, dim3(512), 0, st, a);
     return;
   }
   hipLaunchKernelGGL((k_distill_stats<T, TWO>), dim3(rows * a.nseg), dim3(kThreads), 0, st, a);

@@ -383,6 +383,18 @@ def test_distill_variants(M, V):
     _check_distill(z, "f32", "f32", None, None, None, 1.0, 1.0, 1.0)
 
 
+@pytest.mark.parametrize("kib", [8, 16, 24, 36, 48, 72, 144])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("more", [-63, 0, 1])
+def test_distill_at_the_sizes_of_lds(kib, dtype, more):
+    """Rows that just fill, just fit and just miss each amount of LDS that a row is held in."""
+    V = kib * 1024 // (2 if dtype == "bf16" else 4) + more
+    rng = np.random.default_rng(V)
+    tok, t, y = _targets(rng, 3, V, 3)
+    tok[0, 0] = y[0] = V - 1
+    _check_distill(_logits(rng, 3, V, dtype), dtype, dtype, tok, t, y, 2.0, 0.5, 0.5, inplace=True)
+
+
 @pytest.mark.parametrize("V", [3, 300, 9000, 70001])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T", [1.0, 2.0])
