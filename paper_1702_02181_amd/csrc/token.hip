@@ -600,10 +600,10 @@ __global__ __launch_bounds__(kThreads) void k_token_join(TokenArgs a) {
 
 // ---------------------------------------------------------------- distillation
 // The gradient needs the softmax's sums before its first value, so a row is read twice or held.  k_distill_row holds a
-// row of up to 144 KB (bf16: 72) in LDS and so reads and writes memory once; longer rows go through k_distill_stats (sums of
-// segments) and k_distill_grad (joins them, reads its segment again, mostly from a cache).  TWO: the loss has both terms
-// at different temperatures, so a row has two sums; otherwise one serves, at T where there are soft targets and at 1
-// where there are none.
+// row of up to 144 KB (bf16: 72) in LDS and so reads and writes memory once; longer rows go through k_distill_stats (sums
+// of segments) and k_distill_grad (joins them, reads its segment again, mostly from a cache).  TWO: the loss has both
+// terms at different temperatures, so a row has two sums; otherwise one serves, at T where there are soft targets and at
+// 1 where there are none.
 
 struct DistillArgs {
   int64_t row0;  // first row of this launch
@@ -1025,7 +1025,8 @@ int segments(int64_t rows, int V, int esize) {
   if (bytes < kWholeBytes || rows >= kRowsFull) return 1;
   return (int)std::min<int64_t>((bytes + kSegmentBytes - 1) / kSegmentBytes, kMaxSegments);
 }
-constexpr int64_t kRowsLaunch = 1 << 22;  // rows of one launch: its threads are counted in 32 bits
+// rows of one launch: its threads (at most 512 a segment) are counted in 32 bits
+int64_t rows_of_launch(int nseg) { return ((int64_t)1 << 22) / std::max(nseg, 1); }
 // Two passes over a row that is not held; a workgroup per 32 KB (2,048 rows of 130,001 fp32: 600 us whole, 495 in 32).
 int distill_segments(int64_t rows, int V, int esize) {
   const int64_t bytes = (int64_t)V * esize;
@@ -1097,8 +1098,8 @@ void launch_token(int dtype, const int* order, int64_t rows, int V, const void* 
   const int n = segments(rows, V, dtype == FOLD_BF16 ? 2 : 4);
   TokenArgs a{0, order, logits, (size_t)row_ld(V), V, J, K, n, tokens, logp, entropy, top_token, top_logp,
               static_cast<Stat*>(ws), reinterpret_cast<uint64_t*>(static_cast<Stat*>(ws) + (size_t)rows * n)};
-  for (; a.row0 < rows; a.row0 += kRowsLaunch) {
-    const unsigned r = (unsigned)std::min<int64_t>(rows - a.row0, kRowsLaunch);
+  for (const int64_t most = rows_of_launch(n); a.row0 < rows; a.row0 += most) {
+    const unsigned r = (unsigned)std::min<int64_t>(rows - a.row0, most);
     if (dtype == FOLD_BF16) launch_token_rows<uint16_t>(a, r, st);
     else launch_token_rows<float>(a, r, st);
   }
@@ -1117,8 +1118,8 @@ void launch_distill(int dtype, const int* order, int64_t rows, int V, const void
   DistillArgs a{0, order, logits, (size_t)row_ld(V), V, k, n, teacher_token, teacher_logit, labels, T, soft, hard,
                 scale, kL2E / (uses_soft ? T : 1.f), row_loss, grad, static_cast<Stat*>(ws),
                 reinterpret_cast<float*>(static_cast<Stat*>(ws) + (size_t)rows * n)};
-  for (; a.row0 < rows; a.row0 += kRowsLaunch) {
-    const unsigned r = (unsigned)std::min<int64_t>(rows - a.row0, kRowsLaunch);
+  for (const int64_t most = rows_of_launch(n); a.row0 < rows; a.row0 += most) {
+    const unsigned r = (unsigned)std::min<int64_t>(rows - a.row0, most);
     if (dtype == FOLD_BF16) launch_distill_rows<uint16_t, uint16_t>(a, two, r, st);
     else if (grad_dtype == FOLD_BF16) launch_distill_rows<float, uint16_t>(a, two, r, st);
     else launch_distill_rows<float, float>(a, two, r, st);

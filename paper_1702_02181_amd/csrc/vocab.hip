@@ -3,7 +3,7 @@
 //     states   ds = dz W          K = V: dz runs along K, W across it
 //     weights  dW (+)= dz^T s     K = M: both operands run across K
 //     bias     db (+)= sum_m dz
-// One kernel, k_product, computes C[m][n] = sum_k A(m, k) B(n, k) for operands of either direction.
+// One loop, product(), computes C[m][n] = sum_k A(m, k) B(n, k) for operands of either direction.
 
 #include <hip/hip_runtime.h>
 
@@ -71,8 +71,9 @@ __device__ __forceinline__ uint32_t lds_of(const P* p) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const FOLD_LDS_AS char*)reinterpret_cast<const char*>(p));
 }
 
-// One wave's loads of an operand's stages: NI instructions of 1 KB a stage, instruction t of the workgroup (NI a wave).  e0: the tile's first element.  Elements past
-// the operand's last one are read from a clamped place: they reach results that are not stored.
+// One wave's loads of an operand's stages: NI instructions of 1 KB a stage, instruction t of the workgroup (NI a wave).
+// e0: the tile's first element.  Elements past the operand's last one are read from a clamped place: they reach results
+// that are not stored.
 template <typename T, int DIR, int ELEMS, int KB>
 struct Loader {
   static constexpr int NI = ELEMS * KB / 4096;
@@ -164,7 +165,7 @@ struct ProductArgs {
   int64_t cols;       // columns of out that are written (pad columns up to it as zero)
   const float* bias;  // [N] or NULL
   int add;            // out += C, the pad columns left alone
-  float* sums;        // [M] (+)= the sums over K of A's elements, or NULL; A across, K of at most SLOTS stages, no pieces
+  float* sums;        // [M] (+)= the sums over K of A's elements, or NULL; A across, all of K loaded before the loop, no pieces
 };
 
 // a value that is the same in all lanes, on the scalar unit (divisions leave it)
@@ -760,12 +761,16 @@ Shape shape_of(int64_t M, int64_t N, int64_t nstage, int esize, int small, int p
   }
   return best;
 }
-// Rows up to which the two gradients of the backward share a launch (33 x 300 x 20,000 bf16, all three gradients: 26.6 us
-// in four launches, 19.0 us in two).
-constexpr int kBothRows = 128;
+// Whether the two gradients of the backward share a launch, in the smallest tiles: batches of one tile row, and of two
+// unless W is so large that reading it twice costs more than a launch (all three gradients, bf16: 33 x 300 x 20,000 26.6
+// us in four launches, 19.0 in two; 100 x 1,024 x 32,000 48 us together, 26 + 37 apart; 100 x 2,048 x 40,000 136 apart;
+// 100 x 4,096 x 32,000 276 and 212; in fp32, where the matrix cores bound it, 100 x 4,096 x 32,000 589 and 659).
+bool together(int64_t M, int H, int V, int esize) {
+  return M <= 64 || (M <= 128 && (esize == 4 || (int64_t)V * row_ld(H) <= (int64_t)1 << 25));
+}
 Shape states_shape(int64_t M, int H, int V, int esize) {
   return shape_of(std::max<int64_t>(M, 1), row_ld(H), (int64_t)row_ld(V) * esize / 128, esize, 1, kPieces,
-                  M <= kBothRows);
+                  together(M, H, V, esize));
 }
 
 unsigned blocks_of(const ProductArgs& g) { return (unsigned)((g.mt * g.nt * g.split + 7) / 8 * 8); }
@@ -822,11 +827,12 @@ void launch_vocab_backward(int dtype, int64_t M, int H, int V, const void* s, co
   const int es = dtype == FOLD_BF16 ? 2 : 4, ldh = row_ld(H), ldv = row_ld(V);
   const int kst = 128 / es;
   const int64_t stages = (M + kst - 1) / kst;
-  // a few rows' sums come from the weights' product, whose tiles of the first column hold all of dz
-  float* sums = dW && stages <= 2 ? db : nullptr;
   const Shape s1 = states_shape(M, H, V, es);
-  const bool both = ds && dW && M > 0 && M <= kBothRows;
+  const bool both = ds && dW && M > 0 && together(M, H, V, es);
   const Shape s2 = shape_of(V, ldh, stages, es, 1, 1, both);
+  // a few rows' sums come from the weights' product, whose tiles of the first column hold all of dz: where every stage is
+  // loaded before its loop (two of 128 bytes, or three of 64, of which a whole one is two)
+  float* sums = dW && stages <= (s2.wm == 4 ? 1 : 2) ? db : nullptr;
   ProductArgs states{{dz, M, ldv}, {W, V, ldh}, M, H, s1.mt, s1.nt, ldv * es / 128, s1.split,
                      s1.split > 1 ? ws : ds, (size_t)ldh, ldh, nullptr, 0, nullptr};
   ProductArgs weights{{dz, M, ldv}, {s, M, ldh}, V, H, s2.mt, s2.nt, (int)stages, 1, dW, (size_t)ldh, ldh, nullptr, add,

@@ -146,6 +146,19 @@ def test_backward(M, H, V, dtype):
     _within(_np(db1), b0 + want[2], bound[2] + U * np.abs(b0 + want[2]), "db +=")
 
 
+@pytest.mark.parametrize("M,dtype", [(1, "bf16"), (33, "bf16"), (64, "bf16"), (65, "bf16"), (128, "bf16"), (129, "bf16"),
+                                     (31, "f32"), (64, "f32"), (65, "f32")])
+def test_weight_gradients_of_few_rows(M, dtype):
+    """The weights' gradient of a wide matrix without the states', where the bias sums come from the largest tiles."""
+    H, V = 1000, 16300
+    s, W, _, dz = _product_case(M, H, V, dtype, M)
+    head = F.VocabHead(_dev(W, dtype), None, H)
+    a = [x.astype(np.float64) for x in (s, dz)]
+    _, dW, db = head.backward(_dev(s, dtype), _dev(dz, dtype), None, True, True)
+    _within(_np(db), a[1].sum(0), (M + 72) * U * np.abs(a[1]).sum(0), "db")
+    _within(_np(dW)[:, :H], a[1].T @ a[0], (M + 72) * U * (np.abs(a[1]).T @ np.abs(a[0])), "dW")
+
+
 def test_backward_of_no_rows():
     import torch
     head = F.VocabHead(_dev(np.ones((100, 70))), None, 70)
@@ -475,6 +488,8 @@ def _chain(head, s, y, tok, t, vocab, stream=None):
 def test_streams_and_graphs(M, H, V, dtype):
     """The chain on a stream of its own, and captured: every replay, with eager work between, equals the eager results
     of the inputs it finds."""
+    import gc
+
     import torch
     s, W, b, _ = _product_case(M, H, V, dtype, 5)
     rng = np.random.default_rng(9)
@@ -487,6 +502,7 @@ def test_streams_and_graphs(M, H, V, dtype):
     other = _chain(head, sd, *a, V, stream=side)
     side.synchronize()
     assert all(torch.equal(x, z) for x, z in zip(eager, other))
+    gc.collect()  # device memory of other tests' garbage, freed by a collection during the recording, would end it
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         out = _chain(head, sd, *a, V)
