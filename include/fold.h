@@ -530,10 +530,10 @@ int32_t fold_adam_step(int64_t n, float* param, uint16_t* param_bf16, const floa
  *
  * All of these calls enqueue on `stream`, never synchronise, never allocate
  * and can be captured.  Matrices and workspaces are 16-byte aligned
- * (FOLD_E_INVALID otherwise); rows is at most 2^31 - 1, vocab at most 2^30 (2^21 for the
- * products).
- * rows = 0 is allowed (buffers that would be read may be NULL).  Workspaces
- * hold nothing between calls; calls that overlap need one each.
+ * (FOLD_E_INVALID otherwise); rows is at most 2^31 - 1, vocab at most 2^30
+ * (2^21 for the products).  rows = 0 is allowed (buffers that would
+ * be read may be NULL).  Workspaces hold nothing between calls; calls that
+ * overlap need one each.
  *
  * fold_vocab_logits: z = states W^T + bias.
  *   dtype         FOLD_F32 or FOLD_BF16: states and W (products of bf16 values
@@ -556,7 +556,8 @@ int32_t fold_adam_step(int64_t n, float* param, uint16_t* param_bf16, const floa
  *   ws  device workspace of >= fold_vocab_workspace_size bytes (may be NULL
  *       where that is 0)
  * FOLD_E_INVALID for sizes out of range, an unknown dtype or flag, NULL or
- * misaligned buffers; FOLD_E_MISMATCH for a workspace that is too small. */
+ * misaligned buffers, an output that overlaps another buffer of the call;
+ * FOLD_E_MISMATCH for a workspace that is too small. */
 #define FOLD_VOCAB_ACCUMULATE 1
 
 int32_t fold_vocab_logits(int32_t dtype, int64_t rows, int32_t hidden, int32_t vocab, const void* states,

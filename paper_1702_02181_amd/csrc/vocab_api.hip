@@ -33,12 +33,22 @@ int32_t guarded(F&& body) {
 
 constexpr int kMaxVocab = 1 << 30;      // columns and their keys are counted in 31 bits
 constexpr int kMaxHeadVocab = 1 << 21;  // a tile of a product is addressed by 32-bit offsets (256 lines of the logits)
-constexpr int64_t kMaxTiles = 1 << 24;  // workgroups of one launch of 256 threads each
+constexpr int64_t kMaxTiles = (1 << 24) - 8;  // workgroups of one launch, rounded up to 8: its threads fit 32 bits
 
 bool known_type(int dtype) { return dtype == FOLD_F32 || dtype == FOLD_BF16; }
 bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 size_t bytes_of(int dtype, int64_t rows, int width) {
   return (size_t)rows * (size_t)row_ld(width) * (dtype == FOLD_BF16 ? 2 : 4);
+}
+
+// whether an output shares memory with another buffer (NULL: no)
+struct Span {
+  const void* p;
+  size_t bytes;
+};
+bool overlap(const Span& a, const Span& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  return x && y && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
 }
 
 int check_rows(const std::string& who, int dtype, int64_t rows, int vocab) {
@@ -101,6 +111,10 @@ int32_t fold_vocab_logits(int32_t dtype, int64_t rows, int32_t hidden, int32_t v
     if (!states || !W || !logits) return vfail(FOLD_E_INVALID, who + ": NULL buffer");
     if (misaligned(states) || misaligned(W) || misaligned(logits))
       return vfail(FOLD_E_INVALID, who + ": states, W and logits must be 16-byte aligned");
+    const Span out{logits, bytes_of(logits_dtype, rows, vocab)};
+    if (overlap(out, {states, bytes_of(dtype, rows, hidden)}) || overlap(out, {W, bytes_of(dtype, vocab, hidden)}) ||
+        overlap(out, {bias, (size_t)vocab * sizeof(float)}))
+      return vfail(FOLD_E_INVALID, who + ": logits overlaps an input");
     launch_vocab_logits(dtype, rows, hidden, vocab, states, W, bias, logits_dtype, logits, st);
     FOLD_HIP_CHECK(hipGetLastError());
     return FOLD_OK;
@@ -135,6 +149,13 @@ int32_t fold_vocab_backward(int32_t dtype, int64_t rows, int32_t hidden, int32_t
     const size_t need = vocab_backward_bytes(dtype, rows, hidden, vocab);
     if (need > 0 && (!ws || ws_bytes < need))
       return vfail(FOLD_E_MISMATCH, who + ": workspace smaller than fold_vocab_workspace_size");
+    const Span all[] = {{d_states, bytes_of(FOLD_F32, rows, hidden)}, {dW, bytes_of(FOLD_F32, vocab, hidden)},
+                        {dbias, (size_t)vocab * sizeof(float)},       {ws, need},
+                        {states, bytes_of(dtype, rows, hidden)},      {W, bytes_of(dtype, vocab, hidden)},
+                        {dlogits, bytes_of(dtype, rows, vocab)}};
+    for (int i = 0; i < 4; ++i)
+      for (int j = i + 1; j < 7; ++j)
+        if (overlap(all[i], all[j])) return vfail(FOLD_E_INVALID, who + ": an output overlaps another buffer");
     launch_vocab_backward(dtype, rows, hidden, vocab, states, W, dlogits, d_states, dW, dbias,
                           flags & FOLD_VOCAB_ACCUMULATE, ws, st);
     FOLD_HIP_CHECK(hipGetLastError());
@@ -178,8 +199,7 @@ int32_t fold_loss_distill(const fold_sched* sched, int32_t dtype, int64_t rows, 
     if (misaligned(logits) || misaligned(dlogits) || misaligned(ws))
       return vfail(FOLD_E_INVALID, who + ": logits, dlogits and the workspace must be 16-byte aligned");
     if (dlogits && !(dlogits == logits && grad_dtype == dtype)) {
-      const char *z = static_cast<const char*>(logits), *d = static_cast<const char*>(dlogits);
-      if (d < z + bytes_of(dtype, rows, vocab) && z < d + bytes_of(grad_dtype, rows, vocab))
+      if (overlap({logits, bytes_of(dtype, rows, vocab)}, {dlogits, bytes_of(grad_dtype, rows, vocab)}))
         return vfail(FOLD_E_INVALID, who + ": dlogits overlaps logits (it may be the same buffer for the same type)");
     }
     const size_t need = distill_workspace_bytes(dtype, rows, vocab, num_teacher);

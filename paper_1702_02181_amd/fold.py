@@ -759,7 +759,10 @@ _HERE_STREAM = contextlib.nullcontext()
 def _on(stream):
     """New tensors belong to the stream that the call runs on."""
     import torch
-    return _HERE_STREAM if stream is None else torch.cuda.stream(stream)
+    if stream is None:
+        return _HERE_STREAM
+    _here("stream", stream)
+    return torch.cuda.stream(stream)
 
 
 class _Raw:
@@ -799,6 +802,7 @@ class VocabHead:
         """[rows, fold_row_ld(vocab)] logits of `states` [rows, fold_row_ld(hidden)], of dtype (the head's)."""
         import torch
         _matrix("states", states, self.hidden, self.dtype)
+        _here("weight", self.weight)
         rows = states.shape[0]
         with _on(stream):
             if out is None:
@@ -814,6 +818,7 @@ class VocabHead:
         tensor to write, or None to leave it out.  accumulate: dW and dbias are added to the tensors given."""
         import torch
         _matrix("states", states, self.hidden, self.dtype)
+        _here("weight", self.weight)
         rows = states.shape[0]
         _matrix("dlogits", dlogits, self.vocab, self.dtype, rows)
         if accumulate and (dW is True or dbias is True):

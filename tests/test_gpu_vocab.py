@@ -555,6 +555,24 @@ def test_wrappers_refuse():
 
 # ---- with the batched path ------------------------------------------------------------------------------------------
 
+def test_wrappers_refuse_another_device():
+    """A stream or a head of another device than the current one."""
+    import types
+
+    import torch
+    head = F.VocabHead(torch.zeros((10, 64), device="cuda"), None, 33)
+    s = torch.zeros((4, 64), device="cuda")
+    other = types.SimpleNamespace(device=torch.device("cuda", torch.cuda.current_device() + 1))
+    for call in (head.logits, lambda x, stream: head.backward(x, x, stream=stream),
+                 lambda x, stream: F.distill_loss(x, 33, stream=stream),
+                 lambda x, stream: F.token_logprobs(x, 33, stream=stream)):
+        with pytest.raises(ValueError, match="stream is on cuda"):
+            call(s, stream=other)
+    head.weight = other
+    with pytest.raises(ValueError, match="weight is on cuda"):
+        head.logits(s)
+
+
 @pytest.mark.parametrize("dtype,tied", [("f32", False), ("bf16", False), ("bf16", True)])
 def test_training_step_with_a_vocabulary(dtype, tied):
     """runner.VocabStep: forward, head, distillation on every node, both backward passes, against the oracle's chain."""

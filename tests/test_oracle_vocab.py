@@ -163,6 +163,31 @@ def test_refusals_of_the_products(F):
     back(rows=0, s=None, W=None, dz=None, ds=b, dW=None, db=None)
 
 
+def test_refusals_of_outputs_that_overlap(F):
+    """4 rows, 64 states, a vocabulary of 128, fp32: states and d_states 1 KB, W and dW 32 KB, logits 2 KB, the bias 512
+    bytes, each just behind the one before."""
+    at, bufs = 1 << 20, {}
+    for name, size in dict(s=1024, W=32768, dz=2048, ds=1024, dW=32768, db=512).items():
+        bufs[name] = _Buf(at)
+        at += size
+
+    def logits(z, bias=None):
+        F.fold_vocab_logits(0, 4, 64, 128, bufs["s"], bufs["W"], bias, 0, z, NULL_STREAM)
+
+    for z in (bufs["s"], bufs["W"], _Buf(bufs["s"].at - 2032), _Buf(bufs["dz"].at - 16)):
+        _refused(F, F.FOLD_E_INVALID, logits, z)
+    _refused(F, F.FOLD_E_INVALID, logits, bufs["dz"], bufs["dz"])
+
+    def back(**kw):
+        b = dict(bufs, **kw)
+        n = F.fold_vocab_workspace_size(0, 4, 64, 128)
+        F.fold_vocab_backward(0, 4, 64, 128, b["s"], b["W"], b["dz"], b["ds"], b["dW"], b["db"], 0,
+                              _Buf(1 << 30) if n else None, n, NULL_STREAM)
+
+    for out, other in (("ds", "s"), ("ds", "dz"), ("dW", "W"), ("db", "dW"), ("dW", "ds"), ("db", "dz")):
+        _refused(F, F.FOLD_E_INVALID, back, **{out: bufs[other]})
+
+
 def test_refusals_of_the_distillation_loss(F):
     b, odd = _Buf(), _Buf(4097)
     big = _Buf(1 << 40)
