@@ -601,9 +601,19 @@ __global__ __launch_bounds__(kThreads) void k_token_join(TokenArgs a) {
 // ---------------------------------------------------------------- distillation
 // The gradient needs the softmax's sums before its first value, so a row is read twice or held.  k_distill_row holds a
 // row of up to 144 KB (bf16: 72) in LDS and so reads and writes memory once; longer rows go through k_distill_stats (sums
-// of segments) and k_distill_grad (joins them, reads its segment again, mostly from a cache).  TWO: the loss has both
-// terms at different temperatures, so a row has two sums; otherwise one serves, at T where there are soft targets and at
-// 1 where there are none.
+// of segments) and k_distill_grad (joins them, reads its segment again, mostly from a cache).  
+// A row has two sums if the loss has both terms and T != 1; otherwise one serves, at T where there are soft targets and at
+// 1 where there are none.  The exponentials bound a held row's passes (two of 16 cycles a wave in each of two passes), so
+// for T = 2 and 4, the usual ones, those at temperature 1 are the others' squares: c, the references and x are then exact
+// binary fractions of those at 1, so 2^(x T) = (2^x)^T up to the product's rounding (8,192 x 32,000 bf16: 289 us with two
+// exponentials, 263 us so).
+// FORM: the sums a row has and how the second comes about.
+enum { kOneSum = -1, kTwoSums = 0, kSquare = 1, kFourth = 2 };
+// 2^x at temperature 1 from 2^x at T, which is 2 ^ FORM
+template <int FORM>
+__device__ __forceinline__ float power(float y) {
+  return FORM == kSquare ? y * y : (y * y) * (y * y);
+}
 
 struct DistillArgs {
   int64_t row0;  // first row of this launch
@@ -618,7 +628,7 @@ struct DistillArgs {
   float c;      // log2 e / the temperature of the soft term (of the only one, if there is one)
   float* row_loss;
   void* grad;   // [rows][ld] or NULL
-  Stat* part;   // [rows][nseg]: s the sum at c, t the sum at temperature 1 (TWO)
+  Stat* part;   // [rows][nseg]: s the sum at c, t the sum at temperature 1 (two sums)
   float* at;    // [rows][k + 1]: the logits of the teacher's tokens and of the label
 };
 
@@ -649,9 +659,10 @@ __device__ __forceinline__ Target target_of(const DistillArgs& a, size_t q) {
 }
 
 // What a row's gradient and loss are made of, from its maximum and sums.
-template <bool TWO>
+template <int FORM>
 struct RowGrad {
-  float m, mc, m1, s, s1;  // the maximum; the references and sums at c and (TWO) at temperature 1
+  static constexpr bool TWO = FORM != kOneSum;
+  float m, mc, m1, s, s1;  // the maximum; the references and sums at c and (two sums) at temperature 1
   float c, invT;
   float wa, wb, ga, gb;    // weights of the soft and hard term, and of 2^x in the gradient
   bool far, bad, empty;
@@ -670,8 +681,11 @@ struct RowGrad {
   }
   // the gradient of a logit that is no target: 0 for -inf, in rows that are not bad
   __device__ __forceinline__ float dense(float z) const {
-    const float d = ga * exp2_(__builtin_fmaf(z, c, -mc));
-    return TWO ? __builtin_fmaf(gb, exp2_(__builtin_fmaf(z, kL2E, -m1)), d) : d;
+    const float y = exp2_(__builtin_fmaf(z, c, -mc));
+    if constexpr (FORM == kOneSum) return ga * y;
+    if constexpr (FORM == kTwoSums) return __builtin_fmaf(gb, exp2_(__builtin_fmaf(z, kL2E, -m1)), ga * y);
+    if constexpr (FORM == kSquare) return y * __builtin_fmaf(gb, y, ga);
+    return __builtin_fmaf(gb, power<FORM>(y), ga * y);
   }
   // the same in a row that is far or bad
   __device__ __forceinline__ float odd(float z) const { return bad ? ga : z == m ? ga + gb : 0.f; }
@@ -698,14 +712,14 @@ struct RowGrad {
 };
 
 // this thread's share of the soft term: q (log q - log p), q = e / es with e = exp(dt)
-template <bool TWO>
-__device__ __forceinline__ float soft_loss(const DistillArgs& a, const RowGrad<TWO>& r, const Target& t, float q,
+template <int FORM>
+__device__ __forceinline__ float soft_loss(const DistillArgs& a, const RowGrad<FORM>& r, const Target& t, float q,
                                            float dt, float es, float z) {
   return t.have && q != 0.f && a.soft != 0.f ? q * (dt - logf(es) - r.logp_soft(z)) : 0.f;
 }
 // the row's loss from the sum of the shares
-template <bool TWO>
-__device__ __forceinline__ float row_loss(const DistillArgs& a, const RowGrad<TWO>& r, const Target& t, float soft,
+template <int FORM>
+__device__ __forceinline__ float row_loss(const DistillArgs& a, const RowGrad<FORM>& r, const Target& t, float soft,
                                           float zy) {
   float loss = t.soft && a.soft != 0.f ? a.soft * a.T * a.T * soft : 0.f;
   if (t.y >= 0 && a.hard != 0.f) loss -= a.hard * r.logp_hard(zy);
@@ -714,8 +728,8 @@ __device__ __forceinline__ float row_loss(const DistillArgs& a, const RowGrad<TW
 
 // The targets' columns inside [lo, hi), written whole after everything else: the first entry of a token takes the mass of
 // all its entries.  tok, mass: every entry's token (-1: does not count) and q.
-template <typename G, bool TWO>
-__device__ __forceinline__ void write_targets(const DistillArgs& a, const RowGrad<TWO>& r, const Target& t,
+template <typename G, int FORM>
+__device__ __forceinline__ void write_targets(const DistillArgs& a, const RowGrad<FORM>& r, const Target& t,
                                               const int* tok, const float* mass, float zj, float zy, G* out, int lo,
                                               int hi) {
   if (t.have && t.tok >= lo && t.tok < hi) {
@@ -757,9 +771,10 @@ __device__ __forceinline__ void store_grad(G* p, const float (&v)[N]) {
 
 // A whole row by one workgroup, in LDS: loaded there directly, its missing columns set to -inf (probability 0, gradient 0),
 // then read three times (maximum, sums, gradient).  LDS holds BYTES >= the row rounded up to a vector a thread.
-template <typename T, typename G, bool TWO, int TH, int BYTES>
+template <typename T, typename G, int FORM, int TH, int BYTES>
 __global__ __launch_bounds__(TH) void k_distill_row(DistillArgs a) {
   constexpr int VEC = 16 / (int)sizeof(T), NW = TH / 64;
+  constexpr bool TWO = FORM != kOneSum;
   static_assert(BYTES % (TH * 16) == 0, "the row rounded up to a vector a thread fits");
   __shared__ __attribute__((aligned(16))) char lds[BYTES];
   __shared__ float red[6][NW];
@@ -813,7 +828,7 @@ __global__ __launch_bounds__(TH) void k_distill_row(DistillArgs a) {
   put(red[0], wave_max(m));
   put(red[1], wave_max(t.have ? t.t : neg_inf()));
   __syncthreads();
-  RowGrad<TWO> r;
+  RowGrad<FORM> r;
   r.m = all(red[0], true);
   r.mc = ref_of(r.m, a.c);
   r.m1 = ref_of(r.m, kL2E);
@@ -828,8 +843,10 @@ __global__ __launch_bounds__(TH) void k_distill_row(DistillArgs a) {
     pass([&](int, float (&v)[VEC]) __attribute__((always_inline)) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        s += exp2_(__builtin_fmaf(v[e], a.c, -r.mc));
-        if constexpr (TWO) s1 += exp2_(__builtin_fmaf(v[e], kL2E, -r.m1));
+        const float y = exp2_(__builtin_fmaf(v[e], a.c, -r.mc));
+        s += y;
+        if constexpr (FORM == kTwoSums) s1 += exp2_(__builtin_fmaf(v[e], kL2E, -r.m1));
+        else if constexpr (TWO) s1 += power<FORM>(y);
       }
     });
   }
@@ -870,10 +887,11 @@ __global__ __launch_bounds__(TH) void k_distill_row(DistillArgs a) {
 }
 
 // One segment's maximum and its sums
-template <typename T, bool TWO>
+template <typename T, int FORM>
 __global__ __launch_bounds__(kThreads) void k_distill_stats(DistillArgs a) {
   __shared__ float red[kWaves];
   constexpr int VEC = 16 / (int)sizeof(T);
+  constexpr bool TWO = FORM != kOneSum;
   const int64_t p = a.row0 + blockIdx.x / a.nseg;
   const int g = (int)(blockIdx.x % a.nseg);
   const size_t q = a.order ? (size_t)a.order[p] : (size_t)p;
@@ -902,8 +920,10 @@ __global__ __launch_bounds__(kThreads) void k_distill_stats(DistillArgs a) {
   auto add = [&](const float (&v)[VEC]) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      s += exp2_(__builtin_fmaf(v[e], a.c, -rc));
-      if constexpr (TWO) s1 += exp2_(__builtin_fmaf(v[e], kL2E, -r1));
+      const float y = exp2_(__builtin_fmaf(v[e], a.c, -rc));
+      s += y;
+      if constexpr (FORM == kTwoSums) s1 += exp2_(__builtin_fmaf(v[e], kL2E, -r1));
+      else if constexpr (TWO) s1 += power<FORM>(y);
     }
   };
   seg.groups(
@@ -935,7 +955,7 @@ __global__ __launch_bounds__(kThreads) void k_distill_stats(DistillArgs a) {
 }
 
 // The loss of a row and one segment of its gradient
-template <typename T, typename G, bool TWO>
+template <typename T, typename G, int FORM>
 __global__ __launch_bounds__(kThreads) void k_distill_grad(DistillArgs a) {
   __shared__ float red[kWaves];
   __shared__ int tok[kMaxTeacherTokens];
@@ -960,7 +980,7 @@ __global__ __launch_bounds__(kThreads) void k_distill_grad(DistillArgs a) {
   const int lane = threadIdx.x & 63;
   Stat st{neg_inf(), 0.f, 0.f, 0.f};
   if (lane < a.nseg) st = a.part[(size_t)p * a.nseg + lane];
-  RowGrad<TWO> r;
+  RowGrad<FORM> r;
   r.m = wave_max(st.m);
   r.mc = ref_of(r.m, a.c);
   r.m1 = ref_of(r.m, kL2E);
@@ -1045,7 +1065,7 @@ void launch_token_rows(const TokenArgs& a, unsigned rows, hipStream_t st) {
   if (a.nseg > 1) hipLaunchKernelGGL(k_token_join<T>, dim3(rows), dim3(kThreads), 0, st, a);
 }
 
-template <typename T, typename G, bool TWO>
+template <typename T, typename G, int FORM>
 void launch_distill_form(const DistillArgs& a, unsigned rows, hipStream_t st) {
   if (a.nseg == 0) {
     // the smallest size that holds the row: LDS decides how many rows a compute unit has at once (32,768 x 8,000 bf16:
@@ -1054,28 +1074,30 @@ void launch_distill_form(const DistillArgs& a, unsigned rows, hipStream_t st) {
     const size_t bytes = a.ld * sizeof(T);
     const dim3 grid(rows);
     if (bytes <= 8 * 1024)
-      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 256, 8 * 1024>), grid, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 256, 8 * 1024>), grid, dim3(256), 0, st, a);
     else if (bytes <= 16 * 1024)
-      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 256, 16 * 1024>), grid, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 256, 16 * 1024>), grid, dim3(256), 0, st, a);
     else if (bytes <= 24 * 1024)
-      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 512, 24 * 1024>), grid, dim3(512), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 512, 24 * 1024>), grid, dim3(512), 0, st, a);
     else if (bytes <= 36 * 1024)
-      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 256, 36 * 1024>), grid, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 256, 36 * 1024>), grid, dim3(256), 0, st, a);
     else if (bytes <= 48 * 1024)
-      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 512, 48 * 1024>), grid, dim3(512), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 512, 48 * 1024>), grid, dim3(512), 0, st, a);
     else if (bytes <= 72 * 1024)
-      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 512, 72 * 1024>), grid, dim3(512), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 512, 72 * 1024>), grid, dim3(512), 0, st, a);
     else if constexpr (sizeof(T) == 4)
-      hipLaunchKernelGGL((k_distill_row<T, G, TWO, 512, kHeldBytes>), grid, dim3(512), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 512, kHeldBytes>), grid, dim3(512), 0, st, a);
     return;
   }
-  hipLaunchKernelGGL((k_distill_stats<T, TWO>), dim3(rows * a.nseg), dim3(kThreads), 0, st, a);
-  hipLaunchKernelGGL((k_distill_grad<T, G, TWO>), dim3(rows * a.nseg), dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL((k_distill_stats<T, FORM>), dim3(rows * a.nseg), dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL((k_distill_grad<T, G, FORM>), dim3(rows * a.nseg), dim3(kThreads), 0, st, a);
 }
 template <typename T, typename G>
 void launch_distill_rows(const DistillArgs& a, bool two, unsigned rows, hipStream_t st) {
-  if (two) launch_distill_form<T, G, true>(a, rows, st);
-  else launch_distill_form<T, G, false>(a, rows, st);
+  if (!two) launch_distill_form<T, G, kOneSum>(a, rows, st);
+  else if (a.T == 2.f) launch_distill_form<T, G, kSquare>(a, rows, st);
+  else if (a.T == 4.f) launch_distill_form<T, G, kFourth>(a, rows, st);
+  else launch_distill_form<T, G, kTwoSums>(a, rows, st);
 }
 
 }  // namespace

@@ -410,7 +410,7 @@ def test_distill_at_the_sizes_of_lds(kib, dtype, more):
 
 @pytest.mark.parametrize("V", [3, 300, 9000, 70001])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("T", [1.0, 2.0])
+@pytest.mark.parametrize("T", [1.0, 2.0, 3.0, 4.0])
 def test_distill_of_hard_rows(V, dtype, T):
     rng = np.random.default_rng(V)
     z = _hard_rows(dtype, V, rng)
