@@ -597,7 +597,7 @@ int32_t fold_vocab_backward(int32_t dtype, int64_t rows, int32_t hidden, int32_t
  *               zero); may be `logits` itself if the types are equal, must not
  *               overlap it otherwise; NULL: the losses alone
  *   ws          device workspace of >= fold_distill_workspace_size bytes (may be
- *               NULL where that is 0: rows that fit LDS)
+ *               NULL where that is 0: rows that a workgroup holds)
  * Sums are fp32.  Logits of -inf (masked) have probability 0; a target there
  * has loss +inf.  A row with a target whose logits are all -inf has loss +inf
  * and gradient 0; one with NaN or +inf has loss and gradient NaN. */

@@ -18,7 +18,6 @@
 
 #include "common.h"
 #include "internal.h"
-#include "dma.h"
 #include "mfma.h"
 
 namespace fold {
@@ -600,13 +599,15 @@ __global__ __launch_bounds__(kThreads) void k_token_join(TokenArgs a) {
 
 // ---------------------------------------------------------------- distillation
 // The gradient needs the softmax's sums before its first value, so a row is read twice or held.  k_distill_row holds a
-// row of up to 144 KB (bf16: 72) in LDS and so reads and writes memory once; longer rows go through k_distill_stats (sums
-// of segments) and k_distill_grad (joins them, reads its segment again, mostly from a cache).  
+// row in its workgroup's registers and so reads and writes memory once (8,192 x 32,000 bf16: 214 us, a copy of the logits
+// 198; held in LDS, where two such rows fit a compute unit and every pass reads it, 263); longer rows, and long ones that
+// are few, go through k_distill_stats (sums of segments) and k_distill_grad (joins them, reads its segment again, mostly
+// from a cache).
 // A row has two sums if the loss has both terms and T != 1; otherwise one serves, at T where there are soft targets and at
-// 1 where there are none.  The exponentials bound a held row's passes (two of 16 cycles a wave in each of two passes), so
-// for T = 2 and 4, the usual ones, those at temperature 1 are the others' squares: c, the references and x are then exact
-// binary fractions of those at 1, so 2^(x T) = (2^x)^T up to the product's rounding (8,192 x 32,000 bf16: 289 us with two
-// exponentials, 263 us so).
+// 1 where there are none.  The exponentials (16 cycles a wave, two a logit in each of two passes) cost more than anything
+// else there, so for T = 2 and 4, the usual ones, those at temperature 1 are powers of the others: c, the references and
+// x are then exact binary fractions of those at 1, so 2^(x T) = (2^x)^T up to the product's rounding (8,192 x 32,000 bf16,
+// held in LDS: 289 us with two exponentials, 263 so).
 // FORM: the sums a row has and how the second comes about.
 enum { kOneSum = -1, kTwoSums = 0, kSquare = 1, kFourth = 2 };
 // 2^x at temperature 1 from 2^x at T, which is 2 ^ FORM
@@ -769,24 +770,33 @@ __device__ __forceinline__ void store_grad(G* p, const float (&v)[N]) {
   }
 }
 
-// A whole row by one workgroup, in LDS: loaded there directly, its missing columns set to -inf (probability 0, gradient 0),
-// then read three times (maximum, sums, gradient).  LDS holds BYTES >= the row rounded up to a vector a thread.
-template <typename T, typename G, int FORM, int TH, int BYTES>
-__global__ __launch_bounds__(TH) void k_distill_row(DistillArgs a) {
+// a word of logits with those after its first `have` set to -inf
+template <typename T>
+__device__ __forceinline__ uint32_t first_of(uint32_t w, int have) {
+  if constexpr (sizeof(T) == 4) return have > 0 ? w : 0xff800000u;
+  return have > 1 ? w : have > 0 ? (w & 0xffffu) | 0xff800000u : 0xff80ff80u;
+}
+
+// A whole row by one workgroup, in its registers: NV vectors a thread, loaded once, the columns that are not there set to
+// -inf (probability 0, gradient 0), then gone through three times (maximum, sums, gradient).
+template <typename T, typename G, int FORM, int TH, int NV>
+__global__ __launch_bounds__(TH, NV <= 9 ? 6 : 4) void k_distill_row(DistillArgs a) {
   constexpr int VEC = 16 / (int)sizeof(T), NW = TH / 64;
   constexpr bool TWO = FORM != kOneSum;
-  static_assert(BYTES % (TH * 16) == 0, "the row rounded up to a vector a thread fits");
-  __shared__ __attribute__((aligned(16))) char lds[BYTES];
   __shared__ float red[6][NW];
   __shared__ int tok[kMaxTeacherTokens];
   __shared__ float mass[kMaxTeacherTokens];
-  const int tid = threadIdx.x, wave = wave_id();
+  const int tid = threadIdx.x;
   const int64_t p = a.row0 + blockIdx.x;
   const size_t q = a.order ? (size_t)a.order[p] : (size_t)p;
-  const Target t = target_of(a, q);
   const T* row = static_cast<const T*>(a.logits) + (size_t)p * a.ld;
   G* out = a.grad ? static_cast<G*>(a.grad) + (size_t)p * a.ld : nullptr;
-  const int nv = (int)(a.ld / VEC), nr = (nv + TH - 1) / TH * TH;
+  const int nv = (int)(a.ld / VEC);
+  uint4 raw[NV];
+#pragma unroll
+  for (int u = 0; u < NV; ++u)
+    if (u * TH < nv) raw[u] = reinterpret_cast<const uint4*>(row)[min(u * TH + tid, nv - 1)];
+  const Target t = target_of(a, q);
   if (!t.any) {
     if (tid == 0) a.row_loss[q] = 0.f;
     if (out) {
@@ -795,13 +805,14 @@ __global__ __launch_bounds__(TH) void k_distill_row(DistillArgs a) {
     }
     return;
   }
-  for (int i = 0; i < nr; i += TH) dma16(row + (size_t)min(i + tid, nv - 1) * VEC, lds + (i + wave * 64) * 16);
-  vm_wait();
-  __syncthreads();
-  T* held = reinterpret_cast<T*>(lds);
-  for (int col = a.V + tid; col < nr * VEC; col += TH) held[col] = from_f32<T>(neg_inf());
-  __syncthreads();
-  const float zj = t.have ? to_f32<T>(held[t.tok]) : 0.f, zy = t.y >= 0 ? to_f32<T>(held[t.y]) : 0.f;
+  const float zj = t.have ? to_f32<T>(row[t.tok]) : 0.f, zy = t.y >= 0 ? to_f32<T>(row[t.y]) : 0.f;
+#pragma unroll
+  for (int u = 0; u < NV; ++u)
+    if (u * TH < nv && (u + 1) * TH * VEC > a.V) {  // the row ends here
+      const int have = a.V - (u * TH + tid) * VEC;
+      raw[u] = make_uint4(first_of<T>(raw[u].x, have), first_of<T>(raw[u].y, have - VEC / 4),
+                          first_of<T>(raw[u].z, have - VEC / 2), first_of<T>(raw[u].w, have - 3 * VEC / 4));
+    }
   auto all = [&](const float* x, bool max) {
     float r = x[0];
 #pragma unroll
@@ -809,16 +820,17 @@ __global__ __launch_bounds__(TH) void k_distill_row(DistillArgs a) {
     return r;
   };
   auto put = [&](float* x, float v) {
-    if ((tid & 63) == 0) x[wave] = v;
+    if ((tid & 63) == 0) x[tid >> 6] = v;
   };
   // f(vector of the row, its values)
   auto pass = [&](auto&& f) __attribute__((always_inline)) {
-#pragma unroll 4
-    for (int i = tid; i < nr; i += TH) {
-      float v[VEC];
-      unpack<T>(*reinterpret_cast<const uint4*>(lds + i * 16), v);
-      f(i, v);
-    }
+#pragma unroll
+    for (int u = 0; u < NV; ++u)
+      if (u * TH < nv) {
+        float v[VEC];
+        unpack<T>(raw[u], v);
+        f(u * TH + tid, v);
+      }
   };
   float m = neg_inf();
   pass([&](int, float (&v)[VEC]) __attribute__((always_inline)) {
@@ -1047,17 +1059,19 @@ int segments(int64_t rows, int V, int esize) {
 }
 // rows of one launch: its threads (at most 512 a segment) are counted in 32 bits
 int64_t rows_of_launch(int nseg) { return ((int64_t)1 << 22) / std::max(nseg, 1); }
-// Two passes over a row that is not held; a workgroup per 32 KB (2,048 rows of 130,001 fp32: 600 us whole, 495 in 32).
+// Two passes over a row that is not held; a workgroup per 32 KB (2,048 rows of 130,001 fp32: 600 us whole, 495 in 16).
 int distill_segments(int64_t rows, int V, int esize) {
   const int64_t bytes = (int64_t)V * esize;
   return (int)std::min<int64_t>((bytes + kSegmentBytes - 1) / kSegmentBytes, kMaxSegments);
 }
 
-// Rows that a workgroup holds in LDS.  Above 72 KB a compute unit has one row at a time, and its loads and stores wait for
-// its arithmetic: bf16 rows, with twice the values a byte, are then faster in segments (8,192 x 40,000: 528 us held, 396
-// in segments; 50,000: 625 and 515; but 32,000, 64 KB: 272 and 329), fp32 rows are not (4,096 x 36,000: 300 and 335).
-constexpr int kHeldBytes = 144 * 1024, kHeldBf16 = 72 * 1024;
-bool held(int V, int esize) { return (size_t)row_ld(V) * esize <= (size_t)(esize == 2 ? kHeldBf16 : kHeldBytes); }
+// Rows that a workgroup holds in its registers.  512 threads hold up to 144 KB, always; 1,024 hold up to 288 KB, one row to
+// a compute unit, where rows fill the chip twice (2,048 x 72,000 fp32: 255 us held, 335 in segments; 2,048 x 131,072 bf16:
+// 298 and 316; 300 rows: 60 and 49; 8 rows: 25 and 16).
+constexpr int kHeldBytes = 144 * 1024, kRowsHeld = 512;
+bool held(int64_t rows, int V, int esize) {
+  return (size_t)row_ld(V) * esize <= (size_t)kHeldBytes * (rows >= kRowsHeld ? 2 : 1);
+}
 
 template <typename T>
 void launch_token_rows(const TokenArgs& a, unsigned rows, hipStream_t st) {
@@ -1068,25 +1082,27 @@ void launch_token_rows(const TokenArgs& a, unsigned rows, hipStream_t st) {
 template <typename T, typename G, int FORM>
 void launch_distill_form(const DistillArgs& a, unsigned rows, hipStream_t st) {
   if (a.nseg == 0) {
-    // the smallest size that holds the row: LDS decides how many rows a compute unit has at once (32,768 x 8,000 bf16:
-    // 352 us in 24 KB, 243 in 16; 16,384 x 9,000 fp32: 263 in 48 KB, 240 in 36; 8,192 x 20,000 bf16, 40 KB: 170 in
-    // 48 KB, 209 in 72)
+    // the smallest size that holds the row: registers decide how many rows a compute unit has at once
     const size_t bytes = a.ld * sizeof(T);
     const dim3 grid(rows);
     if (bytes <= 8 * 1024)
-      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 256, 8 * 1024>), grid, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 256, 2>), grid, dim3(256), 0, st, a);
     else if (bytes <= 16 * 1024)
-      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 256, 16 * 1024>), grid, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 256, 4>), grid, dim3(256), 0, st, a);
     else if (bytes <= 24 * 1024)
-      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 512, 24 * 1024>), grid, dim3(512), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 256, 6>), grid, dim3(256), 0, st, a);
     else if (bytes <= 36 * 1024)
-      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 256, 36 * 1024>), grid, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 256, 9>), grid, dim3(256), 0, st, a);
     else if (bytes <= 48 * 1024)
-      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 512, 48 * 1024>), grid, dim3(512), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 512, 6>), grid, dim3(512), 0, st, a);
     else if (bytes <= 72 * 1024)
-      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 512, 72 * 1024>), grid, dim3(512), 0, st, a);
-    else if constexpr (sizeof(T) == 4)
-      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 512, kHeldBytes>), grid, dim3(512), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 512, 9>), grid, dim3(512), 0, st, a);
+    else if (bytes <= 96 * 1024)
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 512, 12>), grid, dim3(512), 0, st, a);
+    else if (bytes <= 144 * 1024)
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 512, 18>), grid, dim3(512), 0, st, a);
+    else
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 1024, 18>), grid, dim3(1024), 0, st, a);
     return;
   }
   hipLaunchKernelGGL((k_distill_stats<T, FORM>), dim3(rows * a.nseg), dim3(kThreads), 0, st, a);
@@ -1109,7 +1125,7 @@ size_t token_workspace_bytes(int dtype, int64_t rows, int V, int K) {
 
 size_t distill_workspace_bytes(int dtype, int64_t rows, int V, int k) {
   const int es = dtype == FOLD_BF16 ? 2 : 4;
-  if (held(V, es)) return 0;
+  if (held(rows, V, es)) return 0;
   return (size_t)rows * (distill_segments(rows, V, es) * sizeof(Stat) + (size_t)(k + 1) * sizeof(float));
 }
 
@@ -1133,7 +1149,7 @@ void launch_distill(int dtype, const int* order, int64_t rows, int V, const void
   if (rows <= 0) return;
   ProfScope prof("loss_distill", st);
   const int es = dtype == FOLD_BF16 ? 2 : 4;
-  const int n = held(V, es) ? 0 : distill_segments(rows, V, es);
+  const int n = held(rows, V, es) ? 0 : distill_segments(rows, V, es);
   // one temperature serves unless both terms are there and differ
   const bool uses_soft = soft != 0.f && k > 0, uses_hard = hard != 0.f && labels;
   const bool two = uses_soft && uses_hard && T != 1.f;

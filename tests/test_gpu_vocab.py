@@ -396,16 +396,24 @@ def test_distill_variants(M, V):
     _check_distill(z, "f32", "f32", None, None, None, 1.0, 1.0, 1.0)
 
 
-@pytest.mark.parametrize("kib", [8, 16, 24, 36, 48, 72, 144])
+@pytest.mark.parametrize("kib", [8, 16, 24, 36, 48, 72, 96, 144])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("more", [-63, 0, 1])
-def test_distill_at_the_sizes_of_lds(kib, dtype, more):
-    """Rows that just fill, just fit and just miss each amount of LDS that a row is held in."""
+def test_distill_at_the_sizes_of_a_workgroup(kib, dtype, more):
+    """Rows that just fill, just fit and just miss each size that a workgroup holds."""
     V = kib * 1024 // (2 if dtype == "bf16" else 4) + more
     rng = np.random.default_rng(V)
     tok, t, y = _targets(rng, 3, V, 3)
     tok[0, 0] = y[0] = V - 1
     _check_distill(_logits(rng, 3, V, dtype), dtype, dtype, tok, t, y, 2.0, 0.5, 0.5, inplace=True)
+
+
+@pytest.mark.parametrize("M,V,dtype", [(512, 73728, "f32"), (512, 73729, "f32"), (511, 36865, "f32"), (512, 73729, "bf16")])
+def test_distill_of_many_long_rows(M, V, dtype):
+    """Enough rows that long ones are held too, and one too few or a column too many."""
+    rng = np.random.default_rng(V)
+    tok, t, y = _targets(rng, M, V, 3)
+    _check_distill(_logits(rng, M, V, dtype), dtype, dtype, tok, t, y, 2.0, 0.5, 0.5, inplace=True)
 
 
 @pytest.mark.parametrize("V", [3, 300, 9000, 70001])
