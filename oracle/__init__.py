@@ -11,6 +11,8 @@ batched GPU path must reproduce:
     gradients;
   * ``evaluate``  -- forward by memoised recursion, one node at a time and
     unbatched, and backward in reverse topological order;
+  * ``vocab``     -- the vocabulary head: logits and their backward, the
+    distillation loss with its gradient, token log probabilities;
   * ``compare``   -- the error metric the parity tests use.
 
 Dynamic batching is a rewrite: its result equals evaluating every graph on its
