@@ -533,7 +533,8 @@ int32_t fold_adam_step(int64_t n, float* param, uint16_t* param_bf16, const floa
  * (FOLD_E_INVALID otherwise); rows is at most 2^31 - 1, vocab at most 2^30
  * (2^21 for the products).  rows = 0 is allowed (buffers that would
  * be read may be NULL).  Workspaces hold nothing between calls; calls that
- * overlap need one each.
+ * overlap need one each, and fewer rows may need a larger one (long rows that
+ * are few are cut into pieces), so a size is asked for each number of rows.
  *
  * fold_vocab_logits: z = states W^T + bias.
  *   dtype         FOLD_F32 or FOLD_BF16: states and W (products of bf16 values
