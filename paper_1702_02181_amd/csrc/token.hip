@@ -6,9 +6,11 @@
 // s = sum 2^x, and for the entropy t = sum 2^x x.  Then log p = ln 2 (x - log2 s) and H = ln 2 (log2 s - t / s).
 // Partial (m2, s, t) of threads, waves and segments of a row meet by the usual rescaling; all of it is fp32.
 //
-// Values that leave the range where z L is finite: a segment whose largest logit has |m| >= kFar (logits masked by the
-// type's lowest value and nothing else there, for instance) is read once more and its s is the count of logits equal
-// to m: every other one is at least an ulp of m (more than 1e28) below, so its probability is an exact 0.
+// m2 is the maximum's z L, rounded: the maximum's own x is that rounding's error, at most 1/2 while |m2| <= kScaled, but
+// 440 at a maximum of 1e10, where 2^x is no longer finite.  So references are clamped to +-kScaled: what lies far below
+// (whole vectors masked by -1e9, -1e30 or the type's lowest value) then has finite terms, which
+// vanish beside larger logits as they should.  A row, or a segment of one, whose largest logit itself lies outside (`far`) is
+// read once more, with x = (z - m) L: the difference is rounded by itself, so m's term is an exact 1.
 // NaN reaches s by itself (the maximum ignores NaN); +inf and NaN make the row's results NaN; a row of -inf alone is
 // empty.
 
@@ -25,7 +27,8 @@ namespace fold {
 namespace {
 
 constexpr float kL2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kFar = 1e35f;      // |m| from here on: see above (z / T stays finite for T >= 1e-3)
+constexpr float kScaled = 16777216.f;  // 2^24, the largest reference: see above
+constexpr float kNear = kScaled / kL2E;  // the largest |z| whose reference is not clamped, at temperature 1
 constexpr float kFloor = -200.f;   // 2^-200 is 0 in fp32: bounds x where it is multiplied by 2^x
 constexpr int kThreads = 256, kWaves = kThreads / 64;  // of a workgroup, where nothing else is said
 constexpr int kUnroll = 4;         // vectors a thread has in flight
@@ -179,20 +182,39 @@ struct Stat {
   float m, m2, s, t;
 };
 
+// The reference of a maximum at a factor c = L / T; near: kScaled over the largest factor of the row's sums.
 // Rounded here: fused into the subtraction that follows, two references of the same maximum would differ by the product's
-// rounding, which is 1e28 at kFar.
-__device__ __forceinline__ float ref_of(float m, float c) {
+// rounding.
+__device__ __forceinline__ float ref_of(float m, float c, float near) {
 #pragma clang fp contract(off)
-  return fminf(fmaxf(m, -kFar), kFar) * c;
+  return fminf(fmaxf(m, -near), near) * c;
 }
-__device__ __forceinline__ bool is_far(float m) { return fabsf(m) >= kFar && m != neg_inf(); }
+__device__ __forceinline__ bool is_far(float m, float near) { return fabsf(m) > near && m != neg_inf(); }
+// x of a logit seen from a far maximum: z - m rounded by itself
+__device__ __forceinline__ float far_x(float z, float m, float c) {
+#pragma clang fp contract(off)
+  return (z - m) * c;
+}
 
-// s and t seen from the reference m2
-__device__ __forceinline__ void rebase(Stat& a, float m2) {
-  const float d = fmaxf(a.m2 - m2, kFloor), f = exp2_(a.m2 - m2);
-  a.t = f * (a.t + d * a.s);
+// s and t seen from a reference that is d lower than theirs
+__device__ __forceinline__ void shift(Stat& a, float d) {
+  const float f = exp2_(d);
+  a.t = f * (a.t + fmaxf(d, kFloor) * a.s);
   a.s = f * a.s;
+}
+__device__ __forceinline__ void rebase(Stat& a, float m2) {
+  shift(a, a.m2 - m2);
   a.m2 = m2;
+}
+
+// What a segment's sums are shifted by when it joins a row: the segment's largest logit m, the row's `row` >= m.  Near
+// maxima refer to their rounded reference, far ones to themselves; one rounding in either case.  A segment without a
+// logit above -inf has sums of 0 (or NaN) and stays as it is.
+__device__ __forceinline__ float join_shift(float m, float row, float c, float near) {
+  if (m == neg_inf()) return 0.f;
+  const bool far = is_far(m, near);
+  if (is_far(row, near)) return far ? far_x(m, row, c) : -__builtin_fmaf(row, c, -ref_of(m, c, near));
+  return far ? __builtin_fmaf(m, c, -ref_of(row, c, near)) : ref_of(m, c, near) - ref_of(row, c, near);
 }
 
 // The state of a whole row from that of its segments: `bad` for NaN or +inf, `empty` for -inf alone.
@@ -200,7 +222,7 @@ struct RowState {
   float m, m2, s, t;
   bool bad, empty, far;
   __device__ __forceinline__ void close() {
-    far = is_far(m);
+    far = is_far(m, kNear);
     bad = !(s == s) || m == __builtin_inff();
     empty = !bad && m == neg_inf();
   }
@@ -214,7 +236,7 @@ struct RowState {
   __device__ __forceinline__ float entropy() const {
     if (bad) return __builtin_nanf("");
     if (empty) return 0.f;
-    return fmaxf(kLn2 * (far ? log2_(s) : log2_(s) - t / s), 0.f);
+    return fmaxf(kLn2 * (log2_(s) - t / s), 0.f);
   }
 };
 
@@ -486,7 +508,7 @@ __global__ __launch_bounds__(kThreads) void k_token(TokenArgs a) {
   const int64_t p = a.row0 + blockIdx.x / a.nseg;
   const int g = (int)(blockIdx.x % a.nseg);
   const Segment<T> seg = segment_of<T>(static_cast<const T*>(a.logits), a.ld, p, g, a.nseg, a.V);
-  Stat st{neg_inf(), -kFar * kL2E, 0.f, 0.f};
+  Stat st{neg_inf(), ref_of(neg_inf(), kL2E, kNear), 0.f, 0.f};
   Best best{neg_inf(), neg_inf(), seg.v0 + (int)threadIdx.x};
   auto add = [&](const float (&v)[VEC]) __attribute__((always_inline)) {
 #pragma unroll
@@ -498,7 +520,7 @@ __global__ __launch_bounds__(kThreads) void k_token(TokenArgs a) {
   };
   auto meet = [&](int i, float m) __attribute__((always_inline)) {
     best.meet(i, m);
-    const float m2 = ref_of(best.m, kL2E);
+    const float m2 = ref_of(best.m, kL2E, kNear);
     if (m2 > st.m2) rebase(st, m2);
   };
   seg.groups(
@@ -517,20 +539,23 @@ __global__ __launch_bounds__(kThreads) void k_token(TokenArgs a) {
   st.m = best.m;
   RowState r;
   r.m = block_max<kWaves>(st.m, red);
-  r.m2 = ref_of(r.m, kL2E);
-  rebase(st, r.m2);
-  r.s = block_add<kWaves>(st.s, red);
-  r.t = block_add<kWaves>(st.t, red);
-  if (is_far(r.m)) {
-    float n = 0.f;
+  r.m2 = ref_of(r.m, kL2E, kNear);
+  if (is_far(r.m, kNear)) {
+    st.s = st.t = 0.f;
     seg.each([&](int, float (&v)[VEC], int nv) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
-        if (e < nv) n += v[e] == r.m ? 1.f : v[e] == v[e] ? 0.f : v[e];
+        if (e < nv) {
+          const float x = far_x(v[e], r.m, kL2E), y = exp2_(x);
+          st.s += y;
+          st.t = __builtin_fmaf(y, fmaxf(x, kFloor), st.t);
+        }
     });
-    r.s = block_add<kWaves>(n, red);
-    r.t = 0.f;
+  } else {
+    rebase(st, r.m2);
   }
+  r.s = block_add<kWaves>(st.s, red);
+  r.t = block_add<kWaves>(st.t, red);
   if (a.K > 0) top_of_segment<T>(seg, best, a.K, top);
   if (a.nseg == 1) {
     r.close();
@@ -545,14 +570,12 @@ __global__ __launch_bounds__(kThreads) void k_token(TokenArgs a) {
 // The state of a row from its segments' (at most 64): every lane of every wave gets it.
 __device__ __forceinline__ RowState join(const Stat* part, int nseg) {
   const int lane = threadIdx.x & 63;
-  Stat st{neg_inf(), -kFar * kL2E, 0.f, 0.f};
+  Stat st{neg_inf(), 0.f, 0.f, 0.f};
   if (lane < nseg) st = part[lane];
   RowState r;
   r.m = wave_max(st.m);
-  r.m2 = ref_of(r.m, kL2E);
-  const bool nan = st.s != st.s;
-  if (is_far(r.m) && st.m != r.m) st.s = nan ? st.s : 0.f;  // a segment below a far maximum has probability 0
-  else rebase(st, r.m2);
+  r.m2 = ref_of(r.m, kL2E, kNear);
+  shift(st, join_shift(st.m, r.m, kL2E, kNear));
   r.s = wave_add(st.s);
   r.t = wave_add(st.t);
   r.close();
@@ -606,8 +629,8 @@ __global__ __launch_bounds__(kThreads) void k_token_join(TokenArgs a) {
 // A row has two sums if the loss has both terms and T != 1; otherwise one serves, at T where there are soft targets and at
 // 1 where there are none.  The exponentials (16 cycles a wave, two a logit in each of two passes) cost more than anything
 // else there, so for T = 2 and 4, the usual ones, those at temperature 1 are powers of the others: c, the references and
-// x are then exact binary fractions of those at 1, so 2^(x T) = (2^x)^T up to the product's rounding (8,192 x 32,000 bf16,
-// held in LDS: 289 us with two exponentials, 263 so).
+// x are then exact binary fractions of those at 1 (all references are clamped at the same logit), so 2^(x T) = (2^x)^T up to the product's rounding (8,192 x 32,000 bf16:
+// 234 us with two exponentials, at T = 3; 218 at T = 2, 222 at T = 4; 2,048 x 72,000 fp32: 267 and 257).
 // FORM: the sums a row has and how the second comes about.
 enum { kOneSum = -1, kTwoSums = 0, kSquare = 1, kFourth = 2 };
 // 2^x at temperature 1 from 2^x at T, which is 2 ^ FORM
@@ -627,6 +650,7 @@ struct DistillArgs {
   const int* labels;          // [rows] or NULL
   float T, soft, hard, scale;
   float c;      // log2 e / the temperature of the soft term (of the only one, if there is one)
+  float near;   // kScaled over the larger of c and log2 e
   float* row_loss;
   void* grad;   // [rows][ld] or NULL
   Stat* part;   // [rows][nseg]: s the sum at c, t the sum at temperature 1 (two sums)
@@ -670,7 +694,7 @@ struct RowGrad {
   __device__ __forceinline__ void close(const DistillArgs& a, const Target& t) {
     c = a.c;
     invT = 1.f / a.T;
-    far = is_far(m);
+    far = is_far(m, a.near);
     bad = !(s == s) || m == __builtin_inff();
     empty = !bad && m == neg_inf();
     if (!TWO) s1 = s;
@@ -689,14 +713,18 @@ struct RowGrad {
     return __builtin_fmaf(gb, power<FORM>(y), ga * y);
   }
   // the same in a row that is far or bad
-  __device__ __forceinline__ float odd(float z) const { return bad ? ga : z == m ? ga + gb : 0.f; }
-  __device__ __forceinline__ bool is_odd() const { return bad || (far && !empty); }
+  __device__ __forceinline__ float odd(float z) const {
+    if (bad) return ga;
+    const float y = ga * exp2_(far_x(z, m, c));
+    return TWO ? __builtin_fmaf(gb, exp2_(far_x(z, m, kL2E)), y) : y;
+  }
+  __device__ __forceinline__ bool is_odd() const { return bad || far; }
   // the gradient of a target: soft and hard mass on it
   __device__ __forceinline__ float target(float z, float soft_mass, float hard_mass) const {
     if (empty) return 0.f;
     if (bad) return ga;
-    const float pc = far ? (z == m ? 1.f : 0.f) : exp2_(__builtin_fmaf(z, c, -mc));
-    const float p1 = !TWO || far ? pc : exp2_(__builtin_fmaf(z, kL2E, -m1));
+    const float pc = exp2_(far ? far_x(z, m, c) : __builtin_fmaf(z, c, -mc));
+    const float p1 = !TWO ? pc : exp2_(far ? far_x(z, m, kL2E) : __builtin_fmaf(z, kL2E, -m1));
     return wa * (pc / s - soft_mass) + wb * (p1 / s1 - hard_mass);
   }
   // log p at a temperature (its factor, reference and sum)
@@ -842,15 +870,17 @@ __global__ __launch_bounds__(TH, NV <= 9 ? 6 : 4) void k_distill_row(DistillArgs
   __syncthreads();
   RowGrad<FORM> r;
   r.m = all(red[0], true);
-  r.mc = ref_of(r.m, a.c);
-  r.m1 = ref_of(r.m, kL2E);
+  r.mc = ref_of(r.m, a.c, a.near);
+  r.m1 = ref_of(r.m, kL2E, a.near);
   float s = 0.f, s1 = 0.f;
-  if (is_far(r.m)) {
+  if (is_far(r.m, a.near)) {
     pass([&](int, float (&v)[VEC]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) s += v[e] == r.m ? 1.f : v[e] == v[e] ? 0.f : v[e];
+      for (int e = 0; e < VEC; ++e) {
+        s += exp2_(far_x(v[e], r.m, a.c));
+        if constexpr (TWO) s1 += exp2_(far_x(v[e], r.m, kL2E));
+      }
     });
-    s1 = s;
   } else {
     pass([&](int, float (&v)[VEC]) __attribute__((always_inline)) {
 #pragma unroll
@@ -916,11 +946,11 @@ __global__ __launch_bounds__(kThreads) void k_distill_stats(DistillArgs a) {
     if (tg.have) at[threadIdx.x] = to_f32<T>(row[tg.tok]);
     if (threadIdx.x == 0) at[a.k] = tg.y >= 0 ? to_f32<T>(row[tg.y]) : 0.f;
   }
-  float m = neg_inf(), s = 0.f, s1 = 0.f, rc = ref_of(m, a.c), r1 = ref_of(m, kL2E);
+  float m = neg_inf(), s = 0.f, s1 = 0.f, rc = ref_of(m, a.c, a.near), r1 = ref_of(m, kL2E, a.near);
   auto meet = [&](float vm) __attribute__((always_inline)) {
     if (vm > m) {
       m = vm;
-      const float nc = ref_of(m, a.c), n1 = ref_of(m, kL2E);
+      const float nc = ref_of(m, a.c, a.near), n1 = ref_of(m, kL2E, a.near);
       s *= exp2_(rc - nc);
       rc = nc;
       if constexpr (TWO) {
@@ -952,17 +982,21 @@ __global__ __launch_bounds__(kThreads) void k_distill_stats(DistillArgs a) {
         add(v);
       });
   const float M = block_max<kWaves>(m, red);
-  float S = block_add<kWaves>(s * exp2_(rc - ref_of(M, a.c)), red);
-  float S1 = TWO ? block_add<kWaves>(s1 * exp2_(r1 - ref_of(M, kL2E)), red) : 0.f;
-  if (is_far(M)) {
-    float n = 0.f;
+  if (is_far(M, a.near)) {
+    s = s1 = 0.f;
     seg.each([&](int, float (&v)[VEC], int nv) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
-        if (e < nv) n += v[e] == M ? 1.f : v[e] == v[e] ? 0.f : v[e];
+        if (e < nv) {
+          s += exp2_(far_x(v[e], M, a.c));
+          if constexpr (TWO) s1 += exp2_(far_x(v[e], M, kL2E));
+        }
     });
-    S = S1 = block_add<kWaves>(n, red);
+  } else {
+    s *= exp2_(rc - ref_of(M, a.c, a.near));
+    if constexpr (TWO) s1 *= exp2_(r1 - ref_of(M, kL2E, a.near));
   }
+  const float S = block_add<kWaves>(s, red), S1 = TWO ? block_add<kWaves>(s1, red) : 0.f;
   if (threadIdx.x == 0) a.part[(size_t)p * a.nseg + g] = Stat{M, 0.f, S, S1};
 }
 
@@ -994,12 +1028,10 @@ __global__ __launch_bounds__(kThreads) void k_distill_grad(DistillArgs a) {
   if (lane < a.nseg) st = a.part[(size_t)p * a.nseg + lane];
   RowGrad<FORM> r;
   r.m = wave_max(st.m);
-  r.mc = ref_of(r.m, a.c);
-  r.m1 = ref_of(r.m, kL2E);
-  float fc = exp2_(ref_of(st.m, a.c) - r.mc), f1 = exp2_(ref_of(st.m, kL2E) - r.m1);
-  if (is_far(r.m)) fc = f1 = st.m == r.m ? 1.f : 0.f;
-  r.s = wave_add(st.s * fc);
-  r.s1 = wave_add(st.t * f1);
+  r.mc = ref_of(r.m, a.c, a.near);
+  r.m1 = ref_of(r.m, kL2E, a.near);
+  r.s = wave_add(st.s * exp2_(join_shift(st.m, r.m, a.c, a.near)));
+  r.s1 = wave_add(st.t * exp2_(join_shift(st.m, r.m, kL2E, a.near)));
   r.close(a, tg);
   const float tm = block_max<kWaves>(tg.have ? tg.t : neg_inf(), red);
   const float dt = (tg.t - tm) / a.T, ej = tg.have ? expf(dt) : 0.f, es = block_add<kWaves>(ej, red);
@@ -1153,8 +1185,9 @@ void launch_distill(int dtype, const int* order, int64_t rows, int V, const void
   // one temperature serves unless both terms are there and differ
   const bool uses_soft = soft != 0.f && k > 0, uses_hard = hard != 0.f && labels;
   const bool two = uses_soft && uses_hard && T != 1.f;
+  const float c = kL2E / (uses_soft ? T : 1.f);
   DistillArgs a{0, order, logits, (size_t)row_ld(V), V, k, n, teacher_token, teacher_logit, labels, T, soft, hard,
-                scale, kL2E / (uses_soft ? T : 1.f), row_loss, grad, static_cast<Stat*>(ws),
+                scale, c, kScaled / std::max(c, kL2E), row_loss, grad, static_cast<Stat*>(ws),
                 reinterpret_cast<float*>(static_cast<Stat*>(ws) + (size_t)rows * n)};
   for (const int64_t most = rows_of_launch(n); a.row0 < rows; a.row0 += most) {
     const unsigned r = (unsigned)std::min<int64_t>(rows - a.row0, most);
