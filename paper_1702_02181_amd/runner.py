@@ -264,6 +264,18 @@ class TrainStep:
         dev.packed.update(dev.set_tensors, dev.stream)
 
 
+def nodes_with_target(num_nodes: int, vocab: int, labels=None, teacher_token=None, teacher_logit=None):
+    """[N] bool: the nodes whose loss fold_loss_distill computes, with a label in [0, vocab) or a teacher's entry that
+    counts (its token in [0, vocab), its logit not -inf)."""
+    have = torch.zeros(num_nodes, dtype=torch.bool)
+    if labels is not None:
+        have |= ((labels >= 0) & (labels < vocab)).cpu()
+    if teacher_token is not None and teacher_logit is not None:
+        counts = (teacher_token >= 0) & (teacher_token < vocab) & (teacher_logit != -float("inf"))
+        have |= counts.any(1).cpu()
+    return have
+
+
 class VocabStep:
     """One training step of a workload whose nodes each name a token of a vocabulary, through the C ABI: zero the
     gradients, fold_forward, fold_vocab_logits on the whole pool, fold_loss_distill (a teacher's top logits, labels, or
@@ -287,11 +299,7 @@ class VocabStep:
         self.labels = cuda(labels, torch.int32)
         self.teacher_token, self.teacher_logit = cuda(teacher_token, torch.int32), cuda(teacher_logit, torch.float32)
         self.loss_args = dict(temperature=temperature, soft_weight=soft_weight, hard_weight=hard_weight)
-        have = np.zeros(dev.N, bool)
-        if labels is not None:
-            have |= (np.asarray(labels) >= 0) & (np.asarray(labels) < vocab)
-        if teacher_token is not None:
-            have |= ((np.asarray(teacher_token) >= 0) & (np.asarray(teacher_token) < vocab)).any(1)
+        have = nodes_with_target(dev.N, vocab, self.labels, self.teacher_token, self.teacher_logit)
         self.scale = 1.0 / max(1, int(have.sum()))
         dev.alloc_grads(train_table)
         dev.set_upstream(np.zeros_like(w.dh_roots))

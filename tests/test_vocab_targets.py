@@ -1,0 +1,50 @@
+"""Which nodes a vocabulary step counts as having a target: those that fold_loss_distill gives a loss to."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import vocab as OV
+from paper_1702_02181_amd import runner
+
+
+def _targets(N=40, V=11, k=3):
+    rng = np.random.default_rng(4)
+    tok = rng.integers(-1, V + 2, (N, k))
+    t = rng.standard_normal((N, k)).astype(np.float32)
+    y = rng.integers(-2, V + 2, N)
+    t[::3] = -np.inf        # a teacher that pads by logits: valid tokens, no entry that counts
+    t[1::3, 0] = -np.inf
+    tok[2::5] = -1
+    y[::2] = -1
+    y[4] = V
+    return V, tok, t, y
+
+
+@pytest.mark.parametrize("use", ["teacher", "labels", "both", "none"])
+def test_nodes_with_a_target(use):
+    V, tok, t, y = _targets()
+    N = len(y)
+    tok, t = (tok, t) if use in ("teacher", "both") else (None, None)
+    y = y if use in ("labels", "both") else None
+    # by the oracle: logits of one row's NaN make its loss NaN if, and only if, it has a target
+    loss, _ = OV.distill(np.full((N, V), np.nan), tok, t, y, soft=1.0, hard=1.0)
+    tensors = [None if a is None else torch.from_numpy(a) for a in (y, tok, t)]
+    have = runner.nodes_with_target(N, V, *tensors)
+    assert have.dtype == torch.bool and np.array_equal(have.numpy(), np.isnan(loss))
+
+
+@pytest.mark.gpu
+def test_the_loss_is_the_mean_over_nodes_with_a_target():
+    from tests.test_gpu_vocab import _model
+    w = _model("f32")
+    N, V = w.num_nodes, 50
+    rng = np.random.default_rng(5)
+    tok = rng.integers(0, V, (N, 2))
+    t = rng.standard_normal((N, 2)).astype(np.float32)
+    t[::3] = -np.inf
+    step = runner.VocabStep(w, V, None, tok, t)
+    step.gradients()
+    have = np.isfinite(t).any(1)
+    loss = step.node_loss.cpu().numpy()
+    assert (loss[have] != 0).all() and not loss[~have].any()
+    assert step.scale == 1.0 / have.sum()
