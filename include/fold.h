@@ -531,7 +531,9 @@ int32_t fold_adam_step(int64_t n, float* param, uint16_t* param_bf16, const floa
  * All of these calls enqueue on `stream`, never synchronise, never allocate
  * and can be captured.  Matrices and workspaces are 16-byte aligned
  * (FOLD_E_INVALID otherwise); rows is at most 2^31 - 1, vocab at most 2^30
- * (2^21 for the products).  rows = 0 is allowed (buffers that would
+ * (2^21 for the products, whose launches have fewer than 2^24 tiles: rows
+ * times fold_row_ld of either width up to 2^35 always fit, more may be
+ * refused as FOLD_E_INVALID).  rows = 0 is allowed (buffers that would
  * be read may be NULL).  Workspaces hold nothing between calls; calls that
  * overlap need one each, and fewer rows may need a larger one (long rows that
  * are few are cut into pieces), so a size is asked for each number of rows.

@@ -469,7 +469,10 @@ void launch_adam(size_t n, float* p, uint16_t* p_bf16, const float* g, float* m,
 // ---- vocabulary head (vocab.hip, token.hip) ----
 constexpr int kMaxTeacherTokens = 256;  // teacher's entries of a row: one a thread
 constexpr int kMaxTopTokens = 32;       // alternatives of a row
-int64_t vocab_tiles(int64_t rows, int H, int V);  // workgroups of the largest of the head's launches
+// workgroups of the largest of the head's launches: a bound for all of them, and as they are launched
+int64_t vocab_tiles(int64_t rows, int H, int V);
+int64_t vocab_logits_tiles(int dtype, int64_t rows, int H, int V);
+int64_t vocab_backward_tiles(int dtype, int64_t rows, int H, int V);
 void launch_vocab_logits(int dtype, int64_t rows, int H, int V, const void* states, const void* W, const float* bias,
                          int out_dtype, void* logits, hipStream_t st);
 size_t vocab_backward_bytes(int dtype, int64_t rows, int H, int V);

@@ -667,14 +667,12 @@ __global__ __launch_bounds__(256) void k_join(const float* part, int pieces, siz
   }
 }
 
+size_t join_blocks(int pieces, size_t stride) { return pieces > 8 ? (stride + 255) / 256 : (stride + 1023) / 1024; }
 template <bool VEC>
 void join(const float* part, int pieces, size_t stride, size_t n, float* out, int add, hipStream_t st) {
-  if (pieces > 8)
-    hipLaunchKernelGGL((k_join<VEC, 4>), dim3((unsigned)((stride + 255) / 256)), dim3(256), 0, st, part, pieces, stride,
-                       n, out, add);
-  else
-    hipLaunchKernelGGL((k_join<VEC, 1>), dim3((unsigned)((stride + 1023) / 1024)), dim3(256), 0, st, part, pieces,
-                       stride, n, out, add);
+  const dim3 grid((unsigned)join_blocks(pieces, stride));
+  if (pieces > 8) hipLaunchKernelGGL((k_join<VEC, 4>), grid, dim3(256), 0, st, part, pieces, stride, n, out, add);
+  else hipLaunchKernelGGL((k_join<VEC, 1>), grid, dim3(256), 0, st, part, pieces, stride, n, out, add);
 }
 
 // db: column sums.  A workgroup takes 64 16-byte vectors of columns of one of `chunks` pieces of the rows; its four waves
@@ -768,9 +766,18 @@ Shape shape_of(int64_t M, int64_t N, int64_t nstage, int esize, int small, int p
 bool together(int64_t M, int H, int V, int esize) {
   return M <= 64 || (M <= 128 && (esize == 4 || (int64_t)V * row_ld(H) <= (int64_t)1 << 25));
 }
+Shape logits_shape(int64_t M, int H, int V, int esize) {
+  return shape_of(M, row_ld(V), row_ld(H) * esize / 128, esize, 2, 1);
+}
 Shape states_shape(int64_t M, int H, int V, int esize) {
   return shape_of(std::max<int64_t>(M, 1), row_ld(H), (int64_t)row_ld(V) * esize / 128, esize, 1, kPieces,
                   together(M, H, V, esize));
+}
+
+// both: in one launch with the states' gradient
+Shape weights_shape(int64_t M, int H, int V, int esize, bool both) {
+  const int lines = 128 / esize;
+  return shape_of(V, row_ld(H), (M + lines - 1) / lines, esize, 1, 1, both);
 }
 
 unsigned blocks_of(const ProductArgs& g) { return (unsigned)((g.mt * g.nt * g.split + 7) / 8 * 8); }
@@ -797,9 +804,27 @@ void launch(ProductArgs g, const Shape& sh, hipStream_t st) {
 
 }  // namespace
 
+// Workgroups of the largest launch that a call makes: at most vocab_tiles (cheap, whatever the shapes), or counted.
 int64_t vocab_tiles(int64_t M, int H, int V) {
   const int64_t h = tiles_of(row_ld(H), 1), v = tiles_of(row_ld(V), 1), m = std::max<int64_t>(tiles_of(M, 1), 1);
-  return std::max((m * v + 1) / 2, std::max(v * h, m * h * kPieces));
+  return std::max(m * ((v + 1) / 2), std::max(v * h, m * h * kPieces));
+}
+int64_t vocab_logits_tiles(int dtype, int64_t M, int H, int V) {
+  const Shape sh = logits_shape(M, H, V, dtype == FOLD_BF16 ? 2 : 4);
+  return sh.mt * sh.nt;
+}
+int64_t vocab_backward_tiles(int dtype, int64_t M, int H, int V) {
+  const int es = dtype == FOLD_BF16 ? 2 : 4;
+  const Shape s1 = states_shape(M, H, V, es);
+  const int64_t ds = s1.mt * s1.nt * s1.split;
+  int64_t most = s1.split > 1 ? std::max(ds, (int64_t)join_blocks(s1.split, (size_t)M * row_ld(H))) : ds;
+  const Shape s2 = weights_shape(M, H, V, es, false);
+  most = std::max(most, s2.mt * s2.nt);
+  if (together(M, H, V, es)) {
+    const Shape s3 = weights_shape(M, H, V, es, true);
+    most = std::max(most, ds + s3.mt * s3.nt);
+  }
+  return most;  // the bias sums' launches are smaller: at most 2^13 groups of columns
 }
 
 void launch_vocab_logits(int dtype, int64_t M, int H, int V, const void* s, const void* W, const float* bias,
@@ -807,7 +832,7 @@ void launch_vocab_logits(int dtype, int64_t M, int H, int V, const void* s, cons
   if (M <= 0) return;
   ProfScope prof("vocab_logits", st);
   const int es = dtype == FOLD_BF16 ? 2 : 4, ldh = row_ld(H), ldv = row_ld(V);
-  const Shape sh = shape_of(M, ldv, ldh * es / 128, es, 2, 1);
+  const Shape sh = logits_shape(M, H, V, es);
   const ProductArgs g{{s, M, ldh}, {W, V, ldh}, M, V, sh.mt, sh.nt, ldh * es / 128, 1, z, (size_t)ldv, ldv, bias, 0,
                       nullptr};
   if (dtype == FOLD_F32) launch<float, kAlong, kAlong, float>(g, sh, st);
@@ -829,7 +854,7 @@ void launch_vocab_backward(int dtype, int64_t M, int H, int V, const void* s, co
   const int64_t stages = (M + kst - 1) / kst;
   const Shape s1 = states_shape(M, H, V, es);
   const bool both = ds && dW && M > 0 && together(M, H, V, es);
-  const Shape s2 = shape_of(V, ldh, stages, es, 1, 1, both);
+  const Shape s2 = weights_shape(M, H, V, es, both);
   // a few rows' sums come from the weights' product, whose tiles of the first column hold all of dz: where every stage is
   // loaded before its loop (two of 128 bytes, or three of 64, of which a whole one is two)
   float* sums = dW && stages <= (s2.wm == 4 ? 1 : 2) ? db : nullptr;

@@ -58,13 +58,15 @@ int check_rows(const std::string& who, int dtype, int64_t rows, int vocab) {
   return FOLD_OK;
 }
 
-int check_product(const std::string& who, int dtype, int64_t rows, int hidden, int vocab) {
+// tiles: workgroups of the call's largest launch
+template <class F>
+int check_product(const std::string& who, int dtype, int64_t rows, int hidden, int vocab, F&& tiles) {
   const int rc = check_rows(who, dtype, rows, vocab);
   if (rc != FOLD_OK) return rc;
   if (vocab > kMaxHeadVocab) return vfail(FOLD_E_INVALID, who + ": vocabulary size out of range (1 .. 2^21)");
   if (hidden < 1 || hidden > kMaxHidden) return vfail(FOLD_E_INVALID, who + ": hidden size out of range");
-  if (vocab_tiles(rows, hidden, vocab) >= kMaxTiles)
-    return vfail(FOLD_E_INVALID, who + ": rows * vocabulary too large for one call");
+  if (vocab_tiles(rows, hidden, vocab) >= kMaxTiles && tiles(dtype, rows, hidden, vocab) >= kMaxTiles)
+    return vfail(FOLD_E_INVALID, who + ": too many tiles for one launch (rows times the widths)");
   return FOLD_OK;
 }
 
@@ -103,7 +105,7 @@ int32_t fold_vocab_logits(int32_t dtype, int64_t rows, int32_t hidden, int32_t v
                           const void* W, const float* bias, int32_t logits_dtype, void* logits, hipStream_t st) {
   return guarded([&]() -> int32_t {
     const std::string who("fold_vocab_logits");
-    const int rc = check_product(who, dtype, rows, hidden, vocab);
+    const int rc = check_product(who, dtype, rows, hidden, vocab, vocab_logits_tiles);
     if (rc != FOLD_OK) return rc;
     if (!known_type(logits_dtype) || (dtype == FOLD_F32 && logits_dtype != FOLD_F32))
       return vfail(FOLD_E_INVALID, who + ": logits are fp32, or bf16 for a bf16 head");
@@ -125,7 +127,7 @@ int32_t fold_vocab_workspace_size(int32_t dtype, int64_t rows, int32_t hidden, i
   return guarded([&]() -> int32_t {
     const std::string who("fold_vocab_workspace_size");
     if (!bytes) return vfail(FOLD_E_INVALID, who + ": NULL argument");
-    const int rc = check_product(who, dtype, rows, hidden, vocab);
+    const int rc = check_product(who, dtype, rows, hidden, vocab, vocab_backward_tiles);
     if (rc != FOLD_OK) return rc;
     *bytes = vocab_backward_bytes(dtype, rows, hidden, vocab);
     return FOLD_OK;
@@ -137,7 +139,7 @@ int32_t fold_vocab_backward(int32_t dtype, int64_t rows, int32_t hidden, int32_t
                             int32_t flags, void* ws, size_t ws_bytes, hipStream_t st) {
   return guarded([&]() -> int32_t {
     const std::string who("fold_vocab_backward");
-    const int rc = check_product(who, dtype, rows, hidden, vocab);
+    const int rc = check_product(who, dtype, rows, hidden, vocab, vocab_backward_tiles);
     if (rc != FOLD_OK) return rc;
     if (flags & ~FOLD_VOCAB_ACCUMULATE) return vfail(FOLD_E_INVALID, who + ": unknown flag");
     if ((!d_states || rows == 0) && !dW && !dbias) return FOLD_OK;
