@@ -746,10 +746,12 @@ __device__ __forceinline__ float soft_loss(const DistillArgs& a, const RowGrad<F
                                            float dt, float es, float z) {
   return t.have && q != 0.f && a.soft != 0.f ? q * (dt - logf(es) - r.logp_soft(z)) : 0.f;
 }
-// the row's loss from the sum of the shares
+// the loss of a row with a target from the sum of the shares
 template <int FORM>
 __device__ __forceinline__ float row_loss(const DistillArgs& a, const RowGrad<FORM>& r, const Target& t, float soft,
                                           float zy) {
+  if (r.bad) return __builtin_nanf("");
+  if (r.empty) return __builtin_inff();
   float loss = t.soft && a.soft != 0.f ? a.soft * a.T * a.T * soft : 0.f;
   if (t.y >= 0 && a.hard != 0.f) loss -= a.hard * r.logp_hard(zy);
   return loss;

@@ -13,7 +13,7 @@ import pytest
 
 from oracle import vocab as OV
 from paper_1702_02181_amd import fold as F
-from tests.test_gpu_vocab import NAN, U, _check_distill, _dev, _ints, _logits, _np, _rel, _round, _targets, _within
+from tests.test_gpu_vocab import NAN, U, _check_distill, _dev, _hard_rows, _ints, _logits, _np, _rel, _round, _targets, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -90,3 +90,16 @@ def test_one_term_of_logits_of_any_size(soft, hard):
         z = _rows("f32", V, rng)
         tok, t, y = _targets(rng, z.shape[0], V, 3)
         _check_distill(z, "f32", "bf16", tok, t, y, 2.0, soft, hard)
+
+
+@pytest.mark.parametrize("V", [300, "long"])
+@pytest.mark.parametrize("soft,hard", [(0.0, 1.0), (1.0, 0.0), (0.0, 0.0)])
+def test_rows_that_are_no_distribution_under_weights_of_zero(V, soft, hard):
+    """A target makes the loss of a row with NaN or +inf NaN, and that of a row of -inf alone +inf, also where the only
+    target's term has a weight of zero; rows without a target stay at 0."""
+    V = LONG["f32"] if V == "long" else V
+    rng = np.random.default_rng(V + 2)
+    z = np.concatenate([_hard_rows("f32", V, rng)] * 3)
+    tok, t, y = _targets(rng, 60, V, 3)
+    tok[:20], y[20:40] = -1, -1  # a label alone, a teacher alone, both
+    _check_distill(z, "f32", "f32", tok, t, y, 2.0, soft, hard)
