@@ -17,6 +17,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cstdint>
 
 #include "common.h"
 #include "internal.h"
@@ -1091,8 +1092,11 @@ int segments(int64_t rows, int V, int esize) {
   if (bytes < kWholeBytes || rows >= kRowsFull) return 1;
   return (int)std::min<int64_t>((bytes + kSegmentBytes - 1) / kSegmentBytes, kMaxSegments);
 }
-// rows of one launch: its threads (at most 512 a segment) are counted in 32 bits
-int64_t rows_of_launch(int nseg) { return ((int64_t)1 << 22) / std::max(nseg, 1); }
+// rows of one launch of `threads` a row: all its threads are counted in 32 bits
+constexpr int kHeldThreads = 1024;  // the most that hold a row
+constexpr int64_t rows_of_launch(int threads) { return ((int64_t)1 << 31) / threads; }
+static_assert(rows_of_launch(kHeldThreads) * kHeldThreads <= (int64_t)UINT32_MAX &&
+                  rows_of_launch(kMaxSegments * kThreads) >= 1, "a launch's threads");
 // Two passes over a row that is not held; a workgroup per 32 KB (2,048 rows of 130,001 fp32: 600 us whole, 495 in 16).
 int distill_segments(int64_t rows, int V, int esize) {
   const int64_t bytes = (int64_t)V * esize;
@@ -1136,7 +1140,7 @@ void launch_distill_form(const DistillArgs& a, unsigned rows, hipStream_t st) {
     else if (bytes <= 144 * 1024)
       hipLaunchKernelGGL((k_distill_row<T, G, FORM, 512, 18>), grid, dim3(512), 0, st, a);
     else
-      hipLaunchKernelGGL((k_distill_row<T, G, FORM, 1024, 18>), grid, dim3(1024), 0, st, a);
+      hipLaunchKernelGGL((k_distill_row<T, G, FORM, kHeldThreads, 18>), grid, dim3(kHeldThreads), 0, st, a);
     return;
   }
   hipLaunchKernelGGL((k_distill_stats<T, FORM>), dim3(rows * a.nseg), dim3(kThreads), 0, st, a);
@@ -1170,7 +1174,7 @@ void launch_token(int dtype, const int* order, int64_t rows, int V, const void* 
   const int n = segments(rows, V, dtype == FOLD_BF16 ? 2 : 4);
   TokenArgs a{0, order, logits, (size_t)row_ld(V), V, J, K, n, tokens, logp, entropy, top_token, top_logp,
               static_cast<Stat*>(ws), reinterpret_cast<uint64_t*>(static_cast<Stat*>(ws) + (size_t)rows * n)};
-  for (const int64_t most = rows_of_launch(n); a.row0 < rows; a.row0 += most) {
+  for (const int64_t most = rows_of_launch(n * kThreads); a.row0 < rows; a.row0 += most) {
     const unsigned r = (unsigned)std::min<int64_t>(rows - a.row0, most);
     if (dtype == FOLD_BF16) launch_token_rows<uint16_t>(a, r, st);
     else launch_token_rows<float>(a, r, st);
@@ -1191,7 +1195,7 @@ void launch_distill(int dtype, const int* order, int64_t rows, int V, const void
   DistillArgs a{0, order, logits, (size_t)row_ld(V), V, k, n, teacher_token, teacher_logit, labels, T, soft, hard,
                 scale, c, kScaled / std::max(c, kL2E), row_loss, grad, static_cast<Stat*>(ws),
                 reinterpret_cast<float*>(static_cast<Stat*>(ws) + (size_t)rows * n)};
-  for (const int64_t most = rows_of_launch(n); a.row0 < rows; a.row0 += most) {
+  for (const int64_t most = rows_of_launch(n == 0 ? kHeldThreads : n * kThreads); a.row0 < rows; a.row0 += most) {
     const unsigned r = (unsigned)std::min<int64_t>(rows - a.row0, most);
     if (dtype == FOLD_BF16) launch_distill_rows<uint16_t, uint16_t>(a, two, r, st);
     else if (grad_dtype == FOLD_BF16) launch_distill_rows<float, uint16_t>(a, two, r, st);
