@@ -881,8 +881,10 @@ void launch_vocab_backward(int dtype, int64_t M, int H, int V, const void* s, co
       else launch<uint16_t, kAcross, kAcross, float>(weights, s2, st);
     }
   }
-  if (ds && M > 0 && s1.split > 1)
+  if (ds && M > 0 && s1.split > 1) {
+    ProfScope prof("vocab_dstates_join", st);
     join<true>(static_cast<const float*>(ws), s1.split, (size_t)M * ldh, (size_t)M * ldh, ds, 0, st);
+  }
   if (db && !sums) {
     ProfScope prof("vocab_dbias", st);
     const int c = bias_chunks(M, V, es);
