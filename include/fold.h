@@ -601,9 +601,11 @@ int32_t fold_vocab_backward(int32_t dtype, int64_t rows, int32_t hidden, int32_t
  *               overlap it otherwise; NULL: the losses alone
  *   ws          device workspace of >= fold_distill_workspace_size bytes (may be
  *               NULL where that is 0: rows that a workgroup holds)
- * Sums are fp32.  Logits of -inf (masked) have probability 0; a target there
- * has loss +inf.  A row with a target whose logits are all -inf has loss +inf
- * and gradient 0; one with NaN or +inf has loss and gradient NaN. */
+ * Sums are fp32.  Logits may be any finite numbers (a mask of -1e9 or of the
+ * type's lowest value is one); those of -inf (masked) have probability 0, and
+ * a target there has loss +inf.  A row with a target whose logits are all
+ * -inf has loss +inf and gradient 0; one with NaN or +inf has loss and gradient
+ * NaN. */
 int32_t fold_distill_workspace_size(int32_t dtype, int64_t rows, int32_t vocab, int32_t num_teacher, size_t* bytes);
 int32_t fold_loss_distill(const fold_sched* sched, int32_t dtype, int64_t rows, int32_t vocab, const void* logits,
                           int32_t num_teacher, const int32_t* teacher_token, const float* teacher_logit,

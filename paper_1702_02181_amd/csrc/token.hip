@@ -623,15 +623,16 @@ __global__ __launch_bounds__(kThreads) void k_token_join(TokenArgs a) {
 
 // ---------------------------------------------------------------- distillation
 // The gradient needs the softmax's sums before its first value, so a row is read twice or held.  k_distill_row holds a
-// row in its workgroup's registers and so reads and writes memory once (8,192 x 32,000 bf16: 214 us, a copy of the logits
-// 198; held in LDS, where two such rows fit a compute unit and every pass reads it, 263); longer rows, and long ones that
+// row in its workgroup's registers and so reads and writes memory once (8,192 x 32,000 bf16: 208 us, a copy of the logits
+// 200; held in LDS, where two such rows fit a compute unit and every pass reads it, 263); longer rows, and long ones that
 // are few, go through k_distill_stats (sums of segments) and k_distill_grad (joins them, reads its segment again, mostly
 // from a cache).
 // A row has two sums if the loss has both terms and T != 1; otherwise one serves, at T where there are soft targets and at
-// 1 where there are none.  The exponentials (16 cycles a wave, two a logit in each of two passes) cost more than anything
-// else there, so for T = 2 and 4, the usual ones, those at temperature 1 are powers of the others: c, the references and
-// x are then exact binary fractions of those at 1 (all references are clamped at the same logit), so 2^(x T) = (2^x)^T up to the product's rounding (8,192 x 32,000 bf16:
-// 234 us with two exponentials, at T = 3; 218 at T = 2, 222 at T = 4; 2,048 x 72,000 fp32: 267 and 257).
+// 1 where there are none.  Exponentials (16 cycles a wave) would bound the kernel with two a logit in each of two passes,
+// so for T = 2 and 4, the usual ones, those at temperature 1 are powers of the others: c, the references and x are then
+// exact binary fractions of those at 1 (all references are clamped at the same logit), so 2^(x T) = (2^x)^T up to the
+// product's rounding (8,192 x 32,000 bf16, in one run: 232 us with two exponentials, at T = 3, 210 at T = 2, 216 at T = 4,
+// 210 with one sum; 8,192 x 10,000: 74, 67.5, 69 and 66; 2,048 x 72,000 fp32: 266, 256, 258 and 250).
 // FORM: the sums a row has and how the second comes about.
 enum { kOneSum = -1, kTwoSums = 0, kSquare = 1, kFourth = 2 };
 // 2^x at temperature 1 from 2^x at T, which is 2 ^ FORM

@@ -736,7 +736,7 @@ constexpr int kUnits = 256;  // compute units
 // matrix cores bound all of them, 1.0, 1.03 and 1.06.  A workgroup's first loads and its store take about 2 us; pieces
 // cost their sums' way through memory (4 TB/s) and a second launch (3 us).  What the rule gets (best and worst cut tried):
 // states' gradient of 33 x 300 x 20,000 bf16 13 us (335), of 257 x 300 x 20,001 fp32 49 us (4,512), weights' gradient of
-// 2,048 x 256 x 10,000 fp32 95 us (486).
+// 2,048 x 256 x 10,000 fp32 100 us (486).
 // small: the smallest tile's columns / 64 (1 or 2); smallest: that tile alone
 Shape shape_of(int64_t M, int64_t N, int64_t nstage, int esize, int small, int pieces, bool smallest = false) {
   static constexpr struct { int wm, wn; double bf16, f32; } kTiles[] = {
