@@ -316,6 +316,7 @@ class VocabStep:
             self.tensors.append((self.W.float(), self.W, self.dW) if dev.bf16 else (self.W, None, self.dW))
         self.tensors.append((self.bias, None, self.db))
         self.head = F.VocabHead(self.W, self.bias, w.hidden)
+        self.states = dev.h_pool[:dev.N]  # the pool has a row also for a batch without nodes
         self.logits = torch.zeros((dev.N, F.fold_row_ld(vocab)), dtype=dev.tdtype, device=dev.device)
         self.node_loss = None
         self.moments = [(torch.zeros_like(m), torch.zeros_like(m)) for m, _, _ in self.tensors]
@@ -325,12 +326,12 @@ class VocabStep:
         dev, st = self.dev, self.dev.stream
         dev.zero_grads()
         dev.forward()
-        self.head.logits(dev.h_pool, out=self.logits, stream=st)
+        self.head.logits(self.states, out=self.logits, stream=st)
         self.node_loss, _ = F.distill_loss(self.logits, self.vocab, self.teacher_token, self.teacher_logit, self.labels,
                                            scale=self.scale, dlogits=self.logits, sched=dev.sched, stream=st,
                                            **self.loss_args)
         self.db.zero_()
-        self.head.backward(dev.h_pool, self.logits, self.dh_nodes, self.dW, self.db, accumulate=self.tied, stream=st)
+        self.head.backward(self.states, self.logits, self.dh_nodes, self.dW, self.db, accumulate=self.tied, stream=st)
         dev.backward()
 
     def step(self):
@@ -346,5 +347,5 @@ class VocabStep:
         """F.TokenLogprobs of `tokens` [N, num_tokens] (node order) under the current weights."""
         dev = self.dev
         dev.forward()
-        self.head.logits(dev.h_pool, out=self.logits, stream=dev.stream)
+        self.head.logits(self.states, out=self.logits, stream=dev.stream)
         return F.token_logprobs(self.logits, self.vocab, tokens, top_k, sched=dev.sched, stream=dev.stream)

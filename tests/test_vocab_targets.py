@@ -48,3 +48,24 @@ def test_the_loss_is_the_mean_over_nodes_with_a_target():
     loss = step.node_loss.cpu().numpy()
     assert (loss[have] != 0).all() and not loss[~have].any()
     assert step.scale == 1.0 / have.sum()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tied", [False, True])
+def test_a_batch_without_nodes(tied):
+    """Loss rows and score rows of length zero; every gradient and so every step of Adam is zero, as in TrainStep."""
+    import dataclasses
+
+    from tests.test_gpu_vocab import _model
+    w = _model("bf16")
+    none = np.zeros(0, np.int32)
+    empty = dataclasses.replace(w, graph_ptr=np.zeros(1, np.int32), node_op=none, child_ptr=np.zeros(1, np.int32),
+                                child_idx=none, node_input=none, dh_roots=np.zeros((0, w.hidden), np.float32))
+    V = w.leaf_table.shape[0] if tied else 50
+    step = runner.VocabStep(empty, V, none, np.zeros((0, 3), np.int32), np.zeros((0, 3), np.float32), tied=tied)
+    before = step.W.clone()
+    step.step()
+    assert step.node_loss.shape == (0,) and torch.equal(step.W, before)
+    assert not step.dW.any() and not step.db.any()
+    r = step.score(torch.zeros((0, 2), dtype=torch.int32, device="cuda"), 4)
+    assert r.logp.shape == (0, 2) and r.top_token.shape == (0, 4)
