@@ -69,3 +69,35 @@ def test_a_batch_without_nodes(tied):
     assert not step.dW.any() and not step.db.any()
     r = step.score(torch.zeros((0, 2), dtype=torch.int32, device="cuda"), 4)
     assert r.logp.shape == (0, 2) and r.top_token.shape == (0, 4)
+
+
+@pytest.mark.gpu
+def test_the_step_as_a_graph():
+    """gradients() recorded once; every replay, with eager steps of Adam between, gives the eager gradients of the weights
+    that it finds."""
+    import gc
+
+    from tests.test_gpu_vocab import _model, _targets
+    w = _model("bf16")
+    rng = np.random.default_rng(6)
+    V = w.leaf_table.shape[0]
+    tok, t, y = _targets(rng, w.num_nodes, V, 3)
+    step = runner.VocabStep(w, V, y, tok, t, temperature=2.0, soft_weight=0.5, hard_weight=0.5, tied=True)
+    tensors = [g for _, _, g in step.tensors]
+    step.gradients()
+    torch.cuda.synchronize()
+    gc.collect()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step.gradients()
+    loss = step.node_loss
+    for _ in range(3):
+        step.step()
+        step.gradients()
+        want = [g.clone() for g in tensors] + [step.node_loss.clone()]
+        for g in tensors:
+            g.fill_(7.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, tensors + [loss]))
