@@ -639,6 +639,90 @@ int32_t fold_token_logprobs(const fold_sched* sched, int32_t dtype, int64_t rows
                             int32_t num_tokens, const int32_t* tokens, float* logp, float* entropy, int32_t top_k,
                             int32_t* top_token, float* top_logp, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ---- the attention block over node states -----------------------------------
+ * What stands between the states of a forward pass and a head where the nodes
+ * of one batch of graphs look at the states of another (a decoder's chains at
+ * an encoder's trees): layer norm, linear layers with an activation and a
+ * residual, and cross attention, each with its gradient.  Matrices are
+ * [rows, fold_row_ld(width)], any rows (a pool in pool order, roots_out, tokens
+ * of a serving step), 16-byte aligned.  All calls but fold_cross_create and
+ * fold_cross_free enqueue on `stream`, never synchronise, never allocate and
+ * can be captured; workspaces hold nothing between calls, calls that overlap
+ * need one each, and a size is asked for each set of sizes.  Sums, statistics
+ * and softmaxes are fp32; results are rounded once to their type.  Every sum's
+ * order is fixed by sizes.  rows = 0 is allowed.
+ *
+ * fold_layer_norm: per row, over its first `width` values,
+ *     mean = sum x / width,  rstd = (sum (x - mean)^2 / width + eps)^(-1/2),
+ *     y = gamma (x - mean) rstd + beta.
+ *   dtype  of x and y: FOLD_F32 or FOLD_BF16; width 1 .. 4096; rows to 2^31 - 1
+ *   gamma, beta  device [width] fp32, or NULL (1 and 0)
+ *   eps    finite, above 0
+ *   y      device, written whole (pad columns zero); may be x itself
+ *   mean, rstd  device [rows] fp32 (what the gradient needs), or NULL
+ * The pad columns of x are not looked at.
+ * fold_layer_norm_backward: with xh = (x - mean) rstd and g = gamma dy,
+ *     dx = rstd (g - mean(g) - xh mean(g xh)) (+ residual)
+ *     dgamma (+)= sum over the rows of dy xh,   dbeta (+)= sum of dy
+ *   dy_dtype  of dy: dtype, or FOLD_F32
+ *   dx_dtype  of dx and residual: dtype, or FOLD_F32
+ *   residual  device [rows, ld], a gradient that goes by the norm, or NULL
+ *   dx        device, written whole (pad columns zero), or NULL; may be dy or
+ *             residual itself where the types are equal
+ *   dgamma, dbeta  device [width] fp32, or NULL; written, or added to with
+ *             FOLD_BLOCK_ACCUMULATE
+ *   ws        device workspace of >= fold_layer_norm_workspace_size bytes (for
+ *             dgamma or dbeta)
+ *
+ * fold_linear: out = act(x W^T + bias) + residual.
+ *   x         device [rows, fold_row_ld(in_dim)];  in_dim, out_dim 1 .. 16384
+ *   W         device [out_dim, fold_row_ld(in_dim)], one row an output, as the
+ *             vocabulary head's; the pad columns of one of x and W hold zeros,
+ *             of the other any finite values
+ *   bias      device [out_dim] fp32, or NULL
+ *   act       FOLD_ACT_*;  gelu(z) = z Phi(z), Phi the normal distribution
+ *   residual  device [rows, fold_row_ld(out_dim)], or NULL; may be out itself
+ *   out       device [rows, fold_row_ld(out_dim)], written whole (pad columns
+ *             zero)
+ *   pre       device, as out: z = x W^T + bias, which the gradient of an
+ *             activation needs, or NULL
+ * x, W, residual, out and pre are of dtype.
+ * fold_linear_backward: with dz = dout act'(pre) (dout itself for FOLD_ACT_NONE;
+ * relu'(0) = 0), rounded to dtype where it enters a product,
+ *     dx = dz W,   dW (+)= dz^T x,   dbias (+)= sum over the rows of dz
+ *   dout      device [rows, fold_row_ld(out_dim)] of dtype, finite in the pad
+ *             columns (zero for FOLD_ACT_NONE)
+ *   pre       as left by fold_linear (NULL for FOLD_ACT_NONE)
+ *   dpre      device, as pre: receives dz; may be pre or dout itself; NULL for
+ *             FOLD_ACT_NONE
+ *   dx_dtype, dw_dtype  of dx and dW: dtype, or FOLD_F32
+ *   dx, dW, dbias  written whole (pad columns zero), or NULL; with
+ *             FOLD_BLOCK_ACCUMULATE dbias and a dW of FOLD_F32 are added to
+ *   ws        device workspace of >= fold_linear_workspace_size bytes
+ * A residual's gradient is dout.
+ *
+ * Errors of these calls: FOLD_E_INVALID for sizes out of range, unknown types,
+ * activations or flags, NULL or misaligned buffers, an output that overlaps
+ * another buffer where nothing above allows it, products of more than 2^24
+ * tiles; FOLD_E_MISMATCH for a workspace that is too small. */
+enum { FOLD_ACT_NONE = 0, FOLD_ACT_RELU = 1, FOLD_ACT_TANH = 2, FOLD_ACT_GELU = 3 };
+#define FOLD_BLOCK_ACCUMULATE 1
+
+int32_t fold_layer_norm(int32_t dtype, int64_t rows, int32_t width, const void* x, const float* gamma,
+                        const float* beta, float eps, void* y, float* mean, float* rstd, hipStream_t stream);
+int32_t fold_layer_norm_workspace_size(int32_t dtype, int64_t rows, int32_t width, size_t* bytes);
+int32_t fold_layer_norm_backward(int32_t dtype, int64_t rows, int32_t width, const void* x, const float* gamma,
+                                 const float* mean, const float* rstd, int32_t dy_dtype, const void* dy,
+                                 int32_t dx_dtype, const void* residual, void* dx, float* dgamma, float* dbeta,
+                                 int32_t flags, void* ws, size_t ws_bytes, hipStream_t stream);
+int32_t fold_linear(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, const void* x, const void* W,
+                    const float* bias, int32_t act, const void* residual, void* out, void* pre, hipStream_t stream);
+int32_t fold_linear_workspace_size(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, size_t* bytes);
+int32_t fold_linear_backward(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, const void* x, const void* W,
+                             int32_t act, const void* pre, const void* dout, void* dpre, int32_t dx_dtype, void* dx,
+                             int32_t dw_dtype, void* dW, float* dbias, int32_t flags, void* ws, size_t ws_bytes,
+                             hipStream_t stream);
+
 /* ---- a whole step as one HIP graph ----------------------------------------
  * The level loop (Section 2: one batched iteration per depth, so a batch of
  * depth D costs O(D) launches instead of one per node) still issues a few

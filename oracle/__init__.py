@@ -13,6 +13,8 @@ batched GPU path must reproduce:
     unbatched, and backward in reverse topological order;
   * ``vocab``     -- the vocabulary head: logits and their backward, the
     distillation loss with its gradient, token log probabilities;
+  * ``block``     -- the attention block: layer norm, linear layers, cross
+    attention, and their gradients;
   * ``compare``   -- the error metric the parity tests use.
 
 Dynamic batching is a rewrite: its result equals evaluating every graph on its

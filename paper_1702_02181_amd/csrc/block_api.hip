@@ -1,0 +1,182 @@
+// C ABI of the attention block: argument checks of layer norm and the linear layers.
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <string>
+
+#include "checks.h"
+#include "common.h"
+#include "internal.h"
+
+using namespace fold;
+
+namespace {
+
+size_t vector_bytes(int64_t n) { return (size_t)n * sizeof(float); }
+
+int check_norm(const std::string& who, int dtype, int64_t rows, int width) {
+  if (!known_type(dtype)) return api_fail(FOLD_E_INVALID, who + ": unknown dtype");
+  if (rows < 0 || rows > INT32_MAX) return api_fail(FOLD_E_INVALID, who + ": rows out of range");
+  if (width < 1 || width > kMaxHidden) return api_fail(FOLD_E_INVALID, who + ": width out of range (1 .. 4096)");
+  return FOLD_OK;
+}
+
+template <class F>
+int check_linear(const std::string& who, int dtype, int64_t rows, int in_dim, int out_dim, F&& tiles) {
+  if (!known_type(dtype)) return api_fail(FOLD_E_INVALID, who + ": unknown dtype");
+  if (rows < 0 || rows > INT32_MAX) return api_fail(FOLD_E_INVALID, who + ": rows out of range");
+  if (in_dim < 1 || in_dim > kMaxLinear || out_dim < 1 || out_dim > kMaxLinear)
+    return api_fail(FOLD_E_INVALID, who + ": in_dim and out_dim must be 1 .. 16384");
+  if (tiles(dtype, rows, in_dim, out_dim) >= kMaxTiles)
+    return api_fail(FOLD_E_INVALID, who + ": too many tiles for one launch (rows times the widths)");
+  return FOLD_OK;
+}
+
+// a gradient's type: the operator's own, or fp32
+bool grad_type(int type, int dtype) { return type == FOLD_F32 || type == dtype; }
+
+}  // namespace
+
+extern "C" {
+
+int32_t fold_layer_norm(int32_t dtype, int64_t rows, int32_t width, const void* x, const float* gamma, const float* beta,
+                        float eps, void* y, float* mean, float* rstd, hipStream_t st) {
+  return guarded([&]() -> int32_t {
+    const std::string who("fold_layer_norm");
+    const int rc = check_norm(who, dtype, rows, width);
+    if (rc != FOLD_OK) return rc;
+    if (!(eps > 0.f) || !std::isfinite(eps)) return api_fail(FOLD_E_INVALID, who + ": eps must be finite and above 0");
+    if (rows == 0) return FOLD_OK;
+    if (!x || !y) return api_fail(FOLD_E_INVALID, who + ": NULL buffer");
+    if (misaligned(x) || misaligned(y)) return api_fail(FOLD_E_INVALID, who + ": x and y must be 16-byte aligned");
+    const size_t m = bytes_of(dtype, rows, width), v = vector_bytes(width), r = vector_bytes(rows);
+    const Span out[] = {{y, m}, {mean, r}, {rstd, r}};
+    const Span in[] = {{y == x ? nullptr : x, m}, {gamma, v}, {beta, v}};
+    if (any_overlap(out, 3, in, 3)) return api_fail(FOLD_E_INVALID, who + ": an output overlaps another buffer");
+    launch_norm(dtype, rows, width, x, gamma, beta, eps, y, mean, rstd, st);
+    FOLD_HIP_CHECK(hipGetLastError());
+    return FOLD_OK;
+  });
+}
+
+int32_t fold_layer_norm_workspace_size(int32_t dtype, int64_t rows, int32_t width, size_t* bytes) {
+  return guarded([&]() -> int32_t {
+    const std::string who("fold_layer_norm_workspace_size");
+    if (!bytes) return api_fail(FOLD_E_INVALID, who + ": NULL argument");
+    const int rc = check_norm(who, dtype, rows, width);
+    if (rc != FOLD_OK) return rc;
+    *bytes = norm_backward_bytes(dtype, rows, width);
+    return FOLD_OK;
+  });
+}
+
+int32_t fold_layer_norm_backward(int32_t dtype, int64_t rows, int32_t width, const void* x, const float* gamma,
+                                 const float* mean, const float* rstd, int32_t dy_dtype, const void* dy,
+                                 int32_t dx_dtype, const void* residual, void* dx, float* dgamma, float* dbeta,
+                                 int32_t flags, void* ws, size_t ws_bytes, hipStream_t st) {
+  return guarded([&]() -> int32_t {
+    const std::string who("fold_layer_norm_backward");
+    const int rc = check_norm(who, dtype, rows, width);
+    if (rc != FOLD_OK) return rc;
+    if (!grad_type(dy_dtype, dtype) || !grad_type(dx_dtype, dtype))
+      return api_fail(FOLD_E_INVALID, who + ": gradients are of the states' type, or fp32");
+    if (flags & ~FOLD_BLOCK_ACCUMULATE) return api_fail(FOLD_E_INVALID, who + ": unknown flag");
+    if ((!dx || rows == 0) && !dgamma && !dbeta) return FOLD_OK;
+    if (rows > 0 && (!x || !mean || !rstd || !dy)) return api_fail(FOLD_E_INVALID, who + ": NULL buffer");
+    if (misaligned(x) || misaligned(dy) || misaligned(residual) || misaligned(dx) || misaligned(ws))
+      return api_fail(FOLD_E_INVALID, who + ": matrices and the workspace must be 16-byte aligned");
+    const size_t need = dgamma || dbeta ? norm_backward_bytes(dtype, rows, width) : 0;
+    if (need > 0 && (!ws || ws_bytes < need))
+      return api_fail(FOLD_E_MISMATCH, who + ": workspace smaller than fold_layer_norm_workspace_size");
+    const size_t v = vector_bytes(width), r = vector_bytes(rows);
+    const Span out[] = {{dx, bytes_of(dx_dtype, rows, width)}, {dgamma, v}, {dbeta, v}, {ws, need}};
+    const Span in[] = {{x, bytes_of(dtype, rows, width)},
+                       {dx == dy && dx_dtype == dy_dtype ? nullptr : dy, bytes_of(dy_dtype, rows, width)},
+                       {dx == residual ? nullptr : residual, bytes_of(dx_dtype, rows, width)},
+                       {gamma, v},
+                       {mean, r},
+                       {rstd, r}};
+    if (any_overlap(out, 4, in, 6)) return api_fail(FOLD_E_INVALID, who + ": an output overlaps another buffer");
+    launch_norm_backward(dtype, rows, width, x, gamma, mean, rstd, dy_dtype, dy, dx_dtype, residual, dx, dgamma, dbeta,
+                         flags & FOLD_BLOCK_ACCUMULATE, ws, st);
+    FOLD_HIP_CHECK(hipGetLastError());
+    return FOLD_OK;
+  });
+}
+
+int32_t fold_linear(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, const void* x, const void* W,
+                    const float* bias, int32_t act, const void* residual, void* out, void* pre, hipStream_t st) {
+  return guarded([&]() -> int32_t {
+    const std::string who("fold_linear");
+    const int rc = check_linear(who, dtype, rows, in_dim, out_dim, linear_tiles);
+    if (rc != FOLD_OK) return rc;
+    if (act < FOLD_ACT_NONE || act > FOLD_ACT_GELU) return api_fail(FOLD_E_INVALID, who + ": unknown activation");
+    if (rows == 0) return FOLD_OK;
+    if (!x || !W || !out) return api_fail(FOLD_E_INVALID, who + ": NULL buffer");
+    if (misaligned(x) || misaligned(W) || misaligned(residual) || misaligned(out) || misaligned(pre))
+      return api_fail(FOLD_E_INVALID, who + ": matrices must be 16-byte aligned");
+    const size_t m = bytes_of(dtype, rows, out_dim);
+    const Span outs[] = {{out, m}, {pre, m}};
+    const Span in[] = {{x, bytes_of(dtype, rows, in_dim)}, {W, bytes_of(dtype, out_dim, in_dim)},
+                       {bias, vector_bytes(out_dim)}, {residual == out ? nullptr : residual, m}};
+    if (any_overlap(outs, 2, in, 4)) return api_fail(FOLD_E_INVALID, who + ": an output overlaps another buffer");
+    launch_linear(dtype, rows, in_dim, out_dim, x, W, bias, act, residual, out, pre, st);
+    FOLD_HIP_CHECK(hipGetLastError());
+    return FOLD_OK;
+  });
+}
+
+int32_t fold_linear_workspace_size(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, size_t* bytes) {
+  return guarded([&]() -> int32_t {
+    const std::string who("fold_linear_workspace_size");
+    if (!bytes) return api_fail(FOLD_E_INVALID, who + ": NULL argument");
+    const int rc = check_linear(who, dtype, rows, in_dim, out_dim, linear_backward_tiles);
+    if (rc != FOLD_OK) return rc;
+    *bytes = linear_backward_bytes(dtype, rows, in_dim, out_dim);
+    return FOLD_OK;
+  });
+}
+
+int32_t fold_linear_backward(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, const void* x, const void* W,
+                             int32_t act, const void* pre, const void* dout, void* dpre, int32_t dx_dtype, void* dx,
+                             int32_t dw_dtype, void* dW, float* dbias, int32_t flags, void* ws, size_t ws_bytes,
+                             hipStream_t st) {
+  return guarded([&]() -> int32_t {
+    const std::string who("fold_linear_backward");
+    const int rc = check_linear(who, dtype, rows, in_dim, out_dim, linear_backward_tiles);
+    if (rc != FOLD_OK) return rc;
+    if (act < FOLD_ACT_NONE || act > FOLD_ACT_GELU) return api_fail(FOLD_E_INVALID, who + ": unknown activation");
+    if (!grad_type(dx_dtype, dtype) || !grad_type(dw_dtype, dtype))
+      return api_fail(FOLD_E_INVALID, who + ": gradients are of the layer's type, or fp32");
+    if (flags & ~FOLD_BLOCK_ACCUMULATE) return api_fail(FOLD_E_INVALID, who + ": unknown flag");
+    if ((flags & FOLD_BLOCK_ACCUMULATE) && dW && dw_dtype != FOLD_F32)
+      return api_fail(FOLD_E_INVALID, who + ": a dW that is added to is fp32");
+    if ((!dx || rows == 0) && !dW && !dbias) return FOLD_OK;
+    const bool bent = act != FOLD_ACT_NONE;
+    if (rows > 0 && (!dout || (dW && !x) || (dx && !W) || (bent && (!pre || !dpre))))
+      return api_fail(FOLD_E_INVALID, who + ": NULL buffer");
+    if (!bent && (pre || dpre)) return api_fail(FOLD_E_INVALID, who + ": pre and dpre belong to an activation");
+    if (misaligned(x) || misaligned(W) || misaligned(pre) || misaligned(dout) || misaligned(dpre) || misaligned(dx) ||
+        misaligned(dW) || misaligned(ws))
+      return api_fail(FOLD_E_INVALID, who + ": matrices and the workspace must be 16-byte aligned");
+    const size_t need = linear_backward_bytes(dtype, rows, in_dim, out_dim);
+    if (need > 0 && (!ws || ws_bytes < need))
+      return api_fail(FOLD_E_MISMATCH, who + ": workspace smaller than fold_linear_workspace_size");
+    const size_t m = bytes_of(dtype, rows, out_dim);
+    const Span out[] = {{dpre, m}, {dx, bytes_of(dx_dtype, rows, in_dim)}, {dW, bytes_of(dw_dtype, out_dim, in_dim)},
+                        {dbias, vector_bytes(out_dim)}, {ws, need}};
+    const Span others[] = {{x, bytes_of(dtype, rows, in_dim)}, {W, bytes_of(dtype, out_dim, in_dim)},
+                           {dpre == pre ? nullptr : pre, m}, {dpre == dout ? nullptr : dout, m}};
+    // what dpre may be, the other outputs may not
+    const Span elementwise[] = {{pre, m}, {dout, m}};
+    if (any_overlap(out, 5, others, 4) || any_overlap(out + 1, 4, elementwise, 2))
+      return api_fail(FOLD_E_INVALID, who + ": an output overlaps another buffer");
+    launch_linear_backward(dtype, rows, in_dim, out_dim, x, W, act, pre, dout, dpre, dx_dtype, dx, dw_dtype, dW, dbias,
+                           flags & FOLD_BLOCK_ACCUMULATE, ws, st);
+    FOLD_HIP_CHECK(hipGetLastError());
+    return FOLD_OK;
+  });
+}
+
+}  // extern "C"

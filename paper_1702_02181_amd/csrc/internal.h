@@ -490,6 +490,24 @@ void launch_token(int dtype, const int* order, int64_t rows, int V, const void* 
                   const int* tokens, float* logp, float* entropy, int top_k, int* top_token, float* top_logp, void* ws,
                   hipStream_t st);
 
+// ---- the attention block (norm.hip, linear.hip) ----
+constexpr int kMaxLinear = 16384;  // a tile of a product is addressed by 32-bit offsets
+void launch_norm(int dtype, int64_t rows, int n, const void* x, const float* gamma, const float* beta, float eps, void* y,
+                 float* mean, float* rstd, hipStream_t st);
+size_t norm_backward_bytes(int dtype, int64_t rows, int n);
+void launch_norm_backward(int dtype, int64_t rows, int n, const void* x, const float* gamma, const float* mean,
+                          const float* rstd, int dy_dtype, const void* dy, int dx_dtype, const void* residual, void* dx,
+                          float* dgamma, float* dbeta, int add, void* ws, hipStream_t st);
+// workgroups of the largest launch of either direction
+int64_t linear_tiles(int dtype, int64_t rows, int in_dim, int out_dim);
+int64_t linear_backward_tiles(int dtype, int64_t rows, int in_dim, int out_dim);
+void launch_linear(int dtype, int64_t rows, int in_dim, int out_dim, const void* x, const void* W, const float* bias,
+                   int act, const void* residual, void* out, void* pre, hipStream_t st);
+size_t linear_backward_bytes(int dtype, int64_t rows, int in_dim, int out_dim);
+void launch_linear_backward(int dtype, int64_t rows, int in_dim, int out_dim, const void* x, const void* W, int act,
+                            const void* pre, const void* dout, void* dpre, int dx_dtype, void* dx, int dw_dtype, void* dW,
+                            float* dbias, int add, void* ws, hipStream_t st);
+
 // ---- achievable-peak probes (diag.hip) ----
 int32_t probe_mfma(int dtype, bool random_operands, hipStream_t st, double* tflops);
 int32_t probe_copy(void* dst, const void* src, size_t bytes, hipStream_t st, double* gbs);

@@ -10,8 +10,10 @@ The functions keep the ABI's names:
     fold_pack_params, fold_packed_free, fold_workspace_size,
     fold_forward, fold_backward, fold_row_ld, fold_last_error,
     fold_graph_create, fold_graph_launch, fold_graph_num_nodes, fold_graph_free,
-    fold_vocab_logits, fold_vocab_backward, fold_loss_distill, fold_token_logprobs
-``Schedule`` / ``Packed`` / ``StepGraph`` / ``VocabHead``, ``distill_loss`` and ``token_logprobs`` wrap them for tensors.
+    fold_vocab_logits, fold_vocab_backward, fold_loss_distill, fold_token_logprobs,
+    fold_layer_norm, fold_layer_norm_backward, fold_linear, fold_linear_backward
+``Schedule`` / ``Packed`` / ``StepGraph`` / ``VocabHead`` / ``Linear``, ``distill_loss``, ``token_logprobs``,
+``layer_norm`` and ``layer_norm_backward`` wrap them for tensors.
 """
 from __future__ import annotations
 
@@ -119,6 +121,9 @@ class fold_step_buffers(ctypes.Structure):
 
 FOLD_STEP_BACKWARD, FOLD_STEP_ZERO_GRADS = 1, 2
 FOLD_VOCAB_ACCUMULATE = 1
+FOLD_ACT_NONE, FOLD_ACT_RELU, FOLD_ACT_TANH, FOLD_ACT_GELU = 0, 1, 2, 3
+FOLD_BLOCK_ACCUMULATE = 1
+ACTIVATIONS = {"none": FOLD_ACT_NONE, "relu": FOLD_ACT_RELU, "tanh": FOLD_ACT_TANH, "gelu": FOLD_ACT_GELU}
 
 
 class fold_kernel_stat(ctypes.Structure):
@@ -146,7 +151,8 @@ EXPORTS = ["fold_schedule", "fold_sched_get_info", "fold_sched_free", "fold_pack
            "fold_dropout_mask", "fold_forward_noalloc", "fold_schedule_typed", "fold_typed_sched_get_info",
            "fold_typed_sched_free", "fold_level_launches", "fold_trim", "fold_vocab_logits", "fold_vocab_backward",
            "fold_vocab_workspace_size", "fold_loss_distill", "fold_distill_workspace_size", "fold_token_logprobs",
-           "fold_token_workspace_size"]
+           "fold_token_workspace_size", "fold_layer_norm", "fold_layer_norm_workspace_size", "fold_layer_norm_backward",
+           "fold_linear", "fold_linear_workspace_size", "fold_linear_backward"]
 
 _lib = None
 
@@ -257,6 +263,24 @@ def lib():
     L.fold_token_logprobs.restype = c_int32
     L.fold_token_logprobs.argtypes = [c_void_p, c_int32, c_int64, c_int32, c_void_p, c_int32, c_void_p, c_void_p,
                                       c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    L.fold_layer_norm.restype = c_int32
+    L.fold_layer_norm.argtypes = [c_int32, c_int64, c_int32, c_void_p, c_void_p, c_void_p, ctypes.c_float, c_void_p,
+                                  c_void_p, c_void_p, c_void_p]
+    L.fold_layer_norm_workspace_size.restype = c_int32
+    L.fold_layer_norm_workspace_size.argtypes = [c_int32, c_int64, c_int32, POINTER(c_size_t)]
+    L.fold_layer_norm_backward.restype = c_int32
+    L.fold_layer_norm_backward.argtypes = [c_int32, c_int64, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_int32,
+                                           c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p,
+                                           c_size_t, c_void_p]
+    L.fold_linear.restype = c_int32
+    L.fold_linear.argtypes = [c_int32, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p,
+                              c_void_p, c_void_p, c_void_p]
+    L.fold_linear_workspace_size.restype = c_int32
+    L.fold_linear_workspace_size.argtypes = [c_int32, c_int64, c_int32, c_int32, POINTER(c_size_t)]
+    L.fold_linear_backward.restype = c_int32
+    L.fold_linear_backward.argtypes = [c_int32, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
+                                       c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_void_p,
+                                       c_size_t, c_void_p]
     _lib = L
     return L
 
@@ -439,6 +463,42 @@ def fold_token_logprobs(sched, dtype, rows, vocab, logits, num_tokens, tokens, l
     _check(lib().fold_token_logprobs(sched, int(dtype), int(rows), int(vocab), _ptr(logits), int(num_tokens),
                                      _ptr(tokens), _ptr(logp), _ptr(entropy), int(top_k), _ptr(top_token),
                                      _ptr(top_logp), _ptr(ws), int(ws_bytes), _stream(stream)))
+
+
+def fold_layer_norm(dtype, rows, width, x, gamma, beta, eps, y, mean, rstd, stream=None):
+    _check(lib().fold_layer_norm(int(dtype), int(rows), int(width), _ptr(x), _ptr(gamma), _ptr(beta), float(eps), _ptr(y),
+                                 _ptr(mean), _ptr(rstd), _stream(stream)))
+
+
+def fold_layer_norm_workspace_size(dtype, rows, width) -> int:
+    n = c_size_t()
+    _check(lib().fold_layer_norm_workspace_size(int(dtype), int(rows), int(width), byref(n)))
+    return int(n.value)
+
+
+def fold_layer_norm_backward(dtype, rows, width, x, gamma, mean, rstd, dy_dtype, dy, dx_dtype, residual, dx, dgamma, dbeta,
+                             flags, ws, ws_bytes, stream=None):
+    _check(lib().fold_layer_norm_backward(int(dtype), int(rows), int(width), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd),
+                                          int(dy_dtype), _ptr(dy), int(dx_dtype), _ptr(residual), _ptr(dx), _ptr(dgamma),
+                                          _ptr(dbeta), int(flags), _ptr(ws), int(ws_bytes), _stream(stream)))
+
+
+def fold_linear(dtype, rows, in_dim, out_dim, x, W, bias, act, residual, out, pre, stream=None):
+    _check(lib().fold_linear(int(dtype), int(rows), int(in_dim), int(out_dim), _ptr(x), _ptr(W), _ptr(bias), int(act),
+                             _ptr(residual), _ptr(out), _ptr(pre), _stream(stream)))
+
+
+def fold_linear_workspace_size(dtype, rows, in_dim, out_dim) -> int:
+    n = c_size_t()
+    _check(lib().fold_linear_workspace_size(int(dtype), int(rows), int(in_dim), int(out_dim), byref(n)))
+    return int(n.value)
+
+
+def fold_linear_backward(dtype, rows, in_dim, out_dim, x, W, act, pre, dout, dpre, dx_dtype, dx, dw_dtype, dW, dbias, flags,
+                         ws, ws_bytes, stream=None):
+    _check(lib().fold_linear_backward(int(dtype), int(rows), int(in_dim), int(out_dim), _ptr(x), _ptr(W), int(act),
+                                      _ptr(pre), _ptr(dout), _ptr(dpre), int(dx_dtype), _ptr(dx), int(dw_dtype), _ptr(dW),
+                                      _ptr(dbias), int(flags), _ptr(ws), int(ws_bytes), _stream(stream)))
 
 
 def fold_packed_free(handle):
@@ -902,3 +962,145 @@ def token_logprobs(logits, vocab, tokens=None, top_k=0, entropy=True, sched=None
         fold_token_logprobs(None if sched is None else sched.handle, code, rows, vocab, logits, J, tokens, out.logp,
                             out.entropy, top_k, out.top_token, out.top_logp, ws, n, stream or _CURRENT)
     return out
+
+
+# ----------------------------------------------------------------------------- the attention block
+
+_norm_ws = functools.lru_cache(256)(fold_layer_norm_workspace_size)
+_linear_ws = functools.lru_cache(256)(fold_linear_workspace_size)
+
+
+def _bytes(n, device):
+    import torch
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def layer_norm(x, width, gamma=None, beta=None, eps=1e-5, stats=True, out=None, stream=None):
+    """(y, mean [rows], rstd [rows]) of fold_layer_norm for x [rows, fold_row_ld(width)]; without stats the last two are
+    None.  gamma, beta: [width] float32 or None.  out: a tensor to write, x itself for one."""
+    import torch
+    _matrix("x", x, width)
+    code, rows = _code(x.dtype), x.shape[0]
+    for name, t in (("gamma", gamma), ("beta", beta)):
+        if t is not None:
+            _vector(name, t, torch.float32, width)
+    with _on(stream):
+        out = torch.empty_like(x) if out is None else _matrix("out", out, width, x.dtype, rows)
+        mean = torch.empty(rows, dtype=torch.float32, device=x.device) if stats else None
+        rstd = torch.empty(rows, dtype=torch.float32, device=x.device) if stats else None
+        fold_layer_norm(code, rows, width, x, gamma, beta, eps, out, mean, rstd, stream or _CURRENT)
+    return out, mean, rstd
+
+
+def layer_norm_backward(x, width, dy, mean, rstd, gamma=None, residual=None, dx=True, dgamma=True, dbeta=True, dtype=None,
+                        accumulate=False, stream=None):
+    """(dx, dgamma, dbeta) of fold_layer_norm_backward.  dy: of x's type or float32; residual: a gradient that goes by the
+    norm, added to dx, of dx's type.  Each of the three: True for a new tensor (dx of `dtype`, the residual's or x's type by
+    default), a tensor to write, or None to leave it out.  accumulate: dgamma and dbeta are added to the tensors given."""
+    import torch
+    _matrix("x", x, width)
+    rows = x.shape[0]
+    _matrix("dy", dy, width, None, rows)
+    _vector("mean", mean, torch.float32, rows)
+    _vector("rstd", rstd, torch.float32, rows)
+    if gamma is not None:
+        _vector("gamma", gamma, torch.float32, width)
+    if accumulate and (dgamma is True or dbeta is True):
+        raise ValueError("accumulate needs the dgamma and dbeta to add to (or None)")
+    f32 = dict(dtype=torch.float32, device=x.device)
+    with _on(stream):
+        if dx is True:
+            dx = torch.empty(x.shape, dtype=dtype or (x.dtype if residual is None else residual.dtype), device=x.device)
+        elif dx is not None:
+            _matrix("dx", dx, width, dtype, rows)
+        if residual is not None and dx is not None:
+            _matrix("residual", residual, width, dx.dtype, rows)
+        dgamma = torch.empty(width, **f32) if dgamma is True else dgamma
+        dbeta = torch.empty(width, **f32) if dbeta is True else dbeta
+        for name, t in (("dgamma", dgamma), ("dbeta", dbeta)):
+            if t is not None:
+                _vector(name, t, torch.float32, width)
+        code = _code(x.dtype)
+        n = _norm_ws(code, rows, width) if dgamma is not None or dbeta is not None else 0
+        ws = _bytes(n, x.device)
+        fold_layer_norm_backward(code, rows, width, x, gamma, mean, rstd, _code(dy.dtype), dy,
+                                 code if dx is None else _code(dx.dtype), residual, dx, dgamma, dbeta,
+                                 FOLD_BLOCK_ACCUMULATE if accumulate else 0, ws, n, stream or _CURRENT)
+    return dx, dgamma, dbeta
+
+
+class Linear:
+    """The layer out = act(x W^T + bias) + residual (fold_linear, fold_linear_backward).
+
+    weight: [out_dim, fold_row_ld(in_dim)], float32 or bfloat16; bias: [out_dim] float32 or None; activation: "none", "relu",
+    "tanh" or "gelu".  Results and workspaces are new tensors of the calls' stream."""
+
+    def __init__(self, weight, bias=None, in_dim=None, activation="none"):
+        import torch
+        self.in_dim = int(weight.shape[1] if in_dim is None else in_dim)
+        self.weight = _matrix("weight", weight, self.in_dim)
+        self.out_dim, self.dtype = int(weight.shape[0]), weight.dtype
+        self.code = _code(weight.dtype)
+        self.bias = None if bias is None else _vector("bias", bias, torch.float32, self.out_dim)
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation: one of {sorted(ACTIVATIONS)}, got {activation!r}")
+        self.act = ACTIVATIONS[activation]
+
+    def forward(self, x, residual=None, pre=None, out=None, stream=None):
+        """out [rows, fold_row_ld(out_dim)] for x [rows, fold_row_ld(in_dim)]; with pre (True, or a tensor to write) a pair
+        of it and the values before the activation, which backward() needs of a layer that has one."""
+        import torch
+        _matrix("x", x, self.in_dim, self.dtype)
+        _here("weight", self.weight)
+        rows = x.shape[0]
+        if residual is not None:
+            _matrix("residual", residual, self.out_dim, self.dtype, rows)
+        shape, ret = (rows, _row_ld(self.out_dim)), pre is not None and pre is not False
+        with _on(stream):
+            new = lambda: torch.empty(shape, dtype=self.dtype, device=x.device)  # noqa: E731
+            out = new() if out is None else _matrix("out", out, self.out_dim, self.dtype, rows)
+            pre = None if not ret else new() if pre is True else _matrix("pre", pre, self.out_dim, self.dtype, rows)
+            fold_linear(self.code, rows, self.in_dim, self.out_dim, x, self.weight, self.bias, self.act, residual, out, pre,
+                        stream or _CURRENT)
+        return (out, pre) if ret else out
+
+    def backward(self, x, dout, pre=None, dx=True, dW=True, dbias=True, dpre=None, dx_dtype=None, dw_dtype=None,
+                 accumulate=False, stream=None):
+        """(dx, dW, dbias) of `dout` [rows, fold_row_ld(out_dim)].  Each of the three: True for a new tensor (dx of dx_dtype,
+        dW of dw_dtype; float32 by default), a tensor to write, or None to leave it out.  pre: what forward() gave (a layer
+        with an activation); dpre: a tensor for the gradient there (pre or dout itself, for one).  accumulate: dW and dbias
+        are added to the tensors given."""
+        import torch
+        _matrix("x", x, self.in_dim, self.dtype)
+        _here("weight", self.weight)
+        rows = x.shape[0]
+        _matrix("dout", dout, self.out_dim, self.dtype, rows)
+        if accumulate and (dW is True or dbias is True):
+            raise ValueError("accumulate needs the dW and dbias to add to (or None)")
+        if (self.act != FOLD_ACT_NONE) != (pre is not None):
+            raise ValueError("pre: what forward() gave, for a layer with an activation")
+        with _on(stream):
+            if dx is True:
+                dx = torch.empty(x.shape, dtype=dx_dtype or torch.float32, device=x.device)
+            elif dx is not None:
+                _matrix("dx", dx, self.in_dim, dx_dtype, rows)
+            if dW is True:
+                dW = torch.empty(self.weight.shape, dtype=dw_dtype or torch.float32, device=x.device)
+            elif dW is not None:
+                _matrix("dW", dW, self.in_dim, dw_dtype, self.out_dim)
+            if dbias is True:
+                dbias = torch.empty(self.out_dim, dtype=torch.float32, device=x.device)
+            elif dbias is not None:
+                _vector("dbias", dbias, torch.float32, self.out_dim)
+            if pre is not None:
+                _matrix("pre", pre, self.out_dim, self.dtype, rows)
+                dpre = torch.empty_like(pre) if dpre is None else _matrix("dpre", dpre, self.out_dim, self.dtype, rows)
+            elif dpre is not None:
+                raise ValueError("dpre belongs to a layer with an activation")
+            n = _linear_ws(self.code, rows, self.in_dim, self.out_dim)
+            ws = _bytes(n, x.device)
+            fold_linear_backward(self.code, rows, self.in_dim, self.out_dim, x, self.weight, self.act, pre, dout, dpre,
+                                 FOLD_F32 if dx is None else _code(dx.dtype), dx,
+                                 FOLD_F32 if dW is None else _code(dW.dtype), dW, dbias,
+                                 FOLD_BLOCK_ACCUMULATE if accumulate else 0, ws, n, stream or _CURRENT)
+        return dx, dW, dbias
