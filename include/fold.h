@@ -723,6 +723,76 @@ int32_t fold_linear_backward(int32_t dtype, int64_t rows, int32_t in_dim, int32_
                              int32_t dw_dtype, void* dW, float* dbias, int32_t flags, void* ws, size_t ws_bytes,
                              hipStream_t stream);
 
+/* Cross attention: the rows of query sequences (a decoder's nodes) against
+ * those of key sequences of other lengths (an encoder's nodes).  Per query row
+ * and head, over the keys j of its sequence's source that count,
+ *     s_j = scale q . k_j,   p = softmax(s),   o = sum_j p_j v_j,
+ *     lse = log sum_j exp(s_j);
+ * without such a key o = 0 and lse = -inf, and the row takes no part in any
+ * gradient.  Heads are columns: head h is columns [h head_dim, (h+1) head_dim)
+ * of q and of the output, and reads key head h / (heads / kv_heads).
+ *
+ * fold_cross_create checks the lists, lays the work out and returns a plan,
+ * which may be used by any number of calls, concurrent ones too (with a
+ * workspace each).  It synchronises `stream` and must not be captured.
+ *   query_ptr   device [num_seqs + 1]: sequence b is list entries query_ptr[b]
+ *               .. query_ptr[b+1] - 1; starts at 0, ends at num_queries
+ *   query_row   device [num_queries]: the row of a list entry in the query
+ *               matrices, below num_query_rows, each at most once; NULL: row i
+ *               is entry i.  With a schedule: its graph_ptr and node_pos.
+ *   key_ptr, key_row   the same for num_sources key sequences
+ *   source      device [num_seqs]: the key sequence that a query sequence reads
+ *               (several may read one), -1: none; NULL: b reads b
+ * The lists are copied.  FOLD_E_INVALID for sizes out of range (heads to 1,024,
+ * head_dim to 128, heads / kv_heads to 256, queries times heads below 2^31) and
+ * for malformed lists, rows out of range or listed twice.
+ * fold_cross_free waits as fold_sched_free does. */
+typedef struct fold_cross fold_cross;
+typedef struct {
+  int32_t dtype; /* of all matrices: FOLD_F32 or FOLD_BF16 */
+  int32_t heads, kv_heads, head_dim;
+  int32_t num_seqs, num_sources;
+  int32_t num_queries, num_keys;        /* list entries */
+  int32_t num_query_rows, num_key_rows; /* rows of the matrices */
+  const int32_t *query_ptr, *query_row, *key_ptr, *key_row, *source;
+} fold_cross_batch;
+
+int32_t fold_cross_create(const fold_cross_batch* batch, hipStream_t stream, fold_cross** out);
+int32_t fold_cross_free(fold_cross* cross);
+int32_t fold_cross_workspace_size(const fold_cross* cross, size_t* fwd_bytes, size_t* bwd_bytes);
+
+/* The matrices have strides of their own (ld*, in elements, at least their
+ * width), so k and v may be columns of one matrix; they need the alignment of
+ * their elements alone (rows of 16-byte multiples at 16-byte addresses are
+ * faster).  Rows that no list names, and columns beyond the heads, are neither
+ * read nor written.
+ *   q        device [num_query_rows, ldq], heads * head_dim columns
+ *   k, v     device [num_key_rows, ldk], [.., ldv], kv_heads * head_dim columns
+ *   key_mask device [num_keys] bytes in LIST order (a schedule's node order),
+ *            0: the key does not count, whatever its row holds; NULL: all count
+ *   scale    finite, above 0; scores are below 1e9 in magnitude
+ *   out      device [num_query_rows, ldo] of dtype
+ *   lse      device [num_query_rows, heads] fp32, or NULL
+ * fold_cross_backward: the gradients of q, k and v from dout; out and lse as
+ * left by fold_cross_attend.  dq, dk, dv (of dtype, any of them NULL) have the
+ * shapes of q, k and v; listed rows are written (a key that does not count and
+ * a source that nobody reads get 0).  dk and dv are summed over the heads of a
+ * group and over the sequences that read a source, without atomics.
+ * For bf16 the probabilities, and in the gradient the scores' gradients, are
+ * rounded to bf16 where they enter a matrix product; everything else is fp32.
+ * FOLD_E_INVALID for NULL buffers, strides below the width, addresses that are
+ * no multiple of an element's size, a scale out of range or an output that
+ * overlaps another buffer; FOLD_E_MISMATCH for a workspace (16-byte aligned)
+ * that is too small or a plan of another device. */
+int32_t fold_cross_attend(const fold_cross* cross, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                          const void* v, int64_t ldv, const uint8_t* key_mask, float scale, void* out, int64_t ldo,
+                          float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+int32_t fold_cross_backward(const fold_cross* cross, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                            const void* v, int64_t ldv, const uint8_t* key_mask, float scale, const void* out,
+                            int64_t ldo, const float* lse, const void* dout, int64_t lddo, void* dq, int64_t lddq,
+                            void* dk, int64_t lddk, void* dv, int64_t lddv, void* ws, size_t ws_bytes,
+                            hipStream_t stream);
+
 /* ---- a whole step as one HIP graph ----------------------------------------
  * The level loop (Section 2: one batched iteration per depth, so a batch of
  * depth D costs O(D) launches instead of one per node) still issues a few

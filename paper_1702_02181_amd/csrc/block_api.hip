@@ -1,4 +1,4 @@
-// C ABI of the attention block: argument checks of layer norm and the linear layers.
+// C ABI of the attention block: argument checks of layer norm, the linear layers and cross attention.
 
 #include <hip/hip_runtime.h>
 
@@ -7,6 +7,7 @@
 
 #include "checks.h"
 #include "common.h"
+#include "cross.h"
 #include "internal.h"
 
 using namespace fold;
@@ -31,6 +32,23 @@ int check_linear(const std::string& who, int dtype, int64_t rows, int in_dim, in
   if (tiles(dtype, rows, in_dim, out_dim) >= kMaxTiles)
     return api_fail(FOLD_E_INVALID, who + ": too many tiles for one launch (rows times the widths)");
   return FOLD_OK;
+}
+
+// A matrix of cross attention: columns of rows that are ld elements apart.
+struct Cols {
+  const void* p;
+  int64_t ld, rows;
+  int width;  // elements
+};
+// Whether two of them share an element.  Different columns of rows with one stride (k and v side by side) do not.
+bool share(const Cols& a, const Cols& b, int es) {
+  const auto bytes = [&](const Cols& c) { return c.rows > 0 ? (size_t)((c.rows - 1) * c.ld + c.width) * es : (size_t)0; };
+  if (!overlap({a.p, bytes(a)}, {b.p, bytes(b)})) return false;
+  if (a.ld != b.ld) return true;
+  if (reinterpret_cast<uintptr_t>(b.p) < reinterpret_cast<uintptr_t>(a.p)) return share(b, a, es);
+  const int64_t row = a.ld * es;
+  const int64_t d = (int64_t)((reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)) % (uintptr_t)row);
+  return !(d >= (int64_t)a.width * es && d + (int64_t)b.width * es <= row);
 }
 
 // a gradient's type: the operator's own, or fp32
@@ -174,6 +192,127 @@ int32_t fold_linear_backward(int32_t dtype, int64_t rows, int32_t in_dim, int32_
       return api_fail(FOLD_E_INVALID, who + ": an output overlaps another buffer");
     launch_linear_backward(dtype, rows, in_dim, out_dim, x, W, act, pre, dout, dpre, dx_dtype, dx, dw_dtype, dW, dbias,
                            flags & FOLD_BLOCK_ACCUMULATE, ws, st);
+    FOLD_HIP_CHECK(hipGetLastError());
+    return FOLD_OK;
+  });
+}
+
+int32_t fold_cross_create(const fold_cross_batch* batch, hipStream_t st, fold_cross** out) {
+  return guarded([&]() -> int32_t {
+    if (!out) return api_fail(FOLD_E_INVALID, "fold_cross_create: out is NULL");
+    *out = nullptr;
+    if (!batch) return api_fail(FOLD_E_INVALID, "fold_cross_create: batch is NULL");
+    return cross_create(batch, st, out);
+  });
+}
+
+int32_t fold_cross_free(fold_cross* cross) {
+  return guarded([&]() -> int32_t {
+    cross_destroy(cross);
+    return FOLD_OK;
+  });
+}
+
+int32_t fold_cross_workspace_size(const fold_cross* cross, size_t* fwd_bytes, size_t* bwd_bytes) {
+  return guarded([&]() -> int32_t {
+    if (!cross || !fwd_bytes || !bwd_bytes) return api_fail(FOLD_E_INVALID, "fold_cross_workspace_size: NULL argument");
+    *fwd_bytes = cross_forward_bytes(cross->c);
+    *bwd_bytes = cross_backward_bytes(cross->c);
+    return FOLD_OK;
+  });
+}
+
+}  // extern "C"
+
+namespace {
+
+// the checks that both directions share
+int check_cross(const std::string& who, const fold_cross* cross, const Cols* in, int nin, const Cols* out, int nout,
+                const uint8_t* mask, float scale, const void* stats, const void* ws, size_t need, size_t ws_bytes,
+                bool stats_written) {
+  const Cross& c = cross->c;
+  int dev = -1;
+  FOLD_HIP_CHECK(hipGetDevice(&dev));
+  if (dev != c.device) return api_fail(FOLD_E_MISMATCH, who + ": the plan belongs to another device");
+  if (!(scale > 0.f) || !std::isfinite(scale)) return api_fail(FOLD_E_INVALID, who + ": scale must be finite and above 0");
+  const int es = c.dtype == FOLD_BF16 ? 2 : 4;
+  const auto bad = [&](const Cols& m, bool needed) {
+    if (!m.p) return needed && m.rows > 0;
+    return m.ld < m.width || m.ld > INT32_MAX || (reinterpret_cast<uintptr_t>(m.p) & (es - 1)) != 0;
+  };
+  for (int i = 0; i < nin; ++i)
+    if (bad(in[i], true)) return api_fail(FOLD_E_INVALID, who + ": NULL or misaligned matrix, or a stride below its width");
+  for (int i = 0; i < nout; ++i)
+    if (bad(out[i], false)) return api_fail(FOLD_E_INVALID, who + ": misaligned output, or a stride below its width");
+  if (misaligned(ws)) return api_fail(FOLD_E_INVALID, who + ": the workspace must be 16-byte aligned");
+  if (need > 0 && (!ws || ws_bytes < need))
+    return api_fail(FOLD_E_MISMATCH, who + ": workspace smaller than fold_cross_workspace_size");
+  const Cols lists{mask, 1, c.num_keys, 1};
+  const Cols scratch{ws, 1, (int64_t)need, 1};
+  const Cols stat{stats, c.heads, c.query_rows, c.heads};
+  const auto meets = [&](const Cols& a, int ea, const Cols& b, int eb) {  // as plain runs of bytes
+    const auto bytes = [](const Cols& m, int e) { return m.rows > 0 ? (size_t)((m.rows - 1) * m.ld + m.width) * e : (size_t)0; };
+    return overlap({a.p, bytes(a, ea)}, {b.p, bytes(b, eb)});
+  };
+  for (int i = 0; i < nout; ++i) {
+    for (int j = i + 1; j < nout; ++j)
+      if (out[j].p && out[i].p && share(out[i], out[j], es)) return api_fail(FOLD_E_INVALID, who + ": outputs overlap");
+    for (int j = 0; j < nin; ++j)
+      if (out[i].p && in[j].p && share(out[i], in[j], es))
+        return api_fail(FOLD_E_INVALID, who + ": an output overlaps another buffer");
+    if (meets(out[i], es, lists, 1) || meets(out[i], es, scratch, 1) || meets(out[i], es, stat, 4))
+      return api_fail(FOLD_E_INVALID, who + ": an output overlaps another buffer");
+  }
+  for (int j = 0; j < nin; ++j)
+    if (meets(in[j], es, scratch, 1) || (stats_written && meets(in[j], es, stat, 4)))
+      return api_fail(FOLD_E_INVALID, who + ": an output overlaps another buffer");
+  if (meets(lists, 1, scratch, 1) || meets(stat, 4, scratch, 1) || (stats_written && meets(stat, 4, lists, 1)))
+    return api_fail(FOLD_E_INVALID, who + ": an output overlaps another buffer");
+  return FOLD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t fold_cross_attend(const fold_cross* cross, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+                          int64_t ldv, const uint8_t* key_mask, float scale, void* out, int64_t ldo, float* lse, void* ws,
+                          size_t ws_bytes, hipStream_t st) {
+  return guarded([&]() -> int32_t {
+    const std::string who("fold_cross_attend");
+    if (!cross) return api_fail(FOLD_E_INVALID, who + ": cross is NULL");
+    const Cross& c = cross->c;
+    const int wq = c.heads * c.head_dim, wk = c.kv_heads * c.head_dim;
+    const Cols in[] = {{q, ldq, c.query_rows, wq}, {k, ldk, c.key_rows, wk}, {v, ldv, c.key_rows, wk}};
+    const Cols outs[] = {{out, ldo, c.query_rows, wq}};
+    const int rc = check_cross(who, cross, in, 3, outs, 1, key_mask, scale, lse, ws, cross_forward_bytes(c), ws_bytes, true);
+    if (rc != FOLD_OK) return rc;
+    if (c.num_queries == 0) return FOLD_OK;
+    if (!out) return api_fail(FOLD_E_INVALID, who + ": NULL buffer");
+    launch_cross(c, {q, ldq}, {k, ldk}, {v, ldv}, key_mask, scale, out, ldo, lse, ws, st);
+    FOLD_HIP_CHECK(hipGetLastError());
+    return FOLD_OK;
+  });
+}
+
+int32_t fold_cross_backward(const fold_cross* cross, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v,
+                            int64_t ldv, const uint8_t* key_mask, float scale, const void* out, int64_t ldo,
+                            const float* lse, const void* dout, int64_t lddo, void* dq, int64_t lddq, void* dk, int64_t lddk,
+                            void* dv, int64_t lddv, void* ws, size_t ws_bytes, hipStream_t st) {
+  return guarded([&]() -> int32_t {
+    const std::string who("fold_cross_backward");
+    if (!cross) return api_fail(FOLD_E_INVALID, who + ": cross is NULL");
+    const Cross& c = cross->c;
+    if (!dq && !dk && !dv) return FOLD_OK;
+    const int wq = c.heads * c.head_dim, wk = c.kv_heads * c.head_dim;
+    const Cols in[] = {{q, ldq, c.query_rows, wq}, {k, ldk, c.key_rows, wk}, {v, ldv, c.key_rows, wk},
+                       {out, ldo, c.query_rows, wq}, {dout, lddo, c.query_rows, wq}};
+    const Cols outs[] = {{dq, lddq, c.query_rows, wq}, {dk, lddk, c.key_rows, wk}, {dv, lddv, c.key_rows, wk}};
+    const int rc = check_cross(who, cross, in, 5, outs, 3, key_mask, scale, lse, ws, cross_backward_bytes(c), ws_bytes, false);
+    if (rc != FOLD_OK) return rc;
+    if (c.num_queries > 0 && !lse) return api_fail(FOLD_E_INVALID, who + ": NULL lse");
+    launch_cross_backward(c, {q, ldq}, {k, ldk}, {v, ldv}, key_mask, scale, {out, ldo}, lse, {dout, lddo}, dq, lddq, dk, lddk,
+                          dv, lddv, ws, st);
     FOLD_HIP_CHECK(hipGetLastError());
     return FOLD_OK;
   });

@@ -1,0 +1,1013 @@
+// Cross attention on the matrix cores (gfx950), forward and backward.
+//     s = scale q k^T,  p = softmax(s) over the keys that count,  o = p v,  lse = log sum exp s
+//     delta = sum_d do o,  dp = do v^T,  ds = p (dp - delta),  dq = scale ds k,  dk = scale ds^T q,  dv = p^T do
+// Rows are gathered by index into LDS by direct loads; a masked key's, and what lies past the end, come from a block of zeros.
+//
+// Products are 32 x 32 tiles with the axis of the softmax on the accumulators' rows: the forward computes s^T = k q^T, so a
+// lane holds one query's column, its maximum, sum and rescaling are one value a lane, and p^T leaves the accumulators in the
+// layout of the next product's operand: its K values (keys) are permuted, 4 h + 0..3 and 8 + 4 h + 0..3 of 16 for half wave h,
+// and v's fragments are read in the same order.  The keys' gradient holds keys on the lanes and does the same along the
+// queries.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "common.h"
+#include "cross.h"
+#include "dma.h"
+#include "internal.h"
+#include "mfma.h"
+
+namespace fold {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __attribute__((aligned(16))) uint32_t g_zero[4];
+
+#define FOLD_LDS_AS __attribute__((address_space(3)))
+typedef __attribute__((__vector_size__(4 * sizeof(__bf16)))) __bf16 bf16x4_t;
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
+}
+__device__ __forceinline__ float word(const uint4& v, int e) {
+  return __uint_as_float(e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w);
+}
+// the value of the other half wave's lane of the same column, with this lane's
+__device__ __forceinline__ float halves_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float halves_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// LDS that only this wave reads and writes: its direct loads have landed (vm_wait), its reads before them are done
+__device__ __forceinline__ void wave_barrier_lds() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// ---- tiles in LDS ---------------------------------------------------------------------------------------------------
+
+// A row of a tile is U 16-byte units; unit u of row r lies at r U + (u ^ f(r)).  f puts the same unit of 16 consecutive rows
+// into 16 different bank groups (16-byte reads along the rows), and 64 bytes of 4 consecutive rows into different quarters of
+// the banks (transposing reads across them).
+template <int U>
+__device__ __forceinline__ int swizzle(int r) {
+  if constexpr (U % 16 == 0) return ((r & 3) << 2) | ((r >> 2) & 3);
+  else if constexpr (U % 8 == 0) return ((r & 2) << 1) | ((r >> 2) & 3);
+  else return (r >> 2) & 3;  // 4, 12
+}
+template <int U>
+__device__ __forceinline__ int unit_at(int r, int u) {
+  return (r * U + (u ^ swizzle<U>(r))) * 16;
+}
+
+// acc += A B for one step of 32 bytes of K (16 bf16 or 8 fp32 values; a half wave's 16 bytes are its own)
+template <typename T>
+__device__ __forceinline__ f32x16 step_mma(const uint4& a, const uint4& b, f32x16 c) {
+  if constexpr (sizeof(T) == 2) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(word(a, e), word(b, e), c, 0, 0, 0);
+  }
+  return c;
+}
+
+// What leaves an accumulator as the next product's operand: 32 K values (the accumulator's rows) of the lane's column.
+template <typename T>
+struct Probs;
+template <>
+struct Probs<uint16_t> {
+  uint4 v[2];
+  __device__ __forceinline__ explicit Probs(const f32x16& p) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      v[t] = make_uint4(bf16_pair(p[8 * t], p[8 * t + 1]), bf16_pair(p[8 * t + 2], p[8 * t + 3]),
+                        bf16_pair(p[8 * t + 4], p[8 * t + 5]), bf16_pair(p[8 * t + 6], p[8 * t + 7]));
+  }
+};
+template <>
+struct Probs<float> {
+  f32x16 v;
+  __device__ __forceinline__ explicit Probs(const f32x16& p) : v(p) {}
+};
+
+// acc[db] += X^T P: X the tile's rows k0 .. k0 + 31 (K), its columns 32 db .. on the accumulators' rows
+template <typename T, int U, int DB>
+__device__ __forceinline__ void across_mma(const char* tile, int k0, const Probs<T>& p, f32x16 (&acc)[DB], int lane) {
+  const int h = lane >> 5, l32 = lane & 31;
+  if constexpr (sizeof(T) == 2) {
+    const int g = lane >> 4, gi = lane & 15;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int k = k0 + 16 * t + 4 * h + (gi >> 2);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const int col = 32 * db + 16 * (g & 1) + 4 * (gi & 3);
+        const int in = (col & 7) * 2, u = col >> 3;
+        const bf16x4_t lo =
+            __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FOLD_LDS_AS bf16x4_t*)(tile + unit_at<U>(k, u) + in));
+        const bf16x4_t hi =
+            __builtin_amdgcn_ds_read_tr16_b64_v4bf16((FOLD_LDS_AS bf16x4_t*)(tile + unit_at<U>(k + 8, u) + in));
+        const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(a.x, a.y, b.x, b.y)),
+                                                          __builtin_bit_cast(bf16x8, p.v[t]), acc[db], 0, 0, 0);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int k = k0 + 8 * (r >> 2) + 4 * h + (r & 3);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const float a = *reinterpret_cast<const float*>(tile + unit_at<U>(k, 8 * db + (l32 >> 2)) + (l32 & 3) * 4);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p.v[r], acc[db], 0, 0, 0);
+      }
+    }
+  }
+}
+
+// 16 bytes of a row from element e0 (d elements are there), zero past its end
+template <typename T, bool VEC>
+__device__ __forceinline__ uint4 row_unit(const T* row, int e0, int d) {
+  constexpr int E = 16 / (int)sizeof(T);
+  uint4 v = make_uint4(0, 0, 0, 0);
+  if constexpr (VEC) {
+    if (e0 < d) v = *reinterpret_cast<const uint4*>(row + e0);
+  } else {
+    T e[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) e[i] = e0 + i < d ? row[e0 + i] : T(0);
+    v = *reinterpret_cast<const uint4*>(e);
+  }
+  return v;
+}
+
+// One wave's share of the loads of a tile of ROWS rows that NW waves load together: NI instructions of 1 KB.
+template <typename T, int DP, int ROWS, int NW, bool VEC>
+struct TileLoader {
+  static constexpr int U = DP * (int)sizeof(T) / 16, E = 16 / (int)sizeof(T), NI = ROWS * U / (64 * NW);
+  static_assert(NI * 64 * NW == ROWS * U, "whole instructions");
+  int part, lane;
+  __device__ __forceinline__ TileLoader(int part_, int lane_) : part(part_), lane(lane_) {}
+  __device__ __forceinline__ int place(int i) const { return (part * NI + i) * 64 + lane; }
+  __device__ __forceinline__ int row(int i) const { return place(i) / U; }
+  __device__ __forceinline__ int unit(int i) const { return place(i) % U ^ swizzle<U>(row(i)); }
+  // idx[i]: the matrix row of tile row row(i), -1: zeros
+  __device__ __forceinline__ void load(const T* base, int64_t ld, int d, const int (&idx)[NI], char* lds) const {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int e0 = unit(i) * E;
+        const void* src = idx[i] >= 0 && e0 < d ? static_cast<const void*>(base + (int64_t)idx[i] * ld + e0)
+                                                : static_cast<const void*>(g_zero);
+        dma16_untracked(src, lds + (part * NI + i) * 1024);
+      }
+    } else {
+      uint4 v[NI];
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        v[i] = idx[i] >= 0 ? row_unit<T, false>(base + (int64_t)idx[i] * ld, unit(i) * E, d) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) *reinterpret_cast<uint4*>(lds + place(i) * 16) = v[i];
+    }
+  }
+};
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void store4(T* p, const float (&v)[4], int d0, int d) {
+  if constexpr (VEC) {
+    if (d0 >= d) return;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(p + d0) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+    else *reinterpret_cast<float4*>(p + d0) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (d0 + e < d) p[d0 + e] = from_f32<T>(v[e]);
+  }
+}
+
+struct Args {
+  const void *q, *k, *v, *dout;
+  int64_t ldq, ldk, ldv, lddo;
+  const int *q_row, *k_row;
+  const uint8_t* mask;
+  float scale;
+  int heads, group, d;
+  unsigned magic;  // x / group = x * magic >> 20 for x < 2^10, group <= 256
+  void *out, *out2;
+  int64_t ldo, ldo2;
+  float* lse;          // written by the forward, read by the backward
+  const float* delta;  // [query rows][heads]
+  float* part;
+};
+__device__ __forceinline__ int row_of(const int* list, int entry) { return list ? list[entry] : entry; }
+
+// the virtual row r of a tile: its query's list entry and its head
+struct Virtual {
+  int entry, head;
+  __device__ __forceinline__ Virtual(const Args& a, int entry0, int head0, int kv_head, int r) {
+    const int x = head0 + r, i = (int)((unsigned)x * a.magic >> 20);
+    entry = entry0 + i;
+    head = kv_head * a.group + (x - i * a.group);
+  }
+};
+
+// ---- forward ----------------------------------------------------------------------------------------------------------
+
+constexpr float kSlack = 8.f;  // the reference is moved when a row's maximum has grown by a factor of 2^8
+
+// The keys that a tile of TK list entries from k0 holds, as bits.
+template <int TK>
+__device__ __forceinline__ uint64_t counting(int k0, int k_end, uint8_t m, int lane) {
+  return __ballot(lane < TK && k0 + lane < k_end && m != 0);
+}
+
+// one value per lane of the running softmax of the lane's query, in base 2
+struct Running {
+  float m = -INFINITY, l = 0.f;
+};
+
+// p^T of one tile from s^T (TK keys x 32 queries), and the accumulators' rescaling
+template <int KB, int DB>
+__device__ __forceinline__ void softmax_tile(f32x16 (&s)[KB], f32x16 (&o)[DB], Running& run, float c, uint64_t bits,
+                                             uint64_t all, int lane) {
+  const int h = lane >> 5;
+  if (bits != all) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const uint32_t w = (uint32_t)(bits >> (32 * kb)) >> (4 * h);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kb][r] = (w >> (8 * (r >> 2) + (r & 3))) & 1 ? s[kb][r] : -INFINITY;
+    }
+  }
+  float top = s[0][0];
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kb][r]);
+  const float m2 = halves_max(top) * c;
+  if (__any(m2 > run.m + kSlack)) {
+    const float m = fmaxf(run.m, m2), alpha = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run.m - m);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+    run.l *= alpha;
+    run.m = m;
+  }
+  const float ref = run.m == -INFINITY ? 0.f : run.m;
+  float sum = 0.f;
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[kb][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kb][r], c, -ref));
+      sum += s[kb][r];
+    }
+  run.l += sum;
+}
+
+template <int TK, typename T, int DP>
+constexpr int tile_bytes() { return TK * DP * (int)sizeof(T); }
+
+// Partial results of a slot: ROWS rows of DP values, then their m and l.
+template <int DP>
+constexpr int slot_floats(int rows) { return rows * (DP + 2); }
+
+// NW = 4: a workgroup's four waves hold 32 virtual rows each and share the keys' tiles.  NW = 1: they hold the same 32 rows,
+// every wave walks every fourth tile in LDS of its own, and they meet at the end.  Two tiles of keys and values lie in LDS:
+// one is multiplied while the next is loaded.
+template <typename T, int DP, int TK, int NW, bool VEC>
+__global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cross(const QTile* tiles, Args a) {
+  constexpr int U = DP * (int)sizeof(T) / 16, NS = U / 2, DB = DP / 32, KB = TK / 32, TB = tile_bytes<TK, T, DP>();
+  constexpr int E = 16 / (int)sizeof(T), ROWS = NW == 4 ? kCrossRows : kCrossFew;
+  constexpr int BUF = 2 * TB;  // a tile of keys and one of values
+  constexpr int MEET = NW == 1 ? 4 * 32 * (DP + 4) * 4 + 4 * 32 * 8 : 0;
+  constexpr int LDS = 2 * BUF * (NW == 1 ? 4 : 1);
+  __shared__ __attribute__((aligned(16))) char lds[LDS > MEET ? LDS : MEET];
+  const QTile t = tiles[blockIdx.x];
+  if (t.rows == 0) return;
+  const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
+  const T* k = static_cast<const T*>(a.k) + t.kv_head * a.d;
+  const T* v = static_cast<const T*>(a.v) + t.kv_head * a.d;
+  const int first = NW == 4 ? 32 * wave : 0;
+  const bool active = first < t.rows;
+  const Virtual vr(a, t.entry, t.head0, t.kv_head, min(first + l32, t.rows - 1));
+  const int qrow = row_of(a.q_row, vr.entry);
+  const bool in = first + l32 < t.rows;
+  uint4 qf[NS];
+  {
+    const T* q = static_cast<const T*>(a.q) + (int64_t)qrow * a.ldq + vr.head * a.d;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) qf[s] = row_unit<T, VEC>(q, (2 * s + h) * E, a.d);
+  }
+  f32x16 o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[db][r] = 0.f;
+  Running run;
+  const float c = a.scale * kLog2e;
+  using L = TileLoader<T, DP, TK, NW, VEC>;
+  const L ld(NW == 4 ? wave : 0, lane);
+  char* mine = lds + (NW == 4 ? 0 : wave * 2 * BUF);
+  constexpr int STRIDE = NW == 4 ? 1 : 4;
+  const int ntile = (t.k_end - t.k_begin + TK - 1) / TK;
+  int idx[L::NI];
+  uint8_t mk = 1;
+  auto rows = [&](int tile) {  // the matrix rows of a tile's keys
+#pragma unroll
+    for (int i = 0; i < L::NI; ++i) {
+      const int e = t.k_begin + tile * TK + ld.row(i);
+      const bool there = e < t.k_end;
+      const int at = there ? e : t.k_end - 1;
+      int r = row_of(a.k_row, at);
+      if (a.mask && a.mask[at] == 0) r = -1;
+      idx[i] = there ? r : -1;
+    }
+  };
+  auto mask_of = [&](int tile) {
+    mk = a.mask ? a.mask[min(t.k_begin + tile * TK + (lane & (TK - 1)), t.k_end - 1)] : (uint8_t)1;
+  };
+  auto issue = [&](int buf) {
+    char* to = mine + buf * BUF;
+    ld.load(k, a.ldk, a.d, idx, to);
+    ld.load(v, a.ldv, a.d, idx, to + TB);
+  };
+  int at = NW == 4 ? 0 : wave;
+  if (at < ntile) {
+    rows(at);
+    mask_of(at);
+    issue(0);
+    if (at + STRIDE < ntile) rows(at + STRIDE);
+  }
+  for (int buf = 0; at < ntile; at += STRIDE, buf ^= 1) {
+    const uint64_t bits = counting<TK>(t.k_begin + at * TK, t.k_end, mk, lane);
+    vm_wait();
+    if constexpr (NW == 4) __syncthreads();
+    else wave_barrier_lds();
+    if (at + STRIDE < ntile) {
+      issue(buf ^ 1);
+      mask_of(at + STRIDE);
+      if (at + 2 * STRIDE < ntile) rows(at + 2 * STRIDE);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (!active) continue;
+    const char *kt = mine + buf * BUF, *vt = kt + TB;
+    f32x16 s[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+#pragma unroll
+      for (int st = 0; st < NS; ++st)
+        s[kb] = step_mma<T>(*reinterpret_cast<const uint4*>(kt + unit_at<U>(32 * kb + l32, 2 * st + h)), qf[st], s[kb]);
+    }
+    softmax_tile<KB, DB>(s, o, run, c, bits, TK == 64 ? ~0ull : (1ull << TK) - 1, lane);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) across_mma<T, U, DB>(vt, 32 * kb, Probs<T>(s[kb]), o, lane);
+  }
+  run.l = halves_sum(run.l);
+  T* out = static_cast<T*>(a.out);
+  if constexpr (NW == 4) {
+    if (!active || !in) return;
+    if (t.slot >= 0) {
+      float* p = a.part + (size_t)t.slot * slot_floats<DP>(ROWS);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          *reinterpret_cast<float4*>(p + (first + l32) * DP + 32 * db + 8 * j + 4 * h) =
+              make_float4(o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]);
+      if (h == 0) {
+        p[ROWS * DP + first + l32] = run.m;
+        p[ROWS * (DP + 1) + first + l32] = run.l;
+      }
+      return;
+    }
+    const float inv = run.l > 0.f || run.l != run.l ? 1.f / run.l : 0.f;
+    T* to = out + (int64_t)qrow * a.ldo + vr.head * a.d;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float w[4] = {o[db][4 * j] * inv, o[db][4 * j + 1] * inv, o[db][4 * j + 2] * inv, o[db][4 * j + 3] * inv};
+        store4<T, VEC>(to, w, 32 * db + 8 * j + 4 * h, a.d);
+      }
+    if (h == 0 && a.lse)
+      a.lse[(int64_t)qrow * a.heads + vr.head] = run.l == 0.f ? -INFINITY : (run.m + __builtin_amdgcn_logf(run.l)) * kLn2;
+  } else {
+    // the waves' rows meet in LDS: [wave][row][DP + 4], then m and l [wave][row]
+    constexpr int RS = DP + 4;
+    float* img = reinterpret_cast<float*>(lds);
+    float* ms = img + 4 * 32 * RS;
+    float* ls = ms + 128;
+    __syncthreads();
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<float4*>(img + (wave * 32 + l32) * RS + 32 * db + 8 * j + 4 * h) =
+            make_float4(o[db][4 * j], o[db][4 * j + 1], o[db][4 * j + 2], o[db][4 * j + 3]);
+    if (h == 0) {
+      ms[wave * 32 + l32] = run.m;
+      ls[wave * 32 + l32] = run.l;
+    }
+    __syncthreads();
+    const int r = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * 4;
+    if (r >= t.rows) return;
+    float m = -INFINITY, l = 0.f, f[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, ms[w * 32 + r]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      f[w] = ms[w * 32 + r] == -INFINITY ? (ls[w * 32 + r] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ms[w * 32 + r] - m);
+      l += f[w] * ls[w * 32 + r];
+    }
+    const Virtual mv(a, t.entry, t.head0, t.kv_head, r);
+    const int row = row_of(a.q_row, mv.entry);
+    float* p = t.slot >= 0 ? a.part + (size_t)t.slot * slot_floats<DP>(ROWS) : nullptr;
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float4 y = *reinterpret_cast<const float4*>(img + (w * 32 + r) * RS + 32 * db + c0);
+        x[0] += f[w] * y.x;
+        x[1] += f[w] * y.y;
+        x[2] += f[w] * y.z;
+        x[3] += f[w] * y.w;
+      }
+      if (p) {
+        *reinterpret_cast<float4*>(p + r * DP + 32 * db + c0) = make_float4(x[0], x[1], x[2], x[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] *= inv;
+        store4<T, VEC>(out + (int64_t)row * a.ldo + mv.head * a.d, x, 32 * db + c0, a.d);
+      }
+    }
+    if (c0 == 0) {
+      if (p) {
+        p[ROWS * DP + r] = m;
+        p[ROWS * (DP + 1) + r] = l;
+      } else if (a.lse) {
+        a.lse[(int64_t)row * a.heads + mv.head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+      }
+    }
+  }
+}
+
+// The pieces of a tile joined, in their order: SOFTMAX, each with its m and l, or plain sums (times the scale).  Eight threads
+// a row.
+template <typename T, int DP, int ROWS, bool SOFTMAX, bool VEC>
+__global__ __launch_bounds__(kThreads) void k_cross_join(const QTile* tiles, Args a) {
+  constexpr int DB = DP / 32;
+  const QTile t = tiles[blockIdx.x];
+  const int c0 = (threadIdx.x & 7) * 4;
+  T* out = static_cast<T*>(a.out);
+  for (int r = threadIdx.x >> 3; r < t.rows; r += kThreads / 8) {
+    const float* p = a.part + (size_t)t.slot * slot_floats<DP>(ROWS);
+    float m = -INFINITY, l = 0.f;
+    if (SOFTMAX)
+      for (int i = 0; i < t.pieces; ++i) m = fmaxf(m, p[(size_t)i * slot_floats<DP>(ROWS) + ROWS * DP + r]);
+    float x[DB][4];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[db][e] = 0.f;
+    for (int i = 0; i < t.pieces; ++i, p += slot_floats<DP>(ROWS)) {
+      float f = 1.f;
+      if (SOFTMAX) {
+        const float mi = p[ROWS * DP + r], li = p[ROWS * (DP + 1) + r];
+        f = mi == -INFINITY ? (li == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(mi - m);
+        l += f * li;
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const float4 y = *reinterpret_cast<const float4*>(p + r * DP + 32 * db + c0);
+        x[db][0] += f * y.x;
+        x[db][1] += f * y.y;
+        x[db][2] += f * y.z;
+        x[db][3] += f * y.w;
+      }
+    }
+    const Virtual v(a, t.entry, t.head0, t.kv_head, r);
+    const int row = row_of(a.q_row, v.entry);
+    const float inv = !SOFTMAX ? a.scale : l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[db][e] *= inv;
+      store4<T, VEC>(out + (int64_t)row * a.ldo + v.head * a.d, x[db], 32 * db + c0, a.d);
+    }
+    if (SOFTMAX && c0 == 0 && a.lse)
+      a.lse[(int64_t)row * a.heads + v.head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+}
+
+// ---- backward ---------------------------------------------------------------------------------------------------------
+
+// delta = sum_d dout out of every listed row and head: eight lanes each
+template <typename T, bool VEC>
+__global__ __launch_bounds__(kThreads) void k_cross_delta(const T* out, int64_t ldo, const T* dout, int64_t lddo,
+                                                          const int* q_row, int64_t n, int heads, int d, float* delta) {
+  constexpr int E = 16 / (int)sizeof(T);
+  const int64_t at = (int64_t)blockIdx.x * (kThreads / 8) + (threadIdx.x >> 3);
+  if (at >= n) return;
+  const int entry = (int)(at / heads), head = (int)(at - (int64_t)entry * heads), row = row_of(q_row, entry);
+  const T *x = out + (int64_t)row * ldo + head * d, *y = dout + (int64_t)row * lddo + head * d;
+  float s = 0.f;
+  for (int e0 = (threadIdx.x & 7) * E; e0 < d; e0 += 8 * E) {
+    const uint4 u = row_unit<T, VEC>(x, e0, d), w = row_unit<T, VEC>(y, e0, d);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      s += to_f32<T>(reinterpret_cast<const T*>(&u)[e]) * to_f32<T>(reinterpret_cast<const T*>(&w)[e]);
+  }
+#pragma unroll
+  for (int o = 1; o < 8; o *= 2) s += __shfl_xor(s, o);
+  if ((threadIdx.x & 7) == 0) delta[(int64_t)row * heads + head] = s;
+}
+
+// The queries' gradient: as the forward with four waves, p recomputed from lse, dq^T += k^T ds^T.
+template <typename T, int DP, int TK, bool VEC>
+__global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cross_dq(const QTile* tiles, Args a) {
+  constexpr int U = DP * (int)sizeof(T) / 16, NS = U / 2, DB = DP / 32, KB = TK / 32, TB = tile_bytes<TK, T, DP>();
+  constexpr int E = 16 / (int)sizeof(T), BUF = 2 * TB;
+  __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
+  const QTile t = tiles[blockIdx.x];
+  if (t.rows == 0) return;
+  const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
+  const T* k = static_cast<const T*>(a.k) + t.kv_head * a.d;
+  const T* v = static_cast<const T*>(a.v) + t.kv_head * a.d;
+  const int first = 32 * wave;
+  const bool active = first < t.rows;
+  const Virtual vr(a, t.entry, t.head0, t.kv_head, min(first + l32, t.rows - 1));
+  const int qrow = row_of(a.q_row, vr.entry);
+  uint4 qf[NS], df[NS];
+  {
+    const T* q = static_cast<const T*>(a.q) + (int64_t)qrow * a.ldq + vr.head * a.d;
+    const T* g = static_cast<const T*>(a.dout) + (int64_t)qrow * a.lddo + vr.head * a.d;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      qf[s] = row_unit<T, VEC>(q, (2 * s + h) * E, a.d);
+      df[s] = row_unit<T, VEC>(g, (2 * s + h) * E, a.d);
+    }
+  }
+  const int64_t stat = (int64_t)qrow * a.heads + vr.head;
+  const float lse = a.lse[stat], delta = a.delta[stat], ref = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  f32x16 dq[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dq[db][r] = 0.f;
+  const float c = a.scale * kLog2e;
+  using L = TileLoader<T, DP, TK, 4, VEC>;
+  const L ld(wave, lane);
+  const int ntile = (t.k_end - t.k_begin + TK - 1) / TK;
+  int idx[L::NI];
+  uint8_t mk = 1;
+  auto rows = [&](int tile) {
+#pragma unroll
+    for (int i = 0; i < L::NI; ++i) {
+      const int e = t.k_begin + tile * TK + ld.row(i);
+      const bool there = e < t.k_end;
+      const int at = there ? e : t.k_end - 1;
+      int r = row_of(a.k_row, at);
+      if (a.mask && a.mask[at] == 0) r = -1;
+      idx[i] = there ? r : -1;
+    }
+  };
+  auto mask_of = [&](int tile) {
+    mk = a.mask ? a.mask[min(t.k_begin + tile * TK + (lane & (TK - 1)), t.k_end - 1)] : (uint8_t)1;
+  };
+  auto issue = [&](int buf) {
+    char* to = lds + buf * BUF;
+    ld.load(k, a.ldk, a.d, idx, to);
+    ld.load(v, a.ldv, a.d, idx, to + TB);
+  };
+  if (ntile > 0) {
+    rows(0);
+    mask_of(0);
+    issue(0);
+    if (ntile > 1) rows(1);
+  }
+  for (int at = 0; at < ntile; ++at) {
+    const uint64_t bits = counting<TK>(t.k_begin + at * TK, t.k_end, mk, lane);
+    vm_wait();
+    __syncthreads();
+    if (at + 1 < ntile) {
+      issue((at + 1) & 1);
+      mask_of(at + 1);
+      if (at + 2 < ntile) rows(at + 2);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (!active) continue;
+    const char *kt = lds + (at & 1) * BUF, *vt = kt + TB;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+#pragma unroll
+      for (int st = 0; st < NS; ++st) {
+        s = step_mma<T>(*reinterpret_cast<const uint4*>(kt + unit_at<U>(32 * kb + l32, 2 * st + h)), qf[st], s);
+        dp = step_mma<T>(*reinterpret_cast<const uint4*>(vt + unit_at<U>(32 * kb + l32, 2 * st + h)), df[st], dp);
+      }
+      const uint32_t w = (uint32_t)(bits >> (32 * kb)) >> (4 * h);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -ref));
+        s[r] = (w >> (8 * (r >> 2) + (r & 3))) & 1 ? p * (dp[r] - delta) : 0.f;
+      }
+      across_mma<T, U, DB>(kt, 32 * kb, Probs<T>(s), dq, lane);
+    }
+  }
+  if (first + l32 >= t.rows) return;
+  if (lse == -INFINITY)  // a row without keys, whatever q and dout hold
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dq[db][r] = 0.f;
+  if (t.slot >= 0) {
+    float* p = a.part + (size_t)t.slot * slot_floats<DP>(kCrossRows);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *reinterpret_cast<float4*>(p + (first + l32) * DP + 32 * db + 8 * j + 4 * h) =
+            make_float4(dq[db][4 * j], dq[db][4 * j + 1], dq[db][4 * j + 2], dq[db][4 * j + 3]);
+    return;
+  }
+  const float scale = a.scale;
+  T* to = static_cast<T*>(a.out) + (int64_t)qrow * a.ldo + vr.head * a.d;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float w[4] = {dq[db][4 * j] * scale, dq[db][4 * j + 1] * scale, dq[db][4 * j + 2] * scale,
+                          dq[db][4 * j + 3] * scale};
+      store4<T, VEC>(to, w, 32 * db + 8 * j + 4 * h, a.d);
+    }
+}
+
+// The gradient of keys and values: a wave holds 32 keys on its lanes, k and v in registers, and walks the row tiles of the
+// sequences that read them: dv^T += do^T p, dk^T += q^T ds.
+template <typename T, int DP, int RQ, bool VEC>
+__global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 2)) void k_cross_dkv(const KTile* tiles,
+                                                                                       const RTile* runs, Args a) {
+  constexpr int U = DP * (int)sizeof(T) / 16, NS = U / 2, DB = DP / 32, QB = RQ / 32, TB = tile_bytes<RQ, T, DP>();
+  constexpr int E = 16 / (int)sizeof(T), BUF = 2 * TB;
+  __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
+  __shared__ __attribute__((aligned(16))) float stats[2][2][RQ];  // [buffer][lse in base 2, delta][row]
+  // the widest fp32 heads leave no registers for v's fragments: every lane keeps its own in LDS
+  constexpr bool KEEP = DP * sizeof(T) > 384;
+  __shared__ uint4 kept[KEEP ? 4 * NS * 64 : 1];
+  const KTile t = tiles[blockIdx.x];
+  if (t.keys == 0) return;
+  const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
+  const int first = 32 * wave, mykey = first + l32;
+  const bool active = first < t.keys;
+  const int ke = t.k_begin + min(mykey, t.keys - 1), krow = row_of(a.k_row, ke);
+  const bool counts = !a.mask || a.mask[ke] != 0;
+  uint4 kf[NS], vf[KEEP ? 1 : NS];
+  {
+    const T* k = static_cast<const T*>(a.k) + (int64_t)krow * a.ldk + t.kv_head * a.d;
+    const T* v = static_cast<const T*>(a.v) + (int64_t)krow * a.ldv + t.kv_head * a.d;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      kf[s] = row_unit<T, VEC>(k, (2 * s + h) * E, a.d);
+      vf[KEEP ? 0 : s] = row_unit<T, VEC>(v, (2 * s + h) * E, a.d);
+      if constexpr (KEEP) kept[(wave * NS + s) * 64 + lane] = vf[0];
+    }
+  }
+  f32x16 dk[DB], dv[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dk[db][r] = dv[db][r] = 0.f;
+  const float c = a.scale * kLog2e;
+  using L = TileLoader<T, DP, RQ, 4, VEC>;
+  const L ld(wave, lane);
+  const T *q = static_cast<const T*>(a.q), *g = static_cast<const T*>(a.dout);
+  int idx[L::NI], head[L::NI];
+  float lse2 = INFINITY, delta = 0.f;  // of the next tile's row `lane`, by wave 0
+  auto rows = [&](int tile) {
+    const RTile rt = runs[tile];
+#pragma unroll
+    for (int i = 0; i < L::NI; ++i) {
+      const Virtual vr(a, rt.entry, rt.head0, t.kv_head, min(ld.row(i), rt.rows - 1));
+      head[i] = vr.head * a.d;
+      idx[i] = row_of(a.q_row, vr.entry);
+      idx[i] = ld.row(i) < rt.rows ? idx[i] : -1;
+    }
+  };
+  auto fetch_stats = [&](int tile) {
+    if (wave != 0) return;
+    const RTile rt = runs[tile];
+    const int r = lane & (RQ - 1);
+    const Virtual vr(a, rt.entry, rt.head0, t.kv_head, min(r, rt.rows - 1));
+    const int64_t at = (int64_t)row_of(a.q_row, vr.entry) * a.heads + vr.head;
+    const float lse = a.lse[at];
+    delta = r < rt.rows ? a.delta[at] : 0.f;
+    lse2 = r < rt.rows && lse != -INFINITY ? lse * kLog2e : INFINITY;
+  };
+  auto issue = [&](int buf) {
+    char* to = lds + buf * BUF;
+    if constexpr (VEC) {
+#pragma unroll
+      for (int i = 0; i < L::NI; ++i) {
+        const int e0 = ld.unit(i) * E;
+        const bool there = idx[i] >= 0 && e0 < a.d;
+        const void* z = g_zero;
+        dma16_untracked(there ? q + (int64_t)idx[i] * a.ldq + head[i] + e0 : z, to + (ld.part * L::NI + i) * 1024);
+        dma16_untracked(there ? g + (int64_t)idx[i] * a.lddo + head[i] + e0 : z, to + TB + (ld.part * L::NI + i) * 1024);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < L::NI; ++i) {
+        uint4 x = make_uint4(0, 0, 0, 0), y = x;
+        if (idx[i] >= 0) {
+          x = row_unit<T, false>(q + (int64_t)idx[i] * a.ldq + head[i], ld.unit(i) * E, a.d);
+          y = row_unit<T, false>(g + (int64_t)idx[i] * a.lddo + head[i], ld.unit(i) * E, a.d);
+        }
+        *reinterpret_cast<uint4*>(to + ld.place(i) * 16) = x;
+        *reinterpret_cast<uint4*>(to + TB + ld.place(i) * 16) = y;
+      }
+    }
+  };
+  if (t.t_begin < t.t_end) {
+    rows(t.t_begin);
+    fetch_stats(t.t_begin);
+    issue(0);
+    if (t.t_begin + 1 < t.t_end) rows(t.t_begin + 1);
+  }
+  for (int at = t.t_begin; at < t.t_end; ++at) {
+    const int buf = (at - t.t_begin) & 1;
+    if (wave == 0 && lane < RQ) {
+      stats[buf][0][lane] = lse2;
+      stats[buf][1][lane] = delta;
+    }
+    vm_wait();
+    __syncthreads();
+    if (at + 1 < t.t_end) {
+      issue(buf ^ 1);
+      fetch_stats(at + 1);
+      if (at + 2 < t.t_end) rows(at + 2);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (!active) continue;
+    const char *qt = lds + buf * BUF, *gt = qt + TB;
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      f32x16 s, dp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+#pragma unroll
+      for (int st = 0; st < NS; ++st) {
+        s = step_mma<T>(*reinterpret_cast<const uint4*>(qt + unit_at<U>(32 * qb + l32, 2 * st + h)), kf[st], s);
+        dp = step_mma<T>(*reinterpret_cast<const uint4*>(gt + unit_at<U>(32 * qb + l32, 2 * st + h)),
+                         KEEP ? kept[(wave * NS + st) * 64 + lane] : vf[KEEP ? 0 : st], dp);
+        if constexpr (KEEP)
+          if (st % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // four steps' fragments in registers at a time
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float4 m = *reinterpret_cast<const float4*>(&stats[buf][0][32 * qb + 8 * j + 4 * h]);
+        const float4 dl = *reinterpret_cast<const float4*>(&stats[buf][1][32 * qb + 8 * j + 4 * h]);
+        const float ref[4] = {m.x, m.y, m.z, m.w}, del[4] = {dl.x, dl.y, dl.z, dl.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * j + e], c, -ref[e]));
+          s[4 * j + e] = p;
+          dp[4 * j + e] = p * (dp[4 * j + e] - del[e]);
+        }
+      }
+      across_mma<T, U, DB>(gt, 32 * qb, Probs<T>(s), dv, lane);
+      across_mma<T, U, DB>(qt, 32 * qb, Probs<T>(dp), dk, lane);
+    }
+  }
+  if (mykey >= t.keys) return;
+  if (t.slot >= 0) {
+    float* p = a.part + ((size_t)t.slot * kCrossKeys + mykey) * 2 * DP;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int d0 = 32 * db + 8 * j + 4 * h;
+        *reinterpret_cast<float4*>(p + d0) = make_float4(dk[db][4 * j], dk[db][4 * j + 1], dk[db][4 * j + 2], dk[db][4 * j + 3]);
+        *reinterpret_cast<float4*>(p + DP + d0) =
+            make_float4(dv[db][4 * j], dv[db][4 * j + 1], dv[db][4 * j + 2], dv[db][4 * j + 3]);
+      }
+    return;
+  }
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float x[4], y[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = counts ? dk[db][4 * j + e] * a.scale : 0.f;
+        y[e] = counts ? dv[db][4 * j + e] : 0.f;
+      }
+      const int d0 = 32 * db + 8 * j + 4 * h;
+      if (a.out) store4<T, VEC>(static_cast<T*>(a.out) + (int64_t)krow * a.ldo + t.kv_head * a.d, x, d0, a.d);
+      if (a.out2) store4<T, VEC>(static_cast<T*>(a.out2) + (int64_t)krow * a.ldo2 + t.kv_head * a.d, y, d0, a.d);
+    }
+}
+
+// The pieces of a tile of keys summed in their order: eight threads a key.
+template <typename T, int DP, bool VEC>
+__global__ __launch_bounds__(kThreads) void k_cross_join_keys(const KTile* tiles, Args a) {
+  const KTile t = tiles[blockIdx.x];
+  const int c0 = (threadIdx.x & 7) * 4;
+  for (int key = threadIdx.x >> 3; key < t.keys; key += kThreads / 8) {
+    const int ke = t.k_begin + key, krow = row_of(a.k_row, ke);
+    const bool counts = !a.mask || a.mask[ke] != 0;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      T* to = static_cast<T*>(which ? a.out2 : a.out);
+      if (!to) continue;
+      to += (int64_t)krow * (which ? a.ldo2 : a.ldo) + t.kv_head * a.d;
+      for (int d0 = c0; d0 < DP; d0 += 32) {
+        float x[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < t.pieces; ++i) {
+          const float4 y = *reinterpret_cast<const float4*>(a.part + ((size_t)(t.slot + i) * kCrossKeys + key) * 2 * DP +
+                                                            which * DP + d0);
+          x[0] += y.x;
+          x[1] += y.y;
+          x[2] += y.z;
+          x[3] += y.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = counts ? x[e] * (which ? 1.f : a.scale) : 0.f;
+        store4<T, VEC>(to, x, d0, a.d);
+      }
+    }
+  }
+}
+
+// ---- launches ---------------------------------------------------------------------------------------------------------
+
+template <typename T, int DP_>
+struct Width {
+  typedef T type;
+  static constexpr int DP = DP_;
+};
+// f(Width<T, DP>) for the width that holds the heads
+template <class F>
+void with_width(int dtype, int d, F&& f) {
+  const auto pick = [&](auto zero) {
+    typedef decltype(zero) T;
+    if (d <= 32) f(Width<T, 32>());
+    else if (d <= 64) f(Width<T, 64>());
+    else if (d <= 96) f(Width<T, 96>());
+    else f(Width<T, 128>());
+  };
+  if (dtype == FOLD_F32) pick(float());
+  else pick(uint16_t());
+}
+// whether the heads' rows of a matrix lie at multiples of 16 bytes
+bool whole_units(const CrossMat& m, int d, int es) {
+  return !m.p || ((reinterpret_cast<uintptr_t>(m.p) & 15) == 0 && m.ld * es % 16 == 0 && d * es % 16 == 0);
+}
+
+Args args_of(const Cross& c, const CrossMat& q, const CrossMat& k, const CrossMat& v, const uint8_t* mask, float scale) {
+  Args a{};
+  a.q = q.p;
+  a.k = k.p;
+  a.v = v.p;
+  a.ldq = q.ld;
+  a.ldk = k.ld;
+  a.ldv = v.ld;
+  a.q_row = c.q_row;
+  a.k_row = c.k_row;
+  a.mask = mask;
+  a.scale = scale;
+  a.heads = c.heads;
+  a.group = c.group;
+  a.d = c.head_dim;
+  a.magic = (1u << 20) / (unsigned)c.group + 1;
+  return a;
+}
+
+}  // namespace
+
+size_t cross_forward_bytes(const Cross& c) {
+  return (size_t)c.fslots * (c.few ? kCrossFew : kCrossRows) * (cross_padded(c.head_dim) + 2) * sizeof(float);
+}
+static size_t delta_floats(const Cross& c) { return ((size_t)c.query_rows * c.heads + 3) / 4 * 4; }
+size_t cross_backward_bytes(const Cross& c) {
+  const int dp = cross_padded(c.head_dim);
+  // the queries' and the keys' pieces follow each other on the stream: one region serves both
+  const size_t dq = (size_t)c.bslots * kCrossRows * (dp + 2), dk = (size_t)c.kslots * kCrossKeys * 2 * dp;
+  return (delta_floats(c) + std::max(dq, dk)) * sizeof(float);
+}
+
+void launch_cross(const Cross& c, CrossMat q, CrossMat k, CrossMat v, const uint8_t* mask, float scale, void* out,
+                  int64_t ldo, float* lse, void* ws, hipStream_t st) {
+  if (c.nfwd == 0) return;
+  Args a = args_of(c, q, k, v, mask, scale);
+  a.out = out;
+  a.ldo = ldo;
+  a.lse = lse;
+  a.part = static_cast<float*>(ws);
+  const int es = c.dtype == FOLD_BF16 ? 2 : 4, d = c.head_dim;
+  const bool vec = whole_units(q, d, es) && whole_units(k, d, es) && whole_units(v, d, es) && whole_units({out, ldo}, d, es);
+  with_width(c.dtype, d, [&](auto w) {
+    typedef typename decltype(w)::type T;
+    constexpr int DP = decltype(w)::DP, TK = sizeof(T) == 2 ? 64 : 32;
+    const auto go = [&](auto vector) {
+      constexpr bool VEC = decltype(vector)::value;
+      {
+        ProfScope prof("cross", st);
+        if constexpr (DP * sizeof(T) <= kCrossFewBytes)
+          if (c.few) hipLaunchKernelGGL((k_cross<T, DP, 32, 1, VEC>), dim3(c.nfwd), dim3(kThreads), 0, st, c.fwd, a);
+        if (!c.few) hipLaunchKernelGGL((k_cross<T, DP, TK, 4, VEC>), dim3(c.nfwd), dim3(kThreads), 0, st, c.fwd, a);
+      }
+      if (c.nfjoin == 0) return;
+      ProfScope prof("cross_join", st);
+      if (c.few)
+        hipLaunchKernelGGL((k_cross_join<T, DP, kCrossFew, true, VEC>), dim3(c.nfjoin), dim3(kThreads), 0, st, c.fjoin, a);
+      else
+        hipLaunchKernelGGL((k_cross_join<T, DP, kCrossRows, true, VEC>), dim3(c.nfjoin), dim3(kThreads), 0, st, c.fjoin, a);
+    };
+    if (vec) go(std::true_type());
+    else go(std::false_type());
+  });
+}
+
+void launch_cross_backward(const Cross& c, CrossMat q, CrossMat k, CrossMat v, const uint8_t* mask, float scale, CrossMat out,
+                           const float* lse, CrossMat dout, void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv,
+                           int64_t lddv, void* ws, hipStream_t st) {
+  Args a = args_of(c, q, k, v, mask, scale);
+  a.dout = dout.p;
+  a.lddo = dout.ld;
+  a.lse = const_cast<float*>(lse);
+  float* delta = static_cast<float*>(ws);
+  a.delta = delta;
+  a.part = delta + delta_floats(c);
+  const int es = c.dtype == FOLD_BF16 ? 2 : 4, d = c.head_dim;
+  const bool vec = whole_units(q, d, es) && whole_units(k, d, es) && whole_units(v, d, es) && whole_units(out, d, es) &&
+                   whole_units(dout, d, es) && whole_units({dq, lddq}, d, es) && whole_units({dk, lddk}, d, es) &&
+                   whole_units({dv, lddv}, d, es);
+  with_width(c.dtype, d, [&](auto w) {
+    typedef typename decltype(w)::type T;
+    constexpr int DP = decltype(w)::DP, TK = sizeof(T) == 2 ? 64 : 32;
+    const auto go = [&](auto vector) {
+      constexpr bool VEC = decltype(vector)::value;
+      const int64_t n = (int64_t)c.num_queries * c.heads;
+      if (n > 0) {
+        ProfScope prof("cross_delta", st);
+        hipLaunchKernelGGL((k_cross_delta<T, VEC>), dim3((unsigned)((n + 31) / 32)), dim3(kThreads), 0, st,
+                           static_cast<const T*>(out.p), out.ld, static_cast<const T*>(dout.p), dout.ld, c.q_row, n, c.heads,
+                           d, delta);
+      }
+      if (dq && c.nback > 0) {
+        Args b = a;
+        b.out = dq;
+        b.ldo = lddq;
+        {
+          ProfScope prof("cross_dq", st);
+          hipLaunchKernelGGL((k_cross_dq<T, DP, TK, VEC>), dim3(c.nback), dim3(kThreads), 0, st, c.back, b);
+        }
+        if (c.nbjoin > 0) {
+          ProfScope prof("cross_dq_join", st);
+          hipLaunchKernelGGL((k_cross_join<T, DP, kCrossRows, false, VEC>), dim3(c.nbjoin), dim3(kThreads), 0, st, c.bjoin, b);
+        }
+      }
+      if ((dk || dv) && c.nkeys > 0) {
+        Args b = a;
+        b.out = dk;
+        b.ldo = lddk;
+        b.out2 = dv;
+        b.ldo2 = lddv;
+        {
+          ProfScope prof("cross_dkv", st);
+          hipLaunchKernelGGL((k_cross_dkv<T, DP, TK, VEC>), dim3(c.nkeys), dim3(kThreads), 0, st, c.keys, c.rows, b);
+        }
+        if (c.nkjoin > 0) {
+          ProfScope prof("cross_dkv_join", st);
+          hipLaunchKernelGGL((k_cross_join_keys<T, DP, VEC>), dim3(c.nkjoin), dim3(kThreads), 0, st, c.kjoin, b);
+        }
+      }
+    };
+    if (vec) go(std::true_type());
+    else go(std::false_type());
+  });
+}
+
+}  // namespace fold

@@ -1,0 +1,377 @@
+// Plans of cross attention: the lists are checked on the GPU, the workgroups are laid out on the host, whose copy of the
+// sequences' lengths lets long ones be cut and the work be spread over the chip.
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <string>
+#include <vector>
+
+#include "checks.h"
+#include "common.h"
+#include "cross.h"
+#include "pool.h"
+
+namespace fold {
+
+namespace {
+
+__global__ __launch_bounds__(256) void k_zero_words(uint32_t* p, size_t n) {
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = 0;
+}
+
+// error bits: 1 a row out of range, 2 a row listed twice
+__global__ __launch_bounds__(256) void k_check_rows(const int32_t* row, int n, int limit, uint32_t* seen, uint32_t* error,
+                                                    int shift) {
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+    const int r = row[i];
+    if (r < 0 || r >= limit) {
+      atomicOr(error, 1u << shift);
+    } else {
+      const uint32_t bit = 1u << (r & 31);
+      if (atomicOr(&seen[r >> 5], bit) & bit) atomicOr(error, 2u << shift);
+    }
+  }
+}
+
+struct Range {
+  int64_t begin, end;
+  int64_t size() const { return end - begin; }
+};
+
+// Workgroups in launch order.  The XCDs take them in turn and each has an L2 of its own, so the workgroups that read the same
+// keys (or rows) follow each other on one XCD: chunks of a group go, the costliest first, to the XCD with the least work.
+template <class Tile>
+struct Spread {
+  struct Chunk {
+    size_t begin, end;
+    int64_t cost;
+  };
+  std::vector<Tile> all;
+  std::vector<int64_t> cost;
+  std::vector<size_t> groups{0};  // where groups begin
+  void add(const Tile& t, int64_t c) {
+    all.push_back(t);
+    cost.push_back(c + 64);  // a workgroup's own start and end
+  }
+  void close() {
+    if (groups.back() != all.size()) groups.push_back(all.size());
+  }
+  std::vector<Tile> order() const {
+    const size_t most = std::max<size_t>(1, std::min<size_t>(64, all.size() / 64));
+    std::vector<Chunk> chunks;
+    for (size_t g = 0; g + 1 < groups.size(); ++g)
+      for (size_t b = groups[g]; b < groups[g + 1]; b += most) {
+        Chunk c{b, std::min(b + most, groups[g + 1]), 0};
+        for (size_t i = c.begin; i < c.end; ++i) c.cost += cost[i];
+        chunks.push_back(c);
+      }
+    // the costliest workgroups first, so that short ones fill the end
+    std::stable_sort(chunks.begin(), chunks.end(), [&](const Chunk& a, const Chunk& b) {
+      return a.cost / (int64_t)(a.end - a.begin) > b.cost / (int64_t)(b.end - b.begin);
+    });
+    std::vector<std::vector<size_t>> lane(8);
+    int64_t load[8] = {0};
+    for (const Chunk& c : chunks) {
+      int x = 0;
+      for (int i = 1; i < 8; ++i)
+        if (load[i] < load[x]) x = i;
+      load[x] += c.cost;
+      for (size_t i = c.begin; i < c.end; ++i) lane[x].push_back(i);
+    }
+    size_t deep = 0;
+    for (const auto& l : lane) deep = std::max(deep, l.size());
+    Tile none{};
+    std::vector<Tile> out(deep * 8, none);
+    for (int x = 0; x < 8; ++x)
+      for (size_t i = 0; i < lane[x].size(); ++i) out[i * 8 + x] = all[lane[x][i]];
+    while (!out.empty() && empty(out.back())) out.pop_back();
+    return out;
+  }
+  static bool empty(const QTile& t) { return t.rows == 0; }
+  static bool empty(const KTile& t) { return t.keys == 0; }
+};
+
+constexpr int kMinPiece = 256;  // keys (or rows) of a piece
+constexpr int kWanted = 512;    // workgroups that fill the chip: two a compute unit
+
+// The length of pieces: what spreads the work evenly over the wanted workgroups, where there are fewer tiles than that; with
+// more tiles only one that is far longer than the others is cut.
+int64_t piece_of(int64_t tiles, int64_t work, int unit) {
+  if (tiles == 0) return kMinPiece;
+  int64_t len = std::max<int64_t>(kMinPiece, (work + kWanted - 1) / kWanted);
+  if (tiles >= kWanted) len = std::max<int64_t>(len, 4 * (work / tiles));
+  return (len + unit - 1) / unit * unit;
+}
+
+struct Lists {
+  const std::vector<int32_t>&qp, &kp, &src;
+  int G, kv_heads;
+  std::vector<std::vector<int>> readers;  // by source: its query sequences; the last entry: those without a source
+};
+
+// tiles of `height` virtual rows, all key heads, in pieces of the keys; the tiles in pieces also go to `join`
+void query_tiles(const Lists& l, int height, std::vector<QTile>* out, std::vector<QTile>* join, int* slots) {
+  const int sources = (int)l.kp.size() - 1;
+  int64_t tiles = 0, work = 0;
+  const auto keys_of = [&](int e) { return e < sources ? (int64_t)l.kp[e + 1] - l.kp[e] : 0; };
+  const auto rows_of = [&](int b) { return ((int64_t)l.qp[b + 1] - l.qp[b]) * l.G; };
+  for (int e = 0; e <= sources; ++e)
+    for (int b : l.readers[e]) {
+      const int64_t n = (rows_of(b) + height - 1) / height * l.kv_heads;
+      tiles += n;
+      work += n * keys_of(e);
+    }
+  const int64_t piece = piece_of(tiles, work, 64);
+  Spread<QTile> s;
+  *slots = 0;
+  for (int e = 0; e <= sources; ++e) {
+    const int64_t nk = keys_of(e), pieces = std::max<int64_t>(1, (nk + piece - 1) / piece);
+    const int64_t each = ((nk + pieces - 1) / pieces + 63) / 64 * 64;
+    for (int h = 0; h < l.kv_heads; ++h) {
+      for (int b : l.readers[e])
+        for (int64_t r = 0; r < rows_of(b); r += height) {
+          QTile t{};
+          t.entry = (int32_t)(l.qp[b] + r / l.G);
+          t.head0 = (int32_t)(r % l.G);
+          t.rows = (int32_t)std::min<int64_t>(height, rows_of(b) - r);
+          t.kv_head = h;
+          const int32_t k0 = e < sources ? l.kp[e] : 0;
+          const int n = (int)(each ? std::max<int64_t>(1, (nk + each - 1) / each) : 1);
+          for (int p = 0; p < n; ++p) {
+            t.k_begin = (int32_t)(k0 + std::min<int64_t>(p * each, nk));
+            t.k_end = (int32_t)(k0 + std::min<int64_t>((p + 1) * each, nk));
+            t.slot = n > 1 ? *slots + p : -1;
+            t.pieces = p == 0 ? n : 0;
+            s.add(t, t.k_end - t.k_begin);
+            if (n > 1 && p == 0) join->push_back(t);
+          }
+          if (n > 1) *slots += n;
+        }
+      s.close();
+    }
+  }
+  *out = s.order();
+}
+
+void key_tiles(const Lists& l, int height, std::vector<KTile>* out, std::vector<KTile>* join, std::vector<RTile>* rows,
+               int* slots) {
+  const int sources = (int)l.kp.size() - 1;
+  std::vector<Range> runs(sources);
+  std::vector<int64_t> count(sources, 0);
+  int64_t tiles = 0, work = 0;
+  for (int e = 0; e < sources; ++e) {
+    runs[e].begin = (int64_t)rows->size();
+    for (int b : l.readers[e]) {
+      const int64_t n = ((int64_t)l.qp[b + 1] - l.qp[b]) * l.G;
+      count[e] += n;
+      for (int64_t r = 0; r < n; r += height)
+        rows->push_back(RTile{(int32_t)(l.qp[b] + r / l.G), (int32_t)(r % l.G), (int32_t)std::min<int64_t>(height, n - r), 0});
+    }
+    runs[e].end = (int64_t)rows->size();
+    const int64_t n = (int64_t)(l.kp[e + 1] - l.kp[e] + kCrossKeys - 1) / kCrossKeys * l.kv_heads;
+    tiles += n;
+    work += n * runs[e].size() * height;
+  }
+  const int64_t piece = piece_of(tiles, work, height) / height;  // row tiles
+  Spread<KTile> s;
+  *slots = 0;
+  for (int e = 0; e < sources; ++e) {
+    const int64_t nr = runs[e].size(), pieces = std::max<int64_t>(1, (nr + piece - 1) / piece);
+    const int64_t each = std::max<int64_t>(1, (nr + pieces - 1) / pieces);
+    const int n = (int)std::max<int64_t>(1, (nr + each - 1) / each);
+    for (int h = 0; h < l.kv_heads; ++h) {
+      for (int32_t k = l.kp[e]; k < l.kp[e + 1]; k += kCrossKeys) {
+        KTile t{};
+        t.k_begin = k;
+        t.keys = std::min<int32_t>(kCrossKeys, l.kp[e + 1] - k);
+        t.kv_head = h;
+        for (int p = 0; p < n; ++p) {
+          t.t_begin = (int32_t)(runs[e].begin + std::min<int64_t>(p * each, nr));
+          t.t_end = (int32_t)(runs[e].begin + std::min<int64_t>((p + 1) * each, nr));
+          t.slot = n > 1 ? *slots + p : -1;
+          t.pieces = p == 0 ? n : 0;
+          s.add(t, (int64_t)(t.t_end - t.t_begin) * height);
+          if (n > 1 && p == 0) join->push_back(t);
+        }
+        if (n > 1) *slots += n;
+      }
+      s.close();
+    }
+  }
+  *out = s.order();
+}
+
+// checks one of the ptr arrays; the total it ends at
+bool check_ptr(const std::vector<int32_t>& p, int total) {
+  if (p[0] != 0 || p.back() != total) return false;
+  for (size_t i = 1; i < p.size(); ++i)
+    if (p[i] < p[i - 1]) return false;
+  return true;
+}
+
+// gives a temporary block back on every path, after its stream has finished with it
+struct Block {
+  int device;
+  hipStream_t st;
+  void* p = nullptr;
+  ~Block() {
+    if (p && hipStreamSynchronize(st) == hipSuccess) pool_free(device, p, false);
+  }
+};
+
+unsigned grid_for(size_t n) { return (unsigned)std::max<size_t>(1, std::min<size_t>((n + 255) / 256, 2048)); }
+
+}  // namespace
+
+int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out) {
+  const std::string who("fold_cross_create");
+  if (!known_type(b->dtype)) return api_fail(FOLD_E_INVALID, who + ": unknown dtype");
+  if (b->heads < 1 || b->heads > 1024 || b->kv_heads < 1 || b->heads % b->kv_heads != 0 || b->heads / b->kv_heads > 256)
+    return api_fail(FOLD_E_INVALID, who + ": heads must be 1 .. 1024, a multiple of kv_heads, at most 256 times");
+  if (b->head_dim < 1 || b->head_dim > kCrossHeadDim) return api_fail(FOLD_E_INVALID, who + ": head_dim must be 1 .. 128");
+  if (b->num_seqs < 0 || b->num_sources < 0 || b->num_queries < 0 || b->num_keys < 0 || b->num_query_rows < 0 ||
+      b->num_key_rows < 0)
+    return api_fail(FOLD_E_INVALID, who + ": negative count");
+  if ((int64_t)b->num_queries * b->heads > INT32_MAX)
+    return api_fail(FOLD_E_INVALID, who + ": queries times heads reach 2^31");
+  if (!b->query_ptr || !b->key_ptr) return api_fail(FOLD_E_INVALID, who + ": NULL query_ptr or key_ptr");
+  if (!b->source && b->num_seqs != b->num_sources)
+    return api_fail(FOLD_E_INVALID, who + ": without `source` there is a key sequence for each query sequence");
+  if (b->num_queries > b->num_query_rows || b->num_keys > b->num_key_rows)
+    return api_fail(FOLD_E_INVALID, who + ": more rows are listed than there are");
+  hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(st, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone)
+    return api_fail(FOLD_E_INVALID, who + ": the stream is being captured (a plan is made before)");
+  (void)hipGetLastError();
+
+  int device = 0;
+  FOLD_HIP_CHECK(hipGetDevice(&device));
+  std::vector<int32_t> qp((size_t)b->num_seqs + 1), kp((size_t)b->num_sources + 1), src((size_t)b->num_seqs);
+  uint32_t error = 0;
+  const size_t qw = b->query_row ? ((size_t)b->num_query_rows + 31) / 32 : 0;
+  const size_t kw = b->key_row ? ((size_t)b->num_key_rows + 31) / 32 : 0;
+  {
+    Block tmp{device, st};
+    tmp.p = pool_alloc(device, (64 + qw + kw) * sizeof(uint32_t), false);
+    if (!tmp.p) return api_fail(FOLD_E_NOMEM, who + ": no device memory");
+    uint32_t* words = static_cast<uint32_t*>(tmp.p);
+    hipLaunchKernelGGL(k_zero_words, dim3(grid_for(64 + qw + kw)), dim3(256), 0, st, words, 64 + qw + kw);
+    if (qw)
+      hipLaunchKernelGGL(k_check_rows, dim3(grid_for(b->num_queries)), dim3(256), 0, st, b->query_row, b->num_queries,
+                         b->num_query_rows, words + 64, words, 0);
+    if (kw)
+      hipLaunchKernelGGL(k_check_rows, dim3(grid_for(b->num_keys)), dim3(256), 0, st, b->key_row, b->num_keys,
+                         b->num_key_rows, words + 64 + qw, words, 2);
+    FOLD_HIP_CHECK(hipGetLastError());
+    const auto fetch = [&](void* to, const void* from, size_t n) {
+      return n == 0 || hipMemcpyAsync(to, from, n, hipMemcpyDeviceToHost, st) == hipSuccess;
+    };
+    if (!fetch(qp.data(), b->query_ptr, qp.size() * 4) || !fetch(kp.data(), b->key_ptr, kp.size() * 4) ||
+        (b->source && !fetch(src.data(), b->source, src.size() * 4)) || !fetch(&error, words, 4) ||
+        hipStreamSynchronize(st) != hipSuccess)
+      return api_fail(FOLD_E_DEVICE, who + ": the lists could not be read");
+  }
+  if (!check_ptr(qp, b->num_queries)) return api_fail(FOLD_E_INVALID, who + ": query_ptr malformed");
+  if (!check_ptr(kp, b->num_keys)) return api_fail(FOLD_E_INVALID, who + ": key_ptr malformed");
+  if (error & 5) return api_fail(FOLD_E_INVALID, who + (error & 1 ? ": query_row" : ": key_row") + " out of range");
+  if (error & 10) return api_fail(FOLD_E_INVALID, who + (error & 2 ? ": query_row" : ": key_row") + " lists a row twice");
+  Lists l{qp, kp, src, b->heads / b->kv_heads, b->kv_heads, {}};
+  l.readers.resize((size_t)b->num_sources + 1);
+  for (int s = 0; s < b->num_seqs; ++s) {
+    const int e = b->source ? src[s] : s;
+    if (e < -1 || e >= b->num_sources) return api_fail(FOLD_E_INVALID, who + ": source out of range");
+    l.readers[e < 0 ? b->num_sources : e].push_back(s);
+  }
+
+  fold_cross* h = new fold_cross;
+  Cross& c = h->c;
+  struct Guard {
+    fold_cross*& h;
+    ~Guard() { cross_destroy(h); }
+  } guard{h};
+  c.device = device;
+  c.dtype = b->dtype;
+  c.heads = b->heads;
+  c.kv_heads = b->kv_heads;
+  c.head_dim = b->head_dim;
+  c.group = l.G;
+  c.num_seqs = b->num_seqs;
+  c.num_sources = b->num_sources;
+  c.num_queries = b->num_queries;
+  c.num_keys = b->num_keys;
+  c.query_rows = b->num_query_rows;
+  c.key_rows = b->num_key_rows;
+  // tiles of 32 rows where those of 128 would be mostly empty
+  int64_t tall = 0, low = 0;
+  for (int s = 0; s < b->num_seqs; ++s) {
+    const int64_t n = (int64_t)(qp[s + 1] - qp[s]) * l.G, e = b->source ? src[s] : s;
+    const int64_t keys = e < 0 ? 0 : kp[e + 1] - kp[e];
+    tall += (n + kCrossRows - 1) / kCrossRows * keys;
+    low += (n + kCrossFew - 1) / kCrossFew * keys;
+  }
+  c.few = low < 2 * tall && cross_padded(c.head_dim) * (c.dtype == FOLD_BF16 ? 2 : 4) <= kCrossFewBytes;
+  std::vector<QTile> fwd, fjoin, back, bjoin;
+  std::vector<KTile> keys, kjoin;
+  std::vector<RTile> rows;
+  query_tiles(l, c.few ? kCrossFew : kCrossRows, &fwd, &fjoin, &c.fslots);
+  query_tiles(l, kCrossRows, &back, &bjoin, &c.bslots);
+  key_tiles(l, c.dtype == FOLD_BF16 ? 64 : 32, &keys, &kjoin, &rows, &c.kslots);
+
+  size_t bytes = 0;
+  std::vector<std::pair<size_t, std::pair<const void*, size_t>>> copies;
+  const auto place = [&](const void* data, size_t n) {
+    const size_t at = bytes;
+    copies.push_back({at, {data, n}});
+    bytes += (n + 255) / 256 * 256;
+    return at;
+  };
+  const size_t at_fwd = place(fwd.data(), fwd.size() * sizeof(QTile)), at_fj = place(fjoin.data(), fjoin.size() * sizeof(QTile)),
+               at_back = place(back.data(), back.size() * sizeof(QTile)),
+               at_bj = place(bjoin.data(), bjoin.size() * sizeof(QTile)),
+               at_keys = place(keys.data(), keys.size() * sizeof(KTile)),
+               at_kj = place(kjoin.data(), kjoin.size() * sizeof(KTile)),
+               at_rows = place(rows.data(), rows.size() * sizeof(RTile));
+  const size_t at_qr = place(nullptr, b->query_row ? (size_t)b->num_queries * 4 : 0);
+  const size_t at_kr = place(nullptr, b->key_row ? (size_t)b->num_keys * 4 : 0);
+  c.blob = pool_alloc(device, std::max<size_t>(bytes, 256), true);
+  if (!c.blob) return api_fail(FOLD_E_NOMEM, who + ": no device memory");
+  char* base = static_cast<char*>(c.blob);
+  bool ok = true;
+  for (const auto& cp : copies)
+    if (cp.second.first && cp.second.second)
+      ok = ok && hipMemcpyAsync(base + cp.first, cp.second.first, cp.second.second, hipMemcpyHostToDevice, st) == hipSuccess;
+  const auto keep = [&](size_t at, const int32_t* from, int n) {
+    if (from && n > 0)
+      ok = ok && hipMemcpyAsync(base + at, from, (size_t)n * 4, hipMemcpyDeviceToDevice, st) == hipSuccess;
+    return from ? reinterpret_cast<int32_t*>(base + at) : nullptr;
+  };
+  c.q_row = keep(at_qr, b->query_row, b->num_queries);
+  c.k_row = keep(at_kr, b->key_row, b->num_keys);
+  if (!(hipStreamSynchronize(st) == hipSuccess && ok)) return api_fail(FOLD_E_DEVICE, who + ": the plan could not be written");
+  c.fwd = reinterpret_cast<QTile*>(base + at_fwd);
+  c.fjoin = reinterpret_cast<QTile*>(base + at_fj);
+  c.back = reinterpret_cast<QTile*>(base + at_back);
+  c.bjoin = reinterpret_cast<QTile*>(base + at_bj);
+  c.keys = reinterpret_cast<KTile*>(base + at_keys);
+  c.kjoin = reinterpret_cast<KTile*>(base + at_kj);
+  c.rows = reinterpret_cast<RTile*>(base + at_rows);
+  c.nfwd = (int)fwd.size();
+  c.nfjoin = (int)fjoin.size();
+  c.nback = (int)back.size();
+  c.nbjoin = (int)bjoin.size();
+  c.nkeys = (int)keys.size();
+  c.nkjoin = (int)kjoin.size();
+  c.nrows = (int)rows.size();
+  *out = h;
+  h = nullptr;
+  return FOLD_OK;
+}
+
+void cross_destroy(fold_cross* h) {
+  if (!h) return;
+  if (h->c.blob) pool_free_after_wait(h->c.device, h->c.blob);
+  delete h;
+}
+
+}  // namespace fold

@@ -11,9 +11,10 @@ The functions keep the ABI's names:
     fold_forward, fold_backward, fold_row_ld, fold_last_error,
     fold_graph_create, fold_graph_launch, fold_graph_num_nodes, fold_graph_free,
     fold_vocab_logits, fold_vocab_backward, fold_loss_distill, fold_token_logprobs,
-    fold_layer_norm, fold_layer_norm_backward, fold_linear, fold_linear_backward
-``Schedule`` / ``Packed`` / ``StepGraph`` / ``VocabHead`` / ``Linear``, ``distill_loss``, ``token_logprobs``,
-``layer_norm`` and ``layer_norm_backward`` wrap them for tensors.
+    fold_layer_norm, fold_layer_norm_backward, fold_linear, fold_linear_backward,
+    fold_cross_create, fold_cross_free, fold_cross_workspace_size, fold_cross_attend, fold_cross_backward
+``Schedule`` / ``Packed`` / ``StepGraph`` / ``VocabHead`` / ``Linear`` / ``CrossAttention``, ``distill_loss``,
+``token_logprobs``, ``layer_norm`` and ``layer_norm_backward`` wrap them for tensors.
 """
 from __future__ import annotations
 
@@ -126,6 +127,13 @@ FOLD_BLOCK_ACCUMULATE = 1
 ACTIVATIONS = {"none": FOLD_ACT_NONE, "relu": FOLD_ACT_RELU, "tanh": FOLD_ACT_TANH, "gelu": FOLD_ACT_GELU}
 
 
+class fold_cross_batch(ctypes.Structure):
+    _fields_ = [("dtype", c_int32), ("heads", c_int32), ("kv_heads", c_int32), ("head_dim", c_int32),
+                ("num_seqs", c_int32), ("num_sources", c_int32), ("num_queries", c_int32), ("num_keys", c_int32),
+                ("num_query_rows", c_int32), ("num_key_rows", c_int32), ("query_ptr", c_void_p), ("query_row", c_void_p),
+                ("key_ptr", c_void_p), ("key_row", c_void_p), ("source", c_void_p)]
+
+
 class fold_kernel_stat(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char * 48), ("launches", c_int64), ("total_ms", ctypes.c_double),
                 ("max_ms", ctypes.c_double)]
@@ -152,7 +160,8 @@ EXPORTS = ["fold_schedule", "fold_sched_get_info", "fold_sched_free", "fold_pack
            "fold_typed_sched_free", "fold_level_launches", "fold_trim", "fold_vocab_logits", "fold_vocab_backward",
            "fold_vocab_workspace_size", "fold_loss_distill", "fold_distill_workspace_size", "fold_token_logprobs",
            "fold_token_workspace_size", "fold_layer_norm", "fold_layer_norm_workspace_size", "fold_layer_norm_backward",
-           "fold_linear", "fold_linear_workspace_size", "fold_linear_backward"]
+           "fold_linear", "fold_linear_workspace_size", "fold_linear_backward", "fold_cross_create",
+           "fold_cross_free", "fold_cross_workspace_size", "fold_cross_attend", "fold_cross_backward"]
 
 _lib = None
 
@@ -281,6 +290,19 @@ def lib():
     L.fold_linear_backward.argtypes = [c_int32, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
                                        c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_void_p,
                                        c_size_t, c_void_p]
+    L.fold_cross_create.restype = c_int32
+    L.fold_cross_create.argtypes = [POINTER(fold_cross_batch), c_void_p, POINTER(c_void_p)]
+    L.fold_cross_free.restype = c_int32
+    L.fold_cross_free.argtypes = [c_void_p]
+    L.fold_cross_workspace_size.restype = c_int32
+    L.fold_cross_workspace_size.argtypes = [c_void_p, POINTER(c_size_t), POINTER(c_size_t)]
+    L.fold_cross_attend.restype = c_int32
+    L.fold_cross_attend.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                                    ctypes.c_float, c_void_p, c_int64, c_void_p, c_void_p, c_size_t, c_void_p]
+    L.fold_cross_backward.restype = c_int32
+    L.fold_cross_backward.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                                      ctypes.c_float, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_int64,
+                                      c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_size_t, c_void_p]
     _lib = L
     return L
 
@@ -499,6 +521,34 @@ def fold_linear_backward(dtype, rows, in_dim, out_dim, x, W, act, pre, dout, dpr
     _check(lib().fold_linear_backward(int(dtype), int(rows), int(in_dim), int(out_dim), _ptr(x), _ptr(W), int(act),
                                       _ptr(pre), _ptr(dout), _ptr(dpre), int(dx_dtype), _ptr(dx), int(dw_dtype), _ptr(dW),
                                       _ptr(dbias), int(flags), _ptr(ws), int(ws_bytes), _stream(stream)))
+
+
+def fold_cross_create(batch: fold_cross_batch, stream=None) -> c_void_p:
+    h = c_void_p()
+    _check(lib().fold_cross_create(byref(batch), _stream(stream), byref(h)))
+    return h
+
+
+def fold_cross_free(handle):
+    _check(lib().fold_cross_free(handle))
+
+
+def fold_cross_workspace_size(cross):
+    f, b = c_size_t(), c_size_t()
+    _check(lib().fold_cross_workspace_size(cross, byref(f), byref(b)))
+    return int(f.value), int(b.value)
+
+
+def fold_cross_attend(cross, q, ldq, k, ldk, v, ldv, key_mask, scale, out, ldo, lse, ws, ws_bytes, stream=None):
+    _check(lib().fold_cross_attend(cross, _ptr(q), int(ldq), _ptr(k), int(ldk), _ptr(v), int(ldv), _ptr(key_mask),
+                                   float(scale), _ptr(out), int(ldo), _ptr(lse), _ptr(ws), int(ws_bytes), _stream(stream)))
+
+
+def fold_cross_backward(cross, q, ldq, k, ldk, v, ldv, key_mask, scale, out, ldo, lse, dout, lddo, dq, lddq, dk, lddk, dv,
+                        lddv, ws, ws_bytes, stream=None):
+    _check(lib().fold_cross_backward(cross, _ptr(q), int(ldq), _ptr(k), int(ldk), _ptr(v), int(ldv), _ptr(key_mask),
+                                     float(scale), _ptr(out), int(ldo), _ptr(lse), _ptr(dout), int(lddo), _ptr(dq), int(lddq),
+                                     _ptr(dk), int(lddk), _ptr(dv), int(lddv), _ptr(ws), int(ws_bytes), _stream(stream)))
 
 
 def fold_packed_free(handle):
@@ -1104,3 +1154,142 @@ class Linear:
                                  FOLD_F32 if dW is None else _code(dW.dtype), dW, dbias,
                                  FOLD_BLOCK_ACCUMULATE if accumulate else 0, ws, n, stream or _CURRENT)
         return dx, dW, dbias
+
+
+def _columns(name, t, width, dtype, rows):
+    """A matrix [rows, width or more] whose rows may lie apart (columns of a wider matrix)."""
+    if not (t.is_cuda and t.dim() == 2 and t.shape[1] >= width and (t.stride(1) == 1 or t.shape[1] <= 1)):
+        raise ValueError(f"{name}: a 2-D CUDA tensor with rows of at least {width} neighbouring elements is needed")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.shape[0] != rows:
+        raise ValueError(f"{name}: expected {rows} rows, got {t.shape[0]}")
+    _here(name, t)
+    return t
+
+
+def _stride(t):
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+class CrossAttention:
+    """Cross attention of query sequences to key sequences (fold_cross_create; forward: fold_cross_attend, backward:
+    fold_cross_backward).
+
+    query_ptr [sequences + 1], key_ptr [sources + 1], query_rows [list entries], key_rows, source [sequences]: int32 CUDA
+    tensors; rows None: row i is list entry i.  With schedules: graph_ptr and the schedule's node_pos (`schedule_rows`).
+    num_query_rows, num_key_rows: rows of the matrices (the list entries by default).  The object is made once for a batch
+    (it synchronises); its calls may be captured.  Results and workspaces are new tensors of the calls' stream."""
+
+    def __init__(self, heads, head_dim, query_ptr, key_ptr, query_rows=None, key_rows=None, num_query_rows=None,
+                 num_key_rows=None, source=None, kv_heads=None, dtype=None, num_queries=None, num_keys=None, stream=None):
+        import torch
+        self.heads, self.head_dim = int(heads), int(head_dim)
+        self.kv_heads = self.heads if kv_heads is None else int(kv_heads)
+        self.dtype = torch.bfloat16 if dtype is None else dtype
+        for name, t in (("query_ptr", query_ptr), ("key_ptr", key_ptr), ("query_rows", query_rows), ("key_rows", key_rows),
+                        ("source", source)):
+            if t is not None:
+                _vector(name, t, torch.int32, t.numel())
+        if query_ptr.numel() < 1 or key_ptr.numel() < 1:
+            raise ValueError("query_ptr and key_ptr have an entry more than there are sequences")
+        # (without a list and a count the end of ptr is read, which waits for the GPU, as making the plan does)
+        count = lambda rows, n, ptr: int(rows.numel()) if rows is not None else int(ptr[-1]) if n is None else int(n)  # noqa: E731
+        self.num_queries = count(query_rows, num_queries, query_ptr)
+        self.num_keys = count(key_rows, num_keys, key_ptr)
+        self.query_rows = self.num_queries if num_query_rows is None else int(num_query_rows)
+        self.key_rows = self.num_keys if num_key_rows is None else int(num_key_rows)
+        if source is not None and source.numel() != query_ptr.numel() - 1:
+            raise ValueError("source has an entry for each query sequence")
+        b = fold_cross_batch(_code(self.dtype), self.heads, self.kv_heads, self.head_dim, query_ptr.numel() - 1,
+                             key_ptr.numel() - 1, self.num_queries, self.num_keys, self.query_rows, self.key_rows,
+                             _ptr(query_ptr), _ptr(query_rows), _ptr(key_ptr), _ptr(key_rows), _ptr(source))
+        self.handle = None
+        with _on(stream):
+            self.handle = fold_cross_create(b, stream)
+        self.ws_bytes = fold_cross_workspace_size(self.handle)
+        self.whole = self.num_queries == self.query_rows, self.num_keys == self.key_rows  # every row is listed
+
+    def __del__(self):
+        h = getattr(self, "handle", None)
+        if h is not None and h.value:
+            try:
+                fold_cross_free(h)
+            except Exception:
+                pass
+            self.handle = None
+
+    def _new(self, rows, width, whole, like):
+        """Zeros where the call leaves something alone: rows that are not listed, pad columns."""
+        import torch
+        make = torch.empty if whole and width % 64 == 0 else torch.zeros
+        return make((rows, _row_ld(width)), dtype=self.dtype, device=like.device)
+
+    def _inputs(self, q, k, v, key_mask, scale):
+        import torch
+        wq, wk = self.heads * self.head_dim, self.kv_heads * self.head_dim
+        _columns("q", q, wq, self.dtype, self.query_rows)
+        _columns("k", k, wk, self.dtype, self.key_rows)
+        _columns("v", v, wk, self.dtype, self.key_rows)
+        if key_mask is not None:
+            if key_mask.dtype == torch.bool:
+                key_mask = key_mask.view(torch.uint8)
+            _vector("key_mask", key_mask, torch.uint8, self.num_keys)
+        return wq, wk, key_mask, self.head_dim ** -0.5 if scale is None else float(scale)
+
+    def forward(self, q, k, v, key_mask=None, scale=None, out=None, lse=True, stream=None):
+        """(out [query rows, fold_row_ld(heads * head_dim)], lse [query rows, heads]) of q [query rows, ...] and k, v [key
+        rows, ...] (columns of wider matrices, for one).  key_mask: uint8 or bool [num_keys] in list order; scale:
+        head_dim^-1/2 by default; out: a tensor to write; lse: a tensor to write, or None to leave it out."""
+        import torch
+        wq, _, key_mask, scale = self._inputs(q, k, v, key_mask, scale)
+        with _on(stream):
+            out = self._new(self.query_rows, wq, self.whole[0], q) if out is None else _columns(
+                "out", out, wq, self.dtype, self.query_rows)
+            if lse is True:
+                lse = (torch.empty if self.whole[0] else torch.zeros)((self.query_rows, self.heads), dtype=torch.float32,
+                                                                      device=q.device)
+            elif lse is not None:
+                _vector("lse", lse, torch.float32, self.query_rows, self.heads)
+            n = self.ws_bytes[0]
+            ws = _bytes(n, q.device)
+            fold_cross_attend(self.handle, q, _stride(q), k, _stride(k), v, _stride(v), key_mask, scale, out, _stride(out),
+                              lse, ws, n, stream or _CURRENT)
+        return out, lse
+
+    def backward(self, q, k, v, out, lse, dout, key_mask=None, scale=None, dq=True, dk=True, dv=True, stream=None):
+        """(dq, dk, dv) of `dout`, shaped as q, k and v are made by forward()'s rules; out and lse as it gave them.  Each of
+        the three: True for a new tensor, a tensor to write (columns of a wider one, for instance), or None."""
+        import torch
+        wq, wk, key_mask, scale = self._inputs(q, k, v, key_mask, scale)
+        _columns("out", out, wq, self.dtype, self.query_rows)
+        _columns("dout", dout, wq, self.dtype, self.query_rows)
+        _vector("lse", lse, torch.float32, self.query_rows, self.heads)
+        with _on(stream):
+            made = []
+            for name, t, rows, w, whole in (("dq", dq, self.query_rows, wq, self.whole[0]),
+                                            ("dk", dk, self.key_rows, wk, self.whole[1]),
+                                            ("dv", dv, self.key_rows, wk, self.whole[1])):
+                made.append(self._new(rows, w, whole, q) if t is True else None if t is None
+                            else _columns(name, t, w, self.dtype, rows))
+            dq, dk, dv = made
+            ld = lambda t: 0 if t is None else _stride(t)  # noqa: E731
+            n = self.ws_bytes[1]
+            ws = _bytes(n, q.device)
+            fold_cross_backward(self.handle, q, _stride(q), k, _stride(k), v, _stride(v), key_mask, scale, out, _stride(out),
+                                lse, dout, _stride(dout), dq, ld(dq), dk, ld(dk), dv, ld(dv), ws, n, stream or _CURRENT)
+        return dq, dk, dv
+
+
+def schedule_rows(sched) -> "torch.Tensor":  # noqa: F821
+    """The schedule's node_pos as a new int32 tensor: the pool row of every node, which with graph_ptr lists a batch's graphs
+    for CrossAttention."""
+    import torch
+    n = sched.info.num_nodes
+    out = torch.empty(n, dtype=torch.int32, device="cuda")
+    if n:
+        torch.cuda.current_stream().synchronize()
+        rc = _hip().hipMemcpy(c_void_p(out.data_ptr()), c_void_p(sched.info.node_pos), c_size_t(4 * n), 3)
+        if rc != 0:
+            raise RuntimeError(f"hipMemcpy failed ({rc})")
+    return out

@@ -111,3 +111,24 @@ def test_oracle_attention_gradients_against_differences():
             return (OB.attend(*[u if j == i else args[j] for j in range(3)], **a)[0] * dout).sum()
         assert abs(_difference(f, t, d) - (got[i] * d).sum()) < 1e-7
     assert not got[1][[1, 2, 4]].any() and not got[2][[1, 2, 4]].any()
+
+
+def test_cross_refuses(F):  # noqa: F811
+    """Sizes that a plan refuses before it looks at a list."""
+    ok = dict(dtype=0, heads=4, kv_heads=2, head_dim=64, num_seqs=3, num_sources=3, num_queries=10, num_keys=20,
+              num_query_rows=10, num_key_rows=20, query_ptr=4096, query_row=None, key_ptr=8192, key_row=None, source=None)
+
+    def create(**kw):
+        F.fold_cross_create(F.fold_cross_batch(**dict(ok, **kw)), NULL_STREAM)
+
+    for kw in (dict(dtype=2), dict(heads=0), dict(heads=1025, kv_heads=1025), dict(kv_heads=0), dict(kv_heads=3), dict(head_dim=0),
+               dict(head_dim=129), dict(heads=514, kv_heads=2), dict(num_seqs=-1), dict(num_keys=-1), dict(num_queries=-1), dict(num_sources=2),
+               dict(num_query_rows=9), dict(num_key_rows=19), dict(query_ptr=None), dict(key_ptr=None),
+               dict(heads=1024, kv_heads=1024, num_queries=1 << 21, num_query_rows=1 << 21)):
+        _refused(F, F.FOLD_E_INVALID, create, **kw)
+    _refused(F, F.FOLD_E_INVALID, F.fold_cross_attend, None, None, 0, None, 0, None, 0, None, 1.0, None, 0, None, None, 0,
+             NULL_STREAM)
+    _refused(F, F.FOLD_E_INVALID, F.fold_cross_backward, None, None, 0, None, 0, None, 0, None, 1.0, None, 0, None, None, 0,
+             None, 0, None, 0, None, 0, None, 0, NULL_STREAM)
+    _refused(F, F.FOLD_E_INVALID, F.fold_cross_workspace_size, None)
+    F.fold_cross_free(None)
