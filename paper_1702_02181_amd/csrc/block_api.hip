@@ -238,7 +238,7 @@ int check_cross(const std::string& who, const fold_cross* cross, const Cols* in,
   const int es = c.dtype == FOLD_BF16 ? 2 : 4;
   const auto bad = [&](const Cols& m, bool needed) {
     if (!m.p) return needed && m.rows > 0;
-    return m.ld < m.width || m.ld > INT32_MAX || (reinterpret_cast<uintptr_t>(m.p) & (es - 1)) != 0;
+    return m.ld < m.width || m.ld * es > INT32_MAX || (reinterpret_cast<uintptr_t>(m.p) & (es - 1)) != 0;
   };
   for (int i = 0; i < nin; ++i)
     if (bad(in[i], true)) return api_fail(FOLD_E_INVALID, who + ": NULL or misaligned matrix, or a stride below its width");

@@ -39,7 +39,7 @@ struct Cross {
   int dtype = 0, heads = 0, kv_heads = 0, head_dim = 0, group = 0;
   int num_seqs = 0, num_sources = 0, num_queries = 0, num_keys = 0, query_rows = 0, key_rows = 0;
   void* blob = nullptr;  // every device array below
-  int32_t *q_row = nullptr, *k_row = nullptr;  // NULL: row = list entry
+  int32_t *q_row = nullptr, *k_row = nullptr;  // the row of every list entry
   QTile* fwd = nullptr;   // the forward's workgroups
   QTile* fjoin = nullptr; // tiles in pieces
   QTile* back = nullptr;  // the queries' gradient's

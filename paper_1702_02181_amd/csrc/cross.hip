@@ -56,6 +56,21 @@ __device__ __forceinline__ void wave_barrier_lds() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// Values that were loaded before a loop are there: without it the compiler waits for them at their use inside the loop, where
+// the wait takes the direct loads in flight with it.
+template <int N>
+__device__ __forceinline__ void arrived(uint4 (&v)[N]) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    u32x4 t = __builtin_bit_cast(u32x4, v[i]);
+    asm volatile("" : "+v"(t));
+    v[i] = __builtin_bit_cast(uint4, t);
+  }
+}
+__device__ __forceinline__ void arrived(float& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void arrived(int& v) { asm volatile("" : "+v"(v)); }
+
 // ---- tiles in LDS ---------------------------------------------------------------------------------------------------
 
 // A row of a tile is U 16-byte units; unit u of row r lies at r U + (u ^ f(r)).  f puts the same unit of 16 consecutive rows
@@ -154,6 +169,12 @@ __device__ __forceinline__ uint4 row_unit(const T* row, int e0, int d) {
   return v;
 }
 
+// a row whose number and whose bytes to the next fit 32 bits: one multiplication into 64
+template <typename T>
+__device__ __forceinline__ const T* row_at(const T* base, int row, uint32_t ldb) {
+  return reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + (uint64_t)(uint32_t)row * ldb);
+}
+
 // One wave's share of the loads of a tile of ROWS rows that NW waves load together: NI instructions of 1 KB.
 template <typename T, int DP, int ROWS, int NW, bool VEC>
 struct TileLoader {
@@ -165,12 +186,12 @@ struct TileLoader {
   __device__ __forceinline__ int row(int i) const { return place(i) / U; }
   __device__ __forceinline__ int unit(int i) const { return place(i) % U ^ swizzle<U>(row(i)); }
   // idx[i]: the matrix row of tile row row(i), -1: zeros
-  __device__ __forceinline__ void load(const T* base, int64_t ld, int d, const int (&idx)[NI], char* lds) const {
+  __device__ __forceinline__ void load(const T* base, uint32_t ldb, int d, const int (&idx)[NI], char* lds) const {
     if constexpr (VEC) {
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int e0 = unit(i) * E;
-        const void* src = idx[i] >= 0 && e0 < d ? static_cast<const void*>(base + (int64_t)idx[i] * ld + e0)
+        const void* src = idx[i] >= 0 && e0 < d ? static_cast<const void*>(row_at(base, idx[i], ldb) + e0)
                                                 : static_cast<const void*>(g_zero);
         dma16_untracked(src, lds + (part * NI + i) * 1024);
       }
@@ -178,7 +199,7 @@ struct TileLoader {
       uint4 v[NI];
 #pragma unroll
       for (int i = 0; i < NI; ++i)
-        v[i] = idx[i] >= 0 ? row_unit<T, false>(base + (int64_t)idx[i] * ld, unit(i) * E, d) : make_uint4(0, 0, 0, 0);
+        v[i] = idx[i] >= 0 ? row_unit<T, false>(row_at(base, idx[i], ldb), unit(i) * E, d) : make_uint4(0, 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < NI; ++i) *reinterpret_cast<uint4*>(lds + place(i) * 16) = v[i];
     }
@@ -200,7 +221,7 @@ __device__ __forceinline__ void store4(T* p, const float (&v)[4], int d0, int d)
 
 struct Args {
   const void *q, *k, *v, *dout;
-  int64_t ldq, ldk, ldv, lddo;
+  uint32_t ldq, ldk, ldv, lddo;  // in bytes
   const int *q_row, *k_row;
   const uint8_t* mask;
   float scale;
@@ -212,7 +233,7 @@ struct Args {
   const float* delta;  // [query rows][heads]
   float* part;
 };
-__device__ __forceinline__ int row_of(const int* list, int entry) { return list ? list[entry] : entry; }
+__device__ __forceinline__ int row_of(const int* list, int entry) { return list[entry]; }
 
 // the virtual row r of a tile: its query's list entry and its head
 struct Virtual {
@@ -228,11 +249,49 @@ struct Virtual {
 
 constexpr float kSlack = 8.f;  // the reference is moved when a row's maximum has grown by a factor of 2^8
 
-// The keys that a tile of TK list entries from k0 holds, as bits.
 template <int TK>
-__device__ __forceinline__ uint64_t counting(int k0, int k_end, uint8_t m, int lane) {
-  return __ballot(lane < TK && k0 + lane < k_end && m != 0);
+constexpr uint64_t all_keys() { return TK == 64 ? ~0ull : (1ull << TK) - 1; }
+
+// A lane mask (on the scalar unit) of the keys that register r of block kb holds: key 8 (r / 4) + r % 4 in the lower half
+// wave, 4 more in the upper.
+__device__ __forceinline__ bool key_in(uint64_t bits, int kb, int r) {
+  const int at = 32 * kb + 8 * (r >> 2) + (r & 3);
+  const uint64_t lo = (bits >> at) & 1, hi = (bits >> (at + 4)) & 1;
+  return __builtin_amdgcn_inverse_ballot_w64((0 - lo & 0xffffffffull) | (0 - hi) << 32);
 }
+
+// The tiles of a run of keys on their way into LDS.  A tile's row numbers and mask are fetched while the tile two before it is
+// multiplied and looked at when its loads are issued, a tile later: a wait for them waits for the direct loads that were issued
+// before them too.
+template <typename T, int DP, int TK, int NW, bool VEC>
+struct KeyFeed {
+  using L = TileLoader<T, DP, TK, NW, VEC>;
+  const Args& a;
+  const L& ld;
+  int k_begin, k_end;
+  int idx[L::NI];
+  uint8_t mk;  // of entry lane % TK
+  __device__ __forceinline__ KeyFeed(const Args& a_, const QTile& t, const L& ld_)
+      : a(a_), ld(ld_), k_begin(t.k_begin), k_end(t.k_end), mk(1) {}
+  __device__ __forceinline__ void fetch(int tile) {
+    const int k0 = k_begin + tile * TK;
+#pragma unroll
+    for (int i = 0; i < L::NI; ++i) idx[i] = row_of(a.k_row, min(k0 + ld.row(i), k_end - 1));
+    if (a.mask) mk = a.mask[min(k0 + (ld.lane & (TK - 1)), k_end - 1)];
+  }
+  // starts the loads of the tile that was fetched; which of its keys count
+  __device__ __forceinline__ uint64_t issue(int tile, const T* k, const T* v, char* kt, char* vt) {
+#pragma unroll
+    for (int i = 0; i < L::NI; ++i) arrived(idx[i]);
+    const uint64_t bits = __ballot(ld.lane < TK && k_begin + tile * TK + ld.lane < k_end && mk != 0);
+    if (bits != all_keys<TK>())
+#pragma unroll
+      for (int i = 0; i < L::NI; ++i) idx[i] = (bits >> ld.row(i)) & 1 ? idx[i] : -1;
+    ld.load(k, a.ldk, a.d, idx, kt);
+    ld.load(v, a.ldv, a.d, idx, vt);
+    return bits;
+  }
+};
 
 // one value per lane of the running softmax of the lane's query, in base 2
 struct Running {
@@ -242,15 +301,12 @@ struct Running {
 // p^T of one tile from s^T (TK keys x 32 queries), and the accumulators' rescaling
 template <int KB, int DB>
 __device__ __forceinline__ void softmax_tile(f32x16 (&s)[KB], f32x16 (&o)[DB], Running& run, float c, uint64_t bits,
-                                             uint64_t all, int lane) {
-  const int h = lane >> 5;
+                                             uint64_t all) {
   if (bits != all) {
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const uint32_t w = (uint32_t)(bits >> (32 * kb)) >> (4 * h);
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[kb][r] = (w >> (8 * (r >> 2) + (r & 3))) & 1 ? s[kb][r] : -INFINITY;
-    }
+      for (int r = 0; r < 16; ++r) s[kb][r] = key_in(bits, kb, r) ? s[kb][r] : -INFINITY;
   }
   float top = s[0][0];
 #pragma unroll
@@ -309,7 +365,7 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
   const bool in = first + l32 < t.rows;
   uint4 qf[NS];
   {
-    const T* q = static_cast<const T*>(a.q) + (int64_t)qrow * a.ldq + vr.head * a.d;
+    const T* q = row_at(static_cast<const T*>(a.q), qrow, a.ldq) + vr.head * a.d;
 #pragma unroll
     for (int s = 0; s < NS; ++s) qf[s] = row_unit<T, VEC>(q, (2 * s + h) * E, a.d);
   }
@@ -325,43 +381,24 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
   char* mine = lds + (NW == 4 ? 0 : wave * 2 * BUF);
   constexpr int STRIDE = NW == 4 ? 1 : 4;
   const int ntile = (t.k_end - t.k_begin + TK - 1) / TK;
-  int idx[L::NI];
-  uint8_t mk = 1;
-  auto rows = [&](int tile) {  // the matrix rows of a tile's keys
-#pragma unroll
-    for (int i = 0; i < L::NI; ++i) {
-      const int e = t.k_begin + tile * TK + ld.row(i);
-      const bool there = e < t.k_end;
-      const int at = there ? e : t.k_end - 1;
-      int r = row_of(a.k_row, at);
-      if (a.mask && a.mask[at] == 0) r = -1;
-      idx[i] = there ? r : -1;
-    }
-  };
-  auto mask_of = [&](int tile) {
-    mk = a.mask ? a.mask[min(t.k_begin + tile * TK + (lane & (TK - 1)), t.k_end - 1)] : (uint8_t)1;
-  };
-  auto issue = [&](int buf) {
-    char* to = mine + buf * BUF;
-    ld.load(k, a.ldk, a.d, idx, to);
-    ld.load(v, a.ldv, a.d, idx, to + TB);
-  };
+  KeyFeed<T, DP, TK, NW, VEC> feed(a, t, ld);
+  auto issue = [&](int tile, int buf) { return feed.issue(tile, k, v, mine + buf * BUF, mine + buf * BUF + TB); };
   int at = NW == 4 ? 0 : wave;
+  uint64_t bits = 0;
+  if (at < ntile) feed.fetch(at);
+  arrived(qf);
   if (at < ntile) {
-    rows(at);
-    mask_of(at);
-    issue(0);
-    if (at + STRIDE < ntile) rows(at + STRIDE);
+    bits = issue(at, 0);
+    if (at + STRIDE < ntile) feed.fetch(at + STRIDE);
   }
   for (int buf = 0; at < ntile; at += STRIDE, buf ^= 1) {
-    const uint64_t bits = counting<TK>(t.k_begin + at * TK, t.k_end, mk, lane);
+    const uint64_t now = bits;
     vm_wait();
     if constexpr (NW == 4) __syncthreads();
     else wave_barrier_lds();
     if (at + STRIDE < ntile) {
-      issue(buf ^ 1);
-      mask_of(at + STRIDE);
-      if (at + 2 * STRIDE < ntile) rows(at + 2 * STRIDE);
+      bits = issue(at + STRIDE, buf ^ 1);
+      if (at + 2 * STRIDE < ntile) feed.fetch(at + 2 * STRIDE);
     }
     __builtin_amdgcn_sched_barrier(0);
     if (!active) continue;
@@ -375,7 +412,7 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
       for (int st = 0; st < NS; ++st)
         s[kb] = step_mma<T>(*reinterpret_cast<const uint4*>(kt + unit_at<U>(32 * kb + l32, 2 * st + h)), qf[st], s[kb]);
     }
-    softmax_tile<KB, DB>(s, o, run, c, bits, TK == 64 ? ~0ull : (1ull << TK) - 1, lane);
+    softmax_tile<KB, DB>(s, o, run, c, now, all_keys<TK>());
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) across_mma<T, U, DB>(vt, 32 * kb, Probs<T>(s[kb]), o, lane);
   }
@@ -558,8 +595,8 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
   const int qrow = row_of(a.q_row, vr.entry);
   uint4 qf[NS], df[NS];
   {
-    const T* q = static_cast<const T*>(a.q) + (int64_t)qrow * a.ldq + vr.head * a.d;
-    const T* g = static_cast<const T*>(a.dout) + (int64_t)qrow * a.lddo + vr.head * a.d;
+    const T* q = row_at(static_cast<const T*>(a.q), qrow, a.ldq) + vr.head * a.d;
+    const T* g = row_at(static_cast<const T*>(a.dout), qrow, a.lddo) + vr.head * a.d;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       qf[s] = row_unit<T, VEC>(q, (2 * s + h) * E, a.d);
@@ -567,7 +604,9 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
     }
   }
   const int64_t stat = (int64_t)qrow * a.heads + vr.head;
-  const float lse = a.lse[stat], delta = a.delta[stat], ref = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  float delta = a.delta[stat];
+  const float lse = a.lse[stat];
+  float ref = lse == -INFINITY ? INFINITY : lse * kLog2e;
   f32x16 dq[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db)
@@ -577,41 +616,25 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
   using L = TileLoader<T, DP, TK, 4, VEC>;
   const L ld(wave, lane);
   const int ntile = (t.k_end - t.k_begin + TK - 1) / TK;
-  int idx[L::NI];
-  uint8_t mk = 1;
-  auto rows = [&](int tile) {
-#pragma unroll
-    for (int i = 0; i < L::NI; ++i) {
-      const int e = t.k_begin + tile * TK + ld.row(i);
-      const bool there = e < t.k_end;
-      const int at = there ? e : t.k_end - 1;
-      int r = row_of(a.k_row, at);
-      if (a.mask && a.mask[at] == 0) r = -1;
-      idx[i] = there ? r : -1;
-    }
-  };
-  auto mask_of = [&](int tile) {
-    mk = a.mask ? a.mask[min(t.k_begin + tile * TK + (lane & (TK - 1)), t.k_end - 1)] : (uint8_t)1;
-  };
-  auto issue = [&](int buf) {
-    char* to = lds + buf * BUF;
-    ld.load(k, a.ldk, a.d, idx, to);
-    ld.load(v, a.ldv, a.d, idx, to + TB);
-  };
+  KeyFeed<T, DP, TK, 4, VEC> feed(a, t, ld);
+  auto issue = [&](int tile) { return feed.issue(tile, k, v, lds + (tile & 1) * BUF, lds + (tile & 1) * BUF + TB); };
+  uint64_t bits = 0;
+  if (ntile > 0) feed.fetch(0);
+  arrived(qf);
+  arrived(df);
+  arrived(ref);
+  arrived(delta);
   if (ntile > 0) {
-    rows(0);
-    mask_of(0);
-    issue(0);
-    if (ntile > 1) rows(1);
+    bits = issue(0);
+    if (ntile > 1) feed.fetch(1);
   }
   for (int at = 0; at < ntile; ++at) {
-    const uint64_t bits = counting<TK>(t.k_begin + at * TK, t.k_end, mk, lane);
+    const uint64_t now = bits;
     vm_wait();
     __syncthreads();
     if (at + 1 < ntile) {
-      issue((at + 1) & 1);
-      mask_of(at + 1);
-      if (at + 2 < ntile) rows(at + 2);
+      bits = issue(at + 1);
+      if (at + 2 < ntile) feed.fetch(at + 2);
     }
     __builtin_amdgcn_sched_barrier(0);
     if (!active) continue;
@@ -626,12 +649,11 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
         s = step_mma<T>(*reinterpret_cast<const uint4*>(kt + unit_at<U>(32 * kb + l32, 2 * st + h)), qf[st], s);
         dp = step_mma<T>(*reinterpret_cast<const uint4*>(vt + unit_at<U>(32 * kb + l32, 2 * st + h)), df[st], dp);
       }
-      const uint32_t w = (uint32_t)(bits >> (32 * kb)) >> (4 * h);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -ref));
-        s[r] = (w >> (8 * (r >> 2) + (r & 3))) & 1 ? p * (dp[r] - delta) : 0.f;
-      }
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -ref)) * (dp[r] - delta);
+      if (now != all_keys<TK>())
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = key_in(now, kb, r) ? s[r] : 0.f;
       across_mma<T, U, DB>(kt, 32 * kb, Probs<T>(s), dq, lane);
     }
   }
@@ -684,8 +706,8 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 2)) void k_cr
   const bool counts = !a.mask || a.mask[ke] != 0;
   uint4 kf[NS], vf[KEEP ? 1 : NS];
   {
-    const T* k = static_cast<const T*>(a.k) + (int64_t)krow * a.ldk + t.kv_head * a.d;
-    const T* v = static_cast<const T*>(a.v) + (int64_t)krow * a.ldv + t.kv_head * a.d;
+    const T* k = row_at(static_cast<const T*>(a.k), krow, a.ldk) + t.kv_head * a.d;
+    const T* v = row_at(static_cast<const T*>(a.v), krow, a.ldv) + t.kv_head * a.d;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       kf[s] = row_unit<T, VEC>(k, (2 * s + h) * E, a.d);
@@ -702,70 +724,82 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 2)) void k_cr
   using L = TileLoader<T, DP, RQ, 4, VEC>;
   const L ld(wave, lane);
   const T *q = static_cast<const T*>(a.q), *g = static_cast<const T*>(a.dout);
-  int idx[L::NI], head[L::NI];
-  float lse2 = INFINITY, delta = 0.f;  // of the next tile's row `lane`, by wave 0
-  auto rows = [&](int tile) {
-    const RTile rt = runs[tile];
+  // A row tile's row numbers are fetched while the tile two before it is multiplied, what they lead to (the loads into LDS,
+  // lse and delta) a tile later, as in KeyFeed; wave 0's lanes also hold a row each for lse and delta.
+  int idx[L::NI], head[L::NI], stat_row = 0, stat_head = 0, nrows = 0;
+  float lse = 0.f, delta = 0.f;  // of row `lane` of the tile that was issued last
+  bool there = false;
+  RTile next = t.t_begin < t.t_end ? runs[t.t_begin] : RTile{};
+  auto fetch = [&](int tile) {  // and the list's entry of the tile after it
+    RTile rt;
+    rt.entry = __builtin_amdgcn_readfirstlane(next.entry);
+    rt.head0 = __builtin_amdgcn_readfirstlane(next.head0);
+    rt.rows = __builtin_amdgcn_readfirstlane(next.rows);
+    next = runs[min(tile + 1, t.t_end - 1)];
+    nrows = rt.rows;
 #pragma unroll
     for (int i = 0; i < L::NI; ++i) {
       const Virtual vr(a, rt.entry, rt.head0, t.kv_head, min(ld.row(i), rt.rows - 1));
       head[i] = vr.head * a.d;
       idx[i] = row_of(a.q_row, vr.entry);
-      idx[i] = ld.row(i) < rt.rows ? idx[i] : -1;
+    }
+    if (wave == 0) {
+      const Virtual vr(a, rt.entry, rt.head0, t.kv_head, min(lane & (RQ - 1), rt.rows - 1));
+      stat_row = row_of(a.q_row, vr.entry);
+      stat_head = vr.head;
     }
   };
-  auto fetch_stats = [&](int tile) {
-    if (wave != 0) return;
-    const RTile rt = runs[tile];
-    const int r = lane & (RQ - 1);
-    const Virtual vr(a, rt.entry, rt.head0, t.kv_head, min(r, rt.rows - 1));
-    const int64_t at = (int64_t)row_of(a.q_row, vr.entry) * a.heads + vr.head;
-    const float lse = a.lse[at];
-    delta = r < rt.rows ? a.delta[at] : 0.f;
-    lse2 = r < rt.rows && lse != -INFINITY ? lse * kLog2e : INFINITY;
-  };
   auto issue = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < L::NI; ++i) arrived(idx[i]);
+    arrived(stat_row);
     char* to = lds + buf * BUF;
     if constexpr (VEC) {
 #pragma unroll
       for (int i = 0; i < L::NI; ++i) {
         const int e0 = ld.unit(i) * E;
-        const bool there = idx[i] >= 0 && e0 < a.d;
+        const bool in = ld.row(i) < nrows && e0 < a.d;
         const void* z = g_zero;
-        dma16_untracked(there ? q + (int64_t)idx[i] * a.ldq + head[i] + e0 : z, to + (ld.part * L::NI + i) * 1024);
-        dma16_untracked(there ? g + (int64_t)idx[i] * a.lddo + head[i] + e0 : z, to + TB + (ld.part * L::NI + i) * 1024);
+        dma16_untracked(in ? row_at(q, idx[i], a.ldq) + head[i] + e0 : z, to + (ld.part * L::NI + i) * 1024);
+        dma16_untracked(in ? row_at(g, idx[i], a.lddo) + head[i] + e0 : z, to + TB + (ld.part * L::NI + i) * 1024);
       }
     } else {
 #pragma unroll
       for (int i = 0; i < L::NI; ++i) {
         uint4 x = make_uint4(0, 0, 0, 0), y = x;
-        if (idx[i] >= 0) {
-          x = row_unit<T, false>(q + (int64_t)idx[i] * a.ldq + head[i], ld.unit(i) * E, a.d);
-          y = row_unit<T, false>(g + (int64_t)idx[i] * a.lddo + head[i], ld.unit(i) * E, a.d);
+        if (ld.row(i) < nrows) {
+          x = row_unit<T, false>(row_at(q, idx[i], a.ldq) + head[i], ld.unit(i) * E, a.d);
+          y = row_unit<T, false>(row_at(g, idx[i], a.lddo) + head[i], ld.unit(i) * E, a.d);
         }
         *reinterpret_cast<uint4*>(to + ld.place(i) * 16) = x;
         *reinterpret_cast<uint4*>(to + TB + ld.place(i) * 16) = y;
       }
     }
+    if (wave == 0) {
+      const int64_t at = (int64_t)stat_row * a.heads + stat_head;
+      lse = a.lse[at];
+      delta = a.delta[at];
+      there = (lane & (RQ - 1)) < nrows;
+    }
   };
+  if (t.t_begin < t.t_end) fetch(t.t_begin);
+  arrived(kf);
+  if constexpr (!KEEP) arrived(vf);
   if (t.t_begin < t.t_end) {
-    rows(t.t_begin);
-    fetch_stats(t.t_begin);
     issue(0);
-    if (t.t_begin + 1 < t.t_end) rows(t.t_begin + 1);
+    if (t.t_begin + 1 < t.t_end) fetch(t.t_begin + 1);
   }
   for (int at = t.t_begin; at < t.t_end; ++at) {
     const int buf = (at - t.t_begin) & 1;
     if (wave == 0 && lane < RQ) {
-      stats[buf][0][lane] = lse2;
-      stats[buf][1][lane] = delta;
+      stats[buf][0][lane] = there && lse != -INFINITY ? lse * kLog2e : INFINITY;  // no row: p = 0
+      stats[buf][1][lane] = there ? delta : 0.f;
     }
     vm_wait();
     __syncthreads();
     if (at + 1 < t.t_end) {
       issue(buf ^ 1);
-      fetch_stats(at + 1);
-      if (at + 2 < t.t_end) rows(at + 2);
+      if (at + 2 < t.t_end) fetch(at + 2);
     }
     __builtin_amdgcn_sched_barrier(0);
     if (!active) continue;
@@ -890,9 +924,10 @@ Args args_of(const Cross& c, const CrossMat& q, const CrossMat& k, const CrossMa
   a.q = q.p;
   a.k = k.p;
   a.v = v.p;
-  a.ldq = q.ld;
-  a.ldk = k.ld;
-  a.ldv = v.ld;
+  const int es = c.dtype == FOLD_BF16 ? 2 : 4;
+  a.ldq = (uint32_t)(q.ld * es);
+  a.ldk = (uint32_t)(k.ld * es);
+  a.ldv = (uint32_t)(v.ld * es);
   a.q_row = c.q_row;
   a.k_row = c.k_row;
   a.mask = mask;
@@ -955,7 +990,7 @@ void launch_cross_backward(const Cross& c, CrossMat q, CrossMat k, CrossMat v, c
                            int64_t lddv, void* ws, hipStream_t st) {
   Args a = args_of(c, q, k, v, mask, scale);
   a.dout = dout.p;
-  a.lddo = dout.ld;
+  a.lddo = (uint32_t)(dout.ld * (c.dtype == FOLD_BF16 ? 2 : 4));
   a.lse = const_cast<float*>(lse);
   float* delta = static_cast<float*>(ws);
   a.delta = delta;

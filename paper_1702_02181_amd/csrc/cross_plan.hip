@@ -34,6 +34,10 @@ __global__ __launch_bounds__(256) void k_check_rows(const int32_t* row, int n, i
   }
 }
 
+__global__ __launch_bounds__(256) void k_identity(int32_t* row, int n) {
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) row[i] = i;
+}
+
 struct Range {
   int64_t begin, end;
   int64_t size() const { return end - begin; }
@@ -332,8 +336,7 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
                at_keys = place(keys.data(), keys.size() * sizeof(KTile)),
                at_kj = place(kjoin.data(), kjoin.size() * sizeof(KTile)),
                at_rows = place(rows.data(), rows.size() * sizeof(RTile));
-  const size_t at_qr = place(nullptr, b->query_row ? (size_t)b->num_queries * 4 : 0);
-  const size_t at_kr = place(nullptr, b->key_row ? (size_t)b->num_keys * 4 : 0);
+  const size_t at_qr = place(nullptr, (size_t)b->num_queries * 4), at_kr = place(nullptr, (size_t)b->num_keys * 4);
   c.blob = pool_alloc(device, std::max<size_t>(bytes, 256), true);
   if (!c.blob) return api_fail(FOLD_E_NOMEM, who + ": no device memory");
   char* base = static_cast<char*>(c.blob);
@@ -342,9 +345,12 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
     if (cp.second.first && cp.second.second)
       ok = ok && hipMemcpyAsync(base + cp.first, cp.second.first, cp.second.second, hipMemcpyHostToDevice, st) == hipSuccess;
   const auto keep = [&](size_t at, const int32_t* from, int n) {
-    if (from && n > 0)
-      ok = ok && hipMemcpyAsync(base + at, from, (size_t)n * 4, hipMemcpyDeviceToDevice, st) == hipSuccess;
-    return from ? reinterpret_cast<int32_t*>(base + at) : nullptr;
+    int32_t* to = reinterpret_cast<int32_t*>(base + at);
+    if (n > 0 && from)
+      ok = ok && hipMemcpyAsync(to, from, (size_t)n * 4, hipMemcpyDeviceToDevice, st) == hipSuccess;
+    else if (n > 0)
+      hipLaunchKernelGGL(k_identity, dim3(grid_for(n)), dim3(256), 0, st, to, n);
+    return to;
   };
   c.q_row = keep(at_qr, b->query_row, b->num_queries);
   c.k_row = keep(at_kr, b->key_row, b->num_keys);
