@@ -219,6 +219,44 @@ __device__ __forceinline__ void store4(T* p, const float (&v)[4], int d0, int d)
   }
 }
 
+// A wave's 32 rows of a result, which lie on the accumulators' columns, to memory through an image in LDS of its own, so that an
+// instruction stores whole rows: stored from the registers, 8 bytes of 32 rows at a time, the keys' gradient of 64 chains of
+// 640 nodes, 16 heads of 64, spent more time on its stores than on its products.  row(r): where row r goes, NULL: nowhere.
+template <typename T, int DP>
+constexpr int image_row() { return DP * (int)sizeof(T) + 16; }
+template <typename T, int DP>
+constexpr int image_bytes() { return 32 * image_row<T, DP>(); }
+template <typename T, int DP, bool VEC, class ROW>
+__device__ __forceinline__ void store_image(const f32x16 (&acc)[DP / 32], float factor, int d, char* img, int lane, ROW&& row) {
+  constexpr int U = DP * (int)sizeof(T) / 16, E = 16 / (int)sizeof(T);
+  const int h = lane >> 5, l32 = lane & 31;
+#pragma unroll
+  for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float w[4] = {acc[db][4 * j] * factor, acc[db][4 * j + 1] * factor, acc[db][4 * j + 2] * factor,
+                          acc[db][4 * j + 3] * factor};
+      store4<T, true>(reinterpret_cast<T*>(img + l32 * image_row<T, DP>()), w, 32 * db + 8 * j + 4 * h, DP);
+    }
+  wave_barrier_lds();
+#pragma unroll 4
+  for (int i = 0; i < 32 * U / 64; ++i) {
+    const int at = i * 64 + lane, r = at / U, e0 = at % U * E;
+    T* to = row(r);
+    const uint4 v = *reinterpret_cast<const uint4*>(img + r * image_row<T, DP>() + at % U * 16);
+    if (!to || e0 >= d) continue;
+    if constexpr (VEC) {
+      *reinterpret_cast<uint4*>(to + e0) = v;
+    } else {
+      const T* e = reinterpret_cast<const T*>(&v);
+#pragma unroll
+      for (int k = 0; k < E; ++k)
+        if (e0 + k < d) to[e0 + k] = e[k];
+    }
+  }
+  wave_barrier_lds();  // before the image is written again
+}
+
 struct Args {
   const void *q, *k, *v, *dout;
   uint32_t ldq, ldk, ldv, lddo;  // in bytes
@@ -351,7 +389,8 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
   constexpr int E = 16 / (int)sizeof(T), ROWS = NW == 4 ? kCrossRows : kCrossFew;
   constexpr int BUF = 2 * TB;  // a tile of keys and one of values
   constexpr int MEET = NW == 1 ? 4 * 32 * (DP + 4) * 4 + 4 * 32 * 8 : 0;
-  constexpr int LDS = 2 * BUF * (NW == 1 ? 4 : 1);
+  constexpr int IMAGES = NW == 4 ? 4 * image_bytes<T, DP>() : 0;
+  constexpr int TILES = 2 * BUF * (NW == 1 ? 4 : 1), LDS = TILES > IMAGES ? TILES : IMAGES;
   __shared__ __attribute__((aligned(16))) char lds[LDS > MEET ? LDS : MEET];
   const QTile t = tiles[blockIdx.x];
   if (t.rows == 0) return;
@@ -419,8 +458,10 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
   run.l = halves_sum(run.l);
   T* out = static_cast<T*>(a.out);
   if constexpr (NW == 4) {
-    if (!active || !in) return;
+    __syncthreads();  // the images lie where the tiles were
+    if (!active) return;
     if (t.slot >= 0) {
+      if (!in) return;
       float* p = a.part + (size_t)t.slot * slot_floats<DP>(ROWS);
 #pragma unroll
       for (int db = 0; db < DB; ++db)
@@ -435,15 +476,12 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
       return;
     }
     const float inv = run.l > 0.f || run.l != run.l ? 1.f / run.l : 0.f;
-    T* to = out + (int64_t)qrow * a.ldo + vr.head * a.d;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float w[4] = {o[db][4 * j] * inv, o[db][4 * j + 1] * inv, o[db][4 * j + 2] * inv, o[db][4 * j + 3] * inv};
-        store4<T, VEC>(to, w, 32 * db + 8 * j + 4 * h, a.d);
-      }
-    if (h == 0 && a.lse)
+    store_image<T, DP, VEC>(o, inv, a.d, lds + wave * image_bytes<T, DP>(), lane, [&](int r) -> T* {
+      if (first + r >= t.rows) return nullptr;
+      const Virtual x(a, t.entry, t.head0, t.kv_head, first + r);
+      return out + (int64_t)row_of(a.q_row, x.entry) * a.ldo + x.head * a.d;
+    });
+    if (h == 0 && in && a.lse)
       a.lse[(int64_t)qrow * a.heads + vr.head] = run.l == 0.f ? -INFINITY : (run.m + __builtin_amdgcn_logf(run.l)) * kLn2;
   } else {
     // the waves' rows meet in LDS: [wave][row][DP + 4], then m and l [wave][row]
@@ -582,8 +620,8 @@ __global__ __launch_bounds__(kThreads) void k_cross_delta(const T* out, int64_t 
 template <typename T, int DP, int TK, bool VEC>
 __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cross_dq(const QTile* tiles, Args a) {
   constexpr int U = DP * (int)sizeof(T) / 16, NS = U / 2, DB = DP / 32, KB = TK / 32, TB = tile_bytes<TK, T, DP>();
-  constexpr int E = 16 / (int)sizeof(T), BUF = 2 * TB;
-  __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
+  constexpr int E = 16 / (int)sizeof(T), BUF = 2 * TB, IMAGES = 4 * image_bytes<T, DP>();
+  __shared__ __attribute__((aligned(16))) char lds[2 * BUF > IMAGES ? 2 * BUF : IMAGES];
   const QTile t = tiles[blockIdx.x];
   if (t.rows == 0) return;
   const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
@@ -657,13 +695,15 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
       across_mma<T, U, DB>(kt, 32 * kb, Probs<T>(s), dq, lane);
     }
   }
-  if (first + l32 >= t.rows) return;
+  __syncthreads();  // the images lie where the tiles were
+  if (!active) return;
   if (lse == -INFINITY)  // a row without keys, whatever q and dout hold
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int r = 0; r < 16; ++r) dq[db][r] = 0.f;
   if (t.slot >= 0) {
+    if (first + l32 >= t.rows) return;
     float* p = a.part + (size_t)t.slot * slot_floats<DP>(kCrossRows);
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -673,39 +713,34 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
             make_float4(dq[db][4 * j], dq[db][4 * j + 1], dq[db][4 * j + 2], dq[db][4 * j + 3]);
     return;
   }
-  const float scale = a.scale;
-  T* to = static_cast<T*>(a.out) + (int64_t)qrow * a.ldo + vr.head * a.d;
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float w[4] = {dq[db][4 * j] * scale, dq[db][4 * j + 1] * scale, dq[db][4 * j + 2] * scale,
-                          dq[db][4 * j + 3] * scale};
-      store4<T, VEC>(to, w, 32 * db + 8 * j + 4 * h, a.d);
-    }
+  store_image<T, DP, VEC>(dq, a.scale, a.d, lds + wave * image_bytes<T, DP>(), lane, [&](int r) -> T* {
+    if (first + r >= t.rows) return nullptr;
+    const Virtual x(a, t.entry, t.head0, t.kv_head, first + r);
+    return static_cast<T*>(a.out) + (int64_t)row_of(a.q_row, x.entry) * a.ldo + x.head * a.d;
+  });
 }
 
 // The gradient of keys and values: a wave holds 32 keys on its lanes, k and v in registers, and walks the row tiles of the
 // sequences that read them: dv^T += do^T p, dk^T += q^T ds.
 template <typename T, int DP, int RQ, bool VEC>
-__global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 2)) void k_cross_dkv(const KTile* tiles,
+__global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 3)) void k_cross_dkv(const KTile* tiles,
                                                                                        const RTile* runs, Args a) {
   constexpr int U = DP * (int)sizeof(T) / 16, NS = U / 2, DB = DP / 32, QB = RQ / 32, TB = tile_bytes<RQ, T, DP>();
-  constexpr int E = 16 / (int)sizeof(T), BUF = 2 * TB;
-  __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
+  constexpr int E = 16 / (int)sizeof(T), BUF = 2 * TB, IMAGES = 4 * image_bytes<T, DP>();
+  __shared__ __attribute__((aligned(16))) char lds[2 * BUF > IMAGES ? 2 * BUF : IMAGES];
   __shared__ __attribute__((aligned(16))) float stats[2][2][RQ];  // [buffer][lse in base 2, delta][row]
   // the widest fp32 heads leave no registers for v's fragments: every lane keeps its own in LDS
-  constexpr bool KEEP = DP * sizeof(T) > 384;
+  constexpr bool KEEP = DP * sizeof(T) > 384 || DP * sizeof(T) == 128;
   __shared__ uint4 kept[KEEP ? 4 * NS * 64 : 1];
   const KTile t = tiles[blockIdx.x];
   if (t.keys == 0) return;
   const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
   const int first = 32 * wave, mykey = first + l32;
   const bool active = first < t.keys;
-  const int ke = t.k_begin + min(mykey, t.keys - 1), krow = row_of(a.k_row, ke);
-  const bool counts = !a.mask || a.mask[ke] != 0;
+  const int ke = t.k_begin + min(mykey, t.keys - 1);
   uint4 kf[NS], vf[KEEP ? 1 : NS];
   {
+    const int krow = row_of(a.k_row, ke);
     const T* k = row_at(static_cast<const T*>(a.k), krow, a.ldk) + t.kv_head * a.d;
     const T* v = row_at(static_cast<const T*>(a.v), krow, a.ldv) + t.kv_head * a.d;
 #pragma unroll
@@ -722,7 +757,12 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 2)) void k_cr
     for (int r = 0; r < 16; ++r) dk[db][r] = dv[db][r] = 0.f;
   const float c = a.scale * kLog2e;
   using L = TileLoader<T, DP, RQ, 4, VEC>;
-  const L ld(wave, lane);
+  // (the lane's places are worked out again for every tile: registers are short in the loop)
+  const auto loader = [&]() {
+    int l = lane;
+    arrived(l);
+    return L(wave, l);
+  };
   const T *q = static_cast<const T*>(a.q), *g = static_cast<const T*>(a.dout);
   // A row tile's row numbers are fetched while the tile two before it is multiplied, what they lead to (the loads into LDS,
   // lse and delta) a tile later, as in KeyFeed; wave 0's lanes also hold a row each for lse and delta.
@@ -731,6 +771,7 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 2)) void k_cr
   bool there = false;
   RTile next = t.t_begin < t.t_end ? runs[t.t_begin] : RTile{};
   auto fetch = [&](int tile) {  // and the list's entry of the tile after it
+    const L ld = loader();
     RTile rt;
     rt.entry = __builtin_amdgcn_readfirstlane(next.entry);
     rt.head0 = __builtin_amdgcn_readfirstlane(next.head0);
@@ -753,6 +794,7 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 2)) void k_cr
 #pragma unroll
     for (int i = 0; i < L::NI; ++i) arrived(idx[i]);
     arrived(stat_row);
+    const L ld = loader();
     char* to = lds + buf * BUF;
     if constexpr (VEC) {
 #pragma unroll
@@ -804,7 +846,7 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 2)) void k_cr
     __builtin_amdgcn_sched_barrier(0);
     if (!active) continue;
     const char *qt = lds + buf * BUF, *gt = qt + TB;
-#pragma unroll
+#pragma unroll 1
     for (int qb = 0; qb < QB; ++qb) {
       f32x16 s, dp;
 #pragma unroll
@@ -831,10 +873,13 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 2)) void k_cr
       }
       across_mma<T, U, DB>(gt, 32 * qb, Probs<T>(s), dv, lane);
       across_mma<T, U, DB>(qt, 32 * qb, Probs<T>(dp), dk, lane);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
-  if (mykey >= t.keys) return;
+  __syncthreads();  // the images lie where the tiles were
+  if (!active) return;
   if (t.slot >= 0) {
+    if (mykey >= t.keys) return;
     float* p = a.part + ((size_t)t.slot * kCrossKeys + mykey) * 2 * DP;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -847,20 +892,20 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 2)) void k_cr
       }
     return;
   }
+  if (a.mask && a.mask[ke] == 0)  // a key that does not count, whatever its row holds
 #pragma unroll
-  for (int db = 0; db < DB; ++db)
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float x[4], y[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[e] = counts ? dk[db][4 * j + e] * a.scale : 0.f;
-        y[e] = counts ? dv[db][4 * j + e] : 0.f;
-      }
-      const int d0 = 32 * db + 8 * j + 4 * h;
-      if (a.out) store4<T, VEC>(static_cast<T*>(a.out) + (int64_t)krow * a.ldo + t.kv_head * a.d, x, d0, a.d);
-      if (a.out2) store4<T, VEC>(static_cast<T*>(a.out2) + (int64_t)krow * a.ldo2 + t.kv_head * a.d, y, d0, a.d);
-    }
+      for (int r = 0; r < 16; ++r) dk[db][r] = dv[db][r] = 0.f;
+  char* img = lds + wave * image_bytes<T, DP>();
+  const auto place = [&](void* to, int64_t ldt) {
+    return [=, &a, &t](int r) -> T* {
+      if (first + r >= t.keys) return nullptr;
+      return static_cast<T*>(to) + (int64_t)row_of(a.k_row, t.k_begin + first + r) * ldt + t.kv_head * a.d;
+    };
+  };
+  if (a.out) store_image<T, DP, VEC>(dk, a.scale, a.d, img, lane, place(a.out, a.ldo));
+  if (a.out2) store_image<T, DP, VEC>(dv, 1.f, a.d, img, lane, place(a.out2, a.ldo2));
 }
 
 // The pieces of a tile of keys summed in their order: eight threads a key.
