@@ -686,6 +686,8 @@ int32_t fold_token_logprobs(const fold_sched* sched, int32_t dtype, int64_t rows
  *             zero)
  *   pre       device, as out: z = x W^T + bias, which the gradient of an
  *             activation needs, or NULL
+ *   ws        device workspace of >= fwd_bytes of fold_linear_workspace_size
+ *             (may be NULL where that is 0)
  * x, W, residual, out and pre are of dtype.
  * fold_linear_backward: with dz = dout act'(pre) (dout itself for FOLD_ACT_NONE;
  * relu'(0) = 0), rounded to dtype where it enters a product,
@@ -698,7 +700,7 @@ int32_t fold_token_logprobs(const fold_sched* sched, int32_t dtype, int64_t rows
  *   dx_dtype, dw_dtype  of dx and dW: dtype, or FOLD_F32
  *   dx, dW, dbias  written whole (pad columns zero), or NULL; with
  *             FOLD_BLOCK_ACCUMULATE dbias and a dW of FOLD_F32 are added to
- *   ws        device workspace of >= fold_linear_workspace_size bytes
+ *   ws        device workspace of >= bwd_bytes of fold_linear_workspace_size
  * A residual's gradient is dout.
  *
  * Errors of these calls: FOLD_E_INVALID for sizes out of range, unknown types,
@@ -716,8 +718,10 @@ int32_t fold_layer_norm_backward(int32_t dtype, int64_t rows, int32_t width, con
                                  int32_t dx_dtype, const void* residual, void* dx, float* dgamma, float* dbeta,
                                  int32_t flags, void* ws, size_t ws_bytes, hipStream_t stream);
 int32_t fold_linear(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, const void* x, const void* W,
-                    const float* bias, int32_t act, const void* residual, void* out, void* pre, hipStream_t stream);
-int32_t fold_linear_workspace_size(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, size_t* bytes);
+                    const float* bias, int32_t act, const void* residual, void* out, void* pre, void* ws, size_t ws_bytes,
+                    hipStream_t stream);
+int32_t fold_linear_workspace_size(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, size_t* fwd_bytes,
+                                   size_t* bwd_bytes);
 int32_t fold_linear_backward(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, const void* x, const void* W,
                              int32_t act, const void* pre, const void* dout, void* dpre, int32_t dx_dtype, void* dx,
                              int32_t dw_dtype, void* dW, float* dbias, int32_t flags, void* ws, size_t ws_bytes,

@@ -124,7 +124,8 @@ int32_t fold_layer_norm_backward(int32_t dtype, int64_t rows, int32_t width, con
 }
 
 int32_t fold_linear(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, const void* x, const void* W,
-                    const float* bias, int32_t act, const void* residual, void* out, void* pre, hipStream_t st) {
+                    const float* bias, int32_t act, const void* residual, void* out, void* pre, void* ws, size_t ws_bytes,
+                    hipStream_t st) {
   return guarded([&]() -> int32_t {
     const std::string who("fold_linear");
     const int rc = check_linear(who, dtype, rows, in_dim, out_dim, linear_tiles);
@@ -132,26 +133,32 @@ int32_t fold_linear(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim
     if (act < FOLD_ACT_NONE || act > FOLD_ACT_GELU) return api_fail(FOLD_E_INVALID, who + ": unknown activation");
     if (rows == 0) return FOLD_OK;
     if (!x || !W || !out) return api_fail(FOLD_E_INVALID, who + ": NULL buffer");
-    if (misaligned(x) || misaligned(W) || misaligned(residual) || misaligned(out) || misaligned(pre))
+    if (misaligned(x) || misaligned(W) || misaligned(residual) || misaligned(out) || misaligned(pre) || misaligned(ws))
       return api_fail(FOLD_E_INVALID, who + ": matrices must be 16-byte aligned");
     const size_t m = bytes_of(dtype, rows, out_dim);
-    const Span outs[] = {{out, m}, {pre, m}};
+    const size_t need = linear_bytes(dtype, rows, in_dim, out_dim);
+    if (need > 0 && (!ws || ws_bytes < need))
+      return api_fail(FOLD_E_MISMATCH, who + ": workspace smaller than fold_linear_workspace_size");
+    const Span outs[] = {{out, m}, {pre, m}, {ws, need}};
     const Span in[] = {{x, bytes_of(dtype, rows, in_dim)}, {W, bytes_of(dtype, out_dim, in_dim)},
                        {bias, vector_bytes(out_dim)}, {residual == out ? nullptr : residual, m}};
-    if (any_overlap(outs, 2, in, 4)) return api_fail(FOLD_E_INVALID, who + ": an output overlaps another buffer");
-    launch_linear(dtype, rows, in_dim, out_dim, x, W, bias, act, residual, out, pre, st);
+    if (any_overlap(outs, 3, in, 4)) return api_fail(FOLD_E_INVALID, who + ": an output overlaps another buffer");
+    launch_linear(dtype, rows, in_dim, out_dim, x, W, bias, act, residual, out, pre, ws, st);
     FOLD_HIP_CHECK(hipGetLastError());
     return FOLD_OK;
   });
 }
 
-int32_t fold_linear_workspace_size(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, size_t* bytes) {
+int32_t fold_linear_workspace_size(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, size_t* fwd_bytes,
+                                   size_t* bwd_bytes) {
   return guarded([&]() -> int32_t {
     const std::string who("fold_linear_workspace_size");
-    if (!bytes) return api_fail(FOLD_E_INVALID, who + ": NULL argument");
-    const int rc = check_linear(who, dtype, rows, in_dim, out_dim, linear_backward_tiles);
+    if (!fwd_bytes || !bwd_bytes) return api_fail(FOLD_E_INVALID, who + ": NULL argument");
+    int rc = check_linear(who, dtype, rows, in_dim, out_dim, linear_tiles);
+    if (rc == FOLD_OK) rc = check_linear(who, dtype, rows, in_dim, out_dim, linear_backward_tiles);
     if (rc != FOLD_OK) return rc;
-    *bytes = linear_backward_bytes(dtype, rows, in_dim, out_dim);
+    *fwd_bytes = linear_bytes(dtype, rows, in_dim, out_dim);
+    *bwd_bytes = linear_backward_bytes(dtype, rows, in_dim, out_dim);
     return FOLD_OK;
   });
 }

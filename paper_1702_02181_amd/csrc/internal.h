@@ -502,7 +502,8 @@ void launch_norm_backward(int dtype, int64_t rows, int n, const void* x, const f
 int64_t linear_tiles(int dtype, int64_t rows, int in_dim, int out_dim);
 int64_t linear_backward_tiles(int dtype, int64_t rows, int in_dim, int out_dim);
 void launch_linear(int dtype, int64_t rows, int in_dim, int out_dim, const void* x, const void* W, const float* bias,
-                   int act, const void* residual, void* out, void* pre, hipStream_t st);
+                   int act, const void* residual, void* out, void* pre, void* ws, hipStream_t st);
+size_t linear_bytes(int dtype, int64_t rows, int in_dim, int out_dim);
 size_t linear_backward_bytes(int dtype, int64_t rows, int in_dim, int out_dim);
 void launch_linear_backward(int dtype, int64_t rows, int in_dim, int out_dim, const void* x, const void* W, int act,
                             const void* pre, const void* dout, void* dpre, int dx_dtype, void* dx, int dw_dtype, void* dW,

@@ -77,6 +77,45 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_linear_few(const T* x, const
   }
 }
 
+// ---- few tiles: K in pieces ------------------------------------------------------------------------------------------------
+
+// out = act(the pieces' sum + bias) + residual, four columns of a row a thread, eight pieces in flight
+template <typename T, int ACT>
+__global__ __launch_bounds__(256) void k_linear_join(const float* part, int pieces, int64_t M, int N, int ld, const float* bias,
+                                                     const T* res, T* out, T* pre) {
+  const size_t n = (size_t)M * ld, i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= n) return;
+  const int col = (int)(i % (size_t)ld);
+  typedef typename Four<T>::raw raw;
+  float s[4] = {0.f, 0.f, 0.f, 0.f}, r[4] = {0.f, 0.f, 0.f, 0.f}, y[4];
+  raw rr{};
+  if (res) rr = *reinterpret_cast<const raw*>(res + i);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s[e] = bias && col + e < N ? bias[col + e] : 0.f;
+  for (int p0 = 0; p0 < pieces; p0 += 8) {
+    float4 v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const float4*>(part + (size_t)min(p0 + u, pieces - 1) * n + i);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const bool in = p0 + u < pieces;
+      s[0] += in ? v[u].x : 0.f;
+      s[1] += in ? v[u].y : 0.f;
+      s[2] += in ? v[u].z : 0.f;
+      s[3] += in ? v[u].w : 0.f;
+    }
+  }
+  if (res) Four<T>::take(rr, r);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const bool in = col + e < N;
+    y[e] = in ? act_value<ACT>(s[e]) + r[e] : 0.f;
+    s[e] = in ? s[e] : 0.f;
+  }
+  if (pre) *reinterpret_cast<raw*>(pre + i) = Four<T>::give(s);
+  *reinterpret_cast<raw*>(out + i) = Four<T>::give(y);
+}
+
 // ---- the gradient of the activation ------------------------------------------------------------------------------------
 
 // dz = dout act'(pre), and the rows' sums of dz (before its rounding).  A workgroup takes 64 16-byte vectors of columns of one
@@ -131,6 +170,13 @@ __global__ __launch_bounds__(256) void k_activation_back(const T* dout, const T*
   }
 }
 
+// Pieces of the rows: eight workgroups a compute unit, whose arithmetic (some 30 instructions a value for gelu) then runs beside
+// the others' loads, each with at least 16 rows.
+int activation_chunks(int64_t M, int N, int es) {
+  const int64_t groups = ((int64_t)row_ld(N) * es + 1023) / 1024;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({2048 / groups, M / 16, 256}));
+}
+
 // out (+)= the sum of the pieces in their order, eight loads in flight, rounded to OUT; n a multiple of 4
 template <typename OUT>
 __global__ __launch_bounds__(256) void k_join_as(const float* part, int pieces, size_t n, OUT* out, int add) {
@@ -162,13 +208,19 @@ __global__ __launch_bounds__(256) void k_join_as(const float* part, int pieces, 
 
 // ---- shapes ----------------------------------------------------------------------------------------------------------
 
-Shape forward_shape(int64_t M, int K, int N, int es) { return shape_of(M, row_ld(N), row_ld(K) * es / 128, es, 2, 1); }
+// A compute unit that has one workgroup of 128 x 128 tiles alone waits for its loads: 16,384 x 1,024 x 4,096 bf16, dW in 256 of
+// them 165 us, in 512 (two pieces) 142, in 256 of 256 x 256 (four pieces) 128.
+constexpr double kAlone = 1.25;
+
+Shape forward_shape(int64_t M, int K, int N, int es) {
+  return shape_of(M, row_ld(N), row_ld(K) * es / 128, es, 2, kPieces, false, kAlone);
+}
 Shape dx_shape(int64_t M, int K, int N, int es) {
-  return shape_of(std::max<int64_t>(M, 1), row_ld(K), (int64_t)row_ld(N) * es / 128, es, 1, kPieces);
+  return shape_of(std::max<int64_t>(M, 1), row_ld(K), (int64_t)row_ld(N) * es / 128, es, 1, kPieces, false, kAlone);
 }
 Shape dw_shape(int64_t M, int K, int N, int es) {
   const int lines = 128 / es;
-  return shape_of(N, row_ld(K), std::max<int64_t>(1, (M + lines - 1) / lines), es, 1, kPieces);
+  return shape_of(N, row_ld(K), std::max<int64_t>(1, (M + lines - 1) / lines), es, 1, kPieces, false, kAlone);
 }
 
 template <typename T, int ACT>
@@ -187,13 +239,24 @@ void few(int M, int K, int N, const void* x, const void* W, const float* bias, c
 
 template <typename T, int ACT>
 void forward(int64_t M, int K, int N, const void* x, const void* W, const float* bias, const void* res, void* out,
-             void* pre, hipStream_t st) {
+             void* pre, void* ws, hipStream_t st) {
   if (M <= kFewRows) return few<T, ACT>((int)M, K, N, x, W, bias, res, out, pre, st);
   const int es = sizeof(T), ldk = row_ld(K), ldn = row_ld(N);
   const Shape sh = forward_shape(M, K, N, es);
-  ProductArgs g{{x, M, ldk}, {W, N, ldk}, M, N, sh.mt, sh.nt, ldk * es / 128, 1, out, (size_t)ldn, ldn, bias, 0, nullptr};
+  ProductArgs g{{x, M, ldk}, {W, N, ldk}, M, N, sh.mt, sh.nt, ldk * es / 128, sh.split, out, (size_t)ldn, ldn, bias, 0, nullptr};
+  if (sh.split > 1) {
+    g.out = ws;
+    g.bias = nullptr;
+    launch<T, kAlong, kAlong, float>(g, sh, st);
+    hipLaunchKernelGGL((k_linear_join<T, ACT>), dim3((unsigned)(((size_t)M * ldn + 1023) / 1024)), dim3(256), 0, st,
+                       static_cast<const float*>(ws), sh.split, M, N, ldn, bias, static_cast<const T*>(res),
+                       static_cast<T*>(out), static_cast<T*>(pre));
+    return;
+  }
   g.residual = res;
   g.pre = pre;
+  if constexpr (ACT == FOLD_ACT_NONE)
+    if (!res && !pre) return launch<T, kAlong, kAlong, T>(g, sh, st);
   launch<T, kAlong, kAlong, T, ACT>(g, sh, st);
 }
 
@@ -220,7 +283,7 @@ void backward(int64_t M, int K, int N, const void* x, const void* W, int act, co
   const T* dz = static_cast<const T*>(dout);
   if ((act != FOLD_ACT_NONE && (dx || dW)) || db) {
     ProfScope prof(act == FOLD_ACT_NONE ? "linear_dbias" : "linear_activation", st);
-    const int c = bias_chunks(M, N, es);
+    const int c = act == FOLD_ACT_NONE ? bias_chunks(M, N, es) : activation_chunks(M, N, es);
     float* part = db && c > 1 ? static_cast<float*>(ws) : nullptr;
     const dim3 grid((unsigned)(((int64_t)ldn * es + 1023) / 1024 * c));
     const auto go = [&](auto kernel) {
@@ -258,7 +321,12 @@ void backward(int64_t M, int K, int N, const void* x, const void* W, int act, co
 
 int64_t linear_tiles(int dtype, int64_t M, int K, int N) {
   const Shape sh = forward_shape(M, K, N, dtype == FOLD_BF16 ? 2 : 4);
-  return M <= kFewRows ? row_ld(N) / 16 : sh.mt * sh.nt;
+  if (M <= kFewRows) return row_ld(N) / 16;
+  return std::max(sh.mt * sh.nt * sh.split, sh.split > 1 ? M * row_ld(N) / 1024 + 1 : 0);
+}
+size_t linear_bytes(int dtype, int64_t M, int K, int N) {
+  const Shape sh = forward_shape(M, K, N, dtype == FOLD_BF16 ? 2 : 4);
+  return M <= kFewRows || sh.split == 1 ? 0 : (size_t)sh.split * M * row_ld(N) * sizeof(float);
 }
 int64_t linear_backward_tiles(int dtype, int64_t M, int K, int N) {
   const int es = dtype == FOLD_BF16 ? 2 : 4;
@@ -268,13 +336,13 @@ int64_t linear_backward_tiles(int dtype, int64_t M, int K, int N) {
 }
 
 void launch_linear(int dtype, int64_t M, int K, int N, const void* x, const void* W, const float* bias, int act,
-                   const void* res, void* out, void* pre, hipStream_t st) {
+                   const void* res, void* out, void* pre, void* ws, hipStream_t st) {
   if (M <= 0) return;
   ProfScope prof("linear", st);
   const auto go = [&](auto a) {
     constexpr int ACT = decltype(a)::value;
-    if (dtype == FOLD_F32) forward<float, ACT>(M, K, N, x, W, bias, res, out, pre, st);
-    else forward<uint16_t, ACT>(M, K, N, x, W, bias, res, out, pre, st);
+    if (dtype == FOLD_F32) forward<float, ACT>(M, K, N, x, W, bias, res, out, pre, ws, st);
+    else forward<uint16_t, ACT>(M, K, N, x, W, bias, res, out, pre, ws, st);
   };
   if (act == FOLD_ACT_RELU) go(std::integral_constant<int, FOLD_ACT_RELU>());
   else if (act == FOLD_ACT_TANH) go(std::integral_constant<int, FOLD_ACT_TANH>());
@@ -285,7 +353,7 @@ void launch_linear(int dtype, int64_t M, int K, int N, const void* x, const void
 size_t linear_backward_bytes(int dtype, int64_t M, int K, int N) {
   const int es = dtype == FOLD_BF16 ? 2 : 4;
   const Shape a = dx_shape(M, K, N, es), b = dw_shape(M, K, N, es);
-  const int c = bias_chunks(M, N, es);
+  const int c = std::max(bias_chunks(M, N, es), activation_chunks(M, N, es));
   // they follow each other on the stream: one region serves all
   const size_t dx = a.split > 1 ? (size_t)a.split * M * row_ld(K) : 0, dw = b.split > 1 ? (size_t)b.split * N * row_ld(K) : 0;
   return std::max({dx, dw, c > 1 ? (size_t)c * row_ld(N) : (size_t)0}) * sizeof(float);

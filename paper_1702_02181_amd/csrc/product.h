@@ -176,17 +176,19 @@ constexpr int kPlain = -1;
 // Activations and their slopes.  gelu(z) = z Phi(z), with Phi by Abramowitz and Stegun's rational approximation 7.1.26 of erf
 // (absolute error 1.5e-7): a reciprocal, an exponential and some ten more instructions.  The library's erf has about 40 and a
 // branch; at K = 1,024 that would take a tile's store longer than its products.
-__device__ __forceinline__ float normal_cdf(float z) {
-  const float x = fabsf(z) * 0.70710678f, t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * x);
+// e: exp(-z^2 / 2)
+__device__ __forceinline__ float normal_cdf(float z, float e) {
+  const float t = __builtin_amdgcn_rcpf(1.f + 0.23164190f * fabsf(z));  // 0.3275911 / sqrt 2
   const float p = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
-  const float tail = 0.5f * p * fast_exp(-x * x);  // Phi(-|z|)
+  const float tail = 0.5f * p * e;  // Phi(-|z|)
   return z < 0.f ? tail : 1.f - tail;
 }
+__device__ __forceinline__ float bell(float z) { return __builtin_amdgcn_exp2f(-0.72134752f * z * z); }
 template <int ACT>
 __device__ __forceinline__ float act_value(float z) {
   if constexpr (ACT == FOLD_ACT_RELU) return z < 0.f ? 0.f : z;
   else if constexpr (ACT == FOLD_ACT_TANH) return tanhf_(z);
-  else if constexpr (ACT == FOLD_ACT_GELU) return z * normal_cdf(z);
+  else if constexpr (ACT == FOLD_ACT_GELU) return z * normal_cdf(z, bell(z));
   else return z;
 }
 template <int ACT>
@@ -195,8 +197,10 @@ __device__ __forceinline__ float act_slope(float z) {
   else if constexpr (ACT == FOLD_ACT_TANH) {
     const float t = tanhf_(z);
     return 1.f - t * t;
-  } else if constexpr (ACT == FOLD_ACT_GELU) return normal_cdf(z) + z * 0.39894228f * fast_exp(-0.5f * z * z);
-  else return 1.f;
+  } else if constexpr (ACT == FOLD_ACT_GELU) {
+    const float e = bell(z);
+    return normal_cdf(z, e) + z * 0.39894228f * e;
+  } else return 1.f;
 }
 
 // four values of OUT, as they are loaded and stored
@@ -354,60 +358,103 @@ struct Four<uint16_t> {
   }
 };
 
-// The same with an activation: blocks of 32 x 32 pass through the wave's image in fp32, after which eight lanes hold 32
-// neighbouring columns of a row.  The value before the activation is stored (rounded for bf16), the activated one meets the
-// residual in fp32 and is rounded once.  The residual's loads run AHEAD blocks ahead of their use.
+// The same with an activation: the value before it is stored (rounded for bf16), the activated one meets the residual in fp32
+// and is rounded once.  Both, and the residual, pass through the wave's image, 32 rows of 128 bytes, so that memory sees whole
+// lines and the arithmetic the accumulators' registers.  A block's residual is loaded while the block before it is stored.
 template <typename OUT, int WM, int WN, int ACT>
 __device__ __forceinline__ void store_activated(const ProductArgs& g, OUT* out, const f32x16 (&acc)[WM][WN], int64_t m0,
                                                 int64_t n0, char* img, int lane) {
-  using F = Four<OUT>;
-  constexpr int BLOCKS = WM * WN, AHEAD = BLOCKS < 4 ? BLOCKS : (sizeof(OUT) == 2 ? 4 : 2);
+  constexpr int VEC = 16 / (int)sizeof(OUT), JG = 4 / (int)sizeof(OUT), BLOCKS = WM * WN / JG, X = 4;
+  static_assert(WN % JG == 0, "whole lines");
   const int rows = (int)min(g.M - m0, (int64_t)(32 * WM)), vals = (int)min(g.N - n0, (int64_t)(32 * WN));
   const int cols = (int)min(g.cols - n0, (int64_t)(32 * WN));
-  const int h = lane >> 5, l32 = lane & 31, r0 = lane >> 3, c0 = (lane & 7) * 4;
+  if (rows <= 0 || cols <= 0) return;
+  const int h = lane >> 5, l32 = lane & 31, r0 = lane >> 3, c0 = (lane & 7) * VEC;
   const size_t corner = (size_t)m0 * g.ld + n0;
   const OUT* res = g.residual ? static_cast<const OUT*>(g.residual) + corner : nullptr;
   OUT* pre = g.pre ? static_cast<OUT*>(g.pre) + corner : nullptr;
   out += corner;
-  typename F::raw r[AHEAD][4];
-  auto place = [&](int b, int x) { return (size_t)(32 * (b / WN) + 8 * x + r0) * g.ld + 32 * (b % WN) + c0; };
-  auto there = [&](int b, int x) { return 32 * (b / WN) + 8 * x + r0 < rows && 32 * (b % WN) + c0 < cols; };
-  auto fetch = [&](int b) {
+  auto row_at = [&](int b, int x) { return 32 * (b / (WN / JG)) + 8 * x + r0; };
+  auto col_at = [&](int b) { return 32 * JG * (b % (WN / JG)) + c0; };
+  auto there = [&](int b, int x) { return row_at(b, x) < rows && col_at(b) < cols; };
+  auto place = [&](int b, int x) { return (size_t)row_at(b, x) * g.ld + col_at(b); };
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  u32x4 r[X] = {};
+  auto fetch = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
-      if (there(b, x)) r[b % AHEAD][x] = *reinterpret_cast<const typename F::raw*>(res + place(b, x));
+    for (int x = 0; x < X; ++x)
+      if (there(b, x)) r[x] = *reinterpret_cast<const u32x4*>(res + place(b, x));
   };
-  if (res)
+  // the image from the accumulators' layout: register 4 q + e of block j is column 32 j + 8 q + 4 h + e of row l32
+  auto write = [&](const float (&v)[JG][16]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int b = 0; b < AHEAD; ++b) fetch(b);
+    for (int j = 0; j < JG; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; q += VEC / 4) {
+        uint4 w;
+        int n;
+        if constexpr (sizeof(OUT) == 4) {
+          n = 32 * j + 8 * q + 4 * h;
+          w = make_uint4(__float_as_uint(v[j][4 * q]), __float_as_uint(v[j][4 * q + 1]), __float_as_uint(v[j][4 * q + 2]),
+                         __float_as_uint(v[j][4 * q + 3]));
+        } else {
+          n = 32 * j + 8 * (q + h);
+          const auto lo = __builtin_amdgcn_permlane32_swap(bf16_pair(v[j][4 * q], v[j][4 * q + 1]),
+                                                           bf16_pair(v[j][4 * q + 4], v[j][4 * q + 5]), false, false);
+          const auto hi = __builtin_amdgcn_permlane32_swap(bf16_pair(v[j][4 * q + 2], v[j][4 * q + 3]),
+                                                           bf16_pair(v[j][4 * q + 6], v[j][4 * q + 7]), false, false);
+          w = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+        }
+        *reinterpret_cast<uint4*>(img + l32 * kImageRow + n * (int)sizeof(OUT)) = w;
+      }
+    wave_fence();
+  };
+  auto store = [&](OUT* to, int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int x = 0; x < X; ++x) {
+      const uint4 v = *reinterpret_cast<const uint4*>(img + (8 * x + r0) * kImageRow + c0 * (int)sizeof(OUT));
+      if (there(b, x)) *reinterpret_cast<uint4*>(to + place(b, x)) = mask_tail<OUT>(v, max(vals - col_at(b), 0));
+    }
+    wave_fence();
+  };
+  if (res) fetch(0);
 #pragma unroll
   for (int b = 0; b < BLOCKS; ++b) {
-    f32x16 c = acc[b / WN][b % WN];
-    if constexpr (BLOCKS >= 16) asm volatile("" : "+a"(c));  // stays in its accumulator registers until here
+    float z[JG][16];
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<uint4*>(img + l32 * kImageRow + (8 * q + 4 * h) * 4) =
-          make_uint4(__float_as_uint(c[4 * q]), __float_as_uint(c[4 * q + 1]), __float_as_uint(c[4 * q + 2]),
-                     __float_as_uint(c[4 * q + 3]));
-    wave_fence();
+    for (int j = 0; j < JG; ++j) {
+      f32x16 c = acc[b / (WN / JG)][JG * (b % (WN / JG)) + j];
+      if constexpr (WM * WN >= 16) asm volatile("" : "+a"(c));  // stays in its accumulator registers until here
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      float z[4];
-      Four<float>::take(*reinterpret_cast<const uint4*>(img + (8 * x + r0) * kImageRow + c0 * 4), z);
-      const int col = 32 * (b % WN) + c0;
-      if (there(b, x)) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = col + e < vals ? z[e] : 0.f;
-        if (pre) *reinterpret_cast<typename F::raw*>(pre + place(b, x)) = F::give(z);
-        float y[4], s[4] = {0.f, 0.f, 0.f, 0.f};
-        if (res) F::take(r[b % AHEAD][x], s);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = col + e < vals ? act_value<ACT>(z[e]) + s[e] : 0.f;
-        *reinterpret_cast<typename F::raw*>(out + place(b, x)) = F::give(y);
-      }
+      for (int e = 0; e < 16; ++e) z[j][e] = c[e];
     }
-    if (res && b + AHEAD < BLOCKS) fetch(b + AHEAD);
-    wave_fence();
+    if (pre) {
+      write(z);
+      store(pre, b);
+    }
+#pragma unroll
+    for (int j = 0; j < JG; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) z[j][e] = act_value<ACT>(z[j][e]);
+    if (res) {
+#pragma unroll
+      for (int x = 0; x < X; ++x) *reinterpret_cast<u32x4*>(img + (8 * x + r0) * kImageRow + c0 * (int)sizeof(OUT)) = r[x];
+      if (b + 1 < BLOCKS) fetch(b + 1);
+      wave_fence();
+#pragma unroll
+      for (int j = 0; j < JG; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float s[4];
+          Four<OUT>::take(*reinterpret_cast<const typename Four<OUT>::raw*>(img + l32 * kImageRow +
+                                                                            (32 * j + 8 * q + 4 * h) * (int)sizeof(OUT)), s);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[j][4 * q + e] += s[e];
+        }
+      wave_fence();
+    }
+    write(z);
+    store(out, b);
   }
 }
 
@@ -862,8 +909,10 @@ constexpr int kUnits = 256;  // compute units
 // cost their sums' way through memory (4 TB/s) and a second launch (3 us).  What the rule gets (best and worst cut tried):
 // states' gradient of 33 x 300 x 20,000 bf16 13 us (335), of 257 x 300 x 20,001 fp32 49 us (4,512), weights' gradient of
 // 2,048 x 256 x 10,000 fp32 100 us (486).
-// small: the smallest tile's columns / 64 (1 or 2); smallest: that tile alone
-Shape shape_of(int64_t M, int64_t N, int64_t nstage, int esize, int small, int pieces, bool smallest = false) {
+// small: the smallest tile's columns / 64 (1 or 2); smallest: that tile alone; alone: what 128 x 128 tiles cost more where a
+// compute unit has no second workgroup
+Shape shape_of(int64_t M, int64_t N, int64_t nstage, int esize, int small, int pieces, bool smallest = false,
+               double alone = 1.0) {
   static constexpr struct { int wm, wn; double bf16, f32; } kTiles[] = {
       {4, 4, 1.0, 1.0}, {2, 2, 1.2, 1.0}, {1, 2, 1.55, 1.03}, {1, 1, 2.2, 1.06}};
   Shape best{0, 0, 0, 0, 0};
@@ -873,7 +922,7 @@ Shape shape_of(int64_t M, int64_t N, int64_t nstage, int esize, int small, int p
     const int64_t mt = tiles_of(M, t.wm), nt = tiles_of(N, t.wn);
     for (int p = 1; p <= pieces && (p == 1 || nstage / p >= 4); p *= 2) {
       const double rounds = (double)((mt * nt * p + kUnits - 1) / kUnits);
-      const double stage = t.wm * t.wn * (esize == 2 ? 0.11 * t.bf16 : 0.49 * t.f32);
+      const double stage = t.wm * t.wn * (esize == 2 ? 0.11 * t.bf16 : 0.49 * t.f32) * (t.wm == 2 && rounds == 1 ? alone : 1.0);
       double us = rounds * (stage * (double)((nstage + p - 1) / p) + 2.0 / (t.wm == 4 ? 1 : 2));
       if (p > 1) us += 3.0 + (double)(p + 1) * M * N * 4 / 4e6;
       if (best.wm == 0 || us < least) {

@@ -283,9 +283,9 @@ def lib():
                                            c_size_t, c_void_p]
     L.fold_linear.restype = c_int32
     L.fold_linear.argtypes = [c_int32, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p,
-                              c_void_p, c_void_p, c_void_p]
+                              c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
     L.fold_linear_workspace_size.restype = c_int32
-    L.fold_linear_workspace_size.argtypes = [c_int32, c_int64, c_int32, c_int32, POINTER(c_size_t)]
+    L.fold_linear_workspace_size.argtypes = [c_int32, c_int64, c_int32, c_int32, POINTER(c_size_t), POINTER(c_size_t)]
     L.fold_linear_backward.restype = c_int32
     L.fold_linear_backward.argtypes = [c_int32, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_void_p,
                                        c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_void_p,
@@ -364,13 +364,13 @@ def fold_row_ld(width: int) -> int:
 
 
 def _ptr(t):
-    return None if t is None else c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream(stream=None):
     import torch
     s = stream if stream is not None else torch.cuda.current_stream()
-    return c_void_p(s.cuda_stream)
+    return s.cuda_stream
 
 
 # ----------------------------------------------------------------------------- raw calls
@@ -505,15 +505,15 @@ def fold_layer_norm_backward(dtype, rows, width, x, gamma, mean, rstd, dy_dtype,
                                           _ptr(dbeta), int(flags), _ptr(ws), int(ws_bytes), _stream(stream)))
 
 
-def fold_linear(dtype, rows, in_dim, out_dim, x, W, bias, act, residual, out, pre, stream=None):
+def fold_linear(dtype, rows, in_dim, out_dim, x, W, bias, act, residual, out, pre, ws, ws_bytes, stream=None):
     _check(lib().fold_linear(int(dtype), int(rows), int(in_dim), int(out_dim), _ptr(x), _ptr(W), _ptr(bias), int(act),
-                             _ptr(residual), _ptr(out), _ptr(pre), _stream(stream)))
+                             _ptr(residual), _ptr(out), _ptr(pre), _ptr(ws), int(ws_bytes), _stream(stream)))
 
 
-def fold_linear_workspace_size(dtype, rows, in_dim, out_dim) -> int:
-    n = c_size_t()
-    _check(lib().fold_linear_workspace_size(int(dtype), int(rows), int(in_dim), int(out_dim), byref(n)))
-    return int(n.value)
+def fold_linear_workspace_size(dtype, rows, in_dim, out_dim):
+    f, b = c_size_t(), c_size_t()
+    _check(lib().fold_linear_workspace_size(int(dtype), int(rows), int(in_dim), int(out_dim), byref(f), byref(b)))
+    return int(f.value), int(b.value)
 
 
 def fold_linear_backward(dtype, rows, in_dim, out_dim, x, W, act, pre, dout, dpre, dx_dtype, dx, dw_dtype, dW, dbias, flags,
@@ -1110,8 +1110,10 @@ class Linear:
             new = lambda: torch.empty(shape, dtype=self.dtype, device=x.device)  # noqa: E731
             out = new() if out is None else _matrix("out", out, self.out_dim, self.dtype, rows)
             pre = None if not ret else new() if pre is True else _matrix("pre", pre, self.out_dim, self.dtype, rows)
+            n = _linear_ws(self.code, rows, self.in_dim, self.out_dim)[0]
+            ws = _bytes(n, x.device)
             fold_linear(self.code, rows, self.in_dim, self.out_dim, x, self.weight, self.bias, self.act, residual, out, pre,
-                        stream or _CURRENT)
+                        ws, n, stream or _CURRENT)
         return (out, pre) if ret else out
 
     def backward(self, x, dout, pre=None, dx=True, dW=True, dbias=True, dpre=None, dx_dtype=None, dw_dtype=None,
@@ -1147,7 +1149,7 @@ class Linear:
                 dpre = torch.empty_like(pre) if dpre is None else _matrix("dpre", dpre, self.out_dim, self.dtype, rows)
             elif dpre is not None:
                 raise ValueError("dpre belongs to a layer with an activation")
-            n = _linear_ws(self.code, rows, self.in_dim, self.out_dim)
+            n = _linear_ws(self.code, rows, self.in_dim, self.out_dim)[1]
             ws = _bytes(n, x.device)
             fold_linear_backward(self.code, rows, self.in_dim, self.out_dim, x, self.weight, self.act, pre, dout, dpre,
                                  FOLD_F32 if dx is None else _code(dx.dtype), dx,

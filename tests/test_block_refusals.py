@@ -43,7 +43,7 @@ def test_linear_refuses(F):  # noqa: F811
     odd = _Buf((1 << 20) + 4)
 
     def fwd(dtype=0, rows=4, k=100, n=70, x=x, W=W, bias=b, act=0, res=None, out=out, pre=None):
-        F.fold_linear(dtype, rows, k, n, x, W, bias, act, res, out, pre, NULL_STREAM)
+        F.fold_linear(dtype, rows, k, n, x, W, bias, act, res, out, pre, None, 0, NULL_STREAM)
 
     for kw in (dict(dtype=2), dict(rows=-1), dict(rows=1 << 31), dict(k=0), dict(k=16385), dict(n=0), dict(n=16385),
                dict(act=4), dict(act=-1), dict(x=None), dict(W=None), dict(out=None), dict(x=odd), dict(W=odd),
@@ -51,7 +51,7 @@ def test_linear_refuses(F):  # noqa: F811
                dict(res=_Buf(out.at + 16)), dict(out=b), dict(rows=(1 << 31) - 1, n=16384)):
         _refused(F, F.FOLD_E_INVALID, fwd, **kw)
     fwd(rows=0, x=None, W=None, out=None)
-    n = F.fold_linear_workspace_size(0, 4, 100, 70)
+    _, n = F.fold_linear_workspace_size(0, 4, 100, 70)
 
     def back(dtype=0, rows=4, k=100, n=70, x=x, W=W, act=2, pre=pre, dout=d, dpre=pre, dxt=0, dx=dx, dwt=0, dw=dw, db=None,
              flags=0, ws=ws, size=n):
@@ -64,7 +64,8 @@ def test_linear_refuses(F):  # noqa: F811
                dict(dw=odd), dict(dx=d), dict(dx=pre, dpre=d), dict(dw=x), dict(db=dw), dict(dpre=x),
                dict(dpre=_Buf(d.at + 16)), dict(dx=dw)):
         _refused(F, F.FOLD_E_INVALID, back, **kw)
-    big = F.fold_linear_workspace_size(0, 4, 4096, 8192)
+    _refused(F, F.FOLD_E_MISMATCH, fwd, rows=80, k=8192, n=64, x=_Buf(1 << 32), W=_Buf(1 << 33))  # few tiles: K in pieces
+    _, big = F.fold_linear_workspace_size(0, 4, 4096, 8192)
     assert big > 0  # few rows: K is cut into pieces
     _refused(F, F.FOLD_E_MISMATCH, back, k=4096, n=8192, act=0, pre=None, dpre=None, x=_Buf(1 << 32), W=_Buf(1 << 33),
              dx=_Buf(1 << 34), dw=_Buf(1 << 35), dout=_Buf(1 << 36), ws=_Buf(1 << 37), size=big - 1)
