@@ -276,6 +276,35 @@ void cut_product(ProductArgs g, const Shape& sh, OUT* out, void* ws, int add, hi
                      sh.split, n, out, add);
 }
 
+// The two gradients of a small batch in one launch, in the smallest tiles: apart, each leaves much of the chip idle and has a
+// launch's start to itself.  `first` workgroups (a multiple of 8) for dx, the rest for dW.
+bool together(const Shape& dx, const Shape& dw) { return dx.wm == 1 && dw.wm == 1; }
+template <typename T, typename OX, typename OW>
+__global__ __launch_bounds__(kThreads, 2) void k_linear_both(ProductArgs states, ProductArgs weights, unsigned first) {
+  __shared__ __attribute__((aligned(16))) ProductLds<1, 1, 128, 2> lds;
+  if (blockIdx.x < first) product<T, kAlong, kAcross, OX, 1, 1, 128, 2>(states, blockIdx.x, lds);
+  else product<T, kAcross, kAcross, OW, 1, 1, 128, 2>(weights, blockIdx.x - first, lds);
+}
+template <typename T, typename OX, typename OW>
+void both_products(ProductArgs x, ProductArgs w, const Shape& s1, const Shape& s2, OX* dx, OW* dw, float* ws, int add,
+                   hipStream_t st) {
+  const size_t nx = (size_t)x.M * x.ld, nw = (size_t)w.M * w.ld;
+  float* wpart = ws + (s1.split > 1 ? s1.split * nx : 0);
+  x.out = s1.split > 1 ? static_cast<void*>(ws) : dx;
+  w.out = s2.split > 1 ? static_cast<void*>(wpart) : dw;
+  w.add = s2.split > 1 ? 0 : add;
+  const unsigned n1 = blocks_of(x), n2 = blocks_of(w);
+  const auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(n1 + n2), dim3(kThreads), 0, st, x, w, n1); };
+  if (s1.split > 1 && s2.split > 1) go(k_linear_both<T, float, float>);
+  else if (s1.split > 1) go(k_linear_both<T, float, OW>);
+  else if (s2.split > 1) go(k_linear_both<T, OX, float>);
+  else go(k_linear_both<T, OX, OW>);
+  if (s1.split > 1)
+    hipLaunchKernelGGL(k_join_as<OX>, dim3((unsigned)((nx + 1023) / 1024)), dim3(256), 0, st, ws, s1.split, nx, dx, 0);
+  if (s2.split > 1)
+    hipLaunchKernelGGL(k_join_as<OW>, dim3((unsigned)((nw + 1023) / 1024)), dim3(256), 0, st, wpart, s2.split, nw, dw, add);
+}
+
 template <typename T>
 void backward(int64_t M, int K, int N, const void* x, const void* W, int act, const void* pre, const void* dout, void* dpre,
               int dx_dtype, void* dx, int dw_dtype, void* dW, float* db, int add, void* ws, hipStream_t st) {
@@ -298,22 +327,37 @@ void backward(int64_t M, int K, int N, const void* x, const void* W, int act, co
     if (part) join<false>(part, c, (size_t)ldn, (size_t)N, db, add, st);
     if (act != FOLD_ACT_NONE) dz = static_cast<const T*>(dpre);
   }
+  const Shape s1 = dx_shape(M, K, N, es), s2 = dw_shape(M, K, N, es);
+  const int lines = 128 / es;
+  const ProductArgs states{{dz, M, ldn}, {W, N, ldk}, M, K, s1.mt, s1.nt, ldn * es / 128, s1.split, nullptr, (size_t)ldk, ldk,
+                           nullptr, 0, nullptr};
+  const ProductArgs weights{{dz, M, ldn}, {x, M, ldk}, N, K, s2.mt, s2.nt, (int)((M + lines - 1) / lines), s2.split, nullptr,
+                            (size_t)ldk, ldk, nullptr, 0, nullptr};
+  if (dx && dW && M > 0 && together(s1, s2)) {
+    ProfScope prof("linear_dx_dw", st);
+    const auto both = [&](auto* px, auto* pw) {
+      both_products<T>(states, weights, s1, s2, px, pw, static_cast<float*>(ws), dw_dtype == FOLD_F32 ? add : 0, st);
+    };
+    if constexpr (sizeof(T) == 2) {
+      T *tx = static_cast<T*>(dx), *tw = static_cast<T*>(dW);
+      if (dx_dtype == FOLD_F32 && dw_dtype == FOLD_F32) both(static_cast<float*>(dx), static_cast<float*>(dW));
+      else if (dx_dtype == FOLD_F32) both(static_cast<float*>(dx), tw);
+      else if (dw_dtype == FOLD_F32) both(tx, static_cast<float*>(dW));
+      else both(tx, tw);
+    } else {
+      both(static_cast<float*>(dx), static_cast<float*>(dW));
+    }
+    return;
+  }
   if (dx && M > 0) {
     ProfScope prof("linear_dx", st);
-    const Shape sh = dx_shape(M, K, N, es);
-    const ProductArgs g{{dz, M, ldn}, {W, N, ldk}, M, K, sh.mt, sh.nt, ldn * es / 128, sh.split, nullptr, (size_t)ldk, ldk,
-                        nullptr, 0, nullptr};
-    if (dx_dtype == FOLD_F32) cut_product<T, kAlong, float>(g, sh, static_cast<float*>(dx), ws, 0, st);
-    else if constexpr (sizeof(T) == 2) cut_product<T, kAlong, uint16_t>(g, sh, static_cast<uint16_t*>(dx), ws, 0, st);
+    if (dx_dtype == FOLD_F32) cut_product<T, kAlong, float>(states, s1, static_cast<float*>(dx), ws, 0, st);
+    else if constexpr (sizeof(T) == 2) cut_product<T, kAlong, uint16_t>(states, s1, static_cast<uint16_t*>(dx), ws, 0, st);
   }
   if (dW) {
     ProfScope prof("linear_dw", st);
-    const Shape sh = dw_shape(M, K, N, es);
-    const int lines = 128 / es;
-    const ProductArgs g{{dz, M, ldn}, {x, M, ldk}, N, K, sh.mt, sh.nt, (int)((M + lines - 1) / lines), sh.split, nullptr,
-                        (size_t)ldk, ldk, nullptr, 0, nullptr};
-    if (dw_dtype == FOLD_F32) cut_product<T, kAcross, float>(g, sh, static_cast<float*>(dW), ws, add, st);
-    else if constexpr (sizeof(T) == 2) cut_product<T, kAcross, uint16_t>(g, sh, static_cast<uint16_t*>(dW), ws, 0, st);
+    if (dw_dtype == FOLD_F32) cut_product<T, kAcross, float>(weights, s2, static_cast<float*>(dW), ws, add, st);
+    else if constexpr (sizeof(T) == 2) cut_product<T, kAcross, uint16_t>(weights, s2, static_cast<uint16_t*>(dW), ws, 0, st);
   }
 }
 
@@ -332,7 +376,7 @@ int64_t linear_backward_tiles(int dtype, int64_t M, int K, int N) {
   const int es = dtype == FOLD_BF16 ? 2 : 4;
   const Shape a = dx_shape(M, K, N, es), b = dw_shape(M, K, N, es);
   const int64_t join = ((int64_t)std::max(a.split > 1 ? (M + 1) * row_ld(K) : 0, b.split > 1 ? (int64_t)N * row_ld(K) : 0)) / 1024 + 1;
-  return std::max({a.mt * a.nt * a.split, b.mt * b.nt * b.split, join});
+  return std::max(a.mt * a.nt * a.split + b.mt * b.nt * b.split, join);
 }
 
 void launch_linear(int dtype, int64_t M, int K, int N, const void* x, const void* W, const float* bias, int act,
@@ -354,9 +398,9 @@ size_t linear_backward_bytes(int dtype, int64_t M, int K, int N) {
   const int es = dtype == FOLD_BF16 ? 2 : 4;
   const Shape a = dx_shape(M, K, N, es), b = dw_shape(M, K, N, es);
   const int c = std::max(bias_chunks(M, N, es), activation_chunks(M, N, es));
-  // they follow each other on the stream: one region serves all
+  // they follow each other on the stream, so one region serves all; in one launch either has its own
   const size_t dx = a.split > 1 ? (size_t)a.split * M * row_ld(K) : 0, dw = b.split > 1 ? (size_t)b.split * N * row_ld(K) : 0;
-  return std::max({dx, dw, c > 1 ? (size_t)c * row_ld(N) : (size_t)0}) * sizeof(float);
+  return std::max({together(a, b) ? dx + dw : std::max(dx, dw), c > 1 ? (size_t)c * row_ld(N) : (size_t)0}) * sizeof(float);
 }
 
 void launch_linear_backward(int dtype, int64_t M, int K, int N, const void* x, const void* W, int act, const void* pre,

@@ -162,7 +162,9 @@ struct NormBackArgs {
   const void* residual;
   void* dx;            // or NULL
   int dx_f32;          // residual and dx are fp32
-  float* part;         // [blocks][2][ld]: the block's sums for gamma and beta; NULL: nobody wants them
+  float* part;         // [blocks][2][ld]: the block's sums for gamma and beta; NULL: nobody wants them, or:
+  float *dgamma, *dbeta;  // a single workgroup writes them itself
+  int add;
 };
 
 // 16 bytes of T, or the same values in fp32 (twice 16 bytes)
@@ -286,7 +288,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_back(NormBackArgs a) {
       }
     }
   }
-  if (!a.part) return;
+  if (!a.part && !a.dgamma && !a.dbeta) return;
   // the wave's rows, then the four waves one after the other
 #pragma unroll
   for (int i = 0; i < NV; ++i)
@@ -309,6 +311,13 @@ __global__ __launch_bounds__(kThreads) void k_norm_back(NormBackArgs a) {
           red[1][at] = w == 0 ? db[i][e] : red[1][at] + db[i][e];
         }
     __syncthreads();
+  }
+  if (!a.part) {
+    for (int c = threadIdx.x; c < a.n; c += kThreads) {
+      if (a.dgamma) a.dgamma[c] = a.add ? a.dgamma[c] + red[0][c] : red[0][c];
+      if (a.dbeta) a.dbeta[c] = a.add ? a.dbeta[c] + red[1][c] : red[1][c];
+    }
+    return;
   }
   for (int c = threadIdx.x; c < 2 * a.ld; c += kThreads)
     a.part[(size_t)blockIdx.x * 2 * a.ld + c] = c < a.ld ? red[0][c] : red[1][c - a.ld];
@@ -406,8 +415,8 @@ void launch_norm(int dtype, int64_t rows, int n, const void* x, const float* gam
 }
 
 size_t norm_backward_bytes(int dtype, int64_t rows, int n) {
-  const int ld = row_ld(n);
-  return (size_t)back_blocks(rows, lanes_of(ld, dtype == FOLD_BF16 ? 2 : 4)) * 2 * ld * sizeof(float);
+  const int ld = row_ld(n), blocks = back_blocks(rows, lanes_of(ld, dtype == FOLD_BF16 ? 2 : 4));
+  return blocks == 1 ? 0 : (size_t)blocks * 2 * ld * sizeof(float);
 }
 
 void launch_norm_backward(int dtype, int64_t rows, int n, const void* x, const float* gamma, const float* mean,
@@ -417,15 +426,15 @@ void launch_norm_backward(int dtype, int64_t rows, int n, const void* x, const f
   const Lanes l = lanes_of(ld, dtype == FOLD_BF16 ? 2 : 4);
   const int blocks = rows > 0 ? back_blocks(rows, l) : 0;
   const bool sums = dgamma || dbeta;
-  float* part = sums ? static_cast<float*>(ws) : nullptr;
+  float* part = sums && blocks != 1 ? static_cast<float*>(ws) : nullptr;
   if (rows > 0) {
     ProfScope prof("layer_norm_back", st);
     const NormBackArgs a{x, rows, n, ld, gamma, mean, rstd, dy, dy_dtype == FOLD_F32, residual, dx, dx_dtype == FOLD_F32,
-                         part};
+                         part, blocks == 1 ? dgamma : nullptr, blocks == 1 ? dbeta : nullptr, add};
     if (dtype == FOLD_F32) norm_rows_back<float>(a, blocks, st);
     else norm_rows_back<uint16_t>(a, blocks, st);
   }
-  if (sums) {
+  if (sums && blocks != 1) {
     ProfScope prof("layer_norm_join", st);
     hipLaunchKernelGGL(k_norm_join, dim3((unsigned)(2 * ld / 32)), dim3(kThreads), 0, st, part, blocks, ld, n, dgamma,
                        dbeta, add);

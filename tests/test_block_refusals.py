@@ -19,9 +19,12 @@ def test_layer_norm_refuses(F):  # noqa: F811
                dict(y=odd), dict(y=_Buf(x.at + 16)), dict(mean=y), dict(rstd=m), dict(gamma=y), dict(mean=x), dict(beta=r)):
         _refused(F, F.FOLD_E_INVALID, norm, **kw)
     norm(rows=0, x=None, y=None)
-    n = F.fold_layer_norm_workspace_size(0, 4, 100)
+    assert F.fold_layer_norm_workspace_size(0, 4, 100) == 0  # few rows: one workgroup
+    x, y, d = (_Buf(1 << k) for k in (30, 31, 32))
+    n = F.fold_layer_norm_workspace_size(0, 4000, 100)
+    assert n > 0
 
-    def back(dtype=0, rows=4, width=100, x=x, gamma=None, mean=m, rstd=r, dyt=0, dy=d, dxt=0, res=None, dx=y, dg=v,
+    def back(dtype=0, rows=4000, width=100, x=x, gamma=None, mean=m, rstd=r, dyt=0, dy=d, dxt=0, res=None, dx=y, dg=v,
              db=None, flags=0, ws=ws, n=n):
         F.fold_layer_norm_backward(dtype, rows, width, x, gamma, mean, rstd, dyt, dy, dxt, res, dx, dg, db, flags, ws, n,
                                    NULL_STREAM)
