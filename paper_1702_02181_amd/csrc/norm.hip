@@ -75,6 +75,20 @@ struct Vec {
   }
 };
 
+// columns col .. col + 3 of a vector of n values; 0 behind its end, `none` where there is no vector
+__device__ __forceinline__ void load4(const float* p, int col, int n, float none, float (&v)[4]) {
+  if (p && col + 4 <= n && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+    const float4 w = *reinterpret_cast<const float4*>(p + col);
+    v[0] = w.x;
+    v[1] = w.y;
+    v[2] = w.z;
+    v[3] = w.w;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = col + e < n ? (p ? p[col + e] : none) : 0.f;
+  }
+}
+
 struct NormArgs {
   const void* x;
   int64_t rows;
@@ -95,6 +109,7 @@ __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
   int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR;
   const T* x = static_cast<const T*>(a.x);
   const float n = (float)a.n;
+  const bool tail = a.n < LPR * NV * VEC;  // (then what lies past the row's values is looked away from)
   auto load = [&](int64_t r, uint4 (&v)[NV]) {
     const uint4* p = reinterpret_cast<const uint4*>(x + (size_t)min(r, a.rows - 1) * a.ld);
 #pragma unroll
@@ -107,10 +122,15 @@ __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      const int col = (i * LPR + gl) * VEC + e;
-      g[i][e] = col < a.n ? (a.gamma ? a.gamma[col] : 1.f) : 0.f;
-      b[i][e] = col < a.n && a.beta ? a.beta[col] : 0.f;
+    for (int e = 0; e < VEC; e += 4) {
+      float t[4], u[4];
+      load4(a.gamma, (i * LPR + gl) * VEC + e, a.n, 1.f, t);
+      load4(a.beta, (i * LPR + gl) * VEC + e, a.n, 0.f, u);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        g[i][e + k] = t[k];
+        b[i][e + k] = u[k];
+      }
     }
   // all waves of the workgroup take part in every round; rows behind the last one are the last one again, and not stored
   for (int64_t first = (int64_t)blockIdx.x * RPB; first < a.rows; first += step, row += step) {
@@ -122,7 +142,7 @@ __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
       V::take(raw[i], v[i]);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        v[i][e] = (i * LPR + gl) * VEC + e < a.n ? v[i][e] : 0.f;
+        if (tail) v[i][e] = (i * LPR + gl) * VEC + e < a.n ? v[i][e] : 0.f;
         sum += v[i][e];
       }
     }
@@ -132,7 +152,8 @@ __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        v[i][e] = (i * LPR + gl) * VEC + e < a.n ? v[i][e] - mean : 0.f;
+        v[i][e] -= mean;
+        if (tail) v[i][e] = (i * LPR + gl) * VEC + e < a.n ? v[i][e] : 0.f;
         sq += v[i][e] * v[i][e];
       }
     const float rstd = 1.f / sqrtf(row_sum<LPR>(sq, red) / n + a.eps);
@@ -140,7 +161,10 @@ __global__ __launch_bounds__(kThreads) void k_norm(NormArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) v[i][e] = (i * LPR + gl) * VEC + e < a.n ? v[i][e] * rstd * g[i][e] + b[i][e] : 0.f;
+      for (int e = 0; e < VEC; ++e) {
+        v[i][e] = v[i][e] * rstd * g[i][e] + b[i][e];
+        if (tail) v[i][e] = (i * LPR + gl) * VEC + e < a.n ? v[i][e] : 0.f;
+      }
       if (i * LPR + gl < vecs && row < a.rows) reinterpret_cast<uint4*>(y)[i * LPR + gl] = V::give(v[i]);
     }
     if (gl == 0 && row < a.rows) {
@@ -167,41 +191,42 @@ struct NormBackArgs {
   int add;
 };
 
-// 16 bytes of T, or the same values in fp32 (twice 16 bytes)
-template <typename T>
+// 16 bytes of T, or, where types are MIXED, perhaps the same values in fp32 (twice 16 bytes)
+template <typename T, bool MIXED>
 struct Pair {
-  uint4 lo, hi;
+  uint4 lo, hi[MIXED ? 1 : 0];
 };
-template <typename T>
-__device__ __forceinline__ Pair<T> load_pair(const void* p, size_t row, int ld, int vec, bool f32) {
-  Pair<T> r;
-  if (sizeof(T) == 2 && f32) {
+template <typename T, bool MIXED>
+__device__ __forceinline__ Pair<T, MIXED> load_pair(const void* p, size_t row, int ld, int vec, bool f32) {
+  Pair<T, MIXED> r;
+  if (MIXED && f32) {
     const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + row * ld) + 2 * vec;
     r.lo = q[0];
-    r.hi = q[1];
+    if constexpr (MIXED) r.hi[0] = q[1];
   } else {
     r.lo = reinterpret_cast<const uint4*>(static_cast<const T*>(p) + row * ld)[vec];
-    r.hi = make_uint4(0, 0, 0, 0);
+    if constexpr (MIXED) r.hi[0] = make_uint4(0, 0, 0, 0);
   }
   return r;
 }
-template <typename T>
-__device__ __forceinline__ void take_pair(const Pair<T>& r, bool f32, float (&v)[Vec<T>::N]) {
-  if (sizeof(T) == 2 && f32) {
-    const float* lo = reinterpret_cast<const float*>(&r.lo);
-    const float* hi = reinterpret_cast<const float*>(&r.hi);
+template <typename T, bool MIXED>
+__device__ __forceinline__ void take_pair(const Pair<T, MIXED>& r, bool f32, float (&v)[Vec<T>::N]) {
+  if constexpr (MIXED)
+    if (f32) {
+      const float* lo = reinterpret_cast<const float*>(&r.lo);
+      const float* hi = reinterpret_cast<const float*>(&r.hi[0]);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      v[e] = lo[e];
-      v[4 + e < Vec<T>::N ? 4 + e : e] = hi[e];
+      for (int e = 0; e < 4; ++e) {
+        v[e] = lo[e];
+        v[4 + e] = hi[e];
+      }
+      return;
     }
-  } else {
-    Vec<T>::take(r.lo, v);
-  }
+  Vec<T>::take(r.lo, v);
 }
 
 // A workgroup walks over rows of the whole matrix and keeps its sums for gamma and beta in registers until the end.
-template <typename T, int LPR, int NV>
+template <typename T, int LPR, int NV, bool MIXED>
 __global__ __launch_bounds__(kThreads) void k_norm_back(NormBackArgs a) {
   using V = Vec<T>;
   constexpr int VEC = V::N, RPB = kThreads / LPR;
@@ -213,15 +238,17 @@ __global__ __launch_bounds__(kThreads) void k_norm_back(NormBackArgs a) {
   const float n = (float)a.n;
   const bool dyf = a.dy_f32, dxf = a.dx_f32;
   uint4 raw[NV];
-  Pair<T> rdy[NV];
+  Pair<T, MIXED> rdy[NV], rres[NV];
   float mean, rstd;
+  const bool added = a.dx && a.residual, tail = a.n < LPR * NV * VEC;
   auto load = [&](int64_t at) {
     const size_t r = (size_t)min(at, a.rows - 1);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int vec = min(i * LPR + gl, vecs - 1);
       raw[i] = reinterpret_cast<const uint4*>(x + r * a.ld)[vec];
-      rdy[i] = load_pair<T>(a.dy, r, a.ld, vec, dyf);
+      rdy[i] = load_pair<T, MIXED>(a.dy, r, a.ld, vec, dyf);
+      if (added) rres[i] = load_pair<T, MIXED>(a.residual, r, a.ld, vec, dxf);
     }
     mean = a.mean[r];
     rstd = a.rstd[r];
@@ -231,10 +258,14 @@ __global__ __launch_bounds__(kThreads) void k_norm_back(NormBackArgs a) {
 #pragma unroll
   for (int i = 0; i < NV; ++i)
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      const int col = (i * LPR + gl) * VEC + e;
-      g[i][e] = col < a.n ? (a.gamma ? a.gamma[col] : 1.f) : 0.f;
-      dg[i][e] = db[i][e] = 0.f;
+    for (int e = 0; e < VEC; e += 4) {
+      float t[4];
+      load4(a.gamma, (i * LPR + gl) * VEC + e, a.n, 1.f, t);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        g[i][e + k] = t[k];
+        dg[i][e + k] = db[i][e + k] = 0.f;
+      }
     }
   for (int64_t first = (int64_t)blockIdx.x * RPB; first < a.rows; first += step, row += step) {
     float xh[NV][VEC], dy[NV][VEC], s1 = 0.f, s2 = 0.f;
@@ -242,22 +273,37 @@ __global__ __launch_bounds__(kThreads) void k_norm_back(NormBackArgs a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       V::take(raw[i], xh[i]);
-      take_pair<T>(rdy[i], dyf, dy[i]);
+      take_pair<T, MIXED>(rdy[i], dyf, dy[i]);
     }
-    load(row + step);
-    Pair<T> res[NV];
-    if (a.dx && a.residual)
+    Pair<T, MIXED> res[NV];
 #pragma unroll
-      for (int i = 0; i < NV; ++i) res[i] = load_pair<T>(a.residual, (size_t)min(row, a.rows - 1), a.ld, min(i * LPR + gl, vecs - 1), dxf);
+    for (int i = 0; i < NV; ++i) res[i] = rres[i];
+    load(row + step);
+    if (tail)  // what lies past the row's values, whatever it is
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const bool in = (i * LPR + gl) * VEC + e < a.n;
+          xh[i][e] = in ? xh[i][e] : m;
+          dy[i][e] = in ? dy[i][e] : 0.f;
+        }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) xh[i][e] = (xh[i][e] - m) * rs;
+    if (row < a.rows)
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          dg[i][e] += dy[i][e] * xh[i][e];
+          db[i][e] += dy[i][e];
+        }
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const bool in = (i * LPR + gl) * VEC + e < a.n && row < a.rows;
-        xh[i][e] = in ? (xh[i][e] - m) * rs : 0.f;
-        dy[i][e] = in ? dy[i][e] : 0.f;
-        dg[i][e] += dy[i][e] * xh[i][e];
-        db[i][e] += dy[i][e];
         dy[i][e] *= g[i][e];
         s1 += dy[i][e];
         s2 += dy[i][e] * xh[i][e];
@@ -269,15 +315,15 @@ __global__ __launch_bounds__(kThreads) void k_norm_back(NormBackArgs a) {
     for (int i = 0; i < NV; ++i) {
       const int vec = i * LPR + gl;
       float r[VEC];
-      if (a.residual) take_pair<T>(res[i], dxf, r);
+      if (added) take_pair<T, MIXED>(res[i], dxf, r);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        const bool in = vec * VEC + e < a.n;
-        const float d = rs * (dy[i][e] - s1 - xh[i][e] * s2) + (a.residual ? r[e] : 0.f);
-        dy[i][e] = in ? d : 0.f;
+        dy[i][e] = rs * (dy[i][e] - s1 - xh[i][e] * s2);
+        if (added) dy[i][e] += r[e];
+        if (tail) dy[i][e] = vec * VEC + e < a.n ? dy[i][e] : 0.f;
       }
       if (vec >= vecs || row >= a.rows) continue;
-      if (sizeof(T) == 2 && dxf) {
+      if (MIXED && dxf) {
         uint4* q = reinterpret_cast<uint4*>(static_cast<float*>(a.dx) + (size_t)row * a.ld) + 2 * vec;
         const float* d = dy[i];
         q[0] = make_uint4(__float_as_uint(d[0]), __float_as_uint(d[1]), __float_as_uint(d[2]), __float_as_uint(d[3]));
@@ -331,12 +377,19 @@ __global__ __launch_bounds__(kThreads) void k_norm_join(const float* part, int p
   const int at = threadIdx.x & 7, group = threadIdx.x >> 3;
   const int c = (blockIdx.x * 8 + at) * 4;  // of 2 ld, a multiple of 32
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int p = group; p < pieces; p += 32) {
-    const float4 v = *reinterpret_cast<const float4*>(part + (size_t)p * 2 * ld + c);
-    s.x += v.x;
-    s.y += v.y;
-    s.z += v.z;
-    s.w += v.w;
+  for (int p0 = group; p0 < pieces; p0 += 32 * 8) {  // eight loads in flight
+    float4 v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      v[u] = *reinterpret_cast<const float4*>(part + (size_t)min(p0 + 32 * u, pieces - 1) * 2 * ld + c);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const bool in = p0 + 32 * u < pieces;
+      s.x += in ? v[u].x : 0.f;
+      s.y += in ? v[u].y : 0.f;
+      s.z += in ? v[u].z : 0.f;
+      s.w += in ? v[u].w : 0.f;
+    }
   }
   red[group][at] = s;
   __syncthreads();
@@ -360,10 +413,11 @@ Lanes lanes_of(int ld, int esize) {
   return {l, (vecs + l - 1) / l};
 }
 
-constexpr int kMostBlocks = 512;
-int back_blocks(int64_t rows, const Lanes& l) {
-  const int64_t rpb = kThreads / l.lpr;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(kMostBlocks, (rows + 4 * rpb - 1) / (4 * rpb)));
+// Workgroups of the backward: what the chip holds at once, two a compute unit, three where registers allow it (bf16, 16
+// values a lane), each with at least four rounds of rows.
+int back_blocks(int64_t rows, const Lanes& l, int esize) {
+  const int64_t rpb = kThreads / l.lpr, most = esize == 2 && l.nv <= 2 ? 768 : 512;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(most, (rows + 4 * rpb - 1) / (4 * rpb)));
 }
 
 // f(LPR, NV) for the smallest NV that is built
@@ -390,7 +444,7 @@ template <typename T>
 void norm_rows(const NormArgs& a, hipStream_t st) {
   with_lanes<T>(lanes_of(a.ld, sizeof(T)), [&](auto lpr, auto nv) {
     constexpr int RPB = kThreads / decltype(lpr)::value;
-    const int64_t blocks = std::min<int64_t>((a.rows + RPB - 1) / RPB, 8 * 256);
+    const int64_t blocks = std::min<int64_t>((a.rows + RPB - 1) / RPB, 5 * 256);
     hipLaunchKernelGGL((k_norm<T, decltype(lpr)::value, decltype(nv)::value>), dim3((unsigned)blocks), dim3(kThreads), 0,
                        st, a);
   });
@@ -398,8 +452,14 @@ void norm_rows(const NormArgs& a, hipStream_t st) {
 template <typename T>
 void norm_rows_back(const NormBackArgs& a, int blocks, hipStream_t st) {
   with_lanes<T>(lanes_of(a.ld, sizeof(T)), [&](auto lpr, auto nv) {
-    hipLaunchKernelGGL((k_norm_back<T, decltype(lpr)::value, decltype(nv)::value>), dim3((unsigned)blocks), dim3(kThreads),
-                       0, st, a);
+    constexpr int L = decltype(lpr)::value, N = decltype(nv)::value;
+    const dim3 grid((unsigned)blocks), block(kThreads);
+    if constexpr (sizeof(T) == 2)
+      if (a.dy_f32 || a.dx_f32) {
+        hipLaunchKernelGGL((k_norm_back<T, L, N, true>), grid, block, 0, st, a);
+        return;
+      }
+    hipLaunchKernelGGL((k_norm_back<T, L, N, false>), grid, block, 0, st, a);
   });
 }
 
@@ -415,16 +475,16 @@ void launch_norm(int dtype, int64_t rows, int n, const void* x, const float* gam
 }
 
 size_t norm_backward_bytes(int dtype, int64_t rows, int n) {
-  const int ld = row_ld(n), blocks = back_blocks(rows, lanes_of(ld, dtype == FOLD_BF16 ? 2 : 4));
+  const int ld = row_ld(n), es = dtype == FOLD_BF16 ? 2 : 4, blocks = back_blocks(rows, lanes_of(ld, es), es);
   return blocks == 1 ? 0 : (size_t)blocks * 2 * ld * sizeof(float);
 }
 
 void launch_norm_backward(int dtype, int64_t rows, int n, const void* x, const float* gamma, const float* mean,
                           const float* rstd, int dy_dtype, const void* dy, int dx_dtype, const void* residual, void* dx,
                           float* dgamma, float* dbeta, int add, void* ws, hipStream_t st) {
-  const int ld = row_ld(n);
-  const Lanes l = lanes_of(ld, dtype == FOLD_BF16 ? 2 : 4);
-  const int blocks = rows > 0 ? back_blocks(rows, l) : 0;
+  const int ld = row_ld(n), es = dtype == FOLD_BF16 ? 2 : 4;
+  const Lanes l = lanes_of(ld, es);
+  const int blocks = rows > 0 ? back_blocks(rows, l, es) : 0;
   const bool sums = dgamma || dbeta;
   float* part = sums && blocks != 1 ? static_cast<float*>(ws) : nullptr;
   if (rows > 0) {
