@@ -16,15 +16,15 @@ struct QTile {
   int32_t entry;           // list entry of the first row's query
   int32_t head0;           // the first row's head within its group
   int32_t rows;            // 0: nothing to do
-  int32_t kv_head;
+  int32_t kv_head;         // the launch's second dimension
   int32_t k_begin, k_end;  // list entries of the keys
-  int32_t slot;            // of the partial results, -1: the results themselves
+  int32_t slot;            // of the partial results (of the first head; a head's follow another's), -1: the results themselves
   int32_t pieces;          // of the tile, by the tile's first piece (its slot is theirs); 0 otherwise
 };
 
 // A workgroup's part of the gradient of keys and values: up to 128 keys against a run of row tiles.
 struct KTile {
-  int32_t k_begin, keys;
+  int32_t k_begin, keys;   // keys 0: nothing to do
   int32_t kv_head;
   int32_t t_begin, t_end;  // row tiles
   int32_t slot, pieces;
@@ -48,7 +48,7 @@ struct Cross {
   KTile* kjoin = nullptr;
   RTile* rows = nullptr;
   int nfwd = 0, nfjoin = 0, nback = 0, nbjoin = 0, nkeys = 0, nkjoin = 0, nrows = 0;
-  int fslots = 0, bslots = 0, kslots = 0;
+  int fslots = 0, bslots = 0, kslots = 0;  // of a head
   bool few = false;  // the forward takes tiles of 32 rows whose four waves share them and cut the keys
 };
 

@@ -264,6 +264,7 @@ struct Args {
   const uint8_t* mask;
   float scale;
   int heads, group, d;
+  int slots;       // of a head
   unsigned magic;  // x / group = x * magic >> 20 for x < 2^10, group <= 256
   void *out, *out2;
   int64_t ldo, ldo2;
@@ -272,6 +273,15 @@ struct Args {
   float* part;
 };
 __device__ __forceinline__ int row_of(const int* list, int entry) { return list[entry]; }
+
+// the workgroup's tile, with its head and its slot among all heads'
+template <class Tile>
+__device__ __forceinline__ Tile tile_of_head(const Tile* tiles, const Args& a) {
+  Tile t = tiles[blockIdx.x];
+  t.kv_head = blockIdx.y;
+  if (t.slot >= 0) t.slot += blockIdx.y * a.slots;
+  return t;
+}
 
 // the virtual row r of a tile: its query's list entry and its head
 struct Virtual {
@@ -392,7 +402,7 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
   constexpr int IMAGES = NW == 4 ? 4 * image_bytes<T, DP>() : 0;
   constexpr int TILES = 2 * BUF * (NW == 1 ? 4 : 1), LDS = TILES > IMAGES ? TILES : IMAGES;
   __shared__ __attribute__((aligned(16))) char lds[LDS > MEET ? LDS : MEET];
-  const QTile t = tiles[blockIdx.x];
+  const QTile t = tile_of_head(tiles, a);
   if (t.rows == 0) return;
   const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
   const T* k = static_cast<const T*>(a.k) + t.kv_head * a.d;
@@ -550,7 +560,7 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
 template <typename T, int DP, int ROWS, bool SOFTMAX, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_cross_join(const QTile* tiles, Args a) {
   constexpr int DB = DP / 32;
-  const QTile t = tiles[blockIdx.x];
+  const QTile t = tile_of_head(tiles, a);
   const int c0 = (threadIdx.x & 7) * 4;
   T* out = static_cast<T*>(a.out);
   for (int r = threadIdx.x >> 3; r < t.rows; r += kThreads / 8) {
@@ -622,7 +632,7 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
   constexpr int U = DP * (int)sizeof(T) / 16, NS = U / 2, DB = DP / 32, KB = TK / 32, TB = tile_bytes<TK, T, DP>();
   constexpr int E = 16 / (int)sizeof(T), BUF = 2 * TB, IMAGES = 4 * image_bytes<T, DP>();
   __shared__ __attribute__((aligned(16))) char lds[2 * BUF > IMAGES ? 2 * BUF : IMAGES];
-  const QTile t = tiles[blockIdx.x];
+  const QTile t = tile_of_head(tiles, a);
   if (t.rows == 0) return;
   const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
   const T* k = static_cast<const T*>(a.k) + t.kv_head * a.d;
@@ -732,7 +742,7 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 3)) void k_cr
   // the widest fp32 heads leave no registers for v's fragments: every lane keeps its own in LDS
   constexpr bool KEEP = DP * sizeof(T) > 384 || DP * sizeof(T) == 128;
   __shared__ uint4 kept[KEEP ? 4 * NS * 64 : 1];
-  const KTile t = tiles[blockIdx.x];
+  const KTile t = tile_of_head(tiles, a);
   if (t.keys == 0) return;
   const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
   const int first = 32 * wave, mykey = first + l32;
@@ -911,7 +921,7 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 3)) void k_cr
 // The pieces of a tile of keys summed in their order: eight threads a key.
 template <typename T, int DP, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_cross_join_keys(const KTile* tiles, Args a) {
-  const KTile t = tiles[blockIdx.x];
+  const KTile t = tile_of_head(tiles, a);
   const int c0 = (threadIdx.x & 7) * 4;
   for (int key = threadIdx.x >> 3; key < t.keys; key += kThreads / 8) {
     const int ke = t.k_begin + key, krow = row_of(a.k_row, ke);
@@ -987,13 +997,14 @@ Args args_of(const Cross& c, const CrossMat& q, const CrossMat& k, const CrossMa
 }  // namespace
 
 size_t cross_forward_bytes(const Cross& c) {
-  return (size_t)c.fslots * (c.few ? kCrossFew : kCrossRows) * (cross_padded(c.head_dim) + 2) * sizeof(float);
+  return (size_t)c.fslots * c.kv_heads * (c.few ? kCrossFew : kCrossRows) * (cross_padded(c.head_dim) + 2) * sizeof(float);
 }
 static size_t delta_floats(const Cross& c) { return ((size_t)c.query_rows * c.heads + 3) / 4 * 4; }
 size_t cross_backward_bytes(const Cross& c) {
   const int dp = cross_padded(c.head_dim);
   // the queries' and the keys' pieces follow each other on the stream: one region serves both
-  const size_t dq = (size_t)c.bslots * kCrossRows * (dp + 2), dk = (size_t)c.kslots * kCrossKeys * 2 * dp;
+  const size_t dq = (size_t)c.bslots * c.kv_heads * kCrossRows * (dp + 2),
+               dk = (size_t)c.kslots * c.kv_heads * kCrossKeys * 2 * dp;
   return (delta_floats(c) + std::max(dq, dk)) * sizeof(float);
 }
 
@@ -1004,6 +1015,7 @@ void launch_cross(const Cross& c, CrossMat q, CrossMat k, CrossMat v, const uint
   a.out = out;
   a.ldo = ldo;
   a.lse = lse;
+  a.slots = c.fslots;
   a.part = static_cast<float*>(ws);
   const int es = c.dtype == FOLD_BF16 ? 2 : 4, d = c.head_dim;
   const bool vec = whole_units(q, d, es) && whole_units(k, d, es) && whole_units(v, d, es) && whole_units({out, ldo}, d, es);
@@ -1015,15 +1027,15 @@ void launch_cross(const Cross& c, CrossMat q, CrossMat k, CrossMat v, const uint
       {
         ProfScope prof("cross", st);
         if constexpr (DP * sizeof(T) <= kCrossFewBytes)
-          if (c.few) hipLaunchKernelGGL((k_cross<T, DP, 32, 1, VEC>), dim3(c.nfwd), dim3(kThreads), 0, st, c.fwd, a);
-        if (!c.few) hipLaunchKernelGGL((k_cross<T, DP, TK, 4, VEC>), dim3(c.nfwd), dim3(kThreads), 0, st, c.fwd, a);
+          if (c.few) hipLaunchKernelGGL((k_cross<T, DP, 32, 1, VEC>), dim3(c.nfwd, c.kv_heads), dim3(kThreads), 0, st, c.fwd, a);
+        if (!c.few) hipLaunchKernelGGL((k_cross<T, DP, TK, 4, VEC>), dim3(c.nfwd, c.kv_heads), dim3(kThreads), 0, st, c.fwd, a);
       }
       if (c.nfjoin == 0) return;
       ProfScope prof("cross_join", st);
       if (c.few)
-        hipLaunchKernelGGL((k_cross_join<T, DP, kCrossFew, true, VEC>), dim3(c.nfjoin), dim3(kThreads), 0, st, c.fjoin, a);
+        hipLaunchKernelGGL((k_cross_join<T, DP, kCrossFew, true, VEC>), dim3(c.nfjoin, c.kv_heads), dim3(kThreads), 0, st, c.fjoin, a);
       else
-        hipLaunchKernelGGL((k_cross_join<T, DP, kCrossRows, true, VEC>), dim3(c.nfjoin), dim3(kThreads), 0, st, c.fjoin, a);
+        hipLaunchKernelGGL((k_cross_join<T, DP, kCrossRows, true, VEC>), dim3(c.nfjoin, c.kv_heads), dim3(kThreads), 0, st, c.fjoin, a);
     };
     if (vec) go(std::true_type());
     else go(std::false_type());
@@ -1059,29 +1071,31 @@ void launch_cross_backward(const Cross& c, CrossMat q, CrossMat k, CrossMat v, c
       if (dq && c.nback > 0) {
         Args b = a;
         b.out = dq;
+        b.slots = c.bslots;
         b.ldo = lddq;
         {
           ProfScope prof("cross_dq", st);
-          hipLaunchKernelGGL((k_cross_dq<T, DP, TK, VEC>), dim3(c.nback), dim3(kThreads), 0, st, c.back, b);
+          hipLaunchKernelGGL((k_cross_dq<T, DP, TK, VEC>), dim3(c.nback, c.kv_heads), dim3(kThreads), 0, st, c.back, b);
         }
         if (c.nbjoin > 0) {
           ProfScope prof("cross_dq_join", st);
-          hipLaunchKernelGGL((k_cross_join<T, DP, kCrossRows, false, VEC>), dim3(c.nbjoin), dim3(kThreads), 0, st, c.bjoin, b);
+          hipLaunchKernelGGL((k_cross_join<T, DP, kCrossRows, false, VEC>), dim3(c.nbjoin, c.kv_heads), dim3(kThreads), 0, st, c.bjoin, b);
         }
       }
       if ((dk || dv) && c.nkeys > 0) {
         Args b = a;
         b.out = dk;
+        b.slots = c.kslots;
         b.ldo = lddk;
         b.out2 = dv;
         b.ldo2 = lddv;
         {
           ProfScope prof("cross_dkv", st);
-          hipLaunchKernelGGL((k_cross_dkv<T, DP, TK, VEC>), dim3(c.nkeys), dim3(kThreads), 0, st, c.keys, c.rows, b);
+          hipLaunchKernelGGL((k_cross_dkv<T, DP, TK, VEC>), dim3(c.nkeys, c.kv_heads), dim3(kThreads), 0, st, c.keys, c.rows, b);
         }
         if (c.nkjoin > 0) {
           ProfScope prof("cross_dkv_join", st);
-          hipLaunchKernelGGL((k_cross_join_keys<T, DP, VEC>), dim3(c.nkjoin), dim3(kThreads), 0, st, c.kjoin, b);
+          hipLaunchKernelGGL((k_cross_join_keys<T, DP, VEC>), dim3(c.nkjoin, c.kv_heads), dim3(kThreads), 0, st, c.kjoin, b);
         }
       }
     };

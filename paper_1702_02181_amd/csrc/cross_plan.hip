@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cstring>
 #include <string>
 #include <vector>
 
@@ -18,6 +19,14 @@ namespace {
 
 __global__ __launch_bounds__(256) void k_zero_words(uint32_t* p, size_t n) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = 0;
+}
+
+// the arrays that the host looks at, and the error word, one after the other
+__global__ __launch_bounds__(256) void k_collect(const int32_t* a, int na, const int32_t* b, int nb, const int32_t* c, int nc,
+                                                 const uint32_t* error, int32_t* out) {
+  const int n = na + nb + nc + 1;
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256)
+    out[i] = i < na ? a[i] : i < na + nb ? b[i - na] : i < na + nb + nc ? c[i - na - nb] : (int32_t)*error;
 }
 
 // error bits: 1 a row out of range, 2 a row listed twice
@@ -43,7 +52,7 @@ struct Range {
   int64_t size() const { return end - begin; }
 };
 
-// Workgroups in launch order.  The XCDs take them in turn and each has an L2 of its own, so the workgroups that read the same
+// Workgroups of a head in launch order.  The XCDs take them in turn and each has an L2 of its own, so the workgroups that read the same
 // keys (or rows) follow each other on one XCD: chunks of a group go, the costliest first, to the XCD with the least work.
 template <class Tile>
 struct Spread {
@@ -89,11 +98,8 @@ struct Spread {
     std::vector<Tile> out(deep * 8, none);
     for (int x = 0; x < 8; ++x)
       for (size_t i = 0; i < lane[x].size(); ++i) out[i * 8 + x] = all[lane[x][i]];
-    while (!out.empty() && empty(out.back())) out.pop_back();
-    return out;
+    return out;  // a multiple of 8: the tiles of every head go to the same XCDs
   }
-  static bool empty(const QTile& t) { return t.rows == 0; }
-  static bool empty(const KTile& t) { return t.keys == 0; }
 };
 
 constexpr int kMinPiece = 256;  // keys (or rows) of a piece
@@ -114,7 +120,7 @@ struct Lists {
   std::vector<std::vector<int>> readers;  // by source: its query sequences; the last entry: those without a source
 };
 
-// tiles of `height` virtual rows, all key heads, in pieces of the keys; the tiles in pieces also go to `join`
+// tiles of `height` virtual rows (launched for every key head) in pieces of the keys; the tiles in pieces also go to `join`
 void query_tiles(const Lists& l, int height, std::vector<QTile>* out, std::vector<QTile>* join, int* slots) {
   const int sources = (int)l.kp.size() - 1;
   int64_t tiles = 0, work = 0;
@@ -132,28 +138,25 @@ void query_tiles(const Lists& l, int height, std::vector<QTile>* out, std::vecto
   for (int e = 0; e <= sources; ++e) {
     const int64_t nk = keys_of(e), pieces = std::max<int64_t>(1, (nk + piece - 1) / piece);
     const int64_t each = ((nk + pieces - 1) / pieces + 63) / 64 * 64;
-    for (int h = 0; h < l.kv_heads; ++h) {
-      for (int b : l.readers[e])
-        for (int64_t r = 0; r < rows_of(b); r += height) {
-          QTile t{};
-          t.entry = (int32_t)(l.qp[b] + r / l.G);
-          t.head0 = (int32_t)(r % l.G);
-          t.rows = (int32_t)std::min<int64_t>(height, rows_of(b) - r);
-          t.kv_head = h;
-          const int32_t k0 = e < sources ? l.kp[e] : 0;
-          const int n = (int)(each ? std::max<int64_t>(1, (nk + each - 1) / each) : 1);
-          for (int p = 0; p < n; ++p) {
-            t.k_begin = (int32_t)(k0 + std::min<int64_t>(p * each, nk));
-            t.k_end = (int32_t)(k0 + std::min<int64_t>((p + 1) * each, nk));
-            t.slot = n > 1 ? *slots + p : -1;
-            t.pieces = p == 0 ? n : 0;
-            s.add(t, t.k_end - t.k_begin);
-            if (n > 1 && p == 0) join->push_back(t);
-          }
-          if (n > 1) *slots += n;
+    const int n = (int)(each ? std::max<int64_t>(1, (nk + each - 1) / each) : 1);
+    const int32_t k0 = e < sources ? l.kp[e] : 0;
+    for (int b : l.readers[e])
+      for (int64_t r = 0; r < rows_of(b); r += height) {
+        QTile t{};
+        t.entry = (int32_t)(l.qp[b] + r / l.G);
+        t.head0 = (int32_t)(r % l.G);
+        t.rows = (int32_t)std::min<int64_t>(height, rows_of(b) - r);
+        for (int p = 0; p < n; ++p) {
+          t.k_begin = (int32_t)(k0 + std::min<int64_t>(p * each, nk));
+          t.k_end = (int32_t)(k0 + std::min<int64_t>((p + 1) * each, nk));
+          t.slot = n > 1 ? *slots + p : -1;
+          t.pieces = p == 0 ? n : 0;
+          s.add(t, t.k_end - t.k_begin);
+          if (n > 1 && p == 0) join->push_back(t);
         }
-      s.close();
-    }
+        if (n > 1) *slots += n;
+      }
+    s.close();
   }
   *out = s.order();
 }
@@ -184,24 +187,21 @@ void key_tiles(const Lists& l, int height, std::vector<KTile>* out, std::vector<
     const int64_t nr = runs[e].size(), pieces = std::max<int64_t>(1, (nr + piece - 1) / piece);
     const int64_t each = std::max<int64_t>(1, (nr + pieces - 1) / pieces);
     const int n = (int)std::max<int64_t>(1, (nr + each - 1) / each);
-    for (int h = 0; h < l.kv_heads; ++h) {
-      for (int32_t k = l.kp[e]; k < l.kp[e + 1]; k += kCrossKeys) {
-        KTile t{};
-        t.k_begin = k;
-        t.keys = std::min<int32_t>(kCrossKeys, l.kp[e + 1] - k);
-        t.kv_head = h;
-        for (int p = 0; p < n; ++p) {
-          t.t_begin = (int32_t)(runs[e].begin + std::min<int64_t>(p * each, nr));
-          t.t_end = (int32_t)(runs[e].begin + std::min<int64_t>((p + 1) * each, nr));
-          t.slot = n > 1 ? *slots + p : -1;
-          t.pieces = p == 0 ? n : 0;
-          s.add(t, (int64_t)(t.t_end - t.t_begin) * height);
-          if (n > 1 && p == 0) join->push_back(t);
-        }
-        if (n > 1) *slots += n;
+    for (int32_t k = l.kp[e]; k < l.kp[e + 1]; k += kCrossKeys) {
+      KTile t{};
+      t.k_begin = k;
+      t.keys = std::min<int32_t>(kCrossKeys, l.kp[e + 1] - k);
+      for (int p = 0; p < n; ++p) {
+        t.t_begin = (int32_t)(runs[e].begin + std::min<int64_t>(p * each, nr));
+        t.t_end = (int32_t)(runs[e].begin + std::min<int64_t>((p + 1) * each, nr));
+        t.slot = n > 1 ? *slots + p : -1;
+        t.pieces = p == 0 ? n : 0;
+        s.add(t, (int64_t)(t.t_end - t.t_begin) * height);
+        if (n > 1 && p == 0) join->push_back(t);
       }
-      s.close();
+      if (n > 1) *slots += n;
     }
+    s.close();
   }
   *out = s.order();
 }
@@ -251,15 +251,17 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
 
   int device = 0;
   FOLD_HIP_CHECK(hipGetDevice(&device));
-  std::vector<int32_t> qp((size_t)b->num_seqs + 1), kp((size_t)b->num_sources + 1), src((size_t)b->num_seqs);
+  const int nq = b->num_seqs + 1, nk = b->num_sources + 1, ns = b->source ? b->num_seqs : 0;
+  std::vector<int32_t> qp(nq), kp(nk), src(ns);
   uint32_t error = 0;
   const size_t qw = b->query_row ? ((size_t)b->num_query_rows + 31) / 32 : 0;
-  const size_t kw = b->key_row ? ((size_t)b->num_key_rows + 31) / 32 : 0;
+  const size_t kw = b->key_row ? ((size_t)b->num_key_rows + 31) / 32 : 0, n = (size_t)nq + nk + ns + 1;
   {
     Block tmp{device, st};
-    tmp.p = pool_alloc(device, (64 + qw + kw) * sizeof(uint32_t), false);
+    tmp.p = pool_alloc(device, (64 + qw + kw + n) * sizeof(uint32_t), false);
     if (!tmp.p) return api_fail(FOLD_E_NOMEM, who + ": no device memory");
     uint32_t* words = static_cast<uint32_t*>(tmp.p);
+    int32_t* lists = reinterpret_cast<int32_t*>(words + 64 + qw + kw);
     hipLaunchKernelGGL(k_zero_words, dim3(grid_for(64 + qw + kw)), dim3(256), 0, st, words, 64 + qw + kw);
     if (qw)
       hipLaunchKernelGGL(k_check_rows, dim3(grid_for(b->num_queries)), dim3(256), 0, st, b->query_row, b->num_queries,
@@ -267,14 +269,22 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
     if (kw)
       hipLaunchKernelGGL(k_check_rows, dim3(grid_for(b->num_keys)), dim3(256), 0, st, b->key_row, b->num_keys,
                          b->num_key_rows, words + 64 + qw, words, 2);
+    hipLaunchKernelGGL(k_collect, dim3(grid_for(n)), dim3(256), 0, st, b->query_ptr, nq, b->key_ptr, nk, b->source, ns, words,
+                       lists);
     FOLD_HIP_CHECK(hipGetLastError());
-    const auto fetch = [&](void* to, const void* from, size_t n) {
-      return n == 0 || hipMemcpyAsync(to, from, n, hipMemcpyDeviceToHost, st) == hipSuccess;
-    };
-    if (!fetch(qp.data(), b->query_ptr, qp.size() * 4) || !fetch(kp.data(), b->key_ptr, kp.size() * 4) ||
-        (b->source && !fetch(src.data(), b->source, src.size() * 4)) || !fetch(&error, words, 4) ||
+    struct Stage {  // pinned, where the lists fit it
+      int* p;
+      ~Stage() { stage_free(p); }
+    } stage{n <= kStageInts ? stage_alloc() : nullptr};
+    std::vector<int32_t> far(stage.p ? 0 : n);
+    int32_t* got = stage.p ? stage.p : far.data();
+    if (hipMemcpyAsync(got, lists, n * sizeof(int32_t), hipMemcpyDeviceToHost, st) != hipSuccess ||
         hipStreamSynchronize(st) != hipSuccess)
       return api_fail(FOLD_E_DEVICE, who + ": the lists could not be read");
+    std::copy(got, got + nq, qp.begin());
+    std::copy(got + nq, got + nq + nk, kp.begin());
+    std::copy(got + nq + nk, got + nq + nk + ns, src.begin());
+    error = (uint32_t)got[n - 1];
   }
   if (!check_ptr(qp, b->num_queries)) return api_fail(FOLD_E_INVALID, who + ": query_ptr malformed");
   if (!check_ptr(kp, b->num_keys)) return api_fail(FOLD_E_INVALID, who + ": key_ptr malformed");
@@ -322,12 +332,12 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
   query_tiles(l, kCrossRows, &back, &bjoin, &c.bslots);
   key_tiles(l, c.dtype == FOLD_BF16 ? 64 : 32, &keys, &kjoin, &rows, &c.kslots);
 
-  size_t bytes = 0;
-  std::vector<std::pair<size_t, std::pair<const void*, size_t>>> copies;
-  const auto place = [&](const void* data, size_t n) {
-    const size_t at = bytes;
-    copies.push_back({at, {data, n}});
-    bytes += (n + 255) / 256 * 256;
+  // one image of all the lists, uploaded whole; the row numbers behind it are copied or made on the device
+  std::vector<char> image;
+  const auto place = [&](const void* data, size_t size) {
+    const size_t at = image.size();
+    image.resize(at + (size + 255) / 256 * 256);
+    if (size) std::memcpy(image.data() + at, data, size);
     return at;
   };
   const size_t at_fwd = place(fwd.data(), fwd.size() * sizeof(QTile)), at_fj = place(fjoin.data(), fjoin.size() * sizeof(QTile)),
@@ -336,20 +346,17 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
                at_keys = place(keys.data(), keys.size() * sizeof(KTile)),
                at_kj = place(kjoin.data(), kjoin.size() * sizeof(KTile)),
                at_rows = place(rows.data(), rows.size() * sizeof(RTile));
-  const size_t at_qr = place(nullptr, (size_t)b->num_queries * 4), at_kr = place(nullptr, (size_t)b->num_keys * 4);
-  c.blob = pool_alloc(device, std::max<size_t>(bytes, 256), true);
+  const size_t at_qr = image.size(), at_kr = at_qr + ((size_t)b->num_queries * 4 + 255) / 256 * 256;
+  c.blob = pool_alloc(device, std::max<size_t>(at_kr + (size_t)b->num_keys * 4, 256), true);
   if (!c.blob) return api_fail(FOLD_E_NOMEM, who + ": no device memory");
   char* base = static_cast<char*>(c.blob);
-  bool ok = true;
-  for (const auto& cp : copies)
-    if (cp.second.first && cp.second.second)
-      ok = ok && hipMemcpyAsync(base + cp.first, cp.second.first, cp.second.second, hipMemcpyHostToDevice, st) == hipSuccess;
-  const auto keep = [&](size_t at, const int32_t* from, int n) {
+  bool ok = image.empty() || hipMemcpyAsync(base, image.data(), image.size(), hipMemcpyHostToDevice, st) == hipSuccess;
+  const auto keep = [&](size_t at, const int32_t* from, int count) {
     int32_t* to = reinterpret_cast<int32_t*>(base + at);
-    if (n > 0 && from)
-      ok = ok && hipMemcpyAsync(to, from, (size_t)n * 4, hipMemcpyDeviceToDevice, st) == hipSuccess;
-    else if (n > 0)
-      hipLaunchKernelGGL(k_identity, dim3(grid_for(n)), dim3(256), 0, st, to, n);
+    if (count > 0 && from)
+      ok = ok && hipMemcpyAsync(to, from, (size_t)count * 4, hipMemcpyDeviceToDevice, st) == hipSuccess;
+    else if (count > 0)
+      hipLaunchKernelGGL(k_identity, dim3(grid_for(count)), dim3(256), 0, st, to, count);
     return to;
   };
   c.q_row = keep(at_qr, b->query_row, b->num_queries);
