@@ -665,8 +665,9 @@ int32_t fold_token_logprobs(const fold_sched* sched, int32_t dtype, int64_t rows
  *     dx = rstd (g - mean(g) - xh mean(g xh)) (+ residual)
  *     dgamma (+)= sum over the rows of dy xh,   dbeta (+)= sum of dy
  *   dy_dtype  of dy: dtype, or FOLD_F32
- *   dx_dtype  of dx and residual: dtype, or FOLD_F32
- *   residual  device [rows, ld], a gradient that goes by the norm, or NULL
+ *   residual  device [rows, ld] of residual_dtype (dtype, or FOLD_F32), a gradient
+ *             that goes by the norm, or NULL
+ *   dx_dtype  of dx: dtype, or FOLD_F32
  *   dx        device, written whole (pad columns zero), or NULL; may be dy or
  *             residual itself where the types are equal
  *   dgamma, dbeta  device [width] fp32, or NULL; written, or added to with
@@ -715,8 +716,8 @@ int32_t fold_layer_norm(int32_t dtype, int64_t rows, int32_t width, const void* 
 int32_t fold_layer_norm_workspace_size(int32_t dtype, int64_t rows, int32_t width, size_t* bytes);
 int32_t fold_layer_norm_backward(int32_t dtype, int64_t rows, int32_t width, const void* x, const float* gamma,
                                  const float* mean, const float* rstd, int32_t dy_dtype, const void* dy,
-                                 int32_t dx_dtype, const void* residual, void* dx, float* dgamma, float* dbeta,
-                                 int32_t flags, void* ws, size_t ws_bytes, hipStream_t stream);
+                                 int32_t residual_dtype, const void* residual, int32_t dx_dtype, void* dx, float* dgamma,
+                                 float* dbeta, int32_t flags, void* ws, size_t ws_bytes, hipStream_t stream);
 int32_t fold_linear(int32_t dtype, int64_t rows, int32_t in_dim, int32_t out_dim, const void* x, const void* W,
                     const float* bias, int32_t act, const void* residual, void* out, void* pre, void* ws, size_t ws_bytes,
                     hipStream_t stream);

@@ -91,13 +91,13 @@ int32_t fold_layer_norm_workspace_size(int32_t dtype, int64_t rows, int32_t widt
 
 int32_t fold_layer_norm_backward(int32_t dtype, int64_t rows, int32_t width, const void* x, const float* gamma,
                                  const float* mean, const float* rstd, int32_t dy_dtype, const void* dy,
-                                 int32_t dx_dtype, const void* residual, void* dx, float* dgamma, float* dbeta,
-                                 int32_t flags, void* ws, size_t ws_bytes, hipStream_t st) {
+                                 int32_t residual_dtype, const void* residual, int32_t dx_dtype, void* dx, float* dgamma,
+                                 float* dbeta, int32_t flags, void* ws, size_t ws_bytes, hipStream_t st) {
   return guarded([&]() -> int32_t {
     const std::string who("fold_layer_norm_backward");
     const int rc = check_norm(who, dtype, rows, width);
     if (rc != FOLD_OK) return rc;
-    if (!grad_type(dy_dtype, dtype) || !grad_type(dx_dtype, dtype))
+    if (!grad_type(dy_dtype, dtype) || !grad_type(dx_dtype, dtype) || (residual && !grad_type(residual_dtype, dtype)))
       return api_fail(FOLD_E_INVALID, who + ": gradients are of the states' type, or fp32");
     if (flags & ~FOLD_BLOCK_ACCUMULATE) return api_fail(FOLD_E_INVALID, who + ": unknown flag");
     if ((!dx || rows == 0) && !dgamma && !dbeta) return FOLD_OK;
@@ -111,13 +111,13 @@ int32_t fold_layer_norm_backward(int32_t dtype, int64_t rows, int32_t width, con
     const Span out[] = {{dx, bytes_of(dx_dtype, rows, width)}, {dgamma, v}, {dbeta, v}, {ws, need}};
     const Span in[] = {{x, bytes_of(dtype, rows, width)},
                        {dx == dy && dx_dtype == dy_dtype ? nullptr : dy, bytes_of(dy_dtype, rows, width)},
-                       {dx == residual ? nullptr : residual, bytes_of(dx_dtype, rows, width)},
+                       {dx == residual && dx_dtype == residual_dtype ? nullptr : residual, bytes_of(residual_dtype, rows, width)},
                        {gamma, v},
                        {mean, r},
                        {rstd, r}};
     if (any_overlap(out, 4, in, 6)) return api_fail(FOLD_E_INVALID, who + ": an output overlaps another buffer");
-    launch_norm_backward(dtype, rows, width, x, gamma, mean, rstd, dy_dtype, dy, dx_dtype, residual, dx, dgamma, dbeta,
-                         flags & FOLD_BLOCK_ACCUMULATE, ws, st);
+    launch_norm_backward(dtype, rows, width, x, gamma, mean, rstd, dy_dtype, dy, dx_dtype, residual_dtype, residual, dx, dgamma,
+                         dbeta, flags & FOLD_BLOCK_ACCUMULATE, ws, st);
     FOLD_HIP_CHECK(hipGetLastError());
     return FOLD_OK;
   });

@@ -610,20 +610,20 @@ template <typename T, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_cross_delta(const T* out, int64_t ldo, const T* dout, int64_t lddo,
                                                           const int* q_row, int64_t n, int heads, int d, float* delta) {
   constexpr int E = 16 / (int)sizeof(T);
-  const int64_t at = (int64_t)blockIdx.x * (kThreads / 8) + (threadIdx.x >> 3);
-  if (at >= n) return;
-  const int entry = (int)(at / heads), head = (int)(at - (int64_t)entry * heads), row = row_of(q_row, entry);
-  const T *x = out + (int64_t)row * ldo + head * d, *y = dout + (int64_t)row * lddo + head * d;
-  float s = 0.f;
-  for (int e0 = (threadIdx.x & 7) * E; e0 < d; e0 += 8 * E) {
-    const uint4 u = row_unit<T, VEC>(x, e0, d), w = row_unit<T, VEC>(y, e0, d);
+  for (int64_t at = (int64_t)blockIdx.x * (kThreads / 8) + (threadIdx.x >> 3); at < n; at += (int64_t)gridDim.x * (kThreads / 8)) {
+    const int entry = (int)(at / heads), head = (int)(at - (int64_t)entry * heads), row = row_of(q_row, entry);
+    const T *x = out + (int64_t)row * ldo + head * d, *y = dout + (int64_t)row * lddo + head * d;
+    float s = 0.f;
+    for (int e0 = (threadIdx.x & 7) * E; e0 < d; e0 += 8 * E) {
+      const uint4 u = row_unit<T, VEC>(x, e0, d), w = row_unit<T, VEC>(y, e0, d);
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      s += to_f32<T>(reinterpret_cast<const T*>(&u)[e]) * to_f32<T>(reinterpret_cast<const T*>(&w)[e]);
+      for (int e = 0; e < E; ++e)
+        s += to_f32<T>(reinterpret_cast<const T*>(&u)[e]) * to_f32<T>(reinterpret_cast<const T*>(&w)[e]);
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o *= 2) s += __shfl_xor(s, o);  // (eight lanes are in or out together)
+    if ((threadIdx.x & 7) == 0) delta[(int64_t)row * heads + head] = s;
   }
-#pragma unroll
-  for (int o = 1; o < 8; o *= 2) s += __shfl_xor(s, o);
-  if ((threadIdx.x & 7) == 0) delta[(int64_t)row * heads + head] = s;
 }
 
 // The queries' gradient: as the forward with four waves, p recomputed from lse, dq^T += k^T ds^T.
@@ -1064,7 +1064,7 @@ void launch_cross_backward(const Cross& c, CrossMat q, CrossMat k, CrossMat v, c
       const int64_t n = (int64_t)c.num_queries * c.heads;
       if (n > 0) {
         ProfScope prof("cross_delta", st);
-        hipLaunchKernelGGL((k_cross_delta<T, VEC>), dim3((unsigned)((n + 31) / 32)), dim3(kThreads), 0, st,
+        hipLaunchKernelGGL((k_cross_delta<T, VEC>), dim3((unsigned)std::min<int64_t>((n + 31) / 32, 1 << 20)), dim3(kThreads), 0, st,
                            static_cast<const T*>(out.p), out.ld, static_cast<const T*>(dout.p), dout.ld, c.q_row, n, c.heads,
                            d, delta);
       }

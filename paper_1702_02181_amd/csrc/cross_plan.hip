@@ -332,6 +332,8 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
   query_tiles(l, kCrossRows, &back, &bjoin, &c.bslots);
   key_tiles(l, c.dtype == FOLD_BF16 ? 64 : 32, &keys, &kjoin, &rows, &c.kslots);
 
+  if ((int64_t)std::max({fwd.size(), back.size(), keys.size()}) >= kMaxTiles)
+    return api_fail(FOLD_E_INVALID, who + ": too many tiles for one launch (sequences and rows)");
   // one image of all the lists, uploaded whole; the row numbers behind it are copied or made on the device
   std::vector<char> image;
   const auto place = [&](const void* data, size_t size) {

@@ -496,8 +496,8 @@ void launch_norm(int dtype, int64_t rows, int n, const void* x, const float* gam
                  float* mean, float* rstd, hipStream_t st);
 size_t norm_backward_bytes(int dtype, int64_t rows, int n);
 void launch_norm_backward(int dtype, int64_t rows, int n, const void* x, const float* gamma, const float* mean,
-                          const float* rstd, int dy_dtype, const void* dy, int dx_dtype, const void* residual, void* dx,
-                          float* dgamma, float* dbeta, int add, void* ws, hipStream_t st);
+                          const float* rstd, int dy_dtype, const void* dy, int dx_dtype, int res_dtype,
+                          const void* residual, void* dx, float* dgamma, float* dbeta, int add, void* ws, hipStream_t st);
 // workgroups of the largest launch of either direction
 int64_t linear_tiles(int dtype, int64_t rows, int in_dim, int out_dim);
 int64_t linear_backward_tiles(int dtype, int64_t rows, int in_dim, int out_dim);

@@ -185,7 +185,7 @@ struct NormBackArgs {
   int dy_f32;          // dy is fp32 (where T is bf16)
   const void* residual;
   void* dx;            // or NULL
-  int dx_f32;          // residual and dx are fp32
+  int dx_f32, res_f32; // dx, the residual are fp32
   float* part;         // [blocks][2][ld]: the block's sums for gamma and beta; NULL: nobody wants them, or:
   float *dgamma, *dbeta;  // a single workgroup writes them itself
   int add;
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_back(NormBackArgs a) {
   int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR;
   const T* x = static_cast<const T*>(a.x);
   const float n = (float)a.n;
-  const bool dyf = a.dy_f32, dxf = a.dx_f32;
+  const bool dyf = a.dy_f32, dxf = a.dx_f32, resf = a.res_f32;
   uint4 raw[NV];
   Pair<T, MIXED> rdy[NV], rres[NV];
   float mean, rstd;
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_back(NormBackArgs a) {
       const int vec = min(i * LPR + gl, vecs - 1);
       raw[i] = reinterpret_cast<const uint4*>(x + r * a.ld)[vec];
       rdy[i] = load_pair<T, MIXED>(a.dy, r, a.ld, vec, dyf);
-      if (added) rres[i] = load_pair<T, MIXED>(a.residual, r, a.ld, vec, dxf);
+      if (added) rres[i] = load_pair<T, MIXED>(a.residual, r, a.ld, vec, resf);
     }
     mean = a.mean[r];
     rstd = a.rstd[r];
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(kThreads) void k_norm_back(NormBackArgs a) {
     for (int i = 0; i < NV; ++i) {
       const int vec = i * LPR + gl;
       float r[VEC];
-      if (added) take_pair<T, MIXED>(res[i], dxf, r);
+      if (added) take_pair<T, MIXED>(res[i], resf, r);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         dy[i][e] = rs * (dy[i][e] - s1 - xh[i][e] * s2);
@@ -455,7 +455,7 @@ void norm_rows_back(const NormBackArgs& a, int blocks, hipStream_t st) {
     constexpr int L = decltype(lpr)::value, N = decltype(nv)::value;
     const dim3 grid((unsigned)blocks), block(kThreads);
     if constexpr (sizeof(T) == 2)
-      if (a.dy_f32 || a.dx_f32) {
+      if (a.dy_f32 || a.dx_f32 || (a.residual && a.res_f32)) {
         hipLaunchKernelGGL((k_norm_back<T, L, N, true>), grid, block, 0, st, a);
         return;
       }
@@ -480,8 +480,8 @@ size_t norm_backward_bytes(int dtype, int64_t rows, int n) {
 }
 
 void launch_norm_backward(int dtype, int64_t rows, int n, const void* x, const float* gamma, const float* mean,
-                          const float* rstd, int dy_dtype, const void* dy, int dx_dtype, const void* residual, void* dx,
-                          float* dgamma, float* dbeta, int add, void* ws, hipStream_t st) {
+                          const float* rstd, int dy_dtype, const void* dy, int dx_dtype, int res_dtype, const void* residual,
+                          void* dx, float* dgamma, float* dbeta, int add, void* ws, hipStream_t st) {
   const int ld = row_ld(n), es = dtype == FOLD_BF16 ? 2 : 4;
   const Lanes l = lanes_of(ld, es);
   const int blocks = rows > 0 ? back_blocks(rows, l, es) : 0;
@@ -490,7 +490,7 @@ void launch_norm_backward(int dtype, int64_t rows, int n, const void* x, const f
   if (rows > 0) {
     ProfScope prof("layer_norm_back", st);
     const NormBackArgs a{x, rows, n, ld, gamma, mean, rstd, dy, dy_dtype == FOLD_F32, residual, dx, dx_dtype == FOLD_F32,
-                         part, blocks == 1 ? dgamma : nullptr, blocks == 1 ? dbeta : nullptr, add};
+                         res_dtype == FOLD_F32, part, blocks == 1 ? dgamma : nullptr, blocks == 1 ? dbeta : nullptr, add};
     if (dtype == FOLD_F32) norm_rows_back<float>(a, blocks, st);
     else norm_rows_back<uint16_t>(a, blocks, st);
   }

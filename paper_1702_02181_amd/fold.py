@@ -279,7 +279,7 @@ def lib():
     L.fold_layer_norm_workspace_size.argtypes = [c_int32, c_int64, c_int32, POINTER(c_size_t)]
     L.fold_layer_norm_backward.restype = c_int32
     L.fold_layer_norm_backward.argtypes = [c_int32, c_int64, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_int32,
-                                           c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_int32, c_void_p,
+                                           c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p,
                                            c_size_t, c_void_p]
     L.fold_linear.restype = c_int32
     L.fold_linear.argtypes = [c_int32, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p,
@@ -498,11 +498,11 @@ def fold_layer_norm_workspace_size(dtype, rows, width) -> int:
     return int(n.value)
 
 
-def fold_layer_norm_backward(dtype, rows, width, x, gamma, mean, rstd, dy_dtype, dy, dx_dtype, residual, dx, dgamma, dbeta,
-                             flags, ws, ws_bytes, stream=None):
+def fold_layer_norm_backward(dtype, rows, width, x, gamma, mean, rstd, dy_dtype, dy, residual_dtype, residual, dx_dtype, dx,
+                             dgamma, dbeta, flags, ws, ws_bytes, stream=None):
     _check(lib().fold_layer_norm_backward(int(dtype), int(rows), int(width), _ptr(x), _ptr(gamma), _ptr(mean), _ptr(rstd),
-                                          int(dy_dtype), _ptr(dy), int(dx_dtype), _ptr(residual), _ptr(dx), _ptr(dgamma),
-                                          _ptr(dbeta), int(flags), _ptr(ws), int(ws_bytes), _stream(stream)))
+                                          int(dy_dtype), _ptr(dy), int(residual_dtype), _ptr(residual), int(dx_dtype),
+                                          _ptr(dx), _ptr(dgamma), _ptr(dbeta), int(flags), _ptr(ws), int(ws_bytes), _stream(stream)))
 
 
 def fold_linear(dtype, rows, in_dim, out_dim, x, W, bias, act, residual, out, pre, ws, ws_bytes, stream=None):
@@ -1037,7 +1037,7 @@ def layer_norm(x, width, gamma=None, beta=None, eps=1e-5, stats=True, out=None, 
     with _on(stream):
         out = torch.empty_like(x) if out is None else _matrix("out", out, width, x.dtype, rows)
         mean = torch.empty(rows, dtype=torch.float32, device=x.device) if stats else None
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device) if stats else None
+        rstd = torch.empty_like(mean) if stats else None
         fold_layer_norm(code, rows, width, x, gamma, beta, eps, out, mean, rstd, stream or _CURRENT)
     return out, mean, rstd
 
@@ -1045,7 +1045,7 @@ def layer_norm(x, width, gamma=None, beta=None, eps=1e-5, stats=True, out=None, 
 def layer_norm_backward(x, width, dy, mean, rstd, gamma=None, residual=None, dx=True, dgamma=True, dbeta=True, dtype=None,
                         accumulate=False, stream=None):
     """(dx, dgamma, dbeta) of fold_layer_norm_backward.  dy: of x's type or float32; residual: a gradient that goes by the
-    norm, added to dx, of dx's type.  Each of the three: True for a new tensor (dx of `dtype`, the residual's or x's type by
+    norm, added to dx, of either type.  Each of the three: True for a new tensor (dx of `dtype`, the residual's or x's type by
     default), a tensor to write, or None to leave it out.  accumulate: dgamma and dbeta are added to the tensors given."""
     import torch
     _matrix("x", x, width)
@@ -1060,11 +1060,11 @@ def layer_norm_backward(x, width, dy, mean, rstd, gamma=None, residual=None, dx=
     f32 = dict(dtype=torch.float32, device=x.device)
     with _on(stream):
         if dx is True:
-            dx = torch.empty(x.shape, dtype=dtype or (x.dtype if residual is None else residual.dtype), device=x.device)
+            dx = torch.empty_like(x, dtype=dtype or (x.dtype if residual is None else residual.dtype))
         elif dx is not None:
             _matrix("dx", dx, width, dtype, rows)
-        if residual is not None and dx is not None:
-            _matrix("residual", residual, width, dx.dtype, rows)
+        if residual is not None:
+            _matrix("residual", residual, width, None, rows)
         dgamma = torch.empty(width, **f32) if dgamma is True else dgamma
         dbeta = torch.empty(width, **f32) if dbeta is True else dbeta
         for name, t in (("dgamma", dgamma), ("dbeta", dbeta)):
@@ -1074,7 +1074,8 @@ def layer_norm_backward(x, width, dy, mean, rstd, gamma=None, residual=None, dx=
         n = _norm_ws(code, rows, width) if dgamma is not None or dbeta is not None else 0
         ws = _bytes(n, x.device)
         fold_layer_norm_backward(code, rows, width, x, gamma, mean, rstd, _code(dy.dtype), dy,
-                                 code if dx is None else _code(dx.dtype), residual, dx, dgamma, dbeta,
+                                 code if residual is None else _code(residual.dtype), residual,
+                                 code if dx is None else _code(dx.dtype), dx, dgamma, dbeta,
                                  FOLD_BLOCK_ACCUMULATE if accumulate else 0, ws, n, stream or _CURRENT)
     return dx, dgamma, dbeta
 

@@ -349,3 +349,152 @@ class VocabStep:
         dev.forward()
         self.head.logits(self.states, out=self.logits, stream=dev.stream)
         return F.token_logprobs(self.logits, self.vocab, tokens, top_k, sched=dev.sched, stream=dev.stream)
+
+
+class CrossBlock:
+    """What lets the nodes of one batch of graphs (the target: a decoder's chains, say) look at the states of another (the
+    source: an encoder's trees), graph by graph, between the target's forward pass and its head.  For target states x and
+    source states s, both in pool order:
+        y = x + Wo attention(Wq norm(x), Wk s, Wv s) + bo,   z = y + W2 act(W1 norm(y) + b1) + b2,   states = norm(z)
+    with `heads` heads (in groups on `kv_heads` of keys) and a feed-forward width of `wide`.  source[g]: the source graph
+    that target graph g reads (g by default; -1: none).  forward() and backward() are launches of the library alone."""
+
+    def __init__(self, target: DeviceRun, source: DeviceRun, heads: int, wide: int, kv_heads=None, source_of=None,
+                 activation: str = "gelu", seed: int = 0):
+        H = target.H
+        if source.H != H or source.tdtype != target.tdtype or H % heads:
+            raise ValueError("target and source have one hidden size, a multiple of the heads, and one type")
+        self.target, self.source, self.st = target, source, target.stream
+        kv = heads if kv_heads is None else kv_heads
+        d = H // heads
+        self.wk = kv * d
+        if source_of is not None:
+            source_of = torch.from_numpy(np.ascontiguousarray(source_of, np.int32)).to(target.device)
+        self.cross = F.CrossAttention(heads, d, target.graph_ptr, source.graph_ptr, F.schedule_rows(target.sched),
+                                      F.schedule_rows(source.sched), source=source_of, kv_heads=kv, dtype=target.tdtype,
+                                      stream=self.st)
+        rng = np.random.default_rng(seed)
+        self.tensors = []  # (fp32 master, bf16 copy or None, gradient)
+        f32 = dict(dtype=torch.float32, device=target.device)
+
+        def vector(n, value):
+            v = torch.full((n,), value, **f32)
+            self.tensors.append((v, None, torch.zeros_like(v)))
+            return v, self.tensors[-1][2]
+
+        def layer(n_out, n_in, act="none"):
+            W = torch.from_numpy(pad_cols(rng.standard_normal((n_out, n_in)) / np.sqrt(n_in), F.fold_row_ld(n_in))).to(target.device)
+            low = W.to(target.tdtype)
+            master = low.float() if target.bf16 else low
+            self.tensors.append((master, low if target.bf16 else None, torch.zeros_like(W)))
+            dW = self.tensors[-1][2]
+            b, db = vector(n_out, 0.0)
+            return F.Linear(low, b, n_in, act), dW, db
+        self.norms = [vector(H, 1.0) + vector(H, 0.0) for _ in range(3)]  # gamma, dgamma, beta, dbeta
+        self.q, self.kv, self.o = layer(heads * d, H), layer(2 * self.wk, H), layer(H, heads * d)
+        self.first, self.second = layer(wide, H, activation), layer(H, wide)
+
+    def _norm(self, i, x):
+        g, _, b, _ = self.norms[i]
+        return F.layer_norm(x, self.target.H, g, b, stream=self.st)
+
+    def _norm_back(self, i, x, dy, stats, residual, dtype):
+        g, dg, _, db = self.norms[i]
+        return F.layer_norm_backward(x, self.target.H, dy, *stats, g, residual=residual, dgamma=dg, dbeta=db, dtype=dtype,
+                                     stream=self.st)[0]
+
+    def _layer_back(self, layer, x, dout, pre=None, dtype=None):
+        lin, dW, db = layer
+        return lin.backward(x, dout, pre, dW=dW, dbias=db, dx_dtype=dtype or self.target.tdtype, stream=self.st)[0]
+
+    def forward(self):
+        """The block's states [target nodes, fold_row_ld(H)] of the two pools as the forward passes left them."""
+        st, N, M = self.st, self.target.N, self.source.N
+        x, s = self.target.h_pool[:N], self.source.h_pool[:M]
+        a, *stats_a = self._norm(0, x)
+        q = self.q[0].forward(a, stream=st)
+        kv = self.kv[0].forward(s, stream=st)
+        o, lse = self.cross.forward(q, kv, kv[:, self.wk:], stream=st)
+        y = self.o[0].forward(o, residual=x, stream=st)
+        b, *stats_b = self._norm(1, y)
+        f, pre = self.first[0].forward(b, pre=True, stream=st)
+        z = self.second[0].forward(f, residual=y, stream=st)
+        out, *stats_z = self._norm(2, z)
+        self.saved = x, s, a, stats_a, q, kv, o, lse, y, b, stats_b, f, pre, z, stats_z
+        return out
+
+    def backward(self, d_states):
+        """(gradient of the target's states, of the source's), fp32 in pool order: the dh_nodes of either fold_backward; the
+        parameters' gradients are written to their tensors.  d_states: fp32, of forward()'s result."""
+        x, s, a, stats_a, q, kv, o, lse, y, b, stats_b, f, pre, z, stats_z = self.saved
+        low = self.target.tdtype
+        dz = self._norm_back(2, z, d_states, stats_z, None, low)
+        df = self._layer_back(self.second, f, dz)
+        db = self._layer_back(self.first, b, df, pre)
+        dy = self._norm_back(1, y, db, stats_b, dz, low)
+        do = self._layer_back(self.o, o, dy)
+        dkv = torch.zeros_like(kv) if kv.shape[1] != 2 * self.wk else torch.empty_like(kv)
+        dq, _, _ = self.cross.backward(q, kv, kv[:, self.wk:], o, lse, do, dk=dkv, dv=dkv[:, self.wk:], stream=self.st)
+        ds = self._layer_back(self.kv, s, dkv, dtype=torch.float32)
+        da = self._layer_back(self.q, a, dq)
+        return self._norm_back(0, x, da, stats_a, dy, torch.float32), ds
+
+
+class CrossStep:
+    """One training step of two batches of graphs, the nodes of the target reading the source's through a CrossBlock and naming
+    tokens of a vocabulary: both forward passes, the block, fold_vocab_logits, fold_loss_distill against `labels` [target nodes]
+    (node order), every backward pass, fold_adam_step on all parameters, both fold_pack_update."""
+
+    def __init__(self, target: gen.Workload, source: gen.Workload, vocab: int, labels, heads: int, wide: int, kv_heads=None,
+                 source_of=None, activation: str = "gelu", seed: int = 0, lr: float = 1e-3, beta1: float = 0.9,
+                 beta2: float = 0.999, eps: float = 1e-8):
+        self.target, self.source = DeviceRun(target), DeviceRun(source)
+        self.block = CrossBlock(self.target, self.source, heads, wide, kv_heads, source_of, activation, seed)
+        dev = self.target
+        self.vocab, self.hyper, self.t = vocab, (lr, beta1, beta2, eps), 0
+        self.labels = torch.from_numpy(np.ascontiguousarray(labels, np.int32)).to(dev.device)
+        self.scale = 1.0 / max(1, int(nodes_with_target(dev.N, vocab, self.labels).sum()))
+        rng = np.random.default_rng(seed + 1)
+        W = torch.from_numpy(pad_cols(0.1 * rng.standard_normal((vocab, dev.H)), dev.ld)).to(dev.device)
+        self.W, self.dW = W.to(dev.tdtype), torch.zeros_like(W)
+        self.bias = torch.zeros(vocab, dtype=torch.float32, device=dev.device)
+        self.db = torch.zeros_like(self.bias)
+        self.head = F.VocabHead(self.W, self.bias, dev.H)
+        self.tensors = []
+        for run, w in ((self.target, target), (self.source, source)):
+            run.alloc_grads(True)
+            run.set_upstream(np.zeros_like(w.dh_roots))
+            self.tensors += trained_tensors(run, True)
+        self.tensors += self.block.tensors
+        self.tensors += [(self.W.float(), self.W, self.dW) if dev.bf16 else (self.W, None, self.dW), (self.bias, None, self.db)]
+        self.moments = [(torch.zeros_like(m), torch.zeros_like(m)) for m, _, _ in self.tensors]
+
+    def logits(self):
+        """The target nodes' logits (pool order) under the current weights."""
+        self.target.forward()
+        self.source.forward()
+        return self.head.logits(self.block.forward())
+
+    def gradients(self):
+        """Zero the accumulated gradients, both forward passes, block, head, loss, all backward passes (launches only)."""
+        self.target.zero_grads()
+        self.source.zero_grads()
+        self.target.forward()
+        self.source.forward()
+        states = self.block.forward()
+        z = self.head.logits(states)
+        self.node_loss, dz = F.distill_loss(z, self.vocab, labels=self.labels, soft_weight=0.0, hard_weight=1.0, scale=self.scale,
+                                            dlogits=z, sched=self.target.sched)
+        d_states, _, _ = self.head.backward(states, dz, dW=self.dW, dbias=self.db)
+        self.target.dh_nodes, self.source.dh_nodes = self.block.backward(d_states)
+        self.target.backward()
+        self.source.backward()
+
+    def step(self):
+        self.t += 1
+        self.gradients()
+        lr, b1, b2, eps = self.hyper
+        for (master, low, grad), (m, v) in zip(self.tensors, self.moments):
+            F.fold_adam_step(master.numel(), master, low, grad, m, v, lr, b1, b2, eps, self.t)
+        for run in (self.target, self.source):
+            run.packed.update(run.set_tensors, run.stream)

@@ -24,15 +24,16 @@ def test_layer_norm_refuses(F):  # noqa: F811
     n = F.fold_layer_norm_workspace_size(0, 4000, 100)
     assert n > 0
 
-    def back(dtype=0, rows=4000, width=100, x=x, gamma=None, mean=m, rstd=r, dyt=0, dy=d, dxt=0, res=None, dx=y, dg=v,
+    def back(dtype=0, rows=4000, width=100, x=x, gamma=None, mean=m, rstd=r, dyt=0, dy=d, rt=0, res=None, dxt=0, dx=y, dg=v,
              db=None, flags=0, ws=ws, n=n):
-        F.fold_layer_norm_backward(dtype, rows, width, x, gamma, mean, rstd, dyt, dy, dxt, res, dx, dg, db, flags, ws, n,
+        F.fold_layer_norm_backward(dtype, rows, width, x, gamma, mean, rstd, dyt, dy, rt, res, dxt, dx, dg, db, flags, ws, n,
                                    NULL_STREAM)
 
     for kw in (dict(dtype=-1), dict(rows=-1), dict(width=0), dict(dyt=1), dict(dxt=1), dict(dyt=2), dict(flags=2),
                dict(x=None), dict(mean=None), dict(rstd=None), dict(dy=None), dict(x=odd), dict(dy=odd), dict(dx=odd),
                dict(res=odd), dict(ws=odd), dict(dx=x), dict(dx=_Buf(d.at + 16)), dict(dg=y), dict(dg=m), dict(db=v),
-               dict(ws=x), dict(dtype=1, dyt=0, dxt=1, dx=d)):
+               dict(ws=x), dict(dtype=1, dyt=0, dxt=1, dx=d),
+               dict(rt=1, res=_Buf(1 << 34)), dict(dtype=1, rt=0, dxt=1, res=_Buf(1 << 34), dx=_Buf(1 << 34))):
         _refused(F, F.FOLD_E_INVALID, back, **kw)
     _refused(F, F.FOLD_E_MISMATCH, back, n=n - 1)
     _refused(F, F.FOLD_E_MISMATCH, back, ws=None)

@@ -133,6 +133,10 @@ def test_layer_norm_backward_parts():
     assert torch.equal(F.layer_norm_backward(xd, n, t, mean, rstd, vec(gamma), dx=t)[0], dx)
     r = dev(rounded(rng.standard_normal((M, n)), "bf16"), "bf16")
     want = F.layer_norm_backward(xd, n, dy, mean, rstd, vec(gamma), residual=r)[0]
+    full = F.layer_norm_backward(xd, n, dy, mean, rstd, vec(gamma), residual=r, dtype=torch.float32)[0]
+    assert full.dtype == torch.float32 and torch.equal(full.bfloat16(), want)  # one rounding, at the end
+    other = F.layer_norm_backward(xd, n, dy, mean, rstd, vec(gamma), residual=r.float(), dtype=torch.bfloat16)[0]
+    assert torch.equal(other, want)
     assert torch.equal(F.layer_norm_backward(xd, n, dy, mean, rstd, vec(gamma), residual=r, dx=r)[0], want)
 
 
