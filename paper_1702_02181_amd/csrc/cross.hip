@@ -274,10 +274,10 @@ struct Args {
 };
 __device__ __forceinline__ int row_of(const int* list, int entry) { return list[entry]; }
 
-// the workgroup's tile, with its head and its slot among all heads'
+// a workgroup's tile, with its head and its slot among all heads'
 template <class Tile>
-__device__ __forceinline__ Tile tile_of_head(const Tile* tiles, const Args& a) {
-  Tile t = tiles[blockIdx.x];
+__device__ __forceinline__ Tile tile_of_head(const Tile* tiles, unsigned index, const Args& a) {
+  Tile t = tiles[index];
   t.kv_head = blockIdx.y;
   if (t.slot >= 0) t.slot += blockIdx.y * a.slots;
   return t;
@@ -402,7 +402,7 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
   constexpr int IMAGES = NW == 4 ? 4 * image_bytes<T, DP>() : 0;
   constexpr int TILES = 2 * BUF * (NW == 1 ? 4 : 1), LDS = TILES > IMAGES ? TILES : IMAGES;
   __shared__ __attribute__((aligned(16))) char lds[LDS > MEET ? LDS : MEET];
-  const QTile t = tile_of_head(tiles, a);
+  const QTile t = tile_of_head(tiles, blockIdx.x, a);
   if (t.rows == 0) return;
   const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
   const T* k = static_cast<const T*>(a.k) + t.kv_head * a.d;
@@ -560,7 +560,7 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
 template <typename T, int DP, int ROWS, bool SOFTMAX, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_cross_join(const QTile* tiles, Args a) {
   constexpr int DB = DP / 32;
-  const QTile t = tile_of_head(tiles, a);
+  const QTile t = tile_of_head(tiles, blockIdx.x, a);
   const int c0 = (threadIdx.x & 7) * 4;
   T* out = static_cast<T*>(a.out);
   for (int r = threadIdx.x >> 3; r < t.rows; r += kThreads / 8) {
@@ -626,13 +626,24 @@ __global__ __launch_bounds__(kThreads) void k_cross_delta(const T* out, int64_t 
   }
 }
 
+// Whether a lane keeps its fragments of v in LDS of its own: where registers are short (the widest fp32 heads, and rows of 128
+// bytes, whose three waves a SIMD have 168 each).
+template <typename T, int DP>
+constexpr bool keep_values() { return DP * sizeof(T) > 384 || DP * sizeof(T) == 128; }
+template <typename T, int DP, int TK>
+struct BackLds {
+  static constexpr int TILES = 4 * tile_bytes<TK, T, DP>(), IMAGES = 4 * image_bytes<T, DP>();
+  __attribute__((aligned(16))) char tiles[TILES > IMAGES ? TILES : IMAGES];
+  __attribute__((aligned(16))) float stats[2][2][TK];  // [buffer][lse in base 2, delta][row]
+  uint4 kept[keep_values<T, DP>() ? 4 * (DP * sizeof(T) / 32) * 64 : 1];
+};
+
 // The queries' gradient: as the forward with four waves, p recomputed from lse, dq^T += k^T ds^T.
 template <typename T, int DP, int TK, bool VEC>
-__global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cross_dq(const QTile* tiles, Args a) {
+__device__ __forceinline__ void queries_back(const QTile* tiles, unsigned index, const Args& a, char* lds) {
   constexpr int U = DP * (int)sizeof(T) / 16, NS = U / 2, DB = DP / 32, KB = TK / 32, TB = tile_bytes<TK, T, DP>();
-  constexpr int E = 16 / (int)sizeof(T), BUF = 2 * TB, IMAGES = 4 * image_bytes<T, DP>();
-  __shared__ __attribute__((aligned(16))) char lds[2 * BUF > IMAGES ? 2 * BUF : IMAGES];
-  const QTile t = tile_of_head(tiles, a);
+  constexpr int E = 16 / (int)sizeof(T), BUF = 2 * TB;
+  const QTile t = tile_of_head(tiles, index, a);
   if (t.rows == 0) return;
   const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
   const T* k = static_cast<const T*>(a.k) + t.kv_head * a.d;
@@ -687,7 +698,7 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
     __builtin_amdgcn_sched_barrier(0);
     if (!active) continue;
     const char *kt = lds + (at & 1) * BUF, *vt = kt + TB;
-#pragma unroll
+#pragma unroll 1
     for (int kb = 0; kb < KB; ++kb) {
       f32x16 s, dp;
 #pragma unroll
@@ -733,16 +744,15 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
 // The gradient of keys and values: a wave holds 32 keys on its lanes, k and v in registers, and walks the row tiles of the
 // sequences that read them: dv^T += do^T p, dk^T += q^T ds.
 template <typename T, int DP, int RQ, bool VEC>
-__global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 3)) void k_cross_dkv(const KTile* tiles,
-                                                                                       const RTile* runs, Args a) {
+__device__ __forceinline__ void keys_back(const KTile* tiles, const RTile* runs, unsigned index, const Args& a,
+                                          BackLds<T, DP, RQ>& mem) {
   constexpr int U = DP * (int)sizeof(T) / 16, NS = U / 2, DB = DP / 32, QB = RQ / 32, TB = tile_bytes<RQ, T, DP>();
-  constexpr int E = 16 / (int)sizeof(T), BUF = 2 * TB, IMAGES = 4 * image_bytes<T, DP>();
-  __shared__ __attribute__((aligned(16))) char lds[2 * BUF > IMAGES ? 2 * BUF : IMAGES];
-  __shared__ __attribute__((aligned(16))) float stats[2][2][RQ];  // [buffer][lse in base 2, delta][row]
-  // the widest fp32 heads leave no registers for v's fragments: every lane keeps its own in LDS
-  constexpr bool KEEP = DP * sizeof(T) > 384 || DP * sizeof(T) == 128;
-  __shared__ uint4 kept[KEEP ? 4 * NS * 64 : 1];
-  const KTile t = tile_of_head(tiles, a);
+  constexpr int E = 16 / (int)sizeof(T), BUF = 2 * TB;
+  constexpr bool KEEP = keep_values<T, DP>();
+  char* lds = mem.tiles;
+  auto& stats = mem.stats;
+  auto& kept = mem.kept;
+  const KTile t = tile_of_head(tiles, index, a);
   if (t.keys == 0) return;
   const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
   const int first = 32 * wave, mykey = first + l32;
@@ -918,10 +928,20 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 3)) void k_cr
   if (a.out2) store_image<T, DP, VEC>(dv, 1.f, a.d, img, lane, place(a.out2, a.ldo2));
 }
 
+// Both gradients in one launch: `nkeys` workgroups for the keys', the rest for the queries'.
+template <typename T, int DP, int TK, bool VEC>
+__global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 3)) void k_cross_back(const KTile* keys, const RTile* runs,
+                                                                                        unsigned nkeys, Args ka,
+                                                                                        const QTile* rows, Args qa) {
+  __shared__ BackLds<T, DP, TK> lds;
+  if (blockIdx.x < nkeys) keys_back<T, DP, TK, VEC>(keys, runs, blockIdx.x, ka, lds);
+  else queries_back<T, DP, TK, VEC>(rows, blockIdx.x - nkeys, qa, lds.tiles);
+}
+
 // The pieces of a tile of keys summed in their order: eight threads a key.
 template <typename T, int DP, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_cross_join_keys(const KTile* tiles, Args a) {
-  const KTile t = tile_of_head(tiles, a);
+  const KTile t = tile_of_head(tiles, blockIdx.x, a);
   const int c0 = (threadIdx.x & 7) * 4;
   for (int key = threadIdx.x >> 3; key < t.keys; key += kThreads / 8) {
     const int ke = t.k_begin + key, krow = row_of(a.k_row, ke);
@@ -1000,12 +1020,12 @@ size_t cross_forward_bytes(const Cross& c) {
   return (size_t)c.fslots * c.kv_heads * (c.few ? kCrossFew : kCrossRows) * (cross_padded(c.head_dim) + 2) * sizeof(float);
 }
 static size_t delta_floats(const Cross& c) { return ((size_t)c.query_rows * c.heads + 3) / 4 * 4; }
+static size_t dq_floats(const Cross& c) {
+  return (size_t)c.bslots * c.kv_heads * kCrossRows * (cross_padded(c.head_dim) + 2);
+}
 size_t cross_backward_bytes(const Cross& c) {
-  const int dp = cross_padded(c.head_dim);
-  // the queries' and the keys' pieces follow each other on the stream: one region serves both
-  const size_t dq = (size_t)c.bslots * c.kv_heads * kCrossRows * (dp + 2),
-               dk = (size_t)c.kslots * c.kv_heads * kCrossKeys * 2 * dp;
-  return (delta_floats(c) + std::max(dq, dk)) * sizeof(float);
+  const size_t dk = (size_t)c.kslots * c.kv_heads * kCrossKeys * 2 * cross_padded(c.head_dim);
+  return (delta_floats(c) + dq_floats(c) + dk) * sizeof(float);
 }
 
 void launch_cross(const Cross& c, CrossMat q, CrossMat k, CrossMat v, const uint8_t* mask, float scale, void* out,
@@ -1068,35 +1088,30 @@ void launch_cross_backward(const Cross& c, CrossMat q, CrossMat k, CrossMat v, c
                            static_cast<const T*>(out.p), out.ld, static_cast<const T*>(dout.p), dout.ld, c.q_row, n, c.heads,
                            d, delta);
       }
-      if (dq && c.nback > 0) {
-        Args b = a;
-        b.out = dq;
-        b.slots = c.bslots;
-        b.ldo = lddq;
-        {
-          ProfScope prof("cross_dq", st);
-          hipLaunchKernelGGL((k_cross_dq<T, DP, TK, VEC>), dim3(c.nback, c.kv_heads), dim3(kThreads), 0, st, c.back, b);
-        }
-        if (c.nbjoin > 0) {
-          ProfScope prof("cross_dq_join", st);
-          hipLaunchKernelGGL((k_cross_join<T, DP, kCrossRows, false, VEC>), dim3(c.nbjoin, c.kv_heads), dim3(kThreads), 0, st, c.bjoin, b);
-        }
+      const bool rows = dq && c.nback > 0, keys = (dk || dv) && c.nkeys > 0;
+      Args qa = a, ka = a;
+      qa.out = dq;
+      qa.slots = c.bslots;
+      qa.ldo = lddq;
+      ka.out = dk;
+      ka.slots = c.kslots;
+      ka.ldo = lddk;
+      ka.out2 = dv;
+      ka.ldo2 = lddv;
+      ka.part = a.part + dq_floats(c);
+      const unsigned nk = keys ? c.nkeys : 0, nq = rows ? c.nback : 0;
+      if (nk + nq > 0) {
+        ProfScope prof("cross_back", st);
+        hipLaunchKernelGGL((k_cross_back<T, DP, TK, VEC>), dim3(nk + nq, c.kv_heads), dim3(kThreads), 0, st, c.keys, c.rows, nk,
+                           ka, c.back, qa);
       }
-      if ((dk || dv) && c.nkeys > 0) {
-        Args b = a;
-        b.out = dk;
-        b.slots = c.kslots;
-        b.ldo = lddk;
-        b.out2 = dv;
-        b.ldo2 = lddv;
-        {
-          ProfScope prof("cross_dkv", st);
-          hipLaunchKernelGGL((k_cross_dkv<T, DP, TK, VEC>), dim3(c.nkeys, c.kv_heads), dim3(kThreads), 0, st, c.keys, c.rows, b);
-        }
-        if (c.nkjoin > 0) {
-          ProfScope prof("cross_dkv_join", st);
-          hipLaunchKernelGGL((k_cross_join_keys<T, DP, VEC>), dim3(c.nkjoin, c.kv_heads), dim3(kThreads), 0, st, c.kjoin, b);
-        }
+      if (rows && c.nbjoin > 0) {
+        ProfScope prof("cross_dq_join", st);
+        hipLaunchKernelGGL((k_cross_join<T, DP, kCrossRows, false, VEC>), dim3(c.nbjoin, c.kv_heads), dim3(kThreads), 0, st, c.bjoin, qa);
+      }
+      if (keys && c.nkjoin > 0) {
+        ProfScope prof("cross_dkv_join", st);
+        hipLaunchKernelGGL((k_cross_join_keys<T, DP, VEC>), dim3(c.nkjoin, c.kv_heads), dim3(kThreads), 0, st, c.kjoin, ka);
       }
     };
     if (vec) go(std::true_type());
