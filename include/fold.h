@@ -673,7 +673,7 @@ int32_t fold_token_logprobs(const fold_sched* sched, int32_t dtype, int64_t rows
  *   dgamma, dbeta  device [width] fp32, or NULL; written, or added to with
  *             FOLD_BLOCK_ACCUMULATE
  *   ws        device workspace of >= fold_layer_norm_workspace_size bytes (for
- *             dgamma or dbeta)
+ *             dgamma or dbeta; may be NULL where that is 0)
  *
  * fold_linear: out = act(x W^T + bias) + residual.
  *   x         device [rows, fold_row_ld(in_dim)];  in_dim, out_dim 1 .. 16384
@@ -749,8 +749,9 @@ int32_t fold_linear_backward(int32_t dtype, int64_t rows, int32_t in_dim, int32_
  *   source      device [num_seqs]: the key sequence that a query sequence reads
  *               (several may read one), -1: none; NULL: b reads b
  * The lists are copied.  FOLD_E_INVALID for sizes out of range (heads to 1,024,
- * head_dim to 128, heads / kv_heads to 256, queries times heads below 2^31) and
- * for malformed lists, rows out of range or listed twice.
+ * head_dim to 128, heads / kv_heads to 256, queries times heads below 2^31, 2^24
+ * workgroups of a head) and for malformed lists, rows out of range or listed
+ * twice.
  * fold_cross_free waits as fold_sched_free does. */
 typedef struct fold_cross fold_cross;
 typedef struct {

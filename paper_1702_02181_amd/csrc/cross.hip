@@ -556,51 +556,70 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void k_cr
 }
 
 // The pieces of a tile joined, in their order: SOFTMAX, each with its m and l, or plain sums (times the scale).  Eight threads
-// a row.
+// a row, 32 rows a workgroup, four pieces in flight.
 template <typename T, int DP, int ROWS, bool SOFTMAX, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_cross_join(const QTile* tiles, Args a) {
-  constexpr int DB = DP / 32;
-  const QTile t = tile_of_head(tiles, blockIdx.x, a);
-  const int c0 = (threadIdx.x & 7) * 4;
+  constexpr int DB = DP / 32, SF = slot_floats<DP>(ROWS), BLOCKS = ROWS / 32, F = 4;
+  const QTile t = tile_of_head(tiles, blockIdx.x / BLOCKS, a);
+  const int c0 = (threadIdx.x & 7) * 4, r = blockIdx.x % BLOCKS * 32 + (threadIdx.x >> 3);
+  if (r >= t.rows) return;
   T* out = static_cast<T*>(a.out);
-  for (int r = threadIdx.x >> 3; r < t.rows; r += kThreads / 8) {
-    const float* p = a.part + (size_t)t.slot * slot_floats<DP>(ROWS);
-    float m = -INFINITY, l = 0.f;
-    if (SOFTMAX)
-      for (int i = 0; i < t.pieces; ++i) m = fmaxf(m, p[(size_t)i * slot_floats<DP>(ROWS) + ROWS * DP + r]);
-    float x[DB][4];
+  const float* p = a.part + (size_t)t.slot * SF;
+  float m = -INFINITY, l = 0.f;
+  if (SOFTMAX)
+    for (int i0 = 0; i0 < t.pieces; i0 += 2 * F) {
+      float mi[2 * F];
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+      for (int u = 0; u < 2 * F; ++u) mi[u] = p[(size_t)min(i0 + u, t.pieces - 1) * SF + ROWS * DP + r];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[db][e] = 0.f;
-    for (int i = 0; i < t.pieces; ++i, p += slot_floats<DP>(ROWS)) {
+      for (int u = 0; u < 2 * F; ++u) m = fmaxf(m, mi[u]);
+    }
+  float x[DB][4];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[db][e] = 0.f;
+  for (int i0 = 0; i0 < t.pieces; i0 += F) {
+    float mi[F], li[F];
+    float4 y[F][DB];
+#pragma unroll
+    for (int u = 0; u < F; ++u) {
+      const float* at = p + (size_t)min(i0 + u, t.pieces - 1) * SF;
+      if (SOFTMAX) {
+        mi[u] = at[ROWS * DP + r];
+        li[u] = at[ROWS * (DP + 1) + r];
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) y[u][db] = *reinterpret_cast<const float4*>(at + r * DP + 32 * db + c0);
+    }
+#pragma unroll
+    for (int u = 0; u < F; ++u) {
+      if (i0 + u >= t.pieces) break;
       float f = 1.f;
       if (SOFTMAX) {
-        const float mi = p[ROWS * DP + r], li = p[ROWS * (DP + 1) + r];
-        f = mi == -INFINITY ? (li == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(mi - m);
-        l += f * li;
+        f = mi[u] == -INFINITY ? (li[u] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(mi[u] - m);
+        l += f * li[u];
       }
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const float4 y = *reinterpret_cast<const float4*>(p + r * DP + 32 * db + c0);
-        x[db][0] += f * y.x;
-        x[db][1] += f * y.y;
-        x[db][2] += f * y.z;
-        x[db][3] += f * y.w;
+        x[db][0] += f * y[u][db].x;
+        x[db][1] += f * y[u][db].y;
+        x[db][2] += f * y[u][db].z;
+        x[db][3] += f * y[u][db].w;
       }
     }
-    const Virtual v(a, t.entry, t.head0, t.kv_head, r);
-    const int row = row_of(a.q_row, v.entry);
-    const float inv = !SOFTMAX ? a.scale : l > 0.f || l != l ? 1.f / l : 0.f;
-#pragma unroll
-    for (int db = 0; db < DB; ++db) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[db][e] *= inv;
-      store4<T, VEC>(out + (int64_t)row * a.ldo + v.head * a.d, x[db], 32 * db + c0, a.d);
-    }
-    if (SOFTMAX && c0 == 0 && a.lse)
-      a.lse[(int64_t)row * a.heads + v.head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
   }
+  const Virtual v(a, t.entry, t.head0, t.kv_head, r);
+  const int row = row_of(a.q_row, v.entry);
+  const float inv = !SOFTMAX ? a.scale : l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[db][e] *= inv;
+    store4<T, VEC>(out + (int64_t)row * a.ldo + v.head * a.d, x[db], 32 * db + c0, a.d);
+  }
+  if (SOFTMAX && c0 == 0 && a.lse)
+    a.lse[(int64_t)row * a.heads + v.head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // ---- backward ---------------------------------------------------------------------------------------------------------
@@ -698,7 +717,7 @@ __device__ __forceinline__ void queries_back(const QTile* tiles, unsigned index,
     __builtin_amdgcn_sched_barrier(0);
     if (!active) continue;
     const char *kt = lds + (at & 1) * BUF, *vt = kt + TB;
-#pragma unroll 1
+#pragma unroll(DP * sizeof(T) == 128 ? 1 : KB)  // (168 registers a lane)
     for (int kb = 0; kb < KB; ++kb) {
       f32x16 s, dp;
 #pragma unroll
@@ -938,34 +957,38 @@ __global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 3)) void k_cr
   else queries_back<T, DP, TK, VEC>(rows, blockIdx.x - nkeys, qa, lds.tiles);
 }
 
-// The pieces of a tile of keys summed in their order: eight threads a key.
+// The pieces of a tile of keys summed in their order: eight threads a key, 32 keys a workgroup, eight pieces in flight; the
+// launch's third dimension is dk and dv.
 template <typename T, int DP, bool VEC>
 __global__ __launch_bounds__(kThreads) void k_cross_join_keys(const KTile* tiles, Args a) {
-  const KTile t = tile_of_head(tiles, blockIdx.x, a);
-  const int c0 = (threadIdx.x & 7) * 4;
-  for (int key = threadIdx.x >> 3; key < t.keys; key += kThreads / 8) {
-    const int ke = t.k_begin + key, krow = row_of(a.k_row, ke);
-    const bool counts = !a.mask || a.mask[ke] != 0;
+  constexpr int BLOCKS = kCrossKeys / 32, F = 8;
+  const KTile t = tile_of_head(tiles, blockIdx.x / BLOCKS, a);
+  const int c0 = (threadIdx.x & 7) * 4, key = blockIdx.x % BLOCKS * 32 + (threadIdx.x >> 3), which = blockIdx.z;
+  T* to = static_cast<T*>(which ? a.out2 : a.out);
+  if (key >= t.keys || !to) return;
+  const int ke = t.k_begin + key, krow = row_of(a.k_row, ke);
+  const bool counts = !a.mask || a.mask[ke] != 0;
+  to += (int64_t)krow * (which ? a.ldo2 : a.ldo) + t.kv_head * a.d;
+  const float* p = a.part + ((size_t)t.slot * kCrossKeys + key) * 2 * DP + which * DP;
+  for (int d0 = c0; d0 < DP; d0 += 32) {
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < t.pieces; i0 += F) {
+      float4 y[F];
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      T* to = static_cast<T*>(which ? a.out2 : a.out);
-      if (!to) continue;
-      to += (int64_t)krow * (which ? a.ldo2 : a.ldo) + t.kv_head * a.d;
-      for (int d0 = c0; d0 < DP; d0 += 32) {
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int i = 0; i < t.pieces; ++i) {
-          const float4 y = *reinterpret_cast<const float4*>(a.part + ((size_t)(t.slot + i) * kCrossKeys + key) * 2 * DP +
-                                                            which * DP + d0);
-          x[0] += y.x;
-          x[1] += y.y;
-          x[2] += y.z;
-          x[3] += y.w;
-        }
+      for (int u = 0; u < F; ++u)
+        y[u] = *reinterpret_cast<const float4*>(p + (size_t)min(i0 + u, t.pieces - 1) * kCrossKeys * 2 * DP + d0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = counts ? x[e] * (which ? 1.f : a.scale) : 0.f;
-        store4<T, VEC>(to, x, d0, a.d);
+      for (int u = 0; u < F; ++u) {
+        if (i0 + u >= t.pieces) break;
+        x[0] += y[u].x;
+        x[1] += y[u].y;
+        x[2] += y[u].z;
+        x[3] += y[u].w;
       }
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = counts ? x[e] * (which ? 1.f : a.scale) : 0.f;
+    store4<T, VEC>(to, x, d0, a.d);
   }
 }
 
@@ -1055,7 +1078,7 @@ void launch_cross(const Cross& c, CrossMat q, CrossMat k, CrossMat v, const uint
       if (c.few)
         hipLaunchKernelGGL((k_cross_join<T, DP, kCrossFew, true, VEC>), dim3(c.nfjoin, c.kv_heads), dim3(kThreads), 0, st, c.fjoin, a);
       else
-        hipLaunchKernelGGL((k_cross_join<T, DP, kCrossRows, true, VEC>), dim3(c.nfjoin, c.kv_heads), dim3(kThreads), 0, st, c.fjoin, a);
+        hipLaunchKernelGGL((k_cross_join<T, DP, kCrossRows, true, VEC>), dim3(c.nfjoin * (kCrossRows / 32), c.kv_heads), dim3(kThreads), 0, st, c.fjoin, a);
     };
     if (vec) go(std::true_type());
     else go(std::false_type());
@@ -1107,11 +1130,11 @@ void launch_cross_backward(const Cross& c, CrossMat q, CrossMat k, CrossMat v, c
       }
       if (rows && c.nbjoin > 0) {
         ProfScope prof("cross_dq_join", st);
-        hipLaunchKernelGGL((k_cross_join<T, DP, kCrossRows, false, VEC>), dim3(c.nbjoin, c.kv_heads), dim3(kThreads), 0, st, c.bjoin, qa);
+        hipLaunchKernelGGL((k_cross_join<T, DP, kCrossRows, false, VEC>), dim3(c.nbjoin * (kCrossRows / 32), c.kv_heads), dim3(kThreads), 0, st, c.bjoin, qa);
       }
       if (keys && c.nkjoin > 0) {
         ProfScope prof("cross_dkv_join", st);
-        hipLaunchKernelGGL((k_cross_join_keys<T, DP, VEC>), dim3(c.nkjoin, c.kv_heads), dim3(kThreads), 0, st, c.kjoin, ka);
+        hipLaunchKernelGGL((k_cross_join_keys<T, DP, VEC>), dim3(c.nkjoin * (kCrossKeys / 32), c.kv_heads, 2), dim3(kThreads), 0, st, c.kjoin, ka);
       }
     };
     if (vec) go(std::true_type());

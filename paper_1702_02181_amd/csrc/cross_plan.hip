@@ -102,21 +102,26 @@ struct Spread {
   }
 };
 
-constexpr int kMinPiece = 256;  // keys (or rows) of a piece
+// Keys (or rows) of a piece at least.  A piece costs its partial results' way through memory and a share of the join, a tile
+// of 32 x 32 scores sixteen times as much on the matrix cores in fp32 as in bf16.  Gradient of 8 sequences of 428 .. 737 nodes
+// against 358 .. 449, two heads of 128 in bf16: 50 us with 256, 67 with 128; of 18 of 172 .. 260 against 12 .. 33, two heads of
+// 75 in fp32: 94 with 256, 58 with 128; of 27 sources of 216 .. 230 read by five of 361 .. 802 each, a head of 16 in fp32: 52
+// with 256, 54 with 128, 63 with 64.
+int min_piece(int dtype) { return dtype == FOLD_BF16 ? 256 : 128; }
 constexpr int kWanted = 512;    // workgroups that fill the chip: two a compute unit
 
 // The length of pieces: what spreads the work evenly over the wanted workgroups, where there are fewer tiles than that; with
 // more tiles only one that is far longer than the others is cut.
-int64_t piece_of(int64_t tiles, int64_t work, int unit) {
-  if (tiles == 0) return kMinPiece;
-  int64_t len = std::max<int64_t>(kMinPiece, (work + kWanted - 1) / kWanted);
+int64_t piece_of(int64_t tiles, int64_t work, int unit, int least) {
+  if (tiles == 0) return least;
+  int64_t len = std::max<int64_t>(least, (work + kWanted - 1) / kWanted);
   if (tiles >= kWanted) len = std::max<int64_t>(len, 4 * (work / tiles));
   return (len + unit - 1) / unit * unit;
 }
 
 struct Lists {
   const std::vector<int32_t>&qp, &kp, &src;
-  int G, kv_heads;
+  int G, kv_heads, least;
   std::vector<std::vector<int>> readers;  // by source: its query sequences; the last entry: those without a source
 };
 
@@ -132,7 +137,7 @@ void query_tiles(const Lists& l, int height, std::vector<QTile>* out, std::vecto
       tiles += n;
       work += n * keys_of(e);
     }
-  const int64_t piece = piece_of(tiles, work, 64);
+  const int64_t piece = piece_of(tiles, work, 64, l.least);
   Spread<QTile> s;
   *slots = 0;
   for (int e = 0; e <= sources; ++e) {
@@ -180,7 +185,7 @@ void key_tiles(const Lists& l, int height, std::vector<KTile>* out, std::vector<
     tiles += n;
     work += n * runs[e].size() * height;
   }
-  const int64_t piece = piece_of(tiles, work, height) / height;  // row tiles
+  const int64_t piece = piece_of(tiles, work, height, l.least) / height;  // row tiles
   Spread<KTile> s;
   *slots = 0;
   for (int e = 0; e < sources; ++e) {
@@ -290,7 +295,7 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
   if (!check_ptr(kp, b->num_keys)) return api_fail(FOLD_E_INVALID, who + ": key_ptr malformed");
   if (error & 5) return api_fail(FOLD_E_INVALID, who + (error & 1 ? ": query_row" : ": key_row") + " out of range");
   if (error & 10) return api_fail(FOLD_E_INVALID, who + (error & 2 ? ": query_row" : ": key_row") + " lists a row twice");
-  Lists l{qp, kp, src, b->heads / b->kv_heads, b->kv_heads, {}};
+  Lists l{qp, kp, src, b->heads / b->kv_heads, b->kv_heads, min_piece(b->dtype), {}};
   l.readers.resize((size_t)b->num_sources + 1);
   for (int s = 0; s < b->num_seqs; ++s) {
     const int e = b->source ? src[s] : s;
@@ -317,13 +322,16 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
   c.query_rows = b->num_query_rows;
   c.key_rows = b->num_key_rows;
   // tiles of 32 rows where those of 128 would be mostly empty
-  int64_t tall = 0, low = 0;
+  int64_t tall = 0, low = 0, least_tiles = 0;
   for (int s = 0; s < b->num_seqs; ++s) {
     const int64_t n = (int64_t)(qp[s + 1] - qp[s]) * l.G, e = b->source ? src[s] : s;
     const int64_t keys = e < 0 ? 0 : kp[e + 1] - kp[e];
+    least_tiles += (n + kCrossRows - 1) / kCrossRows;
     tall += (n + kCrossRows - 1) / kCrossRows * keys;
     low += (n + kCrossFew - 1) / kCrossFew * keys;
   }
+  if (least_tiles >= kMaxTiles)
+    return api_fail(FOLD_E_INVALID, who + ": too many tiles for one launch (sequences and rows)");
   c.few = low < 2 * tall && cross_padded(c.head_dim) * (c.dtype == FOLD_BF16 ? 2 : 4) <= kCrossFewBytes;
   std::vector<QTile> fwd, fjoin, back, bjoin;
   std::vector<KTile> keys, kjoin;
@@ -332,7 +340,7 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
   query_tiles(l, kCrossRows, &back, &bjoin, &c.bslots);
   key_tiles(l, c.dtype == FOLD_BF16 ? 64 : 32, &keys, &kjoin, &rows, &c.kslots);
 
-  if ((int64_t)std::max({fwd.size(), back.size(), keys.size()}) >= kMaxTiles)
+  if ((int64_t)std::max({fwd.size(), back.size() + keys.size(), 4 * fjoin.size(), 4 * bjoin.size(), 4 * kjoin.size()}) >= kMaxTiles)
     return api_fail(FOLD_E_INVALID, who + ": too many tiles for one launch (sequences and rows)");
   // one image of all the lists, uploaded whole; the row numbers behind it are copied or made on the device
   std::vector<char> image;
