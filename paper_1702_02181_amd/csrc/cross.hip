@@ -153,18 +153,42 @@ __device__ __forceinline__ void across_mma(const char* tile, int k0, const Probs
   }
 }
 
-// 16 bytes of a row from element e0 (d elements are there), zero past its end
+// 16 bytes at an address that is a multiple of an element's size alone (global memory takes them at any)
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Loose {
+  uint32_t w[4];
+};
+// 16 bytes of a row from element e0 (d elements are there), zero past its end.  Without whole units the last one is taken from
+// the row's last 16 bytes and moved down: element by element, 61 chains of 615 rows against 65 keys, 4 heads of 50 in fp32,
+// their gradients took 298 us.
 template <typename T, bool VEC>
 __device__ __forceinline__ uint4 row_unit(const T* row, int e0, int d) {
   constexpr int E = 16 / (int)sizeof(T);
   uint4 v = make_uint4(0, 0, 0, 0);
+  if (e0 >= d) return v;
   if constexpr (VEC) {
-    if (e0 < d) v = *reinterpret_cast<const uint4*>(row + e0);
+    v = *reinterpret_cast<const uint4*>(row + e0);
   } else {
-    T e[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) e[i] = e0 + i < d ? row[e0 + i] : T(0);
-    v = *reinterpret_cast<const uint4*>(e);
+    uint64_t lo = 0, hi = 0;
+    int by = 0;
+    if (d >= E) {
+      const int at = min(e0, d - E), bits = (e0 - at) * (int)sizeof(T) * 8;  // 0 .. 112
+      const Loose<T> u = *reinterpret_cast<const Loose<T>*>(row + at);
+      lo = (uint64_t)u.w[1] << 32 | u.w[0];
+      hi = (uint64_t)u.w[3] << 32 | u.w[2];
+      if (bits >= 64) lo = hi, hi = 0;
+      by = bits & 63;
+    } else {  // heads of less than 16 bytes: their only unit
+#pragma unroll 1
+      for (int e = d - 1; e >= 0; --e) {
+        constexpr int B = 8 * (int)sizeof(T);
+        hi = hi << B | lo >> (64 - B);
+        lo = lo << B | (B == 16 ? reinterpret_cast<const uint16_t*>(row)[e] : __float_as_uint((float)row[e]));
+      }
+    }
+    lo = lo >> by | hi << 1 << (63 - by);
+    hi >>= by;
+    v = make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
   }
   return v;
 }
@@ -247,6 +271,8 @@ __device__ __forceinline__ void store_image(const f32x16 (&acc)[DP / 32], float 
     if (!to || e0 >= d) continue;
     if constexpr (VEC) {
       *reinterpret_cast<uint4*>(to + e0) = v;
+    } else if (e0 + E <= d) {
+      *reinterpret_cast<Loose<T>*>(to + e0) = Loose<T>{{v.x, v.y, v.z, v.w}};
     } else {
       const T* e = reinterpret_cast<const T*>(&v);
 #pragma unroll
