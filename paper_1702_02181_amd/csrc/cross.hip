@@ -671,10 +671,12 @@ __global__ __launch_bounds__(kThreads) void k_cross_delta(const T* out, int64_t 
   }
 }
 
+template <typename T, int DP>
+constexpr int waves_back() { return DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 192 || (sizeof(T) == 4 && DP == 64) ? 2 : 1; }
 // Whether a lane keeps its fragments of v in LDS of its own: where registers are short (the widest fp32 heads, and rows of 128
 // bytes, whose three waves a SIMD have 168 each).
 template <typename T, int DP>
-constexpr bool keep_values() { return DP * sizeof(T) > 384 || DP * sizeof(T) == 128; }
+constexpr bool keep_values() { return DP * sizeof(T) > 384 || DP * sizeof(T) == 128 || waves_back<T, DP>() == 2; }
 template <typename T, int DP, int TK>
 struct BackLds {
   static constexpr int TILES = 4 * tile_bytes<TK, T, DP>(), IMAGES = 4 * image_bytes<T, DP>();
@@ -975,7 +977,7 @@ __device__ __forceinline__ void keys_back(const KTile* tiles, const RTile* runs,
 
 // Both gradients in one launch: `nkeys` workgroups for the keys', the rest for the queries'.
 template <typename T, int DP, int TK, bool VEC>
-__global__ __launch_bounds__(kThreads, (DP * sizeof(T) > 128 ? 1 : 3)) void k_cross_back(const KTile* keys, const RTile* runs,
+__global__ __launch_bounds__(kThreads, (waves_back<T, DP>())) void k_cross_back(const KTile* keys, const RTile* runs,
                                                                                         unsigned nkeys, Args ka,
                                                                                         const QTile* rows, Args qa) {
   __shared__ BackLds<T, DP, TK> lds;
