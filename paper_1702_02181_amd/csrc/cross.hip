@@ -685,6 +685,121 @@ struct BackLds {
   uint4 kept[keep_values<T, DP>() ? 4 * (DP * sizeof(T) / 32) * 64 : 1];
 };
 
+// The queries' gradient of a tile of up to 32 rows: all four waves hold them, each takes 32 of 128 keys that lie in LDS, and
+// their sums meet at the end.  With the rows in one wave the other three only load: 216 x 5 sequences of 5 .. 14 rows against
+// 1,628 .. 2,262 keys, 5 heads of 50 in fp32, all gradients: 1,285 us, so 930.
+template <typename T, int DP, bool VEC>
+__device__ __forceinline__ void queries_back_few(const QTile& t, const Args& a, char* lds) {
+  constexpr int U = DP * (int)sizeof(T) / 16, NS = U / 2, DB = DP / 32, KEYS = 128, TB = tile_bytes<KEYS, T, DP>();
+  constexpr int E = 16 / (int)sizeof(T);
+  const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
+  const T* k = static_cast<const T*>(a.k) + t.kv_head * a.d;
+  const T* v = static_cast<const T*>(a.v) + t.kv_head * a.d;
+  uint4 qf[NS], df[NS];
+  float ref, delta;
+  {
+    const Virtual vr(a, t.entry, t.head0, t.kv_head, min(l32, t.rows - 1));
+    const int qrow = row_of(a.q_row, vr.entry);
+    const T* q = row_at(static_cast<const T*>(a.q), qrow, a.ldq) + vr.head * a.d;
+    const T* g = row_at(static_cast<const T*>(a.dout), qrow, a.lddo) + vr.head * a.d;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      qf[s] = row_unit<T, VEC>(q, (2 * s + h) * E, a.d);
+      df[s] = row_unit<T, VEC>(g, (2 * s + h) * E, a.d);
+    }
+    const int64_t stat = (int64_t)qrow * a.heads + vr.head;
+    delta = a.delta[stat];
+    const float lse = a.lse[stat];
+    ref = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  }
+  f32x16 dq[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dq[db][r] = 0.f;
+  const float c = a.scale * kLog2e;
+  using L = TileLoader<T, DP, KEYS, 4, VEC>;
+  const L ld(wave, lane);
+  const char *kt = lds, *vt = lds + TB;
+#pragma unroll 1
+  for (int k0 = t.k_begin; k0 < t.k_end; k0 += KEYS) {
+    if (k0 != t.k_begin) __syncthreads();  // the keys before have been read
+    int idx[L::NI];
+#pragma unroll
+    for (int i = 0; i < L::NI; ++i) idx[i] = row_of(a.k_row, min(k0 + ld.row(i), t.k_end - 1));
+    uint8_t m0 = 1, m1 = 1;
+    if (a.mask) {
+      m0 = a.mask[min(k0 + lane, t.k_end - 1)];
+      m1 = a.mask[min(k0 + 64 + lane, t.k_end - 1)];
+    }
+    const uint64_t b0 = __ballot(k0 + lane < t.k_end && m0 != 0), b1 = __ballot(k0 + 64 + lane < t.k_end && m1 != 0);
+    if ((b0 & b1) != ~0ull)
+#pragma unroll
+      for (int i = 0; i < L::NI; ++i) idx[i] = ((ld.row(i) < 64 ? b0 : b1) >> (ld.row(i) & 63)) & 1 ? idx[i] : -1;
+    const uint64_t bits = ((wave < 2 ? b0 : b1) >> (32 * (wave & 1))) & all_keys<32>();
+    ld.load(k, a.ldk, a.d, idx, lds);
+    __builtin_amdgcn_sched_barrier(0);
+    ld.load(v, a.ldv, a.d, idx, lds + TB);
+    vm_wait();
+    __syncthreads();
+    if (bits == 0) continue;
+    f32x16 s, dp;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+#pragma unroll
+    for (int st = 0; st < NS; ++st) {
+      s = step_mma<T>(*reinterpret_cast<const uint4*>(kt + unit_at<U>(32 * wave + l32, 2 * st + h)), qf[st], s);
+      dp = step_mma<T>(*reinterpret_cast<const uint4*>(vt + unit_at<U>(32 * wave + l32, 2 * st + h)), df[st], dp);
+      if (st % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (registers)
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -ref)) * (dp[r] - delta);
+    if (bits != all_keys<32>())
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = key_in(bits, 0, r) ? s[r] : 0.f;
+    across_mma<T, U, DB>(kt, 32 * wave, Probs<T>(s), dq, lane);
+  }
+  // [wave][row][DP], the 16-byte units of a row in an order of its own
+  float* sums = reinterpret_cast<float*>(lds);
+  const auto at = [&](int w, int r, int u) { return sums + ((w * 32 + r) * (DP / 4) + (u ^ (r & 7))) * 4; };
+  __syncthreads();
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<float4*>(at(wave, l32, 8 * db + 2 * j + h)) =
+          make_float4(dq[db][4 * j], dq[db][4 * j + 1], dq[db][4 * j + 2], dq[db][4 * j + 3]);
+  __syncthreads();
+  const int r = threadIdx.x >> 3;
+  if (r >= t.rows) return;
+  const Virtual vr(a, t.entry, t.head0, t.kv_head, r);
+  const int row = row_of(a.q_row, vr.entry);
+  const bool none = a.lse[(int64_t)row * a.heads + vr.head] == -INFINITY;  // a row without keys, whatever q and dout hold
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+    const int u = 8 * db + (threadIdx.x & 7);
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float4 y = *reinterpret_cast<const float4*>(at(w, r, u));
+      x[0] += y.x;
+      x[1] += y.y;
+      x[2] += y.z;
+      x[3] += y.w;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = none ? 0.f : x[e];
+    if (t.slot >= 0) {
+      *reinterpret_cast<float4*>(a.part + (size_t)t.slot * slot_floats<DP>(kCrossRows) + r * DP + 4 * u) =
+          make_float4(x[0], x[1], x[2], x[3]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] *= a.scale;
+      store4<T, VEC>(static_cast<T*>(a.out) + (int64_t)row * a.ldo + vr.head * a.d, x, 4 * u, a.d);
+    }
+  }
+}
+
 // The queries' gradient: as the forward with four waves, p recomputed from lse, dq^T += k^T ds^T.
 template <typename T, int DP, int TK, bool VEC>
 __device__ __forceinline__ void queries_back(const QTile* tiles, unsigned index, const Args& a, char* lds) {
@@ -692,6 +807,8 @@ __device__ __forceinline__ void queries_back(const QTile* tiles, unsigned index,
   constexpr int E = 16 / (int)sizeof(T), BUF = 2 * TB;
   const QTile t = tile_of_head(tiles, index, a);
   if (t.rows == 0) return;
+  if constexpr (DP * sizeof(T) <= 384 && (VEC || DP < 128))  // (the widest heads leave no registers for a second way)
+    if (t.rows <= 32) return queries_back_few<T, DP, VEC>(t, a, lds);
   const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
   const T* k = static_cast<const T*>(a.k) + t.kv_head * a.d;
   const T* v = static_cast<const T*>(a.v) + t.kv_head * a.d;
@@ -980,9 +1097,12 @@ template <typename T, int DP, int TK, bool VEC>
 __global__ __launch_bounds__(kThreads, (waves_back<T, DP>())) void k_cross_back(const KTile* keys, const RTile* runs,
                                                                                         unsigned nkeys, Args ka,
                                                                                         const QTile* rows, Args qa) {
-  __shared__ BackLds<T, DP, TK> lds;
+  typedef BackLds<T, DP, TK> Lds;
+  constexpr int FEW = 2 * tile_bytes<128, T, DP>(), SUMS = 4 * 32 * DP * 4, LEAST = FEW > SUMS ? FEW : SUMS;
+  __shared__ __attribute__((aligned(16))) char mem[sizeof(Lds) > LEAST ? sizeof(Lds) : LEAST];
+  Lds& lds = *reinterpret_cast<Lds*>(mem);
   if (blockIdx.x < nkeys) keys_back<T, DP, TK, VEC>(keys, runs, blockIdx.x, ka, lds);
-  else queries_back<T, DP, TK, VEC>(rows, blockIdx.x - nkeys, qa, lds.tiles);
+  else queries_back<T, DP, TK, VEC>(rows, blockIdx.x - nkeys, qa, mem);
 }
 
 // The pieces of a tile of keys summed in their order: eight threads a key, 32 keys a workgroup, eight pieces in flight; the
