@@ -2,6 +2,10 @@
 //     s = scale q k^T,  p = softmax(s) over the keys that count,  o = p v,  lse = log sum exp s
 //     delta = sum_d do o,  dp = do v^T,  ds = p (dp - delta),  dq = scale ds k,  dk = scale ds^T q,  dv = p^T do
 // Rows are gathered by index into LDS by direct loads; a masked key's, and what lies past the end, come from a block of zeros.
+// What bounds it: k and v on their way from HBM and the caches (256 sequences of 16 .. 256 rows against 64 .. 512 keys, 8 heads of
+// 128 in bf16: 131 us, 110 without the products, 87 for its bytes at a copy's rate; 64 single rows against 512 .. 4,096 keys, 16
+// heads of 64 on 4: 30 us and a join of 4, at 4.9 TB/s); in the gradient the exponentials beside the products and the loads (64
+// sequences of 256 .. 512 rows against 256 .. 1,024 keys, 16 heads of 64: 387 us, 430 TFLOP/s); in fp32 the matrix cores.
 //
 // Products are 32 x 32 tiles with the axis of the softmax on the accumulators' rows: the forward computes s^T = k q^T, so a
 // lane holds one query's column, its maximum, sum and rescaling are one value a lane, and p^T leaves the accumulators in the
@@ -671,10 +675,12 @@ __global__ __launch_bounds__(kThreads) void k_cross_delta(const T* out, int64_t 
   }
 }
 
+// Waves a SIMD of the gradients: three for rows of 128 bytes (64 chains of 16 heads of 64 in bf16: 375 us, with two 390), two
+// where 256 registers do (5 sequences of 265 .. 443 rows, 32 heads of 50 in fp32: 90 us, with one 113).
 template <typename T, int DP>
 constexpr int waves_back() { return DP * sizeof(T) <= 128 ? 3 : DP * sizeof(T) <= 192 || (sizeof(T) == 4 && DP == 64) ? 2 : 1; }
-// Whether a lane keeps its fragments of v in LDS of its own: where registers are short (the widest fp32 heads, and rows of 128
-// bytes, whose three waves a SIMD have 168 each).
+// Whether a lane keeps its fragments of v in LDS of its own: where registers are short (the widest fp32 heads, and where more
+// than one wave a SIMD share them: 168 each, or 256).
 template <typename T, int DP>
 constexpr bool keep_values() { return DP * sizeof(T) > 384 || DP * sizeof(T) == 128 || waves_back<T, DP>() == 2; }
 template <typename T, int DP, int TK>
@@ -1092,7 +1098,8 @@ __device__ __forceinline__ void keys_back(const KTile* tiles, const RTile* runs,
   if (a.out2) store_image<T, DP, VEC>(dv, 1.f, a.d, img, lane, place(a.out2, a.ldo2));
 }
 
-// Both gradients in one launch: `nkeys` workgroups for the keys', the rest for the queries'.
+// Both gradients in one launch: `nkeys` workgroups for the keys', the rest for the queries', which fill the end.  In two launches
+// 16 sources of 3 .. 127 keys in fp32 took 86 us where one took 65, 64 chains of 16 heads 396 and 386.
 template <typename T, int DP, int TK, bool VEC>
 __global__ __launch_bounds__(kThreads, (waves_back<T, DP>())) void k_cross_back(const KTile* keys, const RTile* runs,
                                                                                         unsigned nkeys, Args ka,
