@@ -321,7 +321,9 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
   c.num_keys = b->num_keys;
   c.query_rows = b->num_query_rows;
   c.key_rows = b->num_key_rows;
-  // tiles of 32 rows where those of 128 would be mostly empty
+  // tiles of 32 rows where those of 128 would be mostly empty: 64 sequences against 500 keys, 8 heads of 64 in bf16, low and tall
+  // tiles: 8 rows of 16 heads on 4 17.7 and 18.5 us, 16 rows 16.8 and 16.6, 64 rows 21.7 and 20.0; 96 rows against 2,000 keys 75.5
+  // and 57.4; single rows need the keys cut among waves
   int64_t tall = 0, low = 0, least_tiles = 0;
   for (int s = 0; s < b->num_seqs; ++s) {
     const int64_t n = (int64_t)(qp[s + 1] - qp[s]) * l.G, e = b->source ? src[s] : s;

@@ -225,6 +225,15 @@ Shape dw_shape(int64_t M, int K, int N, int es) {
   return shape_of(N, row_ld(K), std::max<int64_t>(1, (M + lines - 1) / lines), es, 1, kPieces, false, kAlone);
 }
 
+// Up to 64 rows go by k_linear_few while what a wave multiplies stays short: every block of 16 rows is multiplied along K / 8 by
+// one wave.  Both ways, few rows and tiles: 1 x 4,096 x 4,096 bf16 9.1 and 11.9 us, 32 rows 15.7 and 12.7; 64 x 1,024 x 4,096 9.2
+// and 11.1; 64 x 2,048 x 4,096 14.9 and 13.8; 1 x 16,384 x 1,024 22.5 and 12.8; fp32 1 x 4,096 x 4,096 21.4 and 25.8, 32 rows 28.5
+// and 27.1; 64 x 1,024 x 4,096 16.6 and 17.7, 64 x 2,048 x 1,024 23.3 and 13.9.
+bool few_rows(int64_t M, int K) {
+  const int blocks = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+  return M <= kFewRows && row_ld(K) * blocks <= 4096;
+}
+
 template <typename T, int ACT>
 void few(int M, int K, int N, const void* x, const void* W, const float* bias, const void* res, void* out, void* pre,
          hipStream_t st) {
@@ -242,7 +251,7 @@ void few(int M, int K, int N, const void* x, const void* W, const float* bias, c
 template <typename T, int ACT>
 void forward(int64_t M, int K, int N, const void* x, const void* W, const float* bias, const void* res, void* out,
              void* pre, void* ws, hipStream_t st) {
-  if (M <= kFewRows) return few<T, ACT>((int)M, K, N, x, W, bias, res, out, pre, st);
+  if (few_rows(M, K)) return few<T, ACT>((int)M, K, N, x, W, bias, res, out, pre, st);
   const int es = sizeof(T), ldk = row_ld(K), ldn = row_ld(N);
   const Shape sh = forward_shape(M, K, N, es);
   ProductArgs g{{x, M, ldk}, {W, N, ldk}, M, N, sh.mt, sh.nt, ldk * es / 128, sh.split, out, (size_t)ldn, ldn, bias, 0, nullptr};
@@ -367,12 +376,12 @@ void backward(int64_t M, int K, int N, const void* x, const void* W, int act, co
 
 int64_t linear_tiles(int dtype, int64_t M, int K, int N) {
   const Shape sh = forward_shape(M, K, N, dtype == FOLD_BF16 ? 2 : 4);
-  if (M <= kFewRows) return row_ld(N) / 16;
+  if (few_rows(M, K)) return row_ld(N) / 16;
   return std::max(sh.mt * sh.nt * sh.split, sh.split > 1 ? M * row_ld(N) / 1024 + 1 : 0);
 }
 size_t linear_bytes(int dtype, int64_t M, int K, int N) {
   const Shape sh = forward_shape(M, K, N, dtype == FOLD_BF16 ? 2 : 4);
-  return M <= kFewRows || sh.split == 1 ? 0 : (size_t)sh.split * M * row_ld(N) * sizeof(float);
+  return few_rows(M, K) || sh.split == 1 ? 0 : (size_t)sh.split * M * row_ld(N) * sizeof(float);
 }
 int64_t linear_backward_tiles(int dtype, int64_t M, int K, int N) {
   const int es = dtype == FOLD_BF16 ? 2 : 4;

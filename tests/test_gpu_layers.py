@@ -165,7 +165,8 @@ def test_layer_norm_against_differences(n):
 LAYERS = [(1, 1, 1, "f32"), (1, 1024, 4096, "bf16"), (1, 300, 70, "bf16"), (2, 64, 65, "f32"), (16, 1000, 333, "bf16"),
           (17, 320, 640, "f32"), (33, 75, 1200, "bf16"), (64, 4096, 100, "bf16"), (65, 300, 130, "bf16"), (130, 65, 257, "f32"),
           (257, 512, 300, "bf16"), (300, 1300, 96, "f32"), (1000, 128, 512, "bf16"), (2049, 300, 200, "f32"),
-          (4100, 256, 1024, "bf16"), (3, 16384, 40, "bf16"), (70, 40, 16384, "f32"), (16640, 256, 1280, "bf16")]
+          (4100, 256, 1024, "bf16"), (3, 16384, 40, "bf16"), (70, 40, 16384, "f32"), (16640, 256, 1280, "bf16"),
+          (1, 4200, 70, "bf16"), (1, 4096, 130, "f32"), (33, 2100, 200, "f32"), (64, 1088, 130, "bf16"), (17, 2048, 64, "bf16")]
 
 
 def _layer_case(M, K, N, dtype, seed=0):
