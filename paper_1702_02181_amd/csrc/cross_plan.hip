@@ -323,7 +323,9 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
   c.key_rows = b->num_key_rows;
   // tiles of 32 rows where those of 128 would be mostly empty: 64 sequences against 500 keys, 8 heads of 64 in bf16, low and tall
   // tiles: 8 rows of 16 heads on 4 17.7 and 18.5 us, 16 rows 16.8 and 16.6, 64 rows 21.7 and 20.0; 96 rows against 2,000 keys 75.5
-  // and 57.4; single rows need the keys cut among waves
+  // and 57.4.  Low tiles of bf16 heads above 64 leave one workgroup a compute unit, so where tall ones fill the chip twice over
+  // they stay tall: 256 sequences, 8 heads of 128, single rows against 2,000 keys 379 and 361 us, 8 rows against 500 125 and 111;
+  // 16 sequences 16.5 and 18.2
   int64_t tall = 0, low = 0, least_tiles = 0;
   for (int s = 0; s < b->num_seqs; ++s) {
     const int64_t n = (int64_t)(qp[s + 1] - qp[s]) * l.G, e = b->source ? src[s] : s;
@@ -334,7 +336,8 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
   }
   if (least_tiles >= kMaxTiles)
     return api_fail(FOLD_E_INVALID, who + ": too many tiles for one launch (sequences and rows)");
-  c.few = low < 2 * tall && cross_padded(c.head_dim) * (c.dtype == FOLD_BF16 ? 2 : 4) <= kCrossFewBytes;
+  const bool full = c.dtype == FOLD_BF16 && cross_padded(c.head_dim) > 64 && least_tiles * c.kv_heads >= 4 * 256;
+  c.few = low < 2 * tall && !full && cross_padded(c.head_dim) * (c.dtype == FOLD_BF16 ? 2 : 4) <= kCrossFewBytes;
   std::vector<QTile> fwd, fjoin, back, bjoin;
   std::vector<KTile> keys, kjoin;
   std::vector<RTile> rows;
