@@ -170,6 +170,12 @@ def test_one_query_each(dtype, d):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_short_sequences(dtype):
+    """More tiles than the chip holds at once, of a few rows each."""
+    check(Case(dtype, 8, 8, 96, [2] * 130, [5, 40] * 65, mask=0.1, seed=16))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_one_long_sequence(dtype):
     """A single row against many keys, and a single key sequence that many rows read: both sides in pieces."""
     plan, *_ = check(Case(dtype, 1, 1, 32, [1], [9000], seed=6))
