@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256) void k_join_as(const float* part, int pieces, 
 constexpr double kAlone = 1.25;
 
 Shape forward_shape(int64_t M, int K, int N, int es) {
-  return shape_of(M, row_ld(N), row_ld(K) * es / 128, es, 2, kPieces, false, kAlone);
+  return shape_of(M, row_ld(N), row_ld(K) * es / 128, es, 2, kPieces, false, kAlone, true);
 }
 Shape dx_shape(int64_t M, int K, int N, int es) {
   return shape_of(std::max<int64_t>(M, 1), row_ld(K), (int64_t)row_ld(N) * es / 128, es, 1, kPieces, false, kAlone);

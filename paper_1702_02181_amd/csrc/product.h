@@ -660,7 +660,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_product_both(ProductArgs states
 // compute unit walks its tiles, and the stages of all of them are one stream through the slots.  While a tile's last stages
 // are multiplied the first of the next tile and its bias are loaded, and they land while the tile is stored, so neither
 // the first loads' latency nor the store's is waited for (8,192 x 1,024 x 32,000 bf16: 693 us with a workgroup a tile,
-// 490 us so).  Needs at least SLOTS stages.
+// 490 us so).  Needs at least SLOTS stages, and K in one piece.
 template <typename T, typename OUT, int ACT = kPlain>
 __global__ __launch_bounds__(kThreads, 1) void k_product_chain(ProductArgs g) {
   g.add = 0;  // logits are written
@@ -910,9 +910,12 @@ constexpr int kUnits = 256;  // compute units
 // states' gradient of 33 x 300 x 20,000 bf16 13 us (335), of 257 x 300 x 20,001 fp32 49 us (4,512), weights' gradient of
 // 2,048 x 256 x 10,000 fp32 100 us (486).
 // small: the smallest tile's columns / 64 (1 or 2); smallest: that tile alone; alone: what 128 x 128 tiles cost more where a
-// compute unit has no second workgroup
+// compute unit has no second workgroup; chain: the product goes by k_product_chain where it can, which knows no
+// pieces, so more 256 x 256 tiles than compute units keep K whole.  Such tiles in pieces (workgroups of their own, and a join) and
+// what the rule takes (whole, in tiles of 128 x 128; the last one the chain), bf16 with a residual: 10,300 x 8,192 x 2,048 397 and
+// 367 us, 5,000 x 16,384 x 4,096 737 and 716, 13,000 x 16,384 x 4,096 2,298 and 1,786, 17,000 x 16,384 x 4,096 2,780 and 2,880.
 Shape shape_of(int64_t M, int64_t N, int64_t nstage, int esize, int small, int pieces, bool smallest = false,
-               double alone = 1.0) {
+               double alone = 1.0, bool chain = false) {
   static constexpr struct { int wm, wn; double bf16, f32; } kTiles[] = {
       {4, 4, 1.0, 1.0}, {2, 2, 1.2, 1.0}, {1, 2, 1.55, 1.03}, {1, 1, 2.2, 1.06}};
   Shape best{0, 0, 0, 0, 0};
@@ -920,7 +923,8 @@ Shape shape_of(int64_t M, int64_t N, int64_t nstage, int esize, int small, int p
   for (const auto& t : kTiles) {
     if ((t.wm == 1 && t.wn != small) || (smallest && t.wm != 1)) continue;
     const int64_t mt = tiles_of(M, t.wm), nt = tiles_of(N, t.wn);
-    for (int p = 1; p <= pieces && (p == 1 || nstage / p >= 4); p *= 2) {
+    const int most = chain && t.wm == 4 && mt * nt > kUnits ? 1 : pieces;
+    for (int p = 1; p <= most && (p == 1 || nstage / p >= 4); p *= 2) {
       const double rounds = (double)((mt * nt * p + kUnits - 1) / kUnits);
       const double stage = t.wm * t.wn * (esize == 2 ? 0.11 * t.bf16 : 0.49 * t.f32) * (t.wm == 2 && rounds == 1 ? alone : 1.0);
       double us = rounds * (stage * (double)((nstage + p - 1) / p) + 2.0 / (t.wm == 4 ? 1 : 2));
@@ -933,6 +937,10 @@ Shape shape_of(int64_t M, int64_t N, int64_t nstage, int esize, int small, int p
   }
   return best;
 }
+// Whether a product of 256 x 256 tiles goes by k_product_chain: more tiles than compute units, at least its slots' stages (of 64
+// bytes), and all of K in one piece, since its tiles have no pieces.
+bool chained(const ProductArgs& g) { return g.split == 1 && g.nstage >= 4 && g.mt * g.nt > kUnits; }
+
 unsigned blocks_of(const ProductArgs& g) { return (unsigned)((g.mt * g.nt * g.split + 7) / 8 * 8); }
 
 template <typename T, int AD, int BD, typename OUT, int ACT = kPlain>
@@ -941,7 +949,7 @@ void launch(ProductArgs g, const Shape& sh, hipStream_t st) {
   if (sh.wm == 4) {
     g.nstage *= 2;
     if constexpr (AD == kAlong && BD == kAlong)
-      if (g.nstage >= 4 && g.mt * g.nt > kUnits) {
+      if (chained(g)) {
         hipLaunchKernelGGL((k_product_chain<T, OUT, ACT>), dim3(kUnits), dim3(kThreads), 0, st, g);
         return;
       }
