@@ -628,6 +628,8 @@ def _hip():
         _hiplib = ctypes.CDLL("libamdhip64.so")
         _hiplib.hipMemcpy.restype = ctypes.c_int
         _hiplib.hipMemcpy.argtypes = [c_void_p, c_void_p, c_size_t, ctypes.c_int]
+        _hiplib.hipMemcpyAsync.restype = ctypes.c_int
+        _hiplib.hipMemcpyAsync.argtypes = [c_void_p, c_void_p, c_size_t, ctypes.c_int, c_void_p]
     return _hiplib
 
 
@@ -1284,15 +1286,17 @@ class CrossAttention:
         return dq, dk, dv
 
 
-def schedule_rows(sched) -> "torch.Tensor":  # noqa: F821
-    """The schedule's node_pos as a new int32 tensor: the pool row of every node, which with graph_ptr lists a batch's graphs
-    for CrossAttention."""
+def schedule_rows(sched, stream=None) -> "torch.Tensor":  # noqa: F821
+    """The schedule's node_pos as a new int32 tensor of `stream` (the current one by default): the pool row of every node, which
+    with graph_ptr lists a batch's graphs for CrossAttention.  Waits for the copy, so that any stream may read it."""
     import torch
     n = sched.info.num_nodes
-    out = torch.empty(n, dtype=torch.int32, device="cuda")
-    if n:
-        torch.cuda.current_stream().synchronize()
-        rc = _hip().hipMemcpy(c_void_p(out.data_ptr()), c_void_p(sched.info.node_pos), c_size_t(4 * n), 3)
-        if rc != 0:
-            raise RuntimeError(f"hipMemcpy failed ({rc})")
+    with _on(stream):
+        out = torch.empty(n, dtype=torch.int32, device="cuda")
+        if n:  # (a plain hipMemcpy on the device goes through the null stream, which torch's streams do not wait for)
+            st = torch.cuda.current_stream()
+            rc = _hip().hipMemcpyAsync(out.data_ptr(), sched.info.node_pos, 4 * n, 3, st.cuda_stream)
+            if rc != 0:
+                raise RuntimeError(f"hipMemcpyAsync failed ({rc})")
+            st.synchronize()
     return out

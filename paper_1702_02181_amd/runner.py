@@ -370,9 +370,9 @@ class CrossBlock:
         self.wk = kv * d
         if source_of is not None:
             source_of = torch.from_numpy(np.ascontiguousarray(source_of, np.int32)).to(target.device)
-        self.cross = F.CrossAttention(heads, d, target.graph_ptr, source.graph_ptr, F.schedule_rows(target.sched),
-                                      F.schedule_rows(source.sched), source=source_of, kv_heads=kv, dtype=target.tdtype,
-                                      stream=self.st)
+        self.cross = F.CrossAttention(heads, d, target.graph_ptr, source.graph_ptr, F.schedule_rows(target.sched, self.st),
+                                      F.schedule_rows(source.sched, self.st), source=source_of, kv_heads=kv,
+                                      dtype=target.tdtype, stream=self.st)
         rng = np.random.default_rng(seed)
         self.tensors = []  # (fp32 master, bf16 copy or None, gradient)
         f32 = dict(dtype=torch.float32, device=target.device)
