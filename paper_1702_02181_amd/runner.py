@@ -356,15 +356,25 @@ class CrossBlock:
     source: an encoder's trees), graph by graph, between the target's forward pass and its head.  For target states x and
     source states s, both in pool order:
         y = x + Wo attention(Wq norm(x), Wk s, Wv s) + bo,   z = y + W2 act(W1 norm(y) + b1) + b2,   states = norm(z)
-    with `heads` heads (in groups on `kv_heads` of keys) and a feed-forward width of `wide`.  source[g]: the source graph
-    that target graph g reads (g by default; -1: none).  forward() and backward() are launches of the library alone."""
+    with `heads` heads (in groups on `kv_heads` of keys) and a feed-forward width of `wide`.  source_of[g]: the source graph
+    that target graph g reads (g by default; -1: none).  Everything, the parameters' making too, runs on the runs' stream, which
+    is one for both (None: the current one); forward() and backward() launch the library's kernels and fill pad columns."""
 
     def __init__(self, target: DeviceRun, source: DeviceRun, heads: int, wide: int, kv_heads=None, source_of=None,
                  activation: str = "gelu", seed: int = 0):
         H = target.H
         if source.H != H or source.tdtype != target.tdtype or H % heads:
             raise ValueError("target and source have one hidden size, a multiple of the heads, and one type")
+        if (target.stream is None) != (source.stream is None) or (target.stream is not None and target.stream != source.stream):
+            raise ValueError("target and source run on one stream: the block reads the source's states and returns their gradient")
         self.target, self.source, self.st = target, source, target.stream
+        if self.st is not None:  # the runs' tensors were made on the current stream
+            self.st.wait_stream(torch.cuda.current_stream())
+        with F._on(self.st):
+            self._make(heads, wide, kv_heads, source_of, activation, seed)
+
+    def _make(self, heads, wide, kv_heads, source_of, activation, seed):
+        target, source, H = self.target, self.source, self.target.H
         kv = heads if kv_heads is None else kv_heads
         d = H // heads
         self.wk = kv * d
@@ -433,7 +443,8 @@ class CrossBlock:
         db = self._layer_back(self.first, b, df, pre)
         dy = self._norm_back(1, y, db, stats_b, dz, low)
         do = self._layer_back(self.o, o, dy)
-        dkv = torch.zeros_like(kv) if kv.shape[1] != 2 * self.wk else torch.empty_like(kv)
+        with F._on(self.st):
+            dkv = torch.zeros_like(kv) if kv.shape[1] != 2 * self.wk else torch.empty_like(kv)
         dq, _, _ = self.cross.backward(q, kv, kv[:, self.wk:], o, lse, do, dk=dkv, dv=dkv[:, self.wk:], stream=self.st)
         ds = self._layer_back(self.kv, s, dkv, dtype=torch.float32)
         da = self._layer_back(self.q, a, dq)

@@ -31,3 +31,51 @@ def test_rows_of_a_schedule_on_a_stream():
         assert all(np.array_equal(t.cpu().numpy(), want) for t in copies)
     torch.cuda.synchronize()
     assert np.array_equal(F.schedule_rows(run.sched).cpu().numpy(), want)
+
+
+def _block(stream, kv_heads, busy=False):
+    """out, dx, ds and the parameters' gradients of a block between two runs on `stream`, the current stream busy while the
+    block's passes run."""
+    import torch
+    from paper_1702_02181_amd.runner import CrossBlock, DeviceRun
+    target, source = (DeviceRun(_chains(s), stream=stream, with_backward=False) for s in (2, 3))
+    torch.cuda.synchronize()  # the runs' own tensors
+    rng = np.random.default_rng(4)
+    up = torch.from_numpy(rng.standard_normal((target.N, target.ld)).astype(np.float32)).cuda()
+    target.forward()
+    source.forward()
+    block = CrossBlock(target, source, 4, 200, kv_heads, seed=5)
+    if busy:
+        torch.cuda._sleep(BUSY)
+    out = block.forward()
+    dx, ds = block.backward(up)
+    if stream is None:
+        torch.cuda.synchronize()
+    else:
+        stream.synchronize()
+        with torch.cuda.stream(stream):  # read there, not behind the busy stream
+            return [t.cpu() for t in (out, dx, ds, *(g for _, _, g in block.tensors))]
+    return [t.cpu() for t in (out, dx, ds, *(g for _, _, g in block.tensors))]
+
+
+@pytest.mark.parametrize("kv_heads", [1, 4])  # of 16 columns each: pad columns behind k and v side by side, and none
+def test_block_on_a_stream_of_its_own(kv_heads):
+    import torch
+    want = _block(None, kv_heads)
+    got = _block(torch.cuda.Stream(), kv_heads, busy=True)
+    torch.cuda.synchronize()
+    assert all(torch.isfinite(t.float()).all() for t in got)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_block_of_runs_on_two_streams_is_refused():
+    import torch
+    from paper_1702_02181_amd.runner import CrossBlock, DeviceRun
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    runs = [DeviceRun(_chains(2), stream=s, with_backward=False) for s in (a, b, None)]
+    torch.cuda.synchronize()
+    for target, source in ((runs[0], runs[1]), (runs[0], runs[2]), (runs[2], runs[1])):
+        with pytest.raises(ValueError, match="one stream"):
+            CrossBlock(target, source, 4, 200)
+    CrossBlock(runs[0], runs[0], 4, 200)
+    torch.cuda.synchronize()
