@@ -1200,8 +1200,9 @@ class CrossAttention:
             raise ValueError("query_ptr and key_ptr have an entry more than there are sequences")
         # (without a list and a count the end of ptr is read, which waits for the GPU, as making the plan does)
         count = lambda rows, n, ptr: int(rows.numel()) if rows is not None else int(ptr[-1]) if n is None else int(n)  # noqa: E731
-        self.num_queries = count(query_rows, num_queries, query_ptr)
-        self.num_keys = count(key_rows, num_keys, key_ptr)
+        with _on(stream):
+            self.num_queries = count(query_rows, num_queries, query_ptr)
+            self.num_keys = count(key_rows, num_keys, key_ptr)
         self.query_rows = self.num_queries if num_query_rows is None else int(num_query_rows)
         self.key_rows = self.num_keys if num_key_rows is None else int(num_key_rows)
         if source is not None and source.numel() != query_ptr.numel() - 1:

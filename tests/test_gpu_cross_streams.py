@@ -79,3 +79,19 @@ def test_block_of_runs_on_two_streams_is_refused():
             CrossBlock(target, source, 4, 200)
     CrossBlock(runs[0], runs[0], 4, 200)
     torch.cuda.synchronize()
+
+
+def test_counts_are_read_on_the_stream():
+    """Lists that are written on the plan's stream just before: their ends are read behind that."""
+    import torch
+    side = torch.cuda.Stream()
+    ends = [torch.tensor([0, 3, 7], dtype=torch.int32, device="cuda"), torch.tensor([0, 5, 9], dtype=torch.int32, device="cuda")]
+    lists = [torch.zeros_like(e) for e in ends]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(BUSY)
+        for t, e in zip(lists, ends):
+            t.copy_(e)
+    plan = F.CrossAttention(2, 32, *lists, dtype=torch.float32, stream=side)
+    assert (plan.num_queries, plan.num_keys) == (7, 9)
+    torch.cuda.synchronize()
