@@ -22,17 +22,17 @@ __global__ __launch_bounds__(256) void k_zero_words(uint32_t* p, size_t n) {
 }
 
 // the arrays that the host looks at, and the error word, one after the other
-__global__ __launch_bounds__(256) void k_collect(const int32_t* a, int na, const int32_t* b, int nb, const int32_t* c, int nc,
-                                                 const uint32_t* error, int32_t* out) {
-  const int n = na + nb + nc + 1;
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256)
+__global__ __launch_bounds__(256) void k_collect(const int32_t* a, int64_t na, const int32_t* b, int64_t nb, const int32_t* c,
+                                                 int64_t nc, const uint32_t* error, int32_t* out) {
+  const int64_t n = na + nb + nc + 1;
+  for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256)
     out[i] = i < na ? a[i] : i < na + nb ? b[i - na] : i < na + nb + nc ? c[i - na - nb] : (int32_t)*error;
 }
 
 // error bits: 1 a row out of range, 2 a row listed twice
 __global__ __launch_bounds__(256) void k_check_rows(const int32_t* row, int n, int limit, uint32_t* seen, uint32_t* error,
                                                     int shift) {
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
+  for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) {
     const int r = row[i];
     if (r < 0 || r >= limit) {
       atomicOr(error, 1u << shift);
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256) void k_check_rows(const int32_t* row, int n, i
 }
 
 __global__ __launch_bounds__(256) void k_identity(int32_t* row, int n) {
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) row[i] = i;
+  for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) row[i] = (int32_t)i;
 }
 
 struct Range {
@@ -120,19 +120,25 @@ int64_t piece_of(int64_t tiles, int64_t work, int unit, int least) {
 }
 
 struct Lists {
-  const std::vector<int32_t>&qp, &kp, &src;
+  const std::vector<int32_t>&qp, &kp;
   int G, kv_heads, least;
-  std::vector<std::vector<int>> readers;  // by source: its query sequences; the last entry: those without a source
+  std::vector<int32_t> first, seqs;  // source e's query sequences: seqs[first[e]] .. ; the last entry: those without a source
+  struct Run {
+    const int32_t *b, *e;
+    const int32_t* begin() const { return b; }
+    const int32_t* end() const { return e; }
+  };
+  Run readers(int64_t e) const { return {seqs.data() + first[e], seqs.data() + first[e + 1]}; }
 };
 
 // tiles of `height` virtual rows (launched for every key head) in pieces of the keys; the tiles in pieces also go to `join`
 void query_tiles(const Lists& l, int height, std::vector<QTile>* out, std::vector<QTile>* join, int* slots) {
-  const int sources = (int)l.kp.size() - 1;
+  const int64_t sources = (int64_t)l.kp.size() - 1;
   int64_t tiles = 0, work = 0;
-  const auto keys_of = [&](int e) { return e < sources ? (int64_t)l.kp[e + 1] - l.kp[e] : 0; };
+  const auto keys_of = [&](int64_t e) { return e < sources ? (int64_t)l.kp[e + 1] - l.kp[e] : 0; };
   const auto rows_of = [&](int b) { return ((int64_t)l.qp[b + 1] - l.qp[b]) * l.G; };
-  for (int e = 0; e <= sources; ++e)
-    for (int b : l.readers[e]) {
+  for (int64_t e = 0; e <= sources; ++e)
+    for (int b : l.readers(e)) {
       const int64_t n = (rows_of(b) + height - 1) / height * l.kv_heads;
       tiles += n;
       work += n * keys_of(e);
@@ -140,12 +146,12 @@ void query_tiles(const Lists& l, int height, std::vector<QTile>* out, std::vecto
   const int64_t piece = piece_of(tiles, work, 64, l.least);
   Spread<QTile> s;
   *slots = 0;
-  for (int e = 0; e <= sources; ++e) {
+  for (int64_t e = 0; e <= sources; ++e) {
     const int64_t nk = keys_of(e), pieces = std::max<int64_t>(1, (nk + piece - 1) / piece);
     const int64_t each = ((nk + pieces - 1) / pieces + 63) / 64 * 64;
     const int n = (int)(each ? std::max<int64_t>(1, (nk + each - 1) / each) : 1);
     const int32_t k0 = e < sources ? l.kp[e] : 0;
-    for (int b : l.readers[e])
+    for (int b : l.readers(e))
       for (int64_t r = 0; r < rows_of(b); r += height) {
         QTile t{};
         t.entry = (int32_t)(l.qp[b] + r / l.G);
@@ -168,34 +174,32 @@ void query_tiles(const Lists& l, int height, std::vector<QTile>* out, std::vecto
 
 void key_tiles(const Lists& l, int height, std::vector<KTile>* out, std::vector<KTile>* join, std::vector<RTile>* rows,
                int* slots) {
-  const int sources = (int)l.kp.size() - 1;
+  const int64_t sources = (int64_t)l.kp.size() - 1;
   std::vector<Range> runs(sources);
-  std::vector<int64_t> count(sources, 0);
   int64_t tiles = 0, work = 0;
-  for (int e = 0; e < sources; ++e) {
+  for (int64_t e = 0; e < sources; ++e) {
     runs[e].begin = (int64_t)rows->size();
-    for (int b : l.readers[e]) {
+    for (int b : l.readers(e)) {
       const int64_t n = ((int64_t)l.qp[b + 1] - l.qp[b]) * l.G;
-      count[e] += n;
       for (int64_t r = 0; r < n; r += height)
         rows->push_back(RTile{(int32_t)(l.qp[b] + r / l.G), (int32_t)(r % l.G), (int32_t)std::min<int64_t>(height, n - r), 0});
     }
     runs[e].end = (int64_t)rows->size();
-    const int64_t n = (int64_t)(l.kp[e + 1] - l.kp[e] + kCrossKeys - 1) / kCrossKeys * l.kv_heads;
+    const int64_t n = ((int64_t)l.kp[e + 1] - l.kp[e] + kCrossKeys - 1) / kCrossKeys * l.kv_heads;
     tiles += n;
     work += n * runs[e].size() * height;
   }
   const int64_t piece = piece_of(tiles, work, height, l.least) / height;  // row tiles
   Spread<KTile> s;
   *slots = 0;
-  for (int e = 0; e < sources; ++e) {
+  for (int64_t e = 0; e < sources; ++e) {
     const int64_t nr = runs[e].size(), pieces = std::max<int64_t>(1, (nr + piece - 1) / piece);
     const int64_t each = std::max<int64_t>(1, (nr + pieces - 1) / pieces);
     const int n = (int)std::max<int64_t>(1, (nr + each - 1) / each);
-    for (int32_t k = l.kp[e]; k < l.kp[e + 1]; k += kCrossKeys) {
+    for (int64_t k = l.kp[e]; k < l.kp[e + 1]; k += kCrossKeys) {
       KTile t{};
-      t.k_begin = k;
-      t.keys = std::min<int32_t>(kCrossKeys, l.kp[e + 1] - k);
+      t.k_begin = (int32_t)k;
+      t.keys = (int32_t)std::min<int64_t>(kCrossKeys, l.kp[e + 1] - k);
       for (int p = 0; p < n; ++p) {
         t.t_begin = (int32_t)(runs[e].begin + std::min<int64_t>(p * each, nr));
         t.t_end = (int32_t)(runs[e].begin + std::min<int64_t>((p + 1) * each, nr));
@@ -244,6 +248,12 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
     return api_fail(FOLD_E_INVALID, who + ": negative count");
   if ((int64_t)b->num_queries * b->heads > INT32_MAX)
     return api_fail(FOLD_E_INVALID, who + ": queries times heads reach 2^31");
+  // before a list is looked at: a tile holds at most kCrossKeys keys (kCrossRows rows), so these are too many tiles however they
+  // fall into sequences.  What is left ends 1,024 entries below 2^31, and a list entry plus a tile fits 32 bits.
+  const std::string many = who + ": too many tiles for one launch (sequences, rows and keys)";
+  if (((int64_t)b->num_keys + kCrossKeys - 1) / kCrossKeys >= kMaxTiles ||
+      ((int64_t)b->num_queries * (b->heads / b->kv_heads) + kCrossRows - 1) / kCrossRows >= kMaxTiles)
+    return api_fail(FOLD_E_INVALID, many);
   if (!b->query_ptr || !b->key_ptr) return api_fail(FOLD_E_INVALID, who + ": NULL query_ptr or key_ptr");
   if (!b->source && b->num_seqs != b->num_sources)
     return api_fail(FOLD_E_INVALID, who + ": without `source` there is a key sequence for each query sequence");
@@ -256,7 +266,7 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
 
   int device = 0;
   FOLD_HIP_CHECK(hipGetDevice(&device));
-  const int nq = b->num_seqs + 1, nk = b->num_sources + 1, ns = b->source ? b->num_seqs : 0;
+  const int64_t nq = (int64_t)b->num_seqs + 1, nk = (int64_t)b->num_sources + 1, ns = b->source ? b->num_seqs : 0;
   std::vector<int32_t> qp(nq), kp(nk), src(ns);
   uint32_t error = 0;
   const size_t qw = b->query_row ? ((size_t)b->num_query_rows + 31) / 32 : 0;
@@ -295,12 +305,27 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
   if (!check_ptr(kp, b->num_keys)) return api_fail(FOLD_E_INVALID, who + ": key_ptr malformed");
   if (error & 5) return api_fail(FOLD_E_INVALID, who + (error & 1 ? ": query_row" : ": key_row") + " out of range");
   if (error & 10) return api_fail(FOLD_E_INVALID, who + (error & 2 ? ": query_row" : ": key_row") + " lists a row twice");
-  Lists l{qp, kp, src, b->heads / b->kv_heads, b->kv_heads, min_piece(b->dtype), {}};
-  l.readers.resize((size_t)b->num_sources + 1);
-  for (int s = 0; s < b->num_seqs; ++s) {
+  Lists l{qp, kp, b->heads / b->kv_heads, b->kv_heads, min_piece(b->dtype), {}, {}};
+  const auto source_of = [&](int s) -> int64_t {
     const int e = b->source ? src[s] : s;
-    if (e < -1 || e >= b->num_sources) return api_fail(FOLD_E_INVALID, who + ": source out of range");
-    l.readers[e < 0 ? b->num_sources : e].push_back(s);
+    return e < 0 ? b->num_sources : e;
+  };
+  l.first.assign((size_t)nk + 1, 0);
+  for (int s = 0; s < b->num_seqs; ++s) {
+    if (b->source && (src[s] < -1 || src[s] >= b->num_sources))
+      return api_fail(FOLD_E_INVALID, who + ": source out of range");
+    ++l.first[source_of(s) + 1];
+  }
+  int64_t key_tile_count = 0;
+  for (int64_t e = 0; e < nk; ++e) {
+    if (e < b->num_sources) key_tile_count += ((int64_t)kp[e + 1] - kp[e] + kCrossKeys - 1) / kCrossKeys;
+    l.first[e + 1] += l.first[e];
+  }
+  if (key_tile_count >= kMaxTiles) return api_fail(FOLD_E_INVALID, many);
+  l.seqs.resize(b->num_seqs);
+  {
+    std::vector<int32_t> at(l.first.begin(), l.first.end() - 1);
+    for (int s = 0; s < b->num_seqs; ++s) l.seqs[at[source_of(s)]++] = s;
   }
 
   fold_cross* h = new fold_cross;
@@ -334,8 +359,7 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
     tall += (n + kCrossRows - 1) / kCrossRows * keys;
     low += (n + kCrossFew - 1) / kCrossFew * keys;
   }
-  if (least_tiles >= kMaxTiles)
-    return api_fail(FOLD_E_INVALID, who + ": too many tiles for one launch (sequences and rows)");
+  if (least_tiles >= kMaxTiles) return api_fail(FOLD_E_INVALID, many);
   const bool full = c.dtype == FOLD_BF16 && cross_padded(c.head_dim) > 64 && least_tiles * c.kv_heads >= 4 * 256;
   c.few = low < 2 * tall && !full && cross_padded(c.head_dim) * (c.dtype == FOLD_BF16 ? 2 : 4) <= kCrossFewBytes;
   std::vector<QTile> fwd, fjoin, back, bjoin;
@@ -346,7 +370,7 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
   key_tiles(l, c.dtype == FOLD_BF16 ? 64 : 32, &keys, &kjoin, &rows, &c.kslots);
 
   if ((int64_t)std::max({fwd.size(), back.size() + keys.size(), 4 * fjoin.size(), 4 * bjoin.size(), 4 * kjoin.size()}) >= kMaxTiles)
-    return api_fail(FOLD_E_INVALID, who + ": too many tiles for one launch (sequences and rows)");
+    return api_fail(FOLD_E_INVALID, many);
   // one image of all the lists, uploaded whole; the row numbers behind it are copied or made on the device
   std::vector<char> image;
   const auto place = [&](const void* data, size_t size) {
