@@ -696,8 +696,8 @@ int32_t fold_token_logprobs(const fold_sched* sched, int32_t dtype, int64_t rows
  *   dout      device [rows, fold_row_ld(out_dim)] of dtype, finite in the pad
  *             columns (zero for FOLD_ACT_NONE)
  *   pre       as left by fold_linear (NULL for FOLD_ACT_NONE)
- *   dpre      device, as pre: receives dz; may be pre or dout itself; NULL for
- *             FOLD_ACT_NONE
+ *   dpre      device, as pre: receives dz, also where nothing else is asked
+ *             for; may be pre or dout itself; NULL for FOLD_ACT_NONE
  *   dx_dtype, dw_dtype  of dx and dW: dtype, or FOLD_F32
  *   dx, dW, dbias  written whole (pad columns zero), or NULL; with
  *             FOLD_BLOCK_ACCUMULATE dbias and a dW of FOLD_F32 are added to

@@ -177,8 +177,8 @@ int32_t fold_linear_backward(int32_t dtype, int64_t rows, int32_t in_dim, int32_
     if (flags & ~FOLD_BLOCK_ACCUMULATE) return api_fail(FOLD_E_INVALID, who + ": unknown flag");
     if ((flags & FOLD_BLOCK_ACCUMULATE) && dW && dw_dtype != FOLD_F32)
       return api_fail(FOLD_E_INVALID, who + ": a dW that is added to is fp32");
-    if ((!dx || rows == 0) && !dW && !dbias) return FOLD_OK;
     const bool bent = act != FOLD_ACT_NONE;
+    if (((!dx && !(bent && dpre)) || rows == 0) && !dW && !dbias) return FOLD_OK;
     if (rows > 0 && (!dout || (dW && !x) || (dx && !W) || (bent && (!pre || !dpre))))
       return api_fail(FOLD_E_INVALID, who + ": NULL buffer");
     if (!bent && (pre || dpre)) return api_fail(FOLD_E_INVALID, who + ": pre and dpre belong to an activation");

@@ -321,7 +321,7 @@ void backward(int64_t M, int K, int N, const void* x, const void* W, int act, co
               int dx_dtype, void* dx, int dw_dtype, void* dW, float* db, int add, void* ws, hipStream_t st) {
   const int es = sizeof(T), ldk = row_ld(K), ldn = row_ld(N);
   const T* dz = static_cast<const T*>(dout);
-  if ((act != FOLD_ACT_NONE && (dx || dW)) || db) {
+  if (act != FOLD_ACT_NONE || db) {
     ProfScope prof(act == FOLD_ACT_NONE ? "linear_dbias" : "linear_activation", st);
     const int c = act == FOLD_ACT_NONE ? bias_chunks(M, N, es) : activation_chunks(M, N, es);
     float* part = db && c > 1 ? static_cast<float*>(ws) : nullptr;

@@ -1149,7 +1149,10 @@ class Linear:
                 _vector("dbias", dbias, torch.float32, self.out_dim)
             if pre is not None:
                 _matrix("pre", pre, self.out_dim, self.dtype, rows)
-                dpre = torch.empty_like(pre) if dpre is None else _matrix("dpre", dpre, self.out_dim, self.dtype, rows)
+                if dpre is not None:
+                    _matrix("dpre", dpre, self.out_dim, self.dtype, rows)
+                elif any(t is not None for t in (dx, dW, dbias)):
+                    dpre = torch.empty_like(pre)
             elif dpre is not None:
                 raise ValueError("dpre belongs to a layer with an activation")
             n = _linear_ws(self.code, rows, self.in_dim, self.out_dim)[1]

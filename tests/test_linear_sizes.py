@@ -79,3 +79,17 @@ def test_cut_products_go_by_the_kernel_that_knows_pieces(launches):
             assert int(made[0][1]) >= tiles * split, size
         cut, chains = cut + (split > 1), chains + (names[0] == "k_product_chain")
     assert cut > 500 and chains > 500  # both are drawn
+
+
+def test_gradient_before_the_activation_alone_is_checked():
+    """Asked for by itself it is an output like the others."""
+    from paper_1702_02181_amd import fold as F
+    from tests.test_oracle_vocab import NULL_STREAM, _Buf
+    x, W, z, d, ws = (_Buf(1 << (20 + k)) for k in range(5))
+    for kw in (dict(dpre=x), dict(dpre=_Buf(z.at + 16)), dict(dout=None), dict(pre=None)):
+        a = dict(pre=z, dout=d, dpre=z)
+        a.update(kw)
+        with pytest.raises(F.FoldError) as e:
+            F.fold_linear_backward(0, 4, 100, 70, x, W, F.FOLD_ACT_TANH, a["pre"], a["dout"], a["dpre"], 0, None, 0, None, None, 0,
+                                   ws, 1 << 20, NULL_STREAM)
+        assert e.value.code == F.FOLD_E_INVALID
