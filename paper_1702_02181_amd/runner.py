@@ -427,7 +427,9 @@ class CrossBlock:
         o, lse = self.cross.forward(q, kv, kv[:, self.wk:], stream=st)
         y = self.o[0].forward(o, residual=x, stream=st)
         b, *stats_b = self._norm(1, y)
-        f, pre = self.first[0].forward(b, pre=True, stream=st)
+        bent = self.first[0].act != F.FOLD_ACT_NONE  # (the gradient of a layer without an activation takes no values before it)
+        f = self.first[0].forward(b, pre=bent, stream=st)
+        f, pre = f if bent else (f, None)
         z = self.second[0].forward(f, residual=y, stream=st)
         out, *stats_z = self._norm(2, z)
         self.saved = x, s, a, stats_a, q, kv, o, lse, y, b, stats_b, f, pre, z, stats_z
