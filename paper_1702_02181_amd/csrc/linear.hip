@@ -75,7 +75,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_linear_few(const T* x, const
     const size_t at = (size_t)m * ldn + n;
     if (pre) pre[at] = from_f32<T>(n < N ? z : 0.f);
     const float r = res ? to_f32<T>(res[at]) : 0.f;
-    out[at] = from_f32<T>(n < N ? act_value<ACT>(z) + r : 0.f);
+    out[at] = from_f32<T>(n < N ? act_value<ACT, T>(z) + r : 0.f);
   }
 }
 
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(256) void k_linear_join(const float* part, int piec
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const bool in = col + e < N;
-    y[e] = in ? act_value<ACT>(s[e]) + r[e] : 0.f;
+    y[e] = in ? act_value<ACT, T>(s[e]) + r[e] : 0.f;
     s[e] = in ? s[e] : 0.f;
   }
   if (pre) *reinterpret_cast<raw*>(pre + i) = Four<T>::give(s);
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(256) void k_activation_back(const T* dout, const T*
         T* ov = reinterpret_cast<T*>(&o);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-          const float t = (int)col + e < N ? to_f32<T>(dv[e]) * act_slope<ACT>(to_f32<T>(zv[e])) : 0.f;
+          const float t = (int)col + e < N ? to_f32<T>(dv[e]) * act_slope<ACT, T>(to_f32<T>(zv[e])) : 0.f;
           s[e] += t;
           ov[e] = from_f32<T>(t);
         }
