@@ -778,7 +778,8 @@ int32_t fold_cross_workspace_size(const fold_cross* cross, size_t* fwd_bytes, si
  *   k, v     device [num_key_rows, ldk], [.., ldv], kv_heads * head_dim columns
  *   key_mask device [num_keys] bytes in LIST order (a schedule's node order),
  *            0: the key does not count, whatever its row holds; NULL: all count
- *   scale    finite, above 0; scores are below 1e9 in magnitude
+ *   scale    above 0, below 2^127; scores are below 1e9 in magnitude, q . k
+ *            itself finite
  *   out      device [num_query_rows, ldo] of dtype
  *   lse      device [num_query_rows, heads] fp32, or NULL
  * fold_cross_backward: the gradients of q, k and v from dout; out and lse as
@@ -788,6 +789,8 @@ int32_t fold_cross_workspace_size(const fold_cross* cross, size_t* fwd_bytes, si
  * group and over the sequences that read a source, without atomics.
  * For bf16 the probabilities, and in the gradient the scores' gradients, are
  * rounded to bf16 where they enter a matrix product; everything else is fp32.
+ * The gradient takes its probabilities from lse, exp(s - lse), so that a row's
+ * are off by |lse| 2^-22 of themselves, and sum do o from out as it was rounded.
  * FOLD_E_INVALID for NULL buffers, strides below the width, addresses that are
  * no multiple of an element's size, a scale out of range or an output that
  * overlaps another buffer; FOLD_E_MISMATCH for a workspace (16-byte aligned)

@@ -241,7 +241,8 @@ int check_cross(const std::string& who, const fold_cross* cross, const Cols* in,
   int dev = -1;
   FOLD_HIP_CHECK(hipGetDevice(&dev));
   if (dev != c.device) return api_fail(FOLD_E_MISMATCH, who + ": the plan belongs to another device");
-  if (!(scale > 0.f) || !std::isfinite(scale)) return api_fail(FOLD_E_INVALID, who + ": scale must be finite and above 0");
+  // (below 2^127: the kernels multiply it by log2 e)
+  if (!(scale > 0.f) || scale >= 0x1p127f) return api_fail(FOLD_E_INVALID, who + ": scale must be above 0 and below 2^127");
   const int es = c.dtype == FOLD_BF16 ? 2 : 4;
   const auto bad = [&](const Cols& m, bool needed) {
     if (!m.p) return needed && m.rows > 0;
