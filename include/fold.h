@@ -790,7 +790,10 @@ int32_t fold_cross_workspace_size(const fold_cross* cross, size_t* fwd_bytes, si
  * For bf16 the probabilities, and in the gradient the scores' gradients, are
  * rounded to bf16 where they enter a matrix product; everything else is fp32.
  * The gradient takes its probabilities from lse, exp(s - lse), so that a row's
- * are off by |lse| 2^-22 of themselves, and sum do o from out as it was rounded.
+ * are off by |lse| 2^-22 of themselves, and sum do o from out as it was rounded;
+ * where a source has up to 32 keys (fp32: one) it sums p (do . v) over them in
+ * fp32 instead, so that little of it is lost beside few keys and a single key's
+ * dq and dk are 0.
  * FOLD_E_INVALID for NULL buffers, strides below the width, addresses that are
  * no multiple of an element's size, a scale out of range or an output that
  * overlaps another buffer; FOLD_E_MISMATCH for a workspace (16-byte aligned)

@@ -47,7 +47,9 @@ struct Cross {
   KTile* keys = nullptr;  // the keys' and values' gradient's
   KTile* kjoin = nullptr;
   RTile* rows = nullptr;
-  int nfwd = 0, nfjoin = 0, nback = 0, nbjoin = 0, nkeys = 0, nkjoin = 0, nrows = 0;
+  QTile* brief = nullptr;    // rows of sources whose few keys give delta
+  int32_t* others = nullptr; // list entries of all other rows that read a key; NULL: all entries
+  int nfwd = 0, nfjoin = 0, nback = 0, nbjoin = 0, nkeys = 0, nkjoin = 0, nrows = 0, nbrief = 0, nothers = 0;
   int fslots = 0, bslots = 0, kslots = 0;  // of a head
   bool few = false;  // the forward takes tiles of 32 rows whose four waves share them and cut the keys
 };
@@ -56,6 +58,14 @@ constexpr int kCrossHeadDim = 128;
 constexpr int kCrossRows = 128, kCrossFew = 32;  // virtual rows of a workgroup
 constexpr int kCrossFewBytes = 256;              // of a row that the tiles of 32 rows take: eight tiles of 32 keys in LDS
 constexpr int kCrossKeys = 128;                  // keys of a workgroup of the keys' gradient
+
+
+// Sources of up to so many keys give delta = sum_j p_j dp_j themselves, in fp32, where more keys take it from the forward's rounded
+// out.  Beside few keys dp - delta is small and out's rounding is not: relative errors (L2) of dq in bf16 from out and from the
+// keys, 2 keys 3.7e-3 and 2.3e-3, 4 2.9e-3, 16 2.5e-3, 32 2.43e-3 and 2.37e-3, 256 2.41e-3 and 2.36e-3 (a rounding of the result
+// alone is 1.7e-3).  In fp32 out's rounding is not the largest; a single key, whose gradient is exactly 0, is looked at there too.
+inline int cross_brief(int dtype) { return dtype == FOLD_BF16 ? 32 : 1; }
+constexpr int kCrossBriefRows = 512;  // virtual rows of a workgroup that sums them
 
 inline int cross_padded(int d) { return (d + 31) / 32 * 32; }  // a head's columns as the kernels hold them: 32, 64, 96, 128
 

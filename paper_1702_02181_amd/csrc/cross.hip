@@ -1,6 +1,6 @@
 // Cross attention on the matrix cores (gfx950), forward and backward.
 //     s = scale q k^T,  p = softmax(s) over the keys that count,  o = p v,  lse = log sum exp s
-//     delta = sum_d do o,  dp = do v^T,  ds = p (dp - delta),  dq = scale ds k,  dk = scale ds^T q,  dv = p^T do
+//     dp = do v^T,  delta = sum_d do o = sum_j p dp,  ds = p (dp - delta),  dq = scale ds k,  dk = scale ds^T q,  dv = p^T do
 // Rows are gathered by index into LDS by direct loads; a masked key's, and what lies past the end, come from a block of zeros.
 // What bounds it: k and v on their way from HBM and the caches (256 sequences of 16 .. 256 rows against 64 .. 512 keys, 8 heads of
 // 128 in bf16: 131 us, 110 without the products, 87 for its bytes at a copy's rate; 64 single rows against 512 .. 4,096 keys, 16
@@ -18,6 +18,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "checks.h"
 #include "common.h"
 #include "cross.h"
 #include "dma.h"
@@ -654,24 +655,115 @@ __global__ __launch_bounds__(kThreads) void k_cross_join(const QTile* tiles, Arg
 
 // ---- backward ---------------------------------------------------------------------------------------------------------
 
-// delta = sum_d dout out of every listed row and head: eight lanes each
+// delta = sum_d dout out of rows and heads, out as it was rounded: eight lanes each
+struct DeltaArgs {
+  const void *out, *dout;
+  int64_t ldo, lddo;
+  const int *q_row, *entries;  // the rows' list entries, NULL: all
+  int64_t n;                   // rows times heads
+  int heads, d;
+  float* delta;
+};
 template <typename T, bool VEC>
-__global__ __launch_bounds__(kThreads) void k_cross_delta(const T* out, int64_t ldo, const T* dout, int64_t lddo,
-                                                          const int* q_row, int64_t n, int heads, int d, float* delta) {
+__device__ __forceinline__ void row_deltas(const DeltaArgs& a, unsigned block, unsigned blocks) {
   constexpr int E = 16 / (int)sizeof(T);
-  for (int64_t at = (int64_t)blockIdx.x * (kThreads / 8) + (threadIdx.x >> 3); at < n; at += (int64_t)gridDim.x * (kThreads / 8)) {
-    const int entry = (int)(at / heads), head = (int)(at - (int64_t)entry * heads), row = row_of(q_row, entry);
-    const T *x = out + (int64_t)row * ldo + head * d, *y = dout + (int64_t)row * lddo + head * d;
+  for (int64_t at = (int64_t)block * (kThreads / 8) + (threadIdx.x >> 3); at < a.n; at += (int64_t)blocks * (kThreads / 8)) {
+    const int i = (int)(at / a.heads), head = (int)(at - (int64_t)i * a.heads);
+    const int row = row_of(a.q_row, a.entries ? a.entries[i] : i);
+    const T *x = static_cast<const T*>(a.out) + (int64_t)row * a.ldo + head * a.d;
+    const T* y = static_cast<const T*>(a.dout) + (int64_t)row * a.lddo + head * a.d;
     float s = 0.f;
-    for (int e0 = (threadIdx.x & 7) * E; e0 < d; e0 += 8 * E) {
-      const uint4 u = row_unit<T, VEC>(x, e0, d), w = row_unit<T, VEC>(y, e0, d);
+    for (int e0 = (threadIdx.x & 7) * E; e0 < a.d; e0 += 8 * E) {
+      const uint4 u = row_unit<T, VEC>(x, e0, a.d), w = row_unit<T, VEC>(y, e0, a.d);
 #pragma unroll
       for (int e = 0; e < E; ++e)
         s += to_f32<T>(reinterpret_cast<const T*>(&u)[e]) * to_f32<T>(reinterpret_cast<const T*>(&w)[e]);
     }
 #pragma unroll
     for (int o = 1; o < 8; o *= 2) s += __shfl_xor(s, o);  // (eight lanes are in or out together)
-    if ((threadIdx.x & 7) == 0) delta[(int64_t)row * heads + head] = s;
+    if ((threadIdx.x & 7) == 0) a.delta[(int64_t)row * a.heads + head] = s;
+  }
+}
+template <typename T, bool VEC>
+__global__ __launch_bounds__(kThreads) void k_cross_delta(DeltaArgs a) {
+  row_deltas<T, VEC>(a, blockIdx.x, gridDim.x);
+}
+
+// delta = sum_j p_j dp_j of rows whose source has up to 32 keys, a tile of them: the keys and values lie in LDS, a wave takes every
+// fourth 32 rows and loads the next ones while it looks at the products.  Summed from the first key's dp on, whose products are
+// those of the gradients bit for bit: a row that has one key has dp - delta = 0.  The launch's first `n` workgroups of a head; the
+// rest take all other rows (256 sequences of 64 rows, 8 heads of 64 in bf16, gradients: with 16 keys each 47 us, from out 43; with 8
+// and 100 keys in turn 59, from out 55).
+template <typename T, int DP, bool VEC>
+__global__ __launch_bounds__(kThreads, (DP * sizeof(T) <= 128 ? 4 : DP * sizeof(T) <= 256 ? 3 : 1)) void k_cross_delta_brief(
+    const QTile* tiles, unsigned n, Args a, DeltaArgs others) {
+  constexpr int TK = 32, U = DP * (int)sizeof(T) / 16, NS = U / 2, TB = tile_bytes<TK, T, DP>(), E = 16 / (int)sizeof(T);
+  __shared__ __attribute__((aligned(16))) char lds[2 * TB];
+  if (blockIdx.x >= n) {
+    const unsigned more = gridDim.x - n;
+    return row_deltas<T, VEC>(others, blockIdx.y * more + blockIdx.x - n, gridDim.y * more);
+  }
+  const QTile t = tile_of_head(tiles, blockIdx.x, a);
+  const int lane = threadIdx.x & 63, wave = wave_id(), h = lane >> 5, l32 = lane & 31;
+  const T* k = static_cast<const T*>(a.k) + t.kv_head * a.d;
+  const T* v = static_cast<const T*>(a.v) + t.kv_head * a.d;
+  using L = TileLoader<T, DP, TK, 2, VEC>;  // two waves load the keys, two the values
+  const L ld(wave & 1, lane);
+  int idx[L::NI];
+#pragma unroll
+  for (int i = 0; i < L::NI; ++i) idx[i] = row_of(a.k_row, min(t.k_begin + ld.row(i), t.k_end - 1));
+  const uint8_t mk = a.mask ? a.mask[min(t.k_begin + l32, t.k_end - 1)] : 1;
+  uint4 qf[NS], df[NS];
+  int64_t stat = 0;
+  float lse = 0.f;
+  const auto load = [&](int first) __attribute__((always_inline)) {
+    const Virtual vr(a, t.entry, t.head0, t.kv_head, min(first + l32, t.rows - 1));
+    const int qrow = row_of(a.q_row, vr.entry);
+    const T* q = row_at(static_cast<const T*>(a.q), qrow, a.ldq) + vr.head * a.d;
+    const T* g = row_at(static_cast<const T*>(a.dout), qrow, a.lddo) + vr.head * a.d;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      qf[s] = row_unit<T, VEC>(q, (2 * s + h) * E, a.d);
+      df[s] = row_unit<T, VEC>(g, (2 * s + h) * E, a.d);
+    }
+    stat = (int64_t)qrow * a.heads + vr.head;
+    lse = a.lse[stat];
+  };
+  if (32 * wave < t.rows) load(32 * wave);
+  const uint64_t bits = __ballot(lane < TK && t.k_begin + lane < t.k_end && mk != 0);
+#pragma unroll
+  for (int i = 0; i < L::NI; ++i) idx[i] = (bits >> ld.row(i)) & 1 ? idx[i] : -1;
+  if (wave < 2) ld.load(k, a.ldk, a.d, idx, lds);
+  else ld.load(v, a.ldv, a.d, idx, lds + TB);
+  vm_wait();
+  __syncthreads();
+  const float c = a.scale * kLog2e;
+  const int j = bits ? __builtin_ctzll(bits) : 0;  // the first key: register 4 (j / 8) + j % 4 of half (j / 4) % 2
+  for (int first = 32 * wave; first < t.rows; first += 32 * (kThreads / 64)) {
+    f32x16 s, dp;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+#pragma unroll
+    for (int st = 0; st < NS; ++st) {
+      const int place = unit_at<U>(l32, 2 * st + h);
+      s = step_mma<T>(*reinterpret_cast<const uint4*>(lds + place), qf[st], s);
+      dp = step_mma<T>(*reinterpret_cast<const uint4*>(lds + TB + place), df[st], dp);
+      if (st % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (registers)
+    }
+    const float ref = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    const int64_t at = stat;
+    if (first + 32 * (kThreads / 64) < t.rows) load(first + 32 * (kThreads / 64));
+    float base = 0.f, sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) base = 8 * (r >> 2) + (r & 3) == (j & ~4) ? dp[r] : base;
+    base = __shfl(base, l32 + 32 * ((j >> 2) & 1));
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float term = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -ref)) * (dp[r] - base);
+      sum += key_in(bits, 0, r) ? term : 0.f;
+    }
+    sum = base + halves_sum(sum);
+    if (h == 0 && first + l32 < t.rows) others.delta[at] = sum;
   }
 }
 
@@ -1259,12 +1351,16 @@ void launch_cross_backward(const Cross& c, CrossMat q, CrossMat k, CrossMat v, c
     constexpr int DP = decltype(w)::DP, TK = sizeof(T) == 2 ? 64 : 32;
     const auto go = [&](auto vector) {
       constexpr bool VEC = decltype(vector)::value;
-      const int64_t n = (int64_t)c.num_queries * c.heads;
-      if (n > 0) {
+      const DeltaArgs da{out.p, dout.p, out.ld, dout.ld, c.q_row, c.others, (int64_t)c.nothers * c.heads, c.heads, d, delta};
+      const int64_t blocks = std::min<int64_t>((da.n + 31) / 32, 1 << 20);
+      if (c.nbrief > 0) {
         ProfScope prof("cross_delta", st);
-        hipLaunchKernelGGL((k_cross_delta<T, VEC>), dim3((unsigned)std::min<int64_t>((n + 31) / 32, 1 << 20)), dim3(kThreads), 0, st,
-                           static_cast<const T*>(out.p), out.ld, static_cast<const T*>(dout.p), dout.ld, c.q_row, n, c.heads,
-                           d, delta);
+        const int64_t more = std::min<int64_t>((blocks + c.kv_heads - 1) / c.kv_heads, kMaxTiles - c.nbrief);
+        hipLaunchKernelGGL((k_cross_delta_brief<T, DP, VEC>), dim3((unsigned)(c.nbrief + more), c.kv_heads), dim3(kThreads), 0, st,
+                           c.brief, (unsigned)c.nbrief, a, da);
+      } else if (blocks > 0) {
+        ProfScope prof("cross_delta", st);
+        hipLaunchKernelGGL((k_cross_delta<T, VEC>), dim3((unsigned)blocks), dim3(kThreads), 0, st, da);
       }
       const bool rows = dq && c.nback > 0, keys = (dk || dv) && c.nkeys > 0;
       Args qa = a, ka = a;

@@ -172,6 +172,25 @@ void query_tiles(const Lists& l, int height, std::vector<QTile>* out, std::vecto
   *out = s.order();
 }
 
+// tiles of the rows whose source has up to `most` keys, and the list entries of all others that read a key
+void brief_tiles(const Lists& l, int most, std::vector<QTile>* tiles, std::vector<int32_t>* others) {
+  const int64_t sources = (int64_t)l.kp.size() - 1;
+  for (int64_t e = 0; e < sources; ++e) {
+    const int64_t nk = (int64_t)l.kp[e + 1] - l.kp[e];
+    if (nk == 0) continue;
+    for (int b : l.readers(e)) {
+      const int64_t n = ((int64_t)l.qp[b + 1] - l.qp[b]) * l.G;
+      if (nk > most) {
+        for (int32_t i = l.qp[b]; i < l.qp[b + 1]; ++i) others->push_back(i);
+        continue;
+      }
+      for (int64_t r = 0; r < n; r += kCrossBriefRows)
+        tiles->push_back(QTile{(int32_t)(l.qp[b] + r / l.G), (int32_t)(r % l.G),
+                               (int32_t)std::min<int64_t>(kCrossBriefRows, n - r), 0, l.kp[e], l.kp[e + 1], -1, 0});
+    }
+  }
+}
+
 void key_tiles(const Lists& l, int height, std::vector<KTile>* out, std::vector<KTile>* join, std::vector<RTile>* rows,
                int* slots) {
   const int64_t sources = (int64_t)l.kp.size() - 1;
@@ -368,6 +387,11 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
   query_tiles(l, c.few ? kCrossFew : kCrossRows, &fwd, &fjoin, &c.fslots);
   query_tiles(l, kCrossRows, &back, &bjoin, &c.bslots);
   key_tiles(l, c.dtype == FOLD_BF16 ? 64 : 32, &keys, &kjoin, &rows, &c.kslots);
+  std::vector<QTile> brief;
+  std::vector<int32_t> others;
+  brief_tiles(l, cross_brief(c.dtype), &brief, &others);
+  c.nothers = (int)others.size();
+  if (c.nothers == c.num_queries) others.clear();  // all of them
 
   if ((int64_t)std::max({fwd.size(), back.size() + keys.size(), 4 * fjoin.size(), 4 * bjoin.size(), 4 * kjoin.size()}) >= kMaxTiles)
     return api_fail(FOLD_E_INVALID, many);
@@ -384,7 +408,9 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
                at_bj = place(bjoin.data(), bjoin.size() * sizeof(QTile)),
                at_keys = place(keys.data(), keys.size() * sizeof(KTile)),
                at_kj = place(kjoin.data(), kjoin.size() * sizeof(KTile)),
-               at_rows = place(rows.data(), rows.size() * sizeof(RTile));
+               at_rows = place(rows.data(), rows.size() * sizeof(RTile)),
+               at_brief = place(brief.data(), brief.size() * sizeof(QTile)),
+               at_others = place(others.data(), others.size() * sizeof(int32_t));
   const size_t at_qr = image.size(), at_kr = at_qr + ((size_t)b->num_queries * 4 + 255) / 256 * 256;
   c.blob = pool_alloc(device, std::max<size_t>(at_kr + (size_t)b->num_keys * 4, 256), true);
   if (!c.blob) return api_fail(FOLD_E_NOMEM, who + ": no device memory");
@@ -408,6 +434,8 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
   c.keys = reinterpret_cast<KTile*>(base + at_keys);
   c.kjoin = reinterpret_cast<KTile*>(base + at_kj);
   c.rows = reinterpret_cast<RTile*>(base + at_rows);
+  c.brief = reinterpret_cast<QTile*>(base + at_brief);
+  c.others = others.empty() ? nullptr : reinterpret_cast<int32_t*>(base + at_others);
   c.nfwd = (int)fwd.size();
   c.nfjoin = (int)fjoin.size();
   c.nback = (int)back.size();
@@ -415,6 +443,7 @@ int32_t cross_create(const fold_cross_batch* b, hipStream_t st, fold_cross** out
   c.nkeys = (int)keys.size();
   c.nkjoin = (int)kjoin.size();
   c.nrows = (int)rows.size();
+  c.nbrief = (int)brief.size();
   *out = h;
   h = nullptr;
   return FOLD_OK;

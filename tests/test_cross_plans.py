@@ -87,6 +87,25 @@ static int check(const std::vector<int32_t>& qp, const std::vector<int32_t>& kp,
     }
     CHECK(runs.empty() && row == (int64_t)rows.size());
   }
+  // rows of sources with up to `most` keys in tiles, other rows that read a key listed, each once
+  for (int most : {1, 32, 100}) {
+    std::vector<QTile> tiles;
+    std::vector<int32_t> others;
+    brief_tiles(l, most, &tiles, &others);
+    std::map<int64_t, int64_t> source;
+    for (size_t s = 0; s < src.size(); ++s)
+      for (int64_t i = qp[s]; i < qp[s + 1]; ++i)
+        if (src[s] >= 0 && kp[src[s]] < kp[src[s] + 1]) source[i] = src[s];
+    for (int32_t i : others) CHECK(source.count(i) && kp[source[i] + 1] - kp[source[i]] > most && source.erase(i));
+    std::set<std::pair<int64_t, int>> seen;
+    for (const QTile& t : tiles)
+      for (int r = 0; r < t.rows; ++r) {
+        const int64_t i = t.entry + (t.head0 + r) / G;
+        CHECK(source.count(i) && t.k_begin == kp[source[i]] && t.k_end == kp[source[i] + 1] && t.k_end - t.k_begin <= most);
+        CHECK(t.rows <= kCrossBriefRows && t.slot == -1 && seen.insert({i, (t.head0 + r) % G}).second);
+      }
+    CHECK(seen.size() == source.size() * G);
+  }
   return 0;
 }
 
@@ -94,6 +113,7 @@ int main() {
   const int32_t top = INT32_MAX;  // past the last entry that a plan takes
   if (check({0, 5, 5, 300}, {0, 70, 70, 1000}, {0, 1, 2}, 1, 1, 128)) return 1;
   if (check({0, 1, 2, 3, 260}, {0, 130, 9000}, {1, 1, -1, 0}, 3, 2, 256)) return 1;
+  if (check({0, 9, 700, 701, 720, 730}, {0, 1, 33, 33, 66}, {3, 1, 0, 2, 1}, 4, 2, 256)) return 1;
   if (check({0, 700}, {top - 5000, top - 4999, top}, {1}, 2, 1, 128)) return 1;
   if (check({0, 700, 701}, {top - 100, top}, {0, 0}, 1, 4, 256)) return 1;
   if (check({top - 300, top - 1, top}, {0, 2000}, {0, 0}, 1, 1, 128)) return 1;
