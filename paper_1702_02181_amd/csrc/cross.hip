@@ -104,7 +104,9 @@ __device__ __forceinline__ f32x16 step_mma(const uint4& a, const uint4& b, f32x1
   return c;
 }
 
-// What leaves an accumulator as the next product's operand: 32 K values (the accumulator's rows) of the lane's column.
+// What leaves an accumulator as the next product's operand: 32 K values (the accumulator's rows) of the lane's column.  In bf16
+// p and ds are rounded here, to nearest even (at most 2^-8 of each): the matrix cores multiply k, q, v and dout by operands of
+// their own type, and what the rounding leaves would be a second product of the same length.
 template <typename T>
 struct Probs;
 template <>

@@ -120,7 +120,8 @@ __global__ __launch_bounds__(256) void k_linear_join(const float* part, int piec
 
 // ---- the gradient of the activation ------------------------------------------------------------------------------------
 
-// dz = dout act'(pre), and the rows' sums of dz (before its rounding).  A workgroup takes 64 16-byte vectors of columns of one
+// dz = dout act'(pre), rounded to T as it enters its products beside W and x (in bf16 at most 2^-8 of each; fp32 products are
+// sixteen times as long), and the rows' sums of dz before that.  A workgroup takes 64 16-byte vectors of columns of one
 // of `chunks` pieces of the rows; its four waves take every fourth row, four of them in flight.  One piece writes db itself,
 // more their sums to part [chunks][ld].
 template <typename T, int ACT>
