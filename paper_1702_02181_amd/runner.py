@@ -58,13 +58,15 @@ class DeviceRun:
         self.table = (bf16_tensor(tab) if self.bf16 else torch.from_numpy(tab)).to(device)
         N, R = w.num_nodes, self.sched.info.num_roots
         self.N, self.R = N, R
-        self.h_pool = torch.zeros((max(N, 1), self.ld), dtype=self.tdtype, device=device)
-        self.c_pool = torch.zeros((max(N, 1), self.ld), dtype=torch.float32, device=device)
-        self.roots = torch.zeros((max(R, 1), self.ld), dtype=self.tdtype, device=device)
+        with F._on(stream):  # what is filled, is filled on the calls' stream
+            self.h_pool = torch.zeros((max(N, 1), self.ld), dtype=self.tdtype, device=device)
+            self.c_pool = torch.zeros((max(N, 1), self.ld), dtype=torch.float32, device=device)
+            self.roots = torch.zeros((max(R, 1), self.ld), dtype=self.tdtype, device=device)
         self.fwd_bytes, self.bwd_bytes = F.fold_workspace_size(self.sched.handle, self.packed.handle)
         backward = w.backward if with_backward is None else with_backward
         self.ws_bytes = self.bwd_bytes if backward else self.fwd_bytes
-        self.ws = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=device)
+        with F._on(stream):
+            self.ws = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=device)
         self.grads = None
         self.dh_roots = None
         self.dh_nodes = None
@@ -84,6 +86,10 @@ class DeviceRun:
                        self.c_pool, self.roots, self.ws, self.ws_bytes, self.stream)
 
     def alloc_grads(self, table_grad=True):
+        with F._on(self.stream):
+            return self._alloc_grads(table_grad)
+
+    def _alloc_grads(self, table_grad):
         sets = []
         for p in self.w.params:
             g = gen.NUM_GATES[p.kind] * self.H
@@ -113,12 +119,13 @@ class DeviceRun:
             self.dh_nodes = None
 
     def zero_grads(self):
-        for t in self.grad_tensors:
-            for x in t:
-                if x is not None:
-                    x.zero_()
-        if self.d_table is not None:
-            self.d_table.zero_()
+        with F._on(self.stream):
+            for t in self.grad_tensors:
+                for x in t:
+                    if x is not None:
+                        x.zero_()
+            if self.d_table is not None:
+                self.d_table.zero_()
 
     def backward(self, dh_out=None, dc_out=None, u_mask=None):
         if u_mask is not None:

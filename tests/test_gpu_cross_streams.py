@@ -95,3 +95,30 @@ def test_counts_are_read_on_the_stream():
     plan = F.CrossAttention(2, 32, *lists, dtype=torch.float32, stream=side)
     assert (plan.num_queries, plan.num_keys) == (7, 9)
     torch.cuda.synchronize()
+
+
+def test_a_run_on_a_stream_of_its_own():
+    """States and gradients of a run whose stream does not wait for the busy one that it was made on."""
+    import torch
+    from paper_1702_02181_amd.runner import DeviceRun
+    w = _chains(2)
+    rng = np.random.default_rng(1)
+    up = rng.standard_normal((w.num_nodes, 64)).astype(np.float32)
+
+    def states_and_grads(stream):
+        run = DeviceRun(w, stream=stream, with_backward=True)
+        run.forward()
+        run.alloc_grads()
+        run.set_upstream(np.zeros_like(w.dh_roots), up)
+        run.zero_grads()
+        if stream is not None:
+            torch.cuda._sleep(BUSY)
+        run.zero_grads()
+        run.backward()
+        with torch.cuda.stream(stream or torch.cuda.current_stream()):
+            return [t.cpu() for t in (run.h_pool, run.c_pool, *(x for g in run.grad_tensors for x in g if x is not None), run.d_table)]
+    want, got = states_and_grads(None), states_and_grads(torch.cuda.Stream())
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got[:2], want[:2]))
+    for a, b in zip(got[2:], want[2:]):  # (sums by atomics among them)
+        assert b.any() and (a - b).abs().max() <= 1e-4 * b.abs().max()
