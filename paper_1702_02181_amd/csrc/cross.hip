@@ -5,7 +5,7 @@
 // What bounds it: k and v on their way from HBM and the caches (256 sequences of 16 .. 256 rows against 64 .. 512 keys, 8 heads of
 // 128 in bf16: 131 us, 110 without the products, 87 for its bytes at a copy's rate; 64 single rows against 512 .. 4,096 keys, 16
 // heads of 64 on 4: 30 us and a join of 4, at 4.9 TB/s); in the gradient the exponentials beside the products and the loads (64
-// sequences of 256 .. 512 rows against 256 .. 1,024 keys, 16 heads of 64: 387 us, 430 TFLOP/s); in fp32 the matrix cores.
+// sequences of 256 .. 512 rows against 256 .. 1,024 keys, 16 heads of 64: 379 us, 440 TFLOP/s); in fp32 the matrix cores.
 //
 // Products are 32 x 32 tiles with the axis of the softmax on the accumulators' rows: the forward computes s^T = k q^T, so a
 // lane holds one query's column, its maximum, sum and rescaling are one value a lane, and p^T leaves the accumulators in the

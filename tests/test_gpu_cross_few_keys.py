@@ -119,3 +119,23 @@ def test_masked_rows_beside_few_keys():
     got = plan.backward(q, k, v, out, lse, do, mask, c.scale)
     assert all(torch.isfinite(t).all() for t in got)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 50), ("f32", 60)])
+def test_workspaces_hold_nothing(dtype, d):
+    """Short, long, empty and unread sources and rows without one: a workspace full of NaN changes no bit."""
+    import torch
+    from paper_1702_02181_amd import fold as F
+    from tests.block_common import dev
+    c = Case(dtype, 4, 2, d, [40, 7, 600, 1, 33, 90], [5, 0, 400, 32, 1], source=[0, 2, 3, -1, 1, 4], mask=0.2, seed=8)
+    plan, (q, k, v), mask, do = c.plan(), c.tensors(), c.mask_tensor(), dev(c.dout, dtype)
+    out, lse = plan.forward(q, k, v, mask, c.scale)
+    want = [t.clone() for t in (out, lse, *plan.backward(q, k, v, out, lse, do, mask, c.scale))]
+    got = [torch.zeros_like(t) for t in want]
+    ws = [torch.full((max(n // 4, 4),), float("nan"), device="cuda") for n in plan.ws_bytes]
+    ld = lambda t: t.stride(0)  # noqa: E731
+    F.fold_cross_attend(plan.handle, q, ld(q), k, ld(k), v, ld(v), mask, c.scale, got[0], ld(got[0]), got[1], ws[0], plan.ws_bytes[0])
+    F.fold_cross_backward(plan.handle, q, ld(q), k, ld(k), v, ld(v), mask, c.scale, got[0], ld(got[0]), got[1], do, ld(do), got[2],
+                          ld(got[2]), got[3], ld(got[3]), got[4], ld(got[4]), ws[1], plan.ws_bytes[1])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    assert not any(torch.isnan(t).any() for t in got)
